@@ -8,7 +8,8 @@ probable alternatives are taken from the logits.  Offline (and for activations o
 Formulas.  MX: for every 32 consecutive channels of a row, e = max(floor(log2(largest magnitude)) - emax, -127), the scale is
 2^e, an element is its value / 2^e rounded to the nearest number of its format, ties to even, no further than the largest one:
 4 bits: 0 0.5 1 1.5 2 3 4 6 and their negatives (emax 2); 8 bits: 1 sign, 4 exponent and 3 mantissa bits, up to 448 (emax 8).  A
-row is padded with zeros to a multiple of 128 channels; 4-bit elements stand two to a byte, the even channel in the low half; a scale is one byte, e + 127.
+row is padded with zeros to a multiple of 128 channels; 4-bit elements stand two to a byte, the even channel in the low half; a scale is one byte, e + 127,
+and the four scales of a row's 128 channels stand behind those of the row before it: [128 channels][row][4].
 Norm: h = x + r rounded to the type of x; y = h w / sqrt(mean(h^2) + eps).  Product: Y = X W^T.  Log probabilities: log softmax.
 
 Shapes are those of the workloads in workloads.py and generic ones, ragged ones beside them; weights are N(0, K^-1/2), activations
@@ -145,7 +146,7 @@ def _quantised(x, fmt):
 
 
 def _encoded(x, fmt):
-    """MX form of x: element codes [R, bytes] and scales [R, Kp/32], one byte each."""
+    """MX form of x: element codes [R, bytes] and scales [Kp/128, R, 4], one byte each."""
     data, scales = [], []
     rows = max(1, (1 << 25) // max(1, x.shape[1]))
     for lo in range(0, x.shape[0], rows):
@@ -158,8 +159,8 @@ def _encoded(x, fmt):
             code += (v < 0).to(torch.uint8) * 8
             code = code.reshape(v.shape[0], -1, 2)
             data.append(code[:, :, 0] | code[:, :, 1] << 4)
-        scales.append((e + 127).to(torch.uint8))
-    return torch.cat(data), torch.cat(scales)
+        scales.append((e + 127).to(torch.uint8).reshape(e.shape[0], -1, 4).transpose(0, 1))
+    return torch.cat(data), torch.cat(scales, 1).contiguous()
 
 
 def _decoded(data, scales, fmt):
@@ -169,7 +170,7 @@ def _decoded(data, scales, fmt):
     else:
         table = torch.tensor([0, 0.5, 1, 1.5, 2, 3, 4, 6, 0, -0.5, -1, -1.5, -2, -3, -4, -6], device=data.device)
         v = table[torch.stack((data & 15, data >> 4), 2).int()].reshape(data.shape[0], -1)
-    s = torch.exp2(scales.float() - 127.0)
+    s = torch.exp2(scales.transpose(0, 1).reshape(data.shape[0], -1).float() - 127.0)
     return (v.reshape(v.shape[0], -1, 32) * s[:, :, None]).reshape(v.shape[0], -1)
 
 
