@@ -15,7 +15,10 @@ from typing import Optional
 import numpy as np
 import torch
 
-F16, BF16 = 0, 1
+F16, BF16, F32 = 0, 1, 2
+MX_FP4, MX_FP8 = 0, 1   # microscaled formats
+_ACT_16 = 2             # activations of mx_gemm in 16 bits
+MAX_TOP = 32            # alternatives of token_logprobs
 USE_ENTROPY, USE_NORM, USE_GNS, USE_LBS, USE_ALL = 1, 2, 4, 8, 15
 
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libesparse.so")
@@ -78,6 +81,16 @@ def load_library():
         "esparse_tune_group": (i32, [vp, i32, ll, ll, ll, i32, i32, P(i32), P(C.c_float)]),
         "esparse_tune_save": (i32, [vp, C.c_char_p]),
         "esparse_tune_load": (i32, [vp, C.c_char_p]),
+        "esparse_mx_size": (i32, [ll, ll, i32, P(sz), P(sz)]),
+        "esparse_mx_quantize": (i32, [vp, vp, ll, ll, ll, i32, i32, vp, vp]),
+        "esparse_mx_dequantize": (i32, [vp, vp, vp, ll, ll, i32, i32, vp]),
+        "esparse_mx_packed_size": (i32, [ll, ll, P(sz)]),
+        "esparse_mx_pack": (i32, [vp, vp, vp, ll, ll, vp]),
+        "esparse_mx_gemm_workspace": (i32, [ll, ll, ll, i32, i32, P(sz)]),
+        "esparse_mx_gemm": (i32, [vp, vp, vp, ll, ll, i32, i32, vp, ll, ll, i32, vp, vp, sz]),
+        "esparse_rms_norm": (i32, [vp, vp, ll, vp, ll, vp, ll, ll, C.c_double, i32, vp, vp, i32, vp, vp]),
+        "esparse_token_logprobs_workspace": (i32, [ll, ll, i32, i32, P(sz)]),
+        "esparse_token_logprobs": (i32, [vp, vp, ll, ll, ll, i32, vp, i32, vp, vp, vp, vp, vp, sz]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -96,7 +109,9 @@ EXPORTED = ["esparse_create", "esparse_destroy", "esparse_set_stream", "esparse_
             "esparse_stage_activations", "esparse_spmm_staged", "esparse_dense_gemm_staged",
             "esparse_spmm_num_variants", "esparse_spmm_variant_name", "esparse_dense_packed_size",
             "esparse_dense_pack", "esparse_dense_gemm", "esparse_tune", "esparse_tune_group", "esparse_tune_save",
-            "esparse_tune_load"]
+            "esparse_tune_load", "esparse_mx_size", "esparse_mx_quantize", "esparse_mx_dequantize", "esparse_mx_packed_size",
+            "esparse_mx_pack", "esparse_mx_gemm_workspace", "esparse_mx_gemm", "esparse_rms_norm",
+            "esparse_token_logprobs_workspace", "esparse_token_logprobs"]
 
 
 def _dtype_code(t: torch.Tensor) -> int:
@@ -105,6 +120,17 @@ def _dtype_code(t: torch.Tensor) -> int:
     if t.dtype == torch.bfloat16:
         return BF16
     raise TypeError(f"unsupported dtype {t.dtype}")
+
+
+_CODES = {torch.float16: F16, torch.bfloat16: BF16, torch.float32: F32}
+
+
+def _code(dtype: torch.dtype, name: str, f32: bool = False) -> int:
+    """The library's number of a type that a call takes."""
+    code = _CODES.get(dtype)
+    if code is None or (code == F32 and not f32):
+        raise TypeError(f"{name}: unsupported dtype {dtype}")
+    return code
 
 
 def _ptr(t: Optional[torch.Tensor]):
@@ -145,10 +171,46 @@ def _group_workspace(count: int, M: int, N: int, K: int) -> int:
     return a.value
 
 
+def mx_size(R: int, K: int, fmt: int):
+    """(bytes of the codes, bytes of the scales) of R rows of K channels."""
+    a, b = C.c_size_t(), C.c_size_t()
+    rc = load_library().esparse_mx_size(R, K, fmt, C.byref(a), C.byref(b))
+    if rc:
+        raise EsparseError(rc, f"esparse_mx_size: R = {R}, K = {K}, format {fmt}")
+    return a.value, b.value
+
+
+def mx_packed_size(N: int, K: int) -> int:
+    a = C.c_size_t()
+    rc = load_library().esparse_mx_packed_size(N, K, C.byref(a))
+    if rc:
+        raise EsparseError(rc, f"esparse_mx_packed_size: N = {N}, K = {K}")
+    return a.value
+
+
+def mx_gemm_workspace(M: int, N: int, K: int, act: int, in_place: bool = True) -> int:
+    a = C.c_size_t()
+    rc = load_library().esparse_mx_gemm_workspace(M, N, K, act, int(in_place), C.byref(a))
+    if rc:
+        raise EsparseError(rc, f"esparse_mx_gemm_workspace: M = {M}, N = {N}, K = {K}, activations {act}")
+    return a.value
+
+
+def token_logprobs_workspace(R: int, V: int, dtype: int, top: int) -> int:
+    a = C.c_size_t()
+    rc = load_library().esparse_token_logprobs_workspace(R, V, dtype, top, C.byref(a))
+    if rc:
+        raise EsparseError(rc, f"esparse_token_logprobs_workspace: R = {R}, V = {V}, dtype {dtype}, top = {top}")
+    return a.value
+
+
 # for the calls: sizes asked for before, a function of their arguments alone (typed: 16.0 is not the 16 that was asked for)
 _known_size = functools.lru_cache(4096, typed=True)(compressed_size)
 _known_workspace = functools.lru_cache(4096, typed=True)(spmm_workspace)
 _known_group_workspace = functools.lru_cache(4096, typed=True)(_group_workspace)
+_known_mx_packed_size = functools.lru_cache(4096, typed=True)(mx_packed_size)
+_known_mx_gemm_workspace = functools.lru_cache(4096, typed=True)(mx_gemm_workspace)
+_known_logprobs_workspace = functools.lru_cache(4096, typed=True)(token_logprobs_workspace)
 
 
 def dense_packed_size(N: int, K: int) -> int:
@@ -202,6 +264,31 @@ class Compressed:
     n_keep: int
     m_group: int
     dtype: int
+
+
+@dataclass
+class MX:
+    """Rows of microscaled numbers (include/esparse.h)."""
+    data: torch.Tensor    # uint8 [R, Kp / 2] or [R, Kp], Kp = K rounded up to 128
+    scales: torch.Tensor  # uint8 [Kp / 128, R, 4]
+    K: int
+    fmt: int              # MX_FP4 or MX_FP8
+
+
+@dataclass
+class MXWeight:
+    """Weights in microscaled 4 bits, in the order mx_gemm streams them."""
+    packed: torch.Tensor  # uint8 [mx_packed_size(N, K)]
+    N: int
+    K: int
+
+
+@dataclass
+class TokenLogprobs:
+    logprob: Optional[torch.Tensor]       # float32 [R]
+    entropy: torch.Tensor                 # float32 [R]
+    top_ids: Optional[torch.Tensor]       # int32 [R, top]
+    top_logprobs: Optional[torch.Tensor]  # float32 [R, top]
 
 
 def _raw_stream(device: int) -> int:
@@ -488,3 +575,147 @@ class Context:
 
     def tune_load(self, path: str):
         self._check(self._lib.esparse_tune_load(self._h, path.encode()))
+
+    # -- microscaled numbers and the steps around a product -------------------------------------
+    def _here(self, name: str, *tensors) -> None:
+        for t in tensors:
+            if t is not None and not (t.is_cuda and t.get_device() == self.device):
+                raise ValueError(f"{name}: a tensor is on {t.device}, the context on cuda:{self.device}")
+
+    def _rows(self, name: str, t: torch.Tensor) -> int:
+        """Values from row to row of a matrix whose rows are contiguous."""
+        if t.dim() != 2:
+            raise ValueError(f"{name}: {t.dim()} dimensions instead of two")
+        R, K = t.shape
+        if K > 1 and t.stride(1) != 1:
+            raise ValueError(f"{name}: the values of a row are {t.stride(1)} apart")
+        if R > 1 and t.stride(0) < K:
+            raise ValueError(f"{name}: rows overlap (stride {t.stride(0)} for {K} values)")
+        return t.stride(0) if R > 1 else K
+
+    def _check_mx(self, name: str, x: MX) -> int:
+        """The number of rows; the tensors' shapes are those of the format."""
+        R, steps = x.data.shape[0], (x.K + 127) // 128
+        if x.fmt not in (MX_FP4, MX_FP8):
+            raise ValueError(f"{name}: format {x.fmt} is neither MX_FP4 nor MX_FP8")
+        if tuple(x.data.shape) != (R, steps * (64 if x.fmt == MX_FP4 else 128)) or tuple(x.scales.shape) != (steps, R, 4):
+            raise ValueError(f"{name}: data {tuple(x.data.shape)} and scales {tuple(x.scales.shape)} are not those of {R} rows of {x.K} channels")
+        if x.data.dtype != torch.uint8 or x.scales.dtype != torch.uint8 or not x.data.is_contiguous() or not x.scales.is_contiguous():
+            raise ValueError(f"{name}: data and scales are contiguous uint8 tensors")
+        return R
+
+    def _empty_mx(self, R: int, K: int, fmt: int) -> MX:
+        if fmt not in (MX_FP4, MX_FP8):
+            raise ValueError(f"format {fmt} is neither MX_FP4 nor MX_FP8")
+        steps, dev = (K + 127) // 128, f"cuda:{self.device}"
+        return MX(torch.empty((R, steps * (64 if fmt == MX_FP4 else 128)), dtype=torch.uint8, device=dev),
+                  torch.empty((steps, R, 4), dtype=torch.uint8, device=dev), K, fmt)
+
+    def mx_quantize(self, X: torch.Tensor, fmt: int) -> MX:
+        """X[R, K] (f16, bf16, f32; rows may be apart) in microscaled 8 or 4 bits."""
+        code, ld = _code(X.dtype, "mx_quantize", f32=True), self._rows("mx_quantize", X)
+        self._here("mx_quantize", X)
+        R, K = X.shape
+        out = self._empty_mx(R, K, fmt)
+        self._sync_stream()
+        self._check(self._lib.esparse_mx_quantize(self._h, X.data_ptr(), R, K, ld, code, fmt, out.data.data_ptr(), out.scales.data_ptr()))
+        return out
+
+    def mx_dequantize(self, x: MX, dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
+        """The values [R, K] that x stands for."""
+        code, R = _code(dtype, "mx_dequantize", f32=True), self._check_mx("mx_dequantize", x)
+        self._here("mx_dequantize", x.data, x.scales)
+        out = torch.empty((R, x.K), dtype=dtype, device=x.data.device)
+        self._sync_stream()
+        self._check(self._lib.esparse_mx_dequantize(self._h, x.data.data_ptr(), x.scales.data_ptr(), R, x.K, x.fmt, code, out.data_ptr()))
+        return out
+
+    def mx_pack(self, w: MX) -> MXWeight:
+        """Weights[N, K] in microscaled 4 bits, laid out once for mx_gemm."""
+        N = self._check_mx("mx_pack", w)
+        if w.fmt != MX_FP4:
+            raise ValueError("mx_pack: weights are in 4 bits (MX_FP4)")
+        self._here("mx_pack", w.data, w.scales)
+        packed = torch.empty(mx_packed_size(N, w.K), dtype=torch.uint8, device=w.data.device)
+        self._sync_stream()
+        self._check(self._lib.esparse_mx_pack(self._h, w.data.data_ptr(), w.scales.data_ptr(), N, w.K, packed.data_ptr()))
+        return MXWeight(packed, N, w.K)
+
+    def mx_gemm(self, X, w: MXWeight, *, dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """X . W^T in `dtype` (f16, bf16 or f32).  X: an MX of 8 or 4 bits (dtype: bf16 if not given), or a 16-bit matrix whose rows may be apart
+        (dtype: its own), with which the weights alone are in 4 bits."""
+        if isinstance(X, MX):
+            M, K, act, code, ld = self._check_mx("mx_gemm", X), X.K, X.fmt, 0, 0
+            self._here("mx_gemm", X.data, X.scales, w.packed)
+            x, scales, given = X.data.data_ptr(), X.scales.data_ptr(), torch.bfloat16
+        else:
+            code, ld, act = _code(X.dtype, "mx_gemm"), self._rows("mx_gemm", X), _ACT_16
+            self._here("mx_gemm", X, w.packed)
+            (M, K), x, scales, given = X.shape, X.data_ptr(), None, X.dtype
+        N = w.N
+        if K != w.K:
+            raise ValueError(f"mx_gemm: activations of {K} channels, weights of {w.K}")
+        if w.packed.dtype != torch.uint8 or not w.packed.is_contiguous() or w.packed.numel() != _known_mx_packed_size(N, K):
+            raise ValueError(f"mx_gemm: packed is not the weights of {N} x {K}")
+        if out is None:
+            out = torch.empty((M, N), dtype=dtype or given, device=w.packed.device)
+        else:
+            self._here("mx_gemm", out)
+            if tuple(out.shape) != (M, N) or not out.is_contiguous() or (dtype is not None and out.dtype != dtype):
+                raise ValueError(f"mx_gemm: out is not a contiguous [{M}, {N}] of the type asked for")
+        out_code = _code(out.dtype, "mx_gemm", f32=True)
+        nbytes = _known_mx_gemm_workspace(M, N, K, act, act != _ACT_16 or not (K % 8 or ld % 8 or x % 16))
+        # a block of its own for each call: calls on several streams and captured graphs do not share it
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=out.device) if nbytes else None
+        self._sync_stream()
+        rc = self._lib.esparse_mx_gemm(self._h, x, scales, M, ld, act, code, w.packed.data_ptr(), N, K, out_code, out.data_ptr(), _ptr(ws), nbytes)
+        if rc:
+            self._check(rc)
+        return out
+
+    def rms_norm(self, x: torch.Tensor, weight: torch.Tensor, eps: float = 1e-6, *, residual: Optional[torch.Tensor] = None,
+                 fmt: Optional[int] = None, sum_out: Optional[torch.Tensor] = None):
+        """(y, h): h = x + residual (h is x itself where there is no residual), y = h weight / sqrt(mean(h^2) + eps), in the type of x
+        (fmt None) or as an MX.  sum_out: where to write h; x or residual for an update in place."""
+        code, ldx = _code(x.dtype, "rms_norm"), self._rows("rms_norm", x)
+        R, K = x.shape
+        self._here("rms_norm", x, weight, residual, sum_out)
+        if weight.dtype != x.dtype or tuple(weight.shape) != (K,) or not weight.is_contiguous():
+            raise ValueError(f"rms_norm: weight is not a contiguous [{K}] of the type of x")
+        ldr = 0
+        if residual is not None:
+            if residual.dtype != x.dtype or residual.shape != x.shape:
+                raise ValueError("rms_norm: residual is not of the shape and type of x")
+            ldr = self._rows("rms_norm", residual)
+            if sum_out is None:
+                sum_out = torch.empty((R, K), dtype=x.dtype, device=x.device)
+        if sum_out is not None and (sum_out.dtype != x.dtype or sum_out.shape != x.shape or not sum_out.is_contiguous()):
+            raise ValueError("rms_norm: sum_out is not a contiguous tensor of the shape and type of x")
+        if fmt is None:
+            y, q = torch.empty((R, K), dtype=x.dtype, device=x.device), None
+        else:
+            y, q = None, self._empty_mx(R, K, fmt)
+        self._sync_stream()
+        self._check(self._lib.esparse_rms_norm(self._h, x.data_ptr(), ldx, _ptr(residual), ldr, weight.data_ptr(), R, K, eps, code, _ptr(sum_out), _ptr(y),
+                                               fmt or 0, q.data.data_ptr() if q else None, q.scales.data_ptr() if q else None))
+        return (y if q is None else q), (x if sum_out is None else sum_out)
+
+    def token_logprobs(self, logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, *, top: int = 0) -> TokenLogprobs:
+        """Per row of logits[R, V] (f16, bf16, f32; rows may be apart): ln p of tokens[R] (int64; below 0: none, gives 0), the entropy, and the
+        `top` most probable tokens in order."""
+        code, ld = _code(logits.dtype, "token_logprobs", f32=True), self._rows("token_logprobs", logits)
+        R, V = logits.shape
+        self._here("token_logprobs", logits, tokens)
+        if tokens is not None and (tokens.dtype != torch.int64 or tuple(tokens.shape) != (R,) or not tokens.is_contiguous()):
+            raise ValueError(f"token_logprobs: tokens is not a contiguous int64 [{R}]")
+        dev = logits.device
+        nbytes = _known_logprobs_workspace(R, V, code, top)
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
+        logprob = torch.empty(R, dtype=torch.float32, device=dev) if tokens is not None else None
+        entropy = torch.empty(R, dtype=torch.float32, device=dev)
+        ids = torch.empty((R, top), dtype=torch.int32, device=dev) if top else None
+        lps = torch.empty((R, top), dtype=torch.float32, device=dev) if top else None
+        self._sync_stream()
+        self._check(self._lib.esparse_token_logprobs(self._h, logits.data_ptr(), R, V, ld, code, _ptr(tokens), top, _ptr(logprob), entropy.data_ptr(),
+                                                     _ptr(ids), _ptr(lps), _ptr(ws), nbytes))
+        return TokenLogprobs(logprob, entropy, ids, lps)

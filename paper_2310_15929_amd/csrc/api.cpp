@@ -691,4 +691,211 @@ int esparse_tune_load(esparse_ctx* ctx, const char* path) {
   return rc;
 }
 
+// ---- microscaled numbers, their products, the norm, log probabilities --------------------------------
+// The device of the context for the launches of a call; the caller's own current device again when it returns.
+class DeviceOfCall {
+ public:
+  explicit DeviceOfCall(int device) {
+    if (hipGetDevice(&before_) != hipSuccess) before_ = -1;
+    error_ = before_ == device ? hipSuccess : hipSetDevice(device);
+    if (before_ == device) before_ = -1;
+  }
+  ~DeviceOfCall() {
+    if (before_ >= 0) (void)hipSetDevice(before_);
+  }
+  DeviceOfCall(const DeviceOfCall&) = delete;
+  DeviceOfCall& operator=(const DeviceOfCall&) = delete;
+  hipError_t error() const { return error_; }
+
+ private:
+  int before_ = -1;
+  hipError_t error_ = hipSuccess;
+};
+
+static bool aligned_to(const void* p, size_t q) { return reinterpret_cast<uintptr_t>(p) % q == 0; }
+static size_t dtype_bytes(int dtype) { return dtype == ESPARSE_F32 ? 4 : 2; }
+
+static int check_dtype_or_f32(esparse_ctx* ctx, int dtype) {
+  ESP_REQUIRE(ctx, dtype == ESPARSE_F16 || dtype == ESPARSE_BF16 || dtype == ESPARSE_F32, ESPARSE_EUNSUPPORTED, "dtype %d is not f16 / bf16 / f32", dtype);
+  return ESPARSE_OK;
+}
+static int check_format(esparse_ctx* ctx, int format) {
+  ESP_REQUIRE(ctx, format == ESPARSE_MX_FP4 || format == ESPARSE_MX_FP8, ESPARSE_EUNSUPPORTED, "format %d is neither MX 4 nor MX 8 bits", format);
+  return ESPARSE_OK;
+}
+// rows and channels of a matrix (a launch has fewer than 2^32 threads: up to 1024 for a row, one for eight values)
+static constexpr long long kMaxRows = (1ll << 22) - 1, kMaxValues = 1ll << 34;
+static int check_rows(esparse_ctx* ctx, long long R, long long K, const char* k_name) {
+  ESP_REQUIRE(ctx, R >= 0 && R <= kMaxRows, ESPARSE_EINVAL, "%lld rows are outside [0, 2^22)", R);
+  ESP_REQUIRE(ctx, K >= 1 && K < (1ll << 31), ESPARSE_EINVAL, "%s = %lld out of range", k_name, K);
+  ESP_REQUIRE(ctx, R * K <= kMaxValues, ESPARSE_EINVAL, "%lld x %lld values are more than 2^34", R, K);
+  return ESPARSE_OK;
+}
+
+int esparse_mx_size(long long R, long long K, esparse_mx_format format, size_t* data_bytes, size_t* scale_bytes) {
+  if (format != ESPARSE_MX_FP4 && format != ESPARSE_MX_FP8) return ESPARSE_EUNSUPPORTED;
+  if (R < 0 || R > kMaxRows || K < 1 || K >= (1ll << 31) || R * K > kMaxValues) return ESPARSE_EINVAL;
+  const size_t steps = (size_t)(K + 127) / 128;
+  if (data_bytes) *data_bytes = (size_t)R * steps * (format == ESPARSE_MX_FP4 ? 64 : 128);
+  if (scale_bytes) *scale_bytes = (size_t)R * steps * 4;
+  return ESPARSE_OK;
+}
+
+int esparse_mx_quantize(esparse_ctx* ctx, const void* X, long long R, long long K, long long ldx, esparse_dtype dtype, esparse_mx_format format, void* data,
+                        void* scales) {
+  if (!ctx) return ESPARSE_EINVAL;
+  int rc = check_dtype_or_f32(ctx, dtype);
+  if (rc || (rc = check_format(ctx, format)) || (rc = check_rows(ctx, R, K, "K"))) return rc;
+  if (R == 0) return ESPARSE_OK;
+  ESP_REQUIRE(ctx, X && data && scales, ESPARSE_EINVAL, "X / data / scales is null");
+  ESP_REQUIRE(ctx, ldx >= K, ESPARSE_EINVAL, "ldx = %lld is less than K = %lld", ldx, K);
+  ESP_REQUIRE(ctx, aligned_to(X, dtype_bytes(dtype)), ESPARSE_EINVAL, "X is not aligned to its type");
+  ESP_REQUIRE(ctx, esp_aligned16(data) && esp_aligned16(scales), ESPARSE_EINVAL, "data / scales is not 16-byte aligned");
+  const DeviceOfCall device(ctx->device);
+  ESP_HIP(ctx, device.error());
+  return esp_mx_quantize_device(ctx, X, R, K, ldx, dtype, format, data, scales);
+}
+
+int esparse_mx_dequantize(esparse_ctx* ctx, const void* data, const void* scales, long long R, long long K, esparse_mx_format format, esparse_dtype dtype,
+                          void* out) {
+  if (!ctx) return ESPARSE_EINVAL;
+  int rc = check_dtype_or_f32(ctx, dtype);
+  if (rc || (rc = check_format(ctx, format)) || (rc = check_rows(ctx, R, K, "K"))) return rc;
+  if (R == 0) return ESPARSE_OK;
+  ESP_REQUIRE(ctx, data && scales && out, ESPARSE_EINVAL, "data / scales / out is null");
+  ESP_REQUIRE(ctx, aligned_to(out, dtype_bytes(dtype)), ESPARSE_EINVAL, "out is not aligned to its type");
+  ESP_REQUIRE(ctx, esp_aligned16(data) && esp_aligned16(scales), ESPARSE_EINVAL, "data / scales is not 16-byte aligned");
+  const DeviceOfCall device(ctx->device);
+  ESP_HIP(ctx, device.error());
+  return esp_mx_dequantize_device(ctx, data, scales, R, K, format, dtype, out);
+}
+
+int esparse_mx_packed_size(long long N, long long K, size_t* bytes) {
+  if (!bytes || N < 1 || N > kMaxRows || K < 1 || K >= (1ll << 31) || N * K > kMaxValues) return ESPARSE_EINVAL;
+  *bytes = (size_t)((N + 63) / 64) * 64 * ((size_t)(K + 127) / 128) * (64 + 4);
+  return ESPARSE_OK;
+}
+
+int esparse_mx_pack(esparse_ctx* ctx, const void* data, const void* scales, long long N, long long K, void* packed_out) {
+  if (!ctx) return ESPARSE_EINVAL;
+  const int rc = check_rows(ctx, N, K, "K");
+  if (rc) return rc;
+  ESP_REQUIRE(ctx, N >= 1, ESPARSE_EINVAL, "N = 0");
+  ESP_REQUIRE(ctx, data && scales && packed_out, ESPARSE_EINVAL, "data / scales / packed_out is null");
+  ESP_REQUIRE(ctx, esp_aligned16(data) && esp_aligned16(scales) && esp_aligned16(packed_out), ESPARSE_EINVAL, "data / scales / packed_out is not 16-byte aligned");
+  const DeviceOfCall device(ctx->device);
+  ESP_HIP(ctx, device.error());
+  return esp_mx_pack_device(ctx, data, scales, N, K, packed_out);
+}
+
+static bool mx_gemm_sizes(long long M, long long N, long long K, int act) {
+  return M >= 0 && M <= kMaxRows && N >= 1 && N <= kMaxRows && K >= 1 && K < (1ll << 31) && N * K <= kMaxValues && M * K <= kMaxValues && M * N <= kMaxValues &&
+         act >= ESPARSE_MX_ACT_FP4 && act <= ESPARSE_MX_ACT_16;
+}
+
+int esparse_mx_gemm_workspace(long long M, long long N, long long K, esparse_mx_act act, int in_place, size_t* bytes) {
+  if (!bytes || !mx_gemm_sizes(M, N, K, act) || in_place < 0 || in_place > 1) return ESPARSE_EINVAL;
+  *bytes = M ? esp_mx_gemm_workspace_bytes(M, N, K, act, act != ESPARSE_MX_ACT_16 || (in_place && K % 8 == 0)) : 0;
+  return ESPARSE_OK;
+}
+
+int esparse_mx_gemm(esparse_ctx* ctx, const void* X, const void* x_scales, long long M, long long ldx, esparse_mx_act act, esparse_dtype dtype,
+                    const void* packed_w, long long N, long long K, esparse_dtype out_dtype, void* Y, void* workspace, size_t workspace_bytes) {
+  if (!ctx) return ESPARSE_EINVAL;
+  int rc = check_dtype_or_f32(ctx, out_dtype);
+  if (rc) return rc;
+  ESP_REQUIRE(ctx, act == ESPARSE_MX_ACT_FP4 || act == ESPARSE_MX_ACT_FP8 || act == ESPARSE_MX_ACT_16, ESPARSE_EUNSUPPORTED, "act %d does not exist", (int)act);
+  if (act == ESPARSE_MX_ACT_16 && (rc = check_dtype(ctx, dtype))) return rc;
+  ESP_REQUIRE(ctx, mx_gemm_sizes(M, N, K, act), ESPARSE_EINVAL, "M = %lld, N = %lld or K = %lld out of range", M, N, K);
+  if (M == 0) return ESPARSE_OK;
+  ESP_REQUIRE(ctx, X && packed_w && Y, ESPARSE_EINVAL, "X / packed_w / Y is null");
+  if (act == ESPARSE_MX_ACT_16) {
+    ESP_REQUIRE(ctx, ldx >= K && ldx < (1ll << 40), ESPARSE_EINVAL, "ldx = %lld is less than K = %lld, or too large", ldx, K);
+    ESP_REQUIRE(ctx, aligned_to(X, 2), ESPARSE_EINVAL, "X is not aligned to its type");
+  } else {
+    ESP_REQUIRE(ctx, x_scales, ESPARSE_EINVAL, "x_scales is null");
+    ESP_REQUIRE(ctx, esp_aligned16(X) && esp_aligned16(x_scales), ESPARSE_EINVAL, "X / x_scales is not 16-byte aligned");
+  }
+  ESP_REQUIRE(ctx, esp_aligned16(packed_w) && esp_aligned16(Y), ESPARSE_EINVAL, "packed_w / Y is not 16-byte aligned");
+  const size_t need = esp_mx_gemm_workspace_bytes(M, N, K, act, esp_mx_gemm_in_place(X, ldx, K, act));
+  ESP_REQUIRE(ctx, need == 0 || workspace, ESPARSE_EINVAL, "workspace is null, %zu bytes needed", need);
+  ESP_REQUIRE(ctx, need == 0 || workspace_bytes >= need, ESPARSE_EWORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, need);
+  ESP_REQUIRE(ctx, need == 0 || aligned_to(workspace, 256), ESPARSE_EINVAL, "workspace is not 256-byte aligned");
+  const DeviceOfCall device(ctx->device);
+  ESP_HIP(ctx, device.error());
+  return esp_mx_gemm_device(ctx, X, x_scales, M, ldx, act, dtype, packed_w, N, K, out_dtype, Y, workspace);
+}
+
+int esparse_rms_norm(esparse_ctx* ctx, const void* x, long long ldx, const void* residual, long long ldr, const void* weight, long long R, long long K,
+                     double eps, esparse_dtype dtype, void* sum_out, void* y, esparse_mx_format format, void* data, void* scales) {
+  if (!ctx) return ESPARSE_EINVAL;
+  int rc = check_dtype(ctx, dtype);
+  if (rc || (rc = check_rows(ctx, R, K, "K"))) return rc;
+  ESP_REQUIRE(ctx, std::isfinite(eps) && eps >= 0, ESPARSE_EINVAL, "eps is negative or not finite");
+  if (R == 0) return ESPARSE_OK;
+  ESP_REQUIRE(ctx, x && weight, ESPARSE_EINVAL, "x / weight is null");
+  ESP_REQUIRE(ctx, y ? !data && !scales : data && scales, ESPARSE_EINVAL, "the output is either y or data and scales");
+  if (!y && (rc = check_format(ctx, format))) return rc;
+  ESP_REQUIRE(ctx, ldx >= K && (!residual || ldr >= K), ESPARSE_EINVAL, "ldx = %lld or ldr = %lld is less than K = %lld", ldx, ldr, K);
+  ESP_REQUIRE(ctx, aligned_to(x, 2) && aligned_to(residual, 2) && aligned_to(weight, 2) && aligned_to(sum_out, 2) && aligned_to(y, 2), ESPARSE_EINVAL,
+              "a pointer is not aligned to its type");
+  ESP_REQUIRE(ctx, esp_aligned16(data) && esp_aligned16(scales), ESPARSE_EINVAL, "data / scales is not 16-byte aligned");
+  // in place: element by element, or not at all
+  auto apart = [&](const void* out, size_t out_bytes, const void* in, long long ld, bool may_be_same) {
+    if (!out || !in || (may_be_same && out == in && (ld == K || R == 1))) return true;
+    const uintptr_t o = reinterpret_cast<uintptr_t>(out), i = reinterpret_cast<uintptr_t>(in), in_bytes = 2 * ((size_t)(R - 1) * (size_t)ld + (size_t)K);
+    return o + out_bytes <= i || i + in_bytes <= o;
+  };
+  const size_t bytes16 = 2 * (size_t)R * (size_t)K;
+  ESP_REQUIRE(ctx, apart(sum_out, bytes16, x, ldx, true) && apart(sum_out, bytes16, residual, ldr, true), ESPARSE_EINVAL,
+              "sum_out overlaps x or residual without being the same rows");
+  const void* out = y ? y : data;
+  size_t out_bytes = bytes16, scale_bytes = 0;
+  if (!y) (void)esparse_mx_size(R, K, format, &out_bytes, &scale_bytes);
+  for (const void* in : {x, residual, (const void*)sum_out}) {
+    const long long ld = in == x ? ldx : (in == residual ? ldr : K);
+    ESP_REQUIRE(ctx, apart(out, out_bytes, in, ld, false) && (y || apart(scales, scale_bytes, in, ld, false)), ESPARSE_EINVAL,
+                "the output overlaps an input or sum_out");
+  }
+  const DeviceOfCall device(ctx->device);
+  ESP_HIP(ctx, device.error());
+  return esp_rms_norm_device(ctx, x, ldx, residual, ldr, weight, R, K, eps, dtype, sum_out, y, format, data, scales);
+}
+
+static bool logprobs_sizes(long long R, long long V, int top) {
+  return R >= 0 && R <= kMaxRows && V >= 1 && V <= ESPARSE_MAX_VOCABULARY && top >= 0 && top <= ESPARSE_MAX_TOP && top <= V;
+}
+
+int esparse_token_logprobs_workspace(long long R, long long V, esparse_dtype dtype, int top, size_t* bytes) {
+  if (!bytes || !logprobs_sizes(R, V, top)) return ESPARSE_EINVAL;
+  if (dtype != ESPARSE_F16 && dtype != ESPARSE_BF16 && dtype != ESPARSE_F32) return ESPARSE_EUNSUPPORTED;
+  *bytes = R ? esp_token_logprobs_workspace(R, V, dtype, top) : 0;
+  return ESPARSE_OK;
+}
+
+int esparse_token_logprobs(esparse_ctx* ctx, const void* logits, long long R, long long V, long long ld, esparse_dtype dtype, const int64_t* tokens, int top,
+                           float* logprob, float* entropy, int32_t* top_ids, float* top_logprobs, void* workspace, size_t workspace_bytes) {
+  if (!ctx) return ESPARSE_EINVAL;
+  const int rc = check_dtype_or_f32(ctx, dtype);
+  if (rc) return rc;
+  ESP_REQUIRE(ctx, V <= ESPARSE_MAX_VOCABULARY, ESPARSE_EUNSUPPORTED, "V = %lld is more than %lld", V, (long long)ESPARSE_MAX_VOCABULARY);
+  ESP_REQUIRE(ctx, R >= 0 && R <= kMaxRows && V >= 1, ESPARSE_EINVAL, "R = %lld or V = %lld out of range", R, V);
+  ESP_REQUIRE(ctx, top >= 0 && top <= ESPARSE_MAX_TOP && top <= V, ESPARSE_EINVAL, "top = %d is outside [0, min(%d, V)]", top, ESPARSE_MAX_TOP);
+  if (R == 0) return ESPARSE_OK;
+  ESP_REQUIRE(ctx, logits, ESPARSE_EINVAL, "logits is null");
+  ESP_REQUIRE(ctx, ld >= V && ld < (1ll << 31), ESPARSE_EINVAL, "ld = %lld is less than V = %lld, or too large", ld, V);
+  ESP_REQUIRE(ctx, (tokens != nullptr) == (logprob != nullptr), ESPARSE_EINVAL, "tokens and logprob come together");
+  ESP_REQUIRE(ctx, top == 0 || (top_ids && top_logprobs), ESPARSE_EINVAL, "top_ids / top_logprobs is null");
+  ESP_REQUIRE(ctx, aligned_to(logits, dtype_bytes(dtype)) && aligned_to(tokens, 8) && aligned_to(logprob, 4) && aligned_to(entropy, 4) && aligned_to(top_ids, 4) &&
+                       aligned_to(top_logprobs, 4),
+              ESPARSE_EINVAL, "a pointer is not aligned to its type");
+  const size_t need = esp_token_logprobs_workspace(R, V, dtype, top);
+  ESP_REQUIRE(ctx, need == 0 || workspace, ESPARSE_EINVAL, "workspace is null, %zu bytes needed", need);
+  ESP_REQUIRE(ctx, need == 0 || workspace_bytes >= need, ESPARSE_EWORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, need);
+  ESP_REQUIRE(ctx, need == 0 || aligned_to(workspace, 256), ESPARSE_EINVAL, "workspace is not 256-byte aligned");
+  const DeviceOfCall device(ctx->device);
+  ESP_HIP(ctx, device.error());
+  return esp_token_logprobs_device(ctx, logits, R, V, ld, dtype, reinterpret_cast<const long long*>(tokens), top, logprob, entropy, top_ids, top_logprobs, workspace);
+}
+
 }  // extern "C"

@@ -30,91 +30,14 @@
 #include <atomic>
 
 #include "common.h"
+#include "intrinsics.h"
 
 #define WS_HEADER_BYTES 65536
 #define MAX_SPLIT 16
-// Kernels that need more than the default 64 KiB of dynamic LDS have that limit raised once per device; `done` is the
-// kernel's own mask of the devices where that has happened.
-template <class F>
-static hipError_t raise_dynamic_lds(std::atomic<unsigned long long>& done, int device, F* kernel, size_t bytes) {
-  const unsigned long long bit = 1ull << (device & 63);
-  if (device < 64 && (done.load(std::memory_order_acquire) & bit)) return hipSuccess;
-  hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-  if (e == hipSuccess && device < 64) done.fetch_or(bit, std::memory_order_release);
-  return e;
-}
-
 // fp32 partial tiles the workspace has room for: 16 K splits up to 128 tokens, 4 up to 512, none beyond
 static inline int esp_split_capacity(long long M) { return M <= 128 ? MAX_SPLIT : (M <= 512 ? 4 : 1); }
 #define ESP_MAX_GROUP 4  // products of one shape that may share a launch
 #define FOLD_ROWS_LDS (158 * 1024)     // of the decode kernels that keep the tokens' rows
-
-// ------------------------------------------------------------------------------------------------
-// device-only intrinsics (hipcc also parses kernels in its host pass, where these do not exist)
-// ------------------------------------------------------------------------------------------------
-__device__ __forceinline__ int wave_uniform(int v) {
-#if defined(__HIP_DEVICE_COMPILE__)
-  return __builtin_amdgcn_readfirstlane(v);
-#else
-  return v;
-#endif
-}
-// 16 bytes per lane from global memory straight into LDS: lane l lands at lds_wave_base + 16 l
-__device__ __forceinline__ void global_to_lds_16(const uint4* gsrc, uint4* lds_wave_base) {
-#if defined(__HIP_DEVICE_COMPILE__)
-  __builtin_amdgcn_global_load_lds(gsrc, lds_wave_base, 16, 0, 0);
-#else
-  (void)gsrc;
-  (void)lds_wave_base;
-#endif
-}
-// scheduling hint: the next SIZE instructions of class MASK (0x008 matrix, 0x100 LDS read) form one
-// group; consecutive groups are issued in the order the hints are written
-template <int MASK, int SIZE>
-__device__ __forceinline__ void sched_group() {
-#if defined(__HIP_DEVICE_COMPILE__)
-  __builtin_amdgcn_sched_group_barrier(MASK, SIZE, 0);
-#endif
-}
-// 4 bytes per lane from global memory straight into LDS: lane l lands at lds_wave_base + 4 l
-__device__ __forceinline__ void global_to_lds_4(const uint32_t* gsrc, uint32_t* lds_wave_base) {
-#if defined(__HIP_DEVICE_COMPILE__)
-  __builtin_amdgcn_global_load_lds(gsrc, lds_wave_base, 4, 0, 0);
-#else
-  (void)gsrc;
-  (void)lds_wave_base;
-#endif
-}
-// streaming load: the line is not kept in the caches once read (weights are read once per product)
-typedef unsigned int esp_u32x4 __attribute__((ext_vector_type(4)));
-__device__ __forceinline__ uint4 load_stream_16(const uint4* p) {
-  const esp_u32x4 v = __builtin_nontemporal_load(reinterpret_cast<const esp_u32x4*>(p));
-  return uint4{v.x, v.y, v.z, v.w};
-}
-__device__ __forceinline__ uint32_t load_stream_4(const uint32_t* p) { return __builtin_nontemporal_load(p); }
-__device__ __forceinline__ void sched_fence() {
-#if defined(__HIP_DEVICE_COMPILE__)
-  __builtin_amdgcn_sched_barrier(0);
-#endif
-}
-// NM matrix instructions with ND copies into LDS and NA LDS reads spread evenly among them: after each multiply one copy
-// and a share of the reads.  A matrix instruction occupies its pipe for 16 or 32 clocks, during which the wave can issue
-// other work; issued in bursts (all multiplies, then all copies, then all reads) the copies queue up at the
-// vector-memory issue while the matrix pipe runs dry - measured 5-6 % slower on the prefill shapes.  READS_FIRST: the
-// reads ahead of the copy in each slot (same-box comparisons: 2 % faster for the 8-wave 32x32x32 kernel, 4-8 % slower
-// for the 4-wave kernel with its deeper operand read-ahead, no difference for the other 8-wave kernels).
-template <int NM, int ND, int NA, bool READS_FIRST = false>
-__device__ __forceinline__ void sched_spread() {
-  constexpr int AP = (NA + NM - 1) / NM;
-#pragma unroll
-  for (int p = 0; p < NM; p++) {
-    sched_group<0x008, 1>();
-    if (READS_FIRST && AP > 0) sched_group<0x100, AP>();
-    if (p < ND) sched_group<0x010, 1>();
-    if (!READS_FIRST && AP > 0) sched_group<0x100, AP>();
-  }
-  if (ND > NM) sched_group<0x010, ND - NM>();
-}
 
 // ------------------------------------------------------------------------------------------------
 // instruction wrappers
@@ -179,15 +102,6 @@ __device__ __forceinline__ void expand_4_8(const uint4 v, uint32_t codes, const 
   const uint4 s1 = s_lut[(c1 < LUT48_CODES ? c1 : LUT48_CODES - 1) * COPIES + copy];
   e0 = uint4{byte_perm(v.y, v.x, s0.x), byte_perm(v.y, v.x, s0.y), byte_perm(v.y, v.x, s0.z), byte_perm(v.y, v.x, s0.w)};
   e1 = uint4{byte_perm(v.w, v.z, s1.x), byte_perm(v.w, v.z, s1.y), byte_perm(v.w, v.z, s1.z), byte_perm(v.w, v.z, s1.w)};
-}
-
-template <int DT>
-__device__ __forceinline__ floatx4_t mfma16(uint4 a, uint4 b, floatx4_t c) {
-  if (DT == ESPARSE_F16) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8_t, a), __builtin_bit_cast(half8_t, b), c, 0, 0, 0);
-  } else {
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
-  }
 }
 
 // ------------------------------------------------------------------------------------------------

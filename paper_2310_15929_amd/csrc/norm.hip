@@ -1,0 +1,196 @@
+// The norm in front of a linear layer: h = x + residual (rounded to the type, as it is kept for the next layer), y = h w / sqrt(mean(h^2) + eps),
+// y rounded once, to 16 bits or to microscaled 8 or 4 bits as the product of csrc/mx_matmul.hip takes them.
+// Bound by memory: a row stays in registers between the sum of its squares (fp32) and its output, so that every value is read and written
+// once.  NT threads work on a row, C pieces of eight channels each; 64 threads (a wave) need no barrier.
+#include <hip/hip_runtime.h>
+
+#include "mx.h"
+
+namespace {
+
+constexpr int OUT_16 = -1;  // the output in the type of the input
+
+struct NormArgs {
+  const uint16_t* x;
+  const uint16_t* residual;  // or null
+  const uint16_t* weight;
+  uint16_t* sum_out;  // h, or null; may be x or residual
+  uint16_t* y;
+  unsigned char* data;
+  uint32_t* scales;
+  long long ldx, ldr, R, K;
+  unsigned steps;
+  float eps;
+};
+
+template <int DT>
+__device__ __forceinline__ uint32_t add_pair(uint32_t a, uint32_t b) {
+  const float lo = esp_to_float<DT>((uint16_t)a) + esp_to_float<DT>((uint16_t)b);
+  const float hi = esp_to_float<DT>((uint16_t)(a >> 16)) + esp_to_float<DT>((uint16_t)(b >> 16));
+  return esp_from_float<DT>(lo) | (uint32_t)esp_from_float<DT>(hi) << 16;
+}
+__device__ __forceinline__ void store_8(uint16_t* p, long long left, const uint32_t (&v)[4]) {
+  if (left >= 8) {
+    __builtin_memcpy(p, v, 16);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; i++)
+      if (i < left) p[i] = (uint16_t)(v[i / 2] >> (16 * (i & 1)));
+  }
+}
+template <int DT>
+__device__ __forceinline__ float squares(const uint32_t (&v)[4]) {
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < 4; i++) {
+    const float lo = esp_to_float<DT>((uint16_t)v[i]), hi = esp_to_float<DT>((uint16_t)(v[i] >> 16));
+    s = __builtin_fmaf(lo, lo, s);
+    s = __builtin_fmaf(hi, hi, s);
+  }
+  return s;
+}
+
+// the sum over the NT threads of a row; every thread gets it.  `buf`: one float per wave
+template <int NT>
+__device__ __forceinline__ float row_sum(float v, float* buf) {
+#pragma unroll
+  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+  if constexpr (NT > 64) {
+    const int wave = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) == 0) buf[wave] = v;
+    __syncthreads();
+    v = 0.f;
+#pragma unroll
+    for (int i = 0; i < NT / 64; i++) v += buf[i];
+  }
+  return v;
+}
+
+// output of one piece of eight channels.  Lanes of pieces behind the row's last channel take part (zeros in the padding of a
+// microscaled row); `chunk` differs by one between neighbouring lanes and starts at a multiple of 16
+template <int DT, int OUT>
+__device__ __forceinline__ void norm_out(const NormArgs& a, long long row, unsigned chunk, const uint32_t (&h)[4], const uint32_t (&w)[4], float inv) {
+  float v[8];
+#pragma unroll
+  for (int i = 0; i < 4; i++) {
+    v[2 * i] = esp_to_float<DT>((uint16_t)h[i]) * inv * esp_to_float<DT>((uint16_t)w[i]);
+    v[2 * i + 1] = esp_to_float<DT>((uint16_t)(h[i] >> 16)) * inv * esp_to_float<DT>((uint16_t)(w[i] >> 16));
+  }
+  if constexpr (OUT == OUT_16) {
+    uint32_t o[4];
+#pragma unroll
+    for (int i = 0; i < 4; i++) o[i] = esp_from_float<DT>(v[2 * i]) | (uint32_t)esp_from_float<DT>(v[2 * i + 1]) << 16;
+    store_8(a.y + row * a.K + (long long)chunk * 8, a.K - (long long)chunk * 8, o);
+  } else {
+    if (chunk >= a.steps * 16) return;  // (whole groups of 16 lanes)
+#pragma unroll
+    for (int i = 0; i < 8; i++)
+      if ((long long)chunk * 8 + i >= a.K) v[i] = 0.f;  // (0 times an infinite 1 / norm is no 0)
+    const unsigned e = mx_block_exponent<OUT>(v);
+    mx_store<OUT>(a.data + row * ((long long)a.steps * (OUT == ESPARSE_MX_FP4 ? 64 : 128)), chunk, mx_encode<OUT>(v, e),
+                  a.scales + (long long)(chunk >> 4) * a.R + row, e, threadIdx.x);
+  }
+}
+
+template <int DT, int OUT, int NT, int C>
+__global__ void __launch_bounds__(NT < 256 ? 256 : NT) k_rms_norm(const NormArgs a) {
+  constexpr int ROWS = NT < 256 ? 256 / NT : 1;
+  __shared__ float buf[NT > 64 ? NT / 64 : 1];
+  const unsigned t = threadIdx.x % NT;
+  const long long row = (long long)blockIdx.x * ROWS + threadIdx.x / NT;
+  if (row >= a.R) return;  // (whole waves, and no barrier where a workgroup has several rows)
+  uint32_t h[C][4], r[C][4], w[C][4];
+#pragma unroll
+  for (int j = 0; j < C; j++) load_8(a.x + row * a.ldx + (long long)(j * NT + t) * 8, a.K - (long long)(j * NT + t) * 8, h[j]);
+  if (a.residual) {
+#pragma unroll
+    for (int j = 0; j < C; j++) load_8(a.residual + row * a.ldr + (long long)(j * NT + t) * 8, a.K - (long long)(j * NT + t) * 8, r[j]);
+  }
+#pragma unroll
+  for (int j = 0; j < C; j++) load_8(a.weight + (long long)(j * NT + t) * 8, a.K - (long long)(j * NT + t) * 8, w[j]);
+  float s = 0.f;
+#pragma unroll
+  for (int j = 0; j < C; j++) {
+    if (a.residual) {
+#pragma unroll
+      for (int i = 0; i < 4; i++) h[j][i] = add_pair<DT>(h[j][i], r[j][i]);
+    }
+    if (a.sum_out) store_8(a.sum_out + row * a.K + (long long)(j * NT + t) * 8, a.K - (long long)(j * NT + t) * 8, h[j]);
+    s += squares<DT>(h[j]);
+  }
+  const float inv = 1.f / __builtin_sqrtf(row_sum<NT>(s, buf) / (float)a.K + a.eps);
+#pragma unroll
+  for (int j = 0; j < C; j++) norm_out<DT, OUT>(a, row, j * NT + t, h[j], w[j], inv);
+}
+
+// rows that do not fit the registers of a workgroup are read twice
+template <int DT, int OUT>
+__global__ void __launch_bounds__(1024) k_rms_norm_long(const NormArgs a) {
+  __shared__ float buf[16];
+  const long long row = blockIdx.x;
+  const unsigned chunks = a.steps * 16, t = threadIdx.x;
+  float s = 0.f;
+  uint32_t h[4], r[4], w[4];
+  for (unsigned c = t; c < chunks; c += 1024) {
+    const long long at = (long long)c * 8, left = a.K - at;
+    load_8(a.x + row * a.ldx + at, left, h);
+    if (a.residual) {
+      load_8(a.residual + row * a.ldr + at, left, r);
+#pragma unroll
+      for (int i = 0; i < 4; i++) h[i] = add_pair<DT>(h[i], r[i]);
+    }
+    if (a.sum_out) store_8(a.sum_out + row * a.K + at, left, h);
+    s += squares<DT>(h);
+  }
+  const float inv = 1.f / __builtin_sqrtf(row_sum<1024>(s, buf) / (float)a.K + a.eps);
+  for (unsigned c0 = 0; c0 < chunks; c0 += 1024) {
+    const unsigned c = c0 + t;
+    const long long at = (long long)c * 8, left = a.K - at;
+    if (a.sum_out) {  // this thread's own stores (x or the residual may be gone)
+      load_8(a.sum_out + row * a.K + at, left, h);
+    } else {
+      load_8(a.x + row * a.ldx + at, left, h);
+      if (a.residual) {
+        load_8(a.residual + row * a.ldr + at, left, r);
+#pragma unroll
+        for (int i = 0; i < 4; i++) h[i] = add_pair<DT>(h[i], r[i]);
+      }
+    }
+    load_8(a.weight + at, left, w);
+    norm_out<DT, OUT>(a, row, c, h, w, inv);
+  }
+}
+
+template <int DT, int OUT>
+hipError_t launch(const NormArgs& a, hipStream_t st) {
+  const unsigned chunks = a.steps * 16;
+#define GO(NT, C) \
+  hipLaunchKernelGGL((k_rms_norm<DT, OUT, NT, C>), dim3((unsigned)((a.R + (NT < 256 ? 256 / NT : 1) - 1) / (NT < 256 ? 256 / NT : 1))), dim3(NT < 256 ? 256 : NT), 0, st, a)
+  if (chunks <= 64) GO(64, 1);
+  else if (chunks <= 256) GO(256, 1);
+  else if (chunks <= 512) GO(256, 2);
+  else if (chunks <= 1024) GO(256, 4);
+  else if (chunks <= 2048) GO(1024, 2);
+  else if (chunks <= 4096) GO(1024, 4);
+  else hipLaunchKernelGGL((k_rms_norm_long<DT, OUT>), dim3((unsigned)a.R), dim3(1024), 0, st, a);
+#undef GO
+  return hipGetLastError();
+}
+
+}  // namespace
+
+int esp_rms_norm_device(esparse_ctx* ctx, const void* x, long long ldx, const void* residual, long long ldr, const void* weight, long long R, long long K,
+                        double eps, int dtype, void* sum_out, void* y, int fmt, void* data, void* scales) {
+  const NormArgs a = {(const uint16_t*)x, (const uint16_t*)residual, (const uint16_t*)weight, (uint16_t*)sum_out, (uint16_t*)y, (unsigned char*)data,
+                      (uint32_t*)scales, ldx, ldr, R, K, (unsigned)((K + 127) / 128), (float)eps};
+  if (dtype == ESPARSE_F16) {
+    if (y) ESP_HIP(ctx, (launch<ESPARSE_F16, OUT_16>(a, ctx->stream)));
+    else if (fmt == ESPARSE_MX_FP4) ESP_HIP(ctx, (launch<ESPARSE_F16, ESPARSE_MX_FP4>(a, ctx->stream)));
+    else ESP_HIP(ctx, (launch<ESPARSE_F16, ESPARSE_MX_FP8>(a, ctx->stream)));
+  } else {
+    if (y) ESP_HIP(ctx, (launch<ESPARSE_BF16, OUT_16>(a, ctx->stream)));
+    else if (fmt == ESPARSE_MX_FP4) ESP_HIP(ctx, (launch<ESPARSE_BF16, ESPARSE_MX_FP4>(a, ctx->stream)));
+    else ESP_HIP(ctx, (launch<ESPARSE_BF16, ESPARSE_MX_FP8>(a, ctx->stream)));
+  }
+  return ESPARSE_OK;
+}

@@ -1,0 +1,509 @@
+"""The operators around a 4-bit linear layer on the GPU, against plain 64-bit implementations (oracle/operators_oracle.py).
+
+Tolerances are derived, not fitted.  A rounding to 16 bits is off by at most half a step: 2^-8 (bf16), 2^-11 (f16) of the value.  A sum of n products
+in fp32 is off by at most n 2^-23 times the sum of their magnitudes (one step of truncation for each addition).  With 8-bit activations the scaled matrix
+instruction brings the products of eight consecutive channels to the largest of them, with exponent p, and cuts each to a multiple of 2^(p - 13): the seven
+others lose less than 2^-13 of the largest each.
+"""
+import ctypes as C
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2310_15929_amd as esp
+from oracle import operators_oracle as orc
+
+pytestmark = pytest.mark.gpu
+
+TORCH = {"f16": torch.float16, "bf16": torch.bfloat16, "f32": torch.float32}
+HALF = {torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 ** -8, torch.float32: 2.0 ** -24}
+TINY = {torch.float16: 2.0 ** -25, torch.bfloat16: 2.0 ** -134, torch.float32: 2.0 ** -150}  # half a step of the smallest numbers
+FMT = {"fp4": esp.MX_FP4, "fp8": esp.MX_FP8}
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    assert torch.cuda.is_available()
+    return esp.Context(0)
+
+
+def _rng(*key):
+    return np.random.default_rng([int.from_bytes(str(k).encode(), "little") % (1 << 31) for k in key])
+
+
+def _features(rng, R, K, dtype):
+    x = rng.standard_normal((R, K)) * np.exp(rng.standard_normal(K))
+    return torch.from_numpy(x).to(TORCH[dtype])
+
+
+def _dev(a):
+    return torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+def _mx(x64, fmt):
+    """(MX on the device, its values float64 [R, K]) from the oracle."""
+    code, E = orc.mx_quantize(x64, fmt)
+    return esp.MX(_dev(orc.mx_data(code, fmt)), _dev(orc.mx_scales(E)), x64.shape[1], fmt), orc.mx_values(code, E, fmt)[:, : x64.shape[1]]
+
+
+def _assert_mx(got, x64, fmt, what=""):
+    code, E = orc.mx_quantize(x64, fmt)
+    assert np.array_equal(got.scales.cpu().numpy(), orc.mx_scales(E)), what
+    assert np.array_equal(got.data.cpu().numpy(), orc.mx_data(code, fmt)), what
+
+
+def _np(t):
+    return t.double().cpu().numpy()
+
+
+# ---- quantisation -----------------------------------------------------------------------------------
+@pytest.mark.parametrize("fmt", ["fp4", "fp8"])
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("R,K", [(1, 1), (1, 32), (3, 31), (2, 128), (17, 129), (16, 512), (33, 515), (5, 1000), (40, 4096)])
+def test_quantize_codes_and_scales(ctx, R, K, dtype, fmt):
+    x = _features(_rng(R, K, dtype, fmt), R, K, dtype)
+    _assert_mx(ctx.mx_quantize(x.cuda(), FMT[fmt]), x.double().numpy(), FMT[fmt])
+
+
+@pytest.mark.parametrize("fmt", ["fp4", "fp8"])
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_quantize_every_16_bit_value(ctx, dtype, fmt):
+    """All finite values, each beside a largest value of every distance that matters: blocks of one value, its half, ... and the block's largest."""
+    u = torch.arange(65536, dtype=torch.int32).to(torch.int16).view(TORCH[dtype])
+    u = u[torch.isfinite(u)]
+    for shift in (0, 1, 3, 6, 10, 16):   # the block's largest value: the value times 2^shift, where that is one
+        top = (u.double() * 2.0 ** shift).to(TORCH[dtype])
+        top = torch.where(torch.isfinite(top), top, u)
+        x = torch.zeros(u.numel(), 32, dtype=TORCH[dtype])
+        x[:, 3], x[:, 30] = u, top
+        x[:, 17] = (u.double() * -0.625).to(TORCH[dtype])
+        x = x.reshape(-1, 128) if u.numel() % 4 == 0 else x
+        _assert_mx(ctx.mx_quantize(x.cuda(), FMT[fmt]), x.double().numpy(), FMT[fmt], f"shift {shift}")
+
+
+@pytest.mark.parametrize("fmt", ["fp4", "fp8"])
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+def test_quantize_blocks_that_are_not_finite(ctx, dtype, fmt):
+    x = _features(_rng("nan", dtype), 6, 200, dtype)
+    x[0, 5], x[1, 40], x[2, 199], x[3, :] = math.nan, math.inf, -math.inf, 0.0
+    q = ctx.mx_quantize(x.cuda(), FMT[fmt])
+    _assert_mx(q, x.double().numpy(), FMT[fmt])
+    v = _np(ctx.mx_dequantize(q, TORCH[dtype]))
+    assert np.isnan(v[0, :32]).all() and np.isfinite(v[0, 32:]).all() and np.isnan(v[1, 32:64]).all() and np.isnan(v[2, 192:]).all()
+    assert (v[3] == 0).all() and np.isfinite(v[4:]).all()
+
+
+def test_quantize_f32_extremes(ctx):
+    x = np.zeros((4, 128), np.float32)
+    x[0, :4] = [1e-45, 3e-45, -1e-40, 1e-39]      # subnormal: the scale stays at 2^-127
+    x[0, 32:35] = [3.4e38, -1e38, 1e30]
+    x[1, 64:66] = [np.nextafter(np.float32(1), np.float32(0)), 2.0 ** -30]
+    x[2, 0] = np.float32(2.0) ** -126
+    x[3, 96] = -7.9
+    for fmt in FMT.values():
+        _assert_mx(ctx.mx_quantize(_dev(x), fmt), x.astype(np.float64), fmt)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("offset,ld", [(0, 300), (1, 301), (3, 517), (8, 264)])
+def test_quantize_rows_apart_and_unaligned(ctx, dtype, offset, ld):
+    K = 261
+    base = _features(_rng("strided", ld), 1, 19 * ld + offset, dtype)[0].cuda()
+    x = torch.as_strided(base, (19, K), (ld, 1), offset)
+    _assert_mx(ctx.mx_quantize(x, esp.MX_FP8), x.double().cpu().numpy(), esp.MX_FP8)
+
+
+@pytest.mark.parametrize("fmt", ["fp4", "fp8"])
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("R,K", [(1, 1), (3, 33), (18, 130), (5, 1003), (16, 2048)])
+def test_dequantize(ctx, R, K, dtype, fmt):
+    rng = _rng("read", R, K)
+    q, want = _mx(rng.standard_normal((R, K)) * 10.0 ** rng.integers(-6, 4, (R, 1)), FMT[fmt])
+    got = ctx.mx_dequantize(q, TORCH[dtype])
+    assert torch.equal(got.cpu(), torch.from_numpy(want).to(TORCH[dtype]))
+
+
+@pytest.mark.parametrize("fmt", ["fp4", "fp8"])
+def test_dequantize_every_code_and_scale(ctx, fmt):
+    n = 16 if fmt == "fp4" else 256
+    code = np.tile(np.arange(n, dtype=np.uint8), 256 * 256 // n).reshape(256, 256)
+    E = np.repeat(np.arange(256, dtype=np.uint8)[:, None], 8, 1)
+    q = esp.MX(_dev(orc.mx_data(code, FMT[fmt])), _dev(orc.mx_scales(E)), 256, FMT[fmt])
+    want = torch.from_numpy(orc.mx_values(code, E, FMT[fmt]))
+    for dtype in (torch.float32, torch.bfloat16, torch.float16):
+        got, w = ctx.mx_dequantize(q, dtype).cpu(), want.float().to(dtype)
+        assert torch.equal(torch.isnan(got), torch.isnan(w)) and torch.equal(torch.nan_to_num(got, nan=1.0), torch.nan_to_num(w, nan=1.0))
+
+
+# ---- product ----------------------------------------------------------------------------------------
+@pytest.mark.parametrize("N,K", [(1, 1), (16, 128), (17, 130), (64, 96), (100, 513), (200, 1024)])
+def test_pack(ctx, N, K):
+    x = _rng("pack", N, K).standard_normal((N, K))
+    code, E = orc.mx_quantize(x, orc.FP4)
+    got = ctx.mx_pack(_mx(x, orc.FP4)[0])
+    assert (got.N, got.K) == (N, K) and np.array_equal(got.packed.cpu().numpy(), orc.mx_pack(code, E))
+
+
+def _assert_product(got, x, w, dtype, act, what=""):
+    """Each output is within its rounding and the error of a sum of K products in fp32, with 8-bit activations that of their products too."""
+    want, size = x @ w.T, np.abs(x) @ np.abs(w).T
+    before = (x.shape[1] + 16) * 2.0 ** -23 * size
+    if act == "fp8":
+        top = [np.abs(np.pad(v, ((0, 0), (0, -v.shape[1] % 8)))).reshape(v.shape[0], -1, 8).max(2) for v in (x, w)]
+        before = before + 7 * 2.0 ** -13 * (top[0] @ top[1].T)
+    bound = HALF[dtype] * np.abs(want) + before * (1 + HALF[dtype]) + TINY[dtype]
+    err = np.abs(_np(got) - want)
+    assert got.shape == want.shape and (err <= bound).all(), f"{what} {np.max(err / bound)} at {np.unravel_index(np.argmax(err / bound), err.shape)}"
+
+
+def _product(ctx, M, N, K, act, dtype, out=None, seed=0):
+    rng = _rng("product", M, N, K, act, dtype, seed)
+    w, w64 = _mx(rng.standard_normal((N, K)) * K ** -0.5, orc.FP4)
+    if act == "16":
+        xt = _features(rng, M, K, dtype)
+        X, x64 = xt.cuda(), xt.double().numpy()
+    else:
+        X, x64 = _mx(rng.standard_normal((M, K)) * np.exp(rng.standard_normal(K)), FMT[act])
+    out = TORCH[out or dtype]
+    _assert_product(ctx.mx_gemm(X, ctx.mx_pack(w), dtype=out), x64, w64, out, act, f"{M} x {N} x {K} {act}")
+
+
+@pytest.mark.parametrize("act", ["16", "fp8", "fp4"])
+@pytest.mark.parametrize("N,K", [(1, 1), (15, 32), (64, 128), (65, 100), (130, 257), (300, 1000), (512, 2048)])
+@pytest.mark.parametrize("M", [1, 2, 7, 16, 17, 33, 64, 65, 130])
+def test_product(ctx, M, N, K, act):
+    _product(ctx, M, N, K, act, "bf16" if (M + N) % 2 else "f16")
+
+
+@pytest.mark.parametrize("act", ["16", "fp8", "fp4"])
+@pytest.mark.parametrize("M,N,K", [(256, 512, 640), (257, 1030, 384), (333, 1003, 620), (700, 2100, 1100), (1024, 1536, 512), (48, 5003, 3020), (3, 9000, 4096), (1, 22016, 1024)])
+def test_product_larger(ctx, M, N, K, act):
+    _product(ctx, M, N, K, act, "f16" if M % 2 else "bf16")
+
+
+@pytest.mark.parametrize("act", ["16", "fp8", "fp4"])
+@pytest.mark.parametrize("M,N", [(5, 70), (40, 96), (140, 131), (300, 640)])
+def test_product_in_32_bits(ctx, M, N, act):
+    _product(ctx, M, N, 520, act, "f16", out="f32")
+
+
+@pytest.mark.parametrize("M", [1, 20, 150])
+def test_product_of_each_type_pair(ctx, M):
+    """16-bit activations of one type, outputs of the other."""
+    _product(ctx, M, 192, 256, "16", "f16", out="bf16")
+    _product(ctx, M, 192, 256, "16", "bf16", out="f16")
+
+
+@pytest.mark.parametrize("M", [1, 16, 40, 200])
+@pytest.mark.parametrize("offset,ld", [(0, 264), (1, 257), (8, 300), (4, 1000)])
+def test_product_rows_apart_and_unaligned(ctx, M, offset, ld):
+    rng, K, N = _rng("rows", M, ld), 256, 80
+    base = _features(rng, 1, M * ld + offset, "bf16")[0].cuda()
+    x = torch.as_strided(base, (M, K), (ld, 1), offset)
+    w, w64 = _mx(rng.standard_normal((N, K)), orc.FP4)
+    _assert_product(ctx.mx_gemm(x, ctx.mx_pack(w)), _np(x), w64, torch.bfloat16, "16")
+
+
+@pytest.mark.parametrize("act", ["16", "fp8", "fp4"])
+@pytest.mark.parametrize("M", [1, 30, 150])
+def test_product_of_bad_blocks_stays_in_their_rows(ctx, M, act):
+    """A NaN scale reaches the outputs of its row and of its token only; a padded tail holds none."""
+    rng, N, K = _rng("bad", M), 70, 290
+    x, w = rng.standard_normal((M, K)), rng.standard_normal((N, K))
+    w[3, 200], x[M - 1, 289] = math.nan, math.nan
+    wq, w64 = _mx(w, orc.FP4)
+    if act == "16":
+        xt = torch.from_numpy(x).bfloat16()
+        X, x64 = xt.cuda(), xt.double().numpy()
+    else:
+        X, x64 = _mx(x, FMT[act])
+    got = _np(ctx.mx_gemm(X, ctx.mx_pack(wq), dtype=torch.float32))
+    bad = np.zeros((M, N), bool)
+    bad[:, 3] = bad[M - 1] = True
+    assert np.array_equal(np.isnan(got), bad)
+    _assert_product(torch.from_numpy(np.where(bad, 0, got)[:, 4:]).float(), np.nan_to_num(x64) * (np.arange(M) < M - 1)[:, None], w64[4:], torch.float32, act)
+
+
+def test_product_with_wide_scales(ctx):
+    """Scales from 2^-60 to 2^60 in weights and activations: no block's products disturb another's."""
+    rng, M, N, K = _rng("wide"), 20, 48, 384
+    x = rng.standard_normal((M, K)) * np.ldexp(1.0, rng.integers(-30, 30, (M, K // 32))).repeat(32, 1)
+    w = rng.standard_normal((N, K)) * np.ldexp(1.0, rng.integers(-30, 30, (N, K // 32))).repeat(32, 1)
+    wq, w64 = _mx(w, orc.FP4)
+    for act in ("fp8", "fp4"):
+        X, x64 = _mx(x, FMT[act])
+        _assert_product(ctx.mx_gemm(X, ctx.mx_pack(wq), dtype=torch.float32), x64, w64, torch.float32, act, act)
+    xt = torch.from_numpy(x).bfloat16()
+    _assert_product(ctx.mx_gemm(xt.cuda(), ctx.mx_pack(wq), dtype=torch.float32), xt.double().numpy(), w64, torch.float32, "16", "16")
+
+
+def test_product_leaves_other_memory_alone(ctx):
+    """Guards around the output and behind the workspace keep their pattern, whatever part of a tile is used."""
+    for M, N, K, act in [(1, 5, 40, "16"), (19, 33, 130, "fp8"), (70, 129, 300, "16"), (150, 257, 256, "fp4"), (260, 300, 1000, "fp8"), (300, 1001, 333, "16")]:
+        rng = _rng("guard", M, N)
+        w, w64 = _mx(rng.standard_normal((N, K)), orc.FP4)
+        X, x64 = (_features(rng, M, K, "f16").cuda(), None) if act == "16" else _mx(rng.standard_normal((M, K)), FMT[act])
+        buf = torch.full((M * N + 512,), 7.25, dtype=torch.float16, device="cuda")
+        y = buf[256:256 + M * N].view(M, N)
+        ctx.mx_gemm(X, ctx.mx_pack(w), out=y, dtype=torch.float16)
+        assert (buf[:256] == 7.25).all() and (buf[256 + M * N:] == 7.25).all()
+        _assert_product(y, _np(X) if act == "16" else x64, w64, torch.float16, act)
+
+
+def test_product_is_the_same_every_time(ctx):
+    for M, N, K in [(3, 4096, 4096), (40, 512, 4096), (333, 1003, 1000)]:
+        x = _features(_rng("again", M), M, K, "bf16").cuda()
+        w = ctx.mx_pack(_mx(_rng("again w", N).standard_normal((N, K)), orc.FP4)[0])
+        first = ctx.mx_gemm(x, w)
+        assert all(torch.equal(first, ctx.mx_gemm(x, w)) for _ in range(3))
+
+
+# ---- norm -------------------------------------------------------------------------------------------
+def _norm_bound(y, K, half, tiny):
+    # sum of K squares (relative K 2^-23), its root halves that; root, division, two products: 2^-24 each and the sum's division
+    return np.abs(y) * (half + K * 2.0 ** -24 + 6 * 2.0 ** -24) + tiny
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("residual", [False, True])
+@pytest.mark.parametrize("R,K", [(1, 1), (1, 8), (5, 31), (3, 512), (70, 513), (2, 2048), (3, 4097), (300, 4096), (2, 8192), (3, 13824), (2, 16385), (2, 33000)])
+def test_norm(ctx, R, K, residual, dtype):
+    rng = _rng("norm", R, K)
+    x, r = _features(rng, R, K, dtype), _features(rng, R, K, dtype)
+    w = torch.from_numpy(rng.standard_normal(K)).to(TORCH[dtype])
+    y, h = ctx.rms_norm(x.cuda(), w.cuda(), 1e-5, residual=r.cuda() if residual else None)
+    h64 = (x.double() + r.double()).to(TORCH[dtype]).double() if residual else x.double()
+    assert torch.equal(h.double().cpu(), h64)
+    want = orc.rms_norm(h64.numpy(), w.double().numpy(), 1e-5)
+    assert (np.abs(_np(y) - want) <= _norm_bound(want, K, HALF[TORCH[dtype]], TINY[TORCH[dtype]])).all()
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("fmt", ["fp4", "fp8"])
+@pytest.mark.parametrize("R,K", [(1, 1), (5, 33), (3, 512), (70, 515), (20, 4096), (3, 4097), (2, 13824), (2, 33000)])
+def test_norm_to_mx(ctx, R, K, fmt, dtype):
+    """The codes are those of the exact norm, but where the sum's rounding moves a value across the middle of two of them or a block's largest across a power of two."""
+    rng = _rng("norm mx", R, K)
+    x, r = _features(rng, R, K, dtype), _features(rng, R, K, dtype)
+    w = torch.from_numpy(rng.standard_normal(K)).to(TORCH[dtype])
+    q, h = ctx.rms_norm(x.cuda(), w.cuda(), 1e-5, residual=r.cuda(), fmt=FMT[fmt])
+    h64 = (x.double() + r.double()).to(TORCH[dtype]).double().numpy()
+    want = orc.rms_norm(h64, w.double().numpy(), 1e-5)
+    off = K * 2.0 ** -24 + 6 * 2.0 ** -24
+    got = _np(ctx.mx_dequantize(q, torch.float32))
+    lo, hi = (np.stack([orc.mx_values(*orc.mx_quantize(want * (1 + d), FMT[fmt]), FMT[fmt])[:, :K] for d in (-off, 0.0, off)]) for _ in range(2))
+    lo, hi = lo.min(0), hi.max(0)
+    assert ((got >= lo) & (got <= hi)).all()
+    # the channels behind the last are zeros
+    kp = q.data.shape[1] * (2 if fmt == "fp4" else 1)
+    tail = ctx.mx_dequantize(esp.MX(q.data, q.scales, kp, FMT[fmt]), torch.float32)[:, K:]
+    assert (tail == 0).all()
+
+
+def test_norm_in_place_and_rows_apart(ctx):
+    rng, R, K = _rng("place"), 21, 700
+    x, r = _features(rng, R, K, "bf16").cuda(), _features(rng, R, K, "bf16").cuda()
+    w = torch.from_numpy(rng.standard_normal(K)).bfloat16().cuda()
+    y, h = ctx.rms_norm(x, w, residual=r)
+    for where in ("x", "residual"):
+        a, b = x.clone(), r.clone()
+        y2, h2 = ctx.rms_norm(a, w, residual=b, sum_out=a if where == "x" else b)
+        assert torch.equal(h2, h) and torch.equal(y2, y) and torch.equal(b if where == "x" else a, r if where == "x" else x)
+    wide = torch.zeros(R, 1501, dtype=torch.bfloat16, device="cuda")
+    wide[:, 3:703], wide[:, 801:1501] = x, r
+    y2, h2 = ctx.rms_norm(wide[:, 3:703], w, residual=wide[:, 801:1501])
+    assert torch.equal(h2, h) and torch.equal(y2, y)
+    assert ctx.rms_norm(x, w)[1] is x
+    with pytest.raises(esp.EsparseError, match="overlaps"):
+        ctx.rms_norm(x[:-1], w, residual=r[:-1], sum_out=x[1:])
+
+
+def test_norm_of_extreme_rows(ctx):
+    w = torch.ones(256, dtype=torch.bfloat16, device="cuda")
+    x = torch.ones(5, 256, dtype=torch.bfloat16, device="cuda")
+    x[0], x[1, 7], x[2, 7], x[3] = 0, math.nan, math.inf, 2.0 ** -100
+    y = ctx.rms_norm(x, w, 1e-6)[0].float().cpu()
+    assert (y[0] == 0).all() and torch.isnan(y[1]).all() and torch.isnan(y[2, 7]) and (y[2, :7] == 0).all() and (y[4] == 1).all()
+    assert torch.allclose(y[3], torch.full((256,), 2.0 ** -100 * 1000.0), rtol=0.01, atol=0)
+    q = ctx.rms_norm(x, w, 1e-6, fmt=esp.MX_FP8)[0]
+    v = ctx.mx_dequantize(q, torch.float32).cpu()
+    assert (v[0] == 0).all() and torch.isnan(v[1]).all() and torch.isnan(v[2, :32]).all() and (v[2, 32:] == 0).all()
+    # a row of zeros without eps: 0 times infinity, in the row's channels and not in the padding
+    q = ctx.rms_norm(torch.zeros(2, 40, dtype=torch.bfloat16, device="cuda"), w[:40].contiguous(), 0.0, fmt=esp.MX_FP8)[0]
+    assert torch.isnan(ctx.mx_dequantize(q, torch.float32)).all() and (q.scales.cpu()[0, :, 2:] == 0).all()
+
+
+# ---- log probabilities ------------------------------------------------------------------------------
+def _assert_logprobs(ctx, x, tokens, top, what=""):
+    x64 = x.double().cpu().numpy()
+    lp, ent, ids, tops = orc.token_logprobs(x64, tokens, top)
+    r = ctx.token_logprobs(x, torch.tensor(tokens, dtype=torch.int64, device="cuda"), top=top)
+    V = x.shape[1]
+    # ln s: the terms' errors (exp 2^-22, its argument |d| 2^-23 with p |d| at most 0.37) and the sum's, 2 ln2(V) 2^-24 relative as a tree over runs of 128
+    s_err = 2.0 ** -21 + (128 + 2 * math.log2(V + 1)) * 2.0 ** -24
+    def bound(v):
+        return s_err + 4 * 2.0 ** -24 * (np.abs(v) + 32)
+    def check(got, want, tol):
+        assert np.array_equal(np.isnan(got), np.isnan(want)), what
+        fine = np.isfinite(want)
+        assert np.array_equal(got[~fine & ~np.isnan(want)], want[~fine & ~np.isnan(want)]), what
+        assert (np.abs(got - want)[fine] <= tol[fine]).all(), (what, np.max((np.abs(got - want) / tol)[fine]))
+    check(_np(r.logprob), lp, bound(np.nan_to_num(lp, posinf=0, neginf=0)))
+    # t / s: each term's p d is off by p |d| times the same, the sum of p |d| / s is at most ln V
+    check(_np(r.entropy), ent, bound(np.nan_to_num(ent)) + s_err * (2 + 2 * math.log(V + 1)))
+    if top:
+        assert np.array_equal(r.top_ids.cpu().numpy(), ids), what
+        check(_np(r.top_logprobs), tops, bound(np.nan_to_num(tops, posinf=0, neginf=0)))
+    else:
+        assert r.top_ids is None and r.top_logprobs is None
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("R,V,top", [(1, 1, 1), (3, 2, 2), (2, 31, 20), (5, 100, 32), (4, 1000, 5), (1, 5003, 0), (7, 16384, 20), (3, 32000, 1), (2, 50021, 32),
+                                     (8, 131072, 20), (1, 131073, 3), (2, 300001, 20), (40, 8191, 7), (300, 4099, 4)])
+def test_logprobs(ctx, R, V, top, dtype):
+    rng = _rng("lp", R, V, top)
+    x = torch.from_numpy(rng.standard_normal((R, V)) * 3).to(TORCH[dtype]).cuda()
+    _assert_logprobs(ctx, x, [int(t) for t in rng.integers(0, V, R)], top)
+
+
+@pytest.mark.parametrize("V", [40, 5000, 70000, 140000])
+def test_logprobs_of_masked_rows(ctx, V):
+    """Minus infinity in places, everywhere, everywhere but one; infinities and NaN; equal values; padding and foreign tokens."""
+    rng = _rng("mask", V)
+    for dtype in ("f16", "bf16", "f32"):
+        x = torch.from_numpy(rng.standard_normal((12, V)) * 2).to(TORCH[dtype])
+        x[0, rng.random(V) < 0.7] = -math.inf
+        x[1] = -math.inf
+        x[2] = -math.inf
+        x[2, V // 2] = -5.0
+        x[3, V - 1] = math.nan
+        x[4, 3] = math.inf
+        x[5] = 1.5
+        x[6] = torch.where(torch.arange(V) % 3 == 0, 2.0, -1.0).to(TORCH[dtype])
+        x[7] = 0.0
+        x[7, 5] = -0.0
+        x[8] = torch.finfo(TORCH[dtype]).min
+        x[9, :] = math.nan
+        x[10, 1] = -math.nan
+        x[11, V - 3:] = 60.0
+        tokens = [0, 1, V // 2, 0, 1, 2, -1, -100, 7, 3, 0, V]
+        _assert_logprobs(ctx, x.cuda(), tokens, min(20, V), f"{V} {dtype}")
+        _assert_logprobs(ctx, x.cuda(), [t - 1 if 0 < t < V else t for t in tokens], 1, f"{V} {dtype}")
+
+
+def test_logprobs_far_from_zero(ctx):
+    """A common offset of the logits takes no precision beyond that of the logits themselves."""
+    rng = _rng("far")
+    x = torch.from_numpy(rng.standard_normal((6, 9000)) * 3 + np.array([0, 1e3, -1e3, 3e4, -3e4, 1e5])[:, None]).float()
+    _assert_logprobs(ctx, x.cuda(), [5] * 6, 8)
+
+
+def test_logprobs_rows_apart_and_unaligned(ctx):
+    rng, V = _rng("lp rows"), 3001
+    for dtype in ("f16", "bf16", "f32"):
+        base = torch.from_numpy(rng.standard_normal(9 * 3333 + 5)).to(TORCH[dtype]).cuda()
+        for offset in (0, 1, 3):
+            _assert_logprobs(ctx, torch.as_strided(base, (9, V), (3333, 1), offset), list(range(9)), 6, f"{dtype} {offset}")
+
+
+def test_logprobs_without_tokens(ctx):
+    x = torch.randn(3, 500, device="cuda", generator=torch.Generator("cuda").manual_seed(1))
+    r = ctx.token_logprobs(x, top=2)
+    assert r.logprob is None and torch.equal(r.top_ids.long(), torch.topk(x, 2).indices)
+
+
+def test_logprobs_do_not_depend_on_other_rows(ctx):
+    x = torch.randn(700, 3000, device="cuda", generator=torch.Generator("cuda").manual_seed(2))
+    t = torch.arange(700, device="cuda")
+    many, one = ctx.token_logprobs(x, t, top=5), ctx.token_logprobs(x[:700].clone(), t, top=5)
+    assert torch.equal(many.logprob, one.logprob) and torch.equal(many.entropy, one.entropy) and torch.equal(many.top_ids, one.top_ids)
+
+
+# ---- empty inputs -------------------------------------------------------------------------------------
+def test_no_rows(ctx):
+    x = torch.zeros(0, 64, dtype=torch.bfloat16, device="cuda")
+    w = ctx.mx_pack(ctx.mx_quantize(torch.ones(8, 64, dtype=torch.bfloat16, device="cuda"), esp.MX_FP4))
+    q = ctx.mx_quantize(x, esp.MX_FP8)
+    assert ctx.mx_dequantize(q).shape == (0, 64) and ctx.mx_gemm(q, w).shape == (0, 8) and ctx.mx_gemm(x, w).shape == (0, 8)
+    assert ctx.rms_norm(x, torch.ones(64, dtype=torch.bfloat16, device="cuda"), residual=x)[0].shape == (0, 64)
+    r = ctx.token_logprobs(x, torch.zeros(0, dtype=torch.int64, device="cuda"), top=3)
+    assert r.logprob.shape == (0,) and r.top_ids.shape == (0, 3)
+
+
+# ---- together, as they are used -----------------------------------------------------------------------
+def _run_together(ctx, x, residual, norm_w, layer, head, tokens):
+    """Residual and norm into 8 bits, a 4-bit layer, norm, the vocabulary's product in 32 bits, log probabilities."""
+    q, h = ctx.rms_norm(x, norm_w, 1e-5, residual=residual, fmt=esp.MX_FP8)
+    z = ctx.mx_gemm(q, layer, dtype=x.dtype)
+    y, h = ctx.rms_norm(z, norm_w, 1e-5, residual=h)
+    logits = ctx.mx_gemm(y, head, dtype=torch.float32)
+    r = ctx.token_logprobs(logits, tokens, top=5)
+    return r.logprob, r.entropy, r.top_ids, r.top_logprobs, logits, h
+
+
+def _together_inputs(ctx, M, K=512, V=3000):
+    rng = _rng("together", M)
+    x, r = _features(rng, M, K, "bf16").cuda(), _features(rng, M, K, "bf16").cuda()
+    nw = torch.from_numpy(1 + 0.2 * rng.standard_normal(K)).bfloat16().cuda()
+    wl, wh = (torch.from_numpy(rng.standard_normal((n, K)) * K ** -0.5).bfloat16().cuda() for n in (K, V))
+    layer, head = (ctx.mx_pack(ctx.mx_quantize(w, esp.MX_FP4)) for w in (wl, wh))
+    return x, r, nw, layer, head, torch.from_numpy(rng.integers(0, V, M)).cuda(), wl, wh
+
+
+@pytest.mark.parametrize("M", [1, 20, 300])
+def test_together(ctx, M):
+    """Each step against 64 bits from the device's own input of that step."""
+    x, r, nw, layer, head, tokens, wl, wh = _together_inputs(ctx, M)
+    lp, ent, ids, tops, logits, h = _run_together(ctx, x, r, nw, layer, head, tokens)
+    q, h1 = ctx.rms_norm(x, nw, 1e-5, residual=r, fmt=esp.MX_FP8)
+    w64 = [orc.mx_values(*orc.mx_quantize(w.double().cpu().numpy(), orc.FP4), orc.FP4) for w in (wl, wh)]
+    z = ctx.mx_gemm(q, layer, dtype=torch.bfloat16)
+    _assert_product(z, _np(ctx.mx_dequantize(q, torch.float32)), w64[0], torch.bfloat16, "fp8")
+    y, h2 = ctx.rms_norm(z, nw, 1e-5, residual=h1)
+    assert torch.equal(h, h2)
+    _assert_product(logits, _np(y), w64[1], torch.float32, "16")
+    _assert_logprobs(ctx, logits, [int(t) for t in tokens], 5)
+    again = ctx.token_logprobs(logits, tokens, top=5)
+    assert torch.equal(again.logprob, lp) and torch.equal(again.entropy, ent) and torch.equal(again.top_ids, ids) and torch.equal(again.top_logprobs, tops)
+
+
+@pytest.mark.parametrize("M", [1, 40, 260])
+def test_captured_and_replayed(ctx, M):
+    """Two graphs of the same calls, replayed in turn with eager work between, give what eager calls give on the inputs of the moment."""
+    x, r, nw, layer, head, tokens, *_ = _together_inputs(ctx, M)
+    _run_together(ctx, x, r, nw, layer, head, tokens)
+    torch.cuda.synchronize()
+    graphs = []
+    for _ in range(2):
+        ins = [x.clone(), r.clone(), tokens.clone()]
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs = _run_together(ctx, ins[0], ins[1], nw, layer, head, ins[2])
+        graphs.append((g, ins, outs))
+    gen = torch.Generator("cuda").manual_seed(3)
+    for turn in range(4):
+        for g, ins, outs in graphs:
+            ins[0].copy_(torch.randn(x.shape, device="cuda", generator=gen))
+            ins[2].copy_(torch.randint(0, 3000, tokens.shape, device="cuda", generator=gen))
+            g.replay()
+            want = _run_together(ctx, ins[0], ins[1], nw, layer, head, ins[2])
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(outs, want)), turn
+
+
+def test_on_other_streams(ctx):
+    """Calls on a stream that is not the default one, and two contexts on two streams at once."""
+    x, r, nw, layer, head, tokens, *_ = _together_inputs(ctx, 33)
+    want = _run_together(ctx, x, r, nw, layer, head, tokens)
+    other = esp.Context(0)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    results = []
+    for i in range(6):
+        with torch.cuda.stream(streams[i % 2]):
+            results.append(_run_together((ctx, other)[i % 2], x, r, nw, layer, head, tokens))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for res in results for a, b in zip(res, want))
