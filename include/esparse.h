@@ -302,8 +302,8 @@ int esparse_mx_dequantize(esparse_ctx* ctx, const void* data, const void* scales
  *   ESPARSE_MX_ACT_16  16-bit values (dtype f16 or bf16; ldx values from row to row, x_scales ignored): the weights alone are in 4 bits.  Their scaled numbers are
  *     brought to the type of X in registers (bf16: exact; f16: exact for scales from 2^-23 to 2^13, rounded and limited to f16 beyond) for the
  *     16-bit matrix instruction.
- * workspace: DEVICE scratch of esparse_mx_gemm_workspace bytes (host only; may be 0), 256-byte aligned, overwritten.  in_place: 1 where K and ldx are multiples of 8 and
- * X is 16-byte aligned, or X is MX: its rows are read where they are; 0: they are copied into the workspace first.  M = 0 is a no-op.  A block of W or X with scale 255
+ * workspace: DEVICE scratch of esparse_mx_gemm_workspace bytes (host only; may be 0), 256-byte aligned, overwritten.  aligned: 1 where X is 16-byte aligned and ldx a multiple of 8,
+ * or X is MX; 0 otherwise (then 16-bit rows are copied into the workspace first, as they are for some K).  K and ldx: at most 2^22. M = 0 is a no-op.  A block of W or X with scale 255
  * makes the outputs it takes part in NaN.  With ESPARSE_MX_ACT_FP8 the instruction adds the products of eight consecutive channels after it has cut each to a multiple
  * of 2^(p - 13), p the exponent of the largest of the eight: up to 7 x 2^-13 of the largest are lost, far below the 2^-4 of the 8-bit rounding.
  *  Calls may run at once on several streams if each has its own workspace.  Does not synchronise; can be captured.
@@ -311,7 +311,7 @@ int esparse_mx_dequantize(esparse_ctx* ctx, const void* data, const void* scales
 typedef enum { ESPARSE_MX_ACT_FP4 = 0, ESPARSE_MX_ACT_FP8 = 1, ESPARSE_MX_ACT_16 = 2 } esparse_mx_act;
 int esparse_mx_packed_size(long long N, long long K, size_t* bytes);
 int esparse_mx_pack(esparse_ctx* ctx, const void* data, const void* scales, long long N, long long K, void* packed_out);
-int esparse_mx_gemm_workspace(long long M, long long N, long long K, esparse_mx_act act, int in_place, size_t* bytes);
+int esparse_mx_gemm_workspace(long long M, long long N, long long K, esparse_mx_act act, int aligned, size_t* bytes);
 int esparse_mx_gemm(esparse_ctx* ctx, const void* X, const void* x_scales, long long M, long long ldx, esparse_mx_act act,
                     esparse_dtype dtype, const void* packed_w, long long N, long long K, esparse_dtype out_dtype, void* Y,
                     void* workspace, size_t workspace_bytes);

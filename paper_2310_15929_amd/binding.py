@@ -188,9 +188,9 @@ def mx_packed_size(N: int, K: int) -> int:
     return a.value
 
 
-def mx_gemm_workspace(M: int, N: int, K: int, act: int, in_place: bool = True) -> int:
+def mx_gemm_workspace(M: int, N: int, K: int, act: int, aligned: bool = True) -> int:
     a = C.c_size_t()
-    rc = load_library().esparse_mx_gemm_workspace(M, N, K, act, int(in_place), C.byref(a))
+    rc = load_library().esparse_mx_gemm_workspace(M, N, K, act, int(aligned), C.byref(a))
     if rc:
         raise EsparseError(rc, f"esparse_mx_gemm_workspace: M = {M}, N = {N}, K = {K}, activations {act}")
     return a.value
@@ -664,7 +664,7 @@ class Context:
             if tuple(out.shape) != (M, N) or not out.is_contiguous() or (dtype is not None and out.dtype != dtype):
                 raise ValueError(f"mx_gemm: out is not a contiguous [{M}, {N}] of the type asked for")
         out_code = _code(out.dtype, "mx_gemm", f32=True)
-        nbytes = _known_mx_gemm_workspace(M, N, K, act, act != _ACT_16 or not (K % 8 or ld % 8 or x % 16))
+        nbytes = _known_mx_gemm_workspace(M, N, K, act, act != _ACT_16 or not (ld % 8 or x % 16))
         # a block of its own for each call: calls on several streams and captured graphs do not share it
         ws = torch.empty(nbytes, dtype=torch.uint8, device=out.device) if nbytes else None
         self._sync_stream()

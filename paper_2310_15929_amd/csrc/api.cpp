@@ -788,14 +788,16 @@ int esparse_mx_pack(esparse_ctx* ctx, const void* data, const void* scales, long
   return esp_mx_pack_device(ctx, data, scales, N, K, packed_out);
 }
 
+// K and the stride of 16-bit rows up to 2^22: a tile's operands lie within 32 bits of its first byte
+static constexpr long long kMaxChannels = 1ll << 22;
 static bool mx_gemm_sizes(long long M, long long N, long long K, int act) {
-  return M >= 0 && M <= kMaxRows && N >= 1 && N <= kMaxRows && K >= 1 && K < (1ll << 31) && N * K <= kMaxValues && M * K <= kMaxValues && M * N <= kMaxValues &&
+  return M >= 0 && M <= kMaxRows && N >= 1 && N <= kMaxRows && K >= 1 && K <= kMaxChannels && N * K <= kMaxValues && M * K <= kMaxValues && M * N <= kMaxValues &&
          act >= ESPARSE_MX_ACT_FP4 && act <= ESPARSE_MX_ACT_16;
 }
 
-int esparse_mx_gemm_workspace(long long M, long long N, long long K, esparse_mx_act act, int in_place, size_t* bytes) {
-  if (!bytes || !mx_gemm_sizes(M, N, K, act) || in_place < 0 || in_place > 1) return ESPARSE_EINVAL;
-  *bytes = M ? esp_mx_gemm_workspace_bytes(M, N, K, act, act != ESPARSE_MX_ACT_16 || (in_place && K % 8 == 0)) : 0;
+int esparse_mx_gemm_workspace(long long M, long long N, long long K, esparse_mx_act act, int aligned, size_t* bytes) {
+  if (!bytes || !mx_gemm_sizes(M, N, K, act) || aligned < 0 || aligned > 1) return ESPARSE_EINVAL;
+  *bytes = M ? esp_mx_gemm_workspace_bytes(M, N, K, act, aligned) : 0;
   return ESPARSE_OK;
 }
 
@@ -810,20 +812,21 @@ int esparse_mx_gemm(esparse_ctx* ctx, const void* X, const void* x_scales, long 
   if (M == 0) return ESPARSE_OK;
   ESP_REQUIRE(ctx, X && packed_w && Y, ESPARSE_EINVAL, "X / packed_w / Y is null");
   if (act == ESPARSE_MX_ACT_16) {
-    ESP_REQUIRE(ctx, ldx >= K && ldx < (1ll << 40), ESPARSE_EINVAL, "ldx = %lld is less than K = %lld, or too large", ldx, K);
+    ESP_REQUIRE(ctx, ldx >= K && ldx <= kMaxChannels, ESPARSE_EINVAL, "ldx = %lld is outside [K, %lld]", ldx, kMaxChannels);
     ESP_REQUIRE(ctx, aligned_to(X, 2), ESPARSE_EINVAL, "X is not aligned to its type");
   } else {
     ESP_REQUIRE(ctx, x_scales, ESPARSE_EINVAL, "x_scales is null");
     ESP_REQUIRE(ctx, esp_aligned16(X) && esp_aligned16(x_scales), ESPARSE_EINVAL, "X / x_scales is not 16-byte aligned");
   }
   ESP_REQUIRE(ctx, esp_aligned16(packed_w) && esp_aligned16(Y), ESPARSE_EINVAL, "packed_w / Y is not 16-byte aligned");
-  const size_t need = esp_mx_gemm_workspace_bytes(M, N, K, act, esp_mx_gemm_in_place(X, ldx, K, act));
+  const bool aligned = act != ESPARSE_MX_ACT_16 || (esp_aligned16(X) && ldx % 8 == 0);
+  const size_t need = esp_mx_gemm_workspace_bytes(M, N, K, act, aligned);
   ESP_REQUIRE(ctx, need == 0 || workspace, ESPARSE_EINVAL, "workspace is null, %zu bytes needed", need);
   ESP_REQUIRE(ctx, need == 0 || workspace_bytes >= need, ESPARSE_EWORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, need);
   ESP_REQUIRE(ctx, need == 0 || aligned_to(workspace, 256), ESPARSE_EINVAL, "workspace is not 256-byte aligned");
   const DeviceOfCall device(ctx->device);
   ESP_HIP(ctx, device.error());
-  return esp_mx_gemm_device(ctx, X, x_scales, M, ldx, act, dtype, packed_w, N, K, out_dtype, Y, workspace);
+  return esp_mx_gemm_device(ctx, X, x_scales, M, ldx, act, dtype, packed_w, N, K, out_dtype, Y, workspace, aligned);
 }
 
 int esparse_rms_norm(esparse_ctx* ctx, const void* x, long long ldx, const void* residual, long long ldr, const void* weight, long long R, long long K,

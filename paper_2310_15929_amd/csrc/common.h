@@ -188,10 +188,10 @@ bool esp_variant_is_decode_kernel(int v);
 int esp_mx_quantize_device(esparse_ctx* ctx, const void* X, long long R, long long K, long long ldx, int dtype, int fmt, void* data, void* scales);
 int esp_mx_dequantize_device(esparse_ctx* ctx, const void* data, const void* scales, long long R, long long K, int fmt, int dtype, void* out);
 int esp_mx_pack_device(esparse_ctx* ctx, const void* data, const void* scales, long long N, long long K, void* packed);
-bool esp_mx_gemm_in_place(const void* X, long long ldx, long long K, int act);  // whether the rows of X are read where they are
-size_t esp_mx_gemm_workspace_bytes(long long M, long long N, long long K, int act, bool in_place);
+// aligned: rows of X begin at multiples of 16 bytes (or X is microscaled)
+size_t esp_mx_gemm_workspace_bytes(long long M, long long N, long long K, int act, bool aligned);
 int esp_mx_gemm_device(esparse_ctx* ctx, const void* X, const void* xs, long long M, long long ldx, int act, int dtype, const void* packed, long long N,
-                       long long K, int out, void* Y, void* workspace);
+                       long long K, int out, void* Y, void* workspace, bool aligned);
 int esp_rms_norm_device(esparse_ctx* ctx, const void* x, long long ldx, const void* residual, long long ldr, const void* weight, long long R, long long K,
                         double eps, int dtype, void* sum_out, void* y, int fmt, void* data, void* scales);
 size_t esp_token_logprobs_workspace(long long R, long long V, int dtype, int top);

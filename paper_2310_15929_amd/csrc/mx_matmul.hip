@@ -21,8 +21,8 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
-#include <cstdlib>
 #include <type_traits>
+#include <utility>
 
 #include "intrinsics.h"
 #include "mx.h"
@@ -50,6 +50,9 @@ struct MxTilePlan {
   float* partial;
   unsigned nrb, ntb, nsplit, per_split, band;  // row and token blocks, ranges of K and their stages, row blocks of a band
 };
+
+template <int ACT>
+constexpr int kRowBytes = ACT == ACT_FP4 ? 64 : (ACT == ACT_FP8 ? 128 : 256);  // of a token and 128 channels
 
 // B operand of one token tile and 128 channels: 16 bytes (4 bits), 32 (8 bits), 4 x 16 (16 bits, one for each j)
 template <int ACT>
@@ -132,100 +135,168 @@ __device__ __forceinline__ void store_4(const MxGemmArgs& a, long long t, long l
 }
 
 // ------------------------------------------------------------------------------------------------
-// rows kernel: a workgroup of NW waves owns RT row tiles and one token tile of 16; wave w takes the steps w, w + NW, ... of K straight
-// from memory into registers; the NW sums of an output are added in the order of the waves.
+// rows kernel (few tokens, bound by reading the weights): a workgroup of NW waves owns RT row tiles and MT token tiles over all of K; wave w takes
+// the groups w, w + NW, ... of U steps straight from memory into registers, the loads of a group under way while the one before it is
+// multiplied; the NW sums of an output are added in the order of the waves.
 // ------------------------------------------------------------------------------------------------
-template <int ACT, int DT, int RT, int NW>
+template <int ACT, int MT, int RT, int U>
+struct MxGroup {
+  uint4 w[U][RT];
+  uint32_t s[U][(RT + 3) / 4];
+  MxB<ACT> b[U][MT];
+};
+
+template <int ACT, int DT, int MT, int RT, int NW, int U>
 __global__ void __launch_bounds__(NW * 64) k_mx_rows(const MxGemmArgs a) {
-  __shared__ floatx4_t s_acc[NW * RT * 64];
+  __shared__ floatx4_t s_acc[NW * RT * MT * 64];
   const unsigned lane = threadIdx.x & 63u, wave = (unsigned)wave_uniform((int)(threadIdx.x >> 6)), c = lane & 15u, g = lane >> 4;
-  const unsigned rt0 = blockIdx.x * RT;
-  const long long t0 = (long long)blockIdx.y * 16;
-  const bool real = t0 + c < a.M;
-  const long long tok = real ? t0 + c : a.M - 1;
-  const unsigned char* x = a.x + tok * a.ldx;
+  // row groups that share scale words run on one XCD (= blockIdx % 8)
+  const unsigned groups = (a.nrt + RT - 1) / RT, per = (groups + 7) / 8, grp = (blockIdx.x & 7u) * per + (blockIdx.x >> 3);
+  if ((blockIdx.x >> 3) >= per || grp >= groups) return;
+  const unsigned rt0 = grp * RT;
+  const long long t0 = (long long)blockIdx.y * (16 * MT);
+  const unsigned char* x[MT];
+  const uint32_t* xs[MT];
+  bool real[MT];
+#pragma unroll
+  for (int j = 0; j < MT; j++) {
+    const long long t = t0 + 16 * j + c;
+    real[j] = t < a.M;
+    const long long tok = real[j] ? t : a.M - 1;
+    x[j] = a.x + tok * a.ldx + (ACT == ACT_16 ? 64u : 16u) * g;
+    xs[j] = a.xs + tok;
+  }
   const uint4* w = a.w + (long long)rt0 * a.nks * 64 + lane;
   const uint32_t* ws = a.ws + (long long)(rt0 >> 2) * a.nks * 64 + lane;
   const unsigned shift = 8u * (rt0 & 3u);
-  floatx4_t acc[RT];
+  floatx4_t acc[RT][MT];
 #pragma unroll
-  for (int i = 0; i < RT; i++) acc[i] = floatx4_t{0.f, 0.f, 0.f, 0.f};
-  for (unsigned ks = wave; ks < a.nks; ks += NW) {
-    uint4 wv[RT];
+  for (int i = 0; i < RT; i++)
 #pragma unroll
-    for (int i = 0; i < RT; i++) wv[i] = load_stream_16(w + ((long long)i * a.nks + ks) * 64);
-    const uint32_t sc = ws[(long long)ks * 64] >> shift;
-    MxB<ACT> b;
+    for (int j = 0; j < MT; j++) acc[i][j] = floatx4_t{0.f, 0.f, 0.f, 0.f};
+
+  auto load_step = [&](MxGroup<ACT, MT, RT, U>& r, int u, unsigned ks) {
+#pragma unroll
+    for (int i = 0; i < RT; i++) r.w[u][i] = load_stream_16(w + ((long long)(RT <= 4 || rt0 + i < a.nrt ? i : 0) * a.nks + ks) * 64);
+#pragma unroll
+    for (int i = 0; i < RT; i += 4) r.s[u][i / 4] = ws[((long long)(RT <= 4 || rt0 + i < a.nrt ? i / 4 : 0) * a.nks + ks) * 64];
+#pragma unroll
+    for (int j = 0; j < MT; j++) {
+      MxB<ACT>& b = r.b[u][j];
+      if constexpr (ACT == ACT_16) {
+#pragma unroll
+        for (int v = 0; v < 4; v++) b.v[v] = uint4{0u, 0u, 0u, 0u};
+        if (real[j]) {
+#pragma unroll
+          for (int v = 0; v < 4; v++)
+            if (128ll * ks + 32 * g + 8 * v < a.K) b.v[v] = *reinterpret_cast<const uint4*>(x[j] + 256ull * ks + 16 * v);  // (K is a multiple of 8)
+        }
+      } else {
+        b.v[0] = *reinterpret_cast<const uint4*>(x[j] + (unsigned long long)ks * kRowBytes<ACT>);
+        if constexpr (ACT == ACT_FP8) b.v[1] = *reinterpret_cast<const uint4*>(x[j] + (unsigned long long)ks * kRowBytes<ACT> + 64);
+        b.s = xs[j][(long long)ks * a.M];
+      }
+    }
+  };
+  auto multiply_step = [&](const MxGroup<ACT, MT, RT, U>& r, int u) {
     if constexpr (ACT == ACT_16) {
 #pragma unroll
-      for (int j = 0; j < 4; j++) {
-        const long long k = 128ll * ks + 32 * g + 8 * j;  // (K is a multiple of 8)
-        b.v[j] = uint4{0u, 0u, 0u, 0u};
-        if (k < a.K) b.v[j] = *reinterpret_cast<const uint4*>(x + 2 * k);
-      }
-#pragma unroll
       for (int i = 0; i < RT; i++) {
-        const float s = mx_widen_scale(sc >> (8 * i));
-        acc[i] = mfma16<DT>(mx_widen<DT>(wv[i].x, s), b.v[0], acc[i]);
-        acc[i] = mfma16<DT>(mx_widen<DT>(wv[i].y, s), b.v[1], acc[i]);
-        acc[i] = mfma16<DT>(mx_widen<DT>(wv[i].z, s), b.v[2], acc[i]);
-        acc[i] = mfma16<DT>(mx_widen<DT>(wv[i].w, s), b.v[3], acc[i]);
+        const float s = mx_widen_scale((r.s[u][i / 4] >> shift) >> (8 * (i % 4)));
+        const uint32_t word[4] = {r.w[u][i].x, r.w[u][i].y, r.w[u][i].z, r.w[u][i].w};
+#pragma unroll
+        for (int v = 0; v < 4; v++) {
+          const uint4 wide = mx_widen<DT>(word[v], s);
+#pragma unroll
+          for (int j = 0; j < MT; j++) acc[i][j] = mfma16<DT>(wide, r.b[u][j].v[v], acc[i][j]);
+        }
       }
     } else {
-      if constexpr (ACT == ACT_FP4) {
-        b.v[0] = *reinterpret_cast<const uint4*>(x + 64ull * ks + 16 * g);
-      } else {
-        b.v[0] = *reinterpret_cast<const uint4*>(x + 128ull * ks + 16 * g);
-        b.v[1] = *reinterpret_cast<const uint4*>(x + 128ull * ks + 64 + 16 * g);
+#pragma unroll
+      for (int j = 0; j < MT; j++) {
+        MxB<ACT> b = r.b[u][j];
+        b.s >>= 8 * g;
+#pragma unroll
+        for (int i = 0; i < RT; i += 4) {
+          const uint32_t sc = r.s[u][i / 4] >> shift;
+          acc[i][j] = mx_mfma<ACT, 0>(r.w[u][i], sc, b, acc[i][j]);
+          if constexpr (RT > 1) acc[i + 1][j] = mx_mfma<ACT, 1>(r.w[u][i + 1], sc, b, acc[i + 1][j]);
+          if constexpr (RT > 2) {
+            acc[i + 2][j] = mx_mfma<ACT, 2>(r.w[u][i + 2], sc, b, acc[i + 2][j]);
+            acc[i + 3][j] = mx_mfma<ACT, 3>(r.w[u][i + 3], sc, b, acc[i + 3][j]);
+          }
+        }
       }
-      b.s = a.xs[(long long)ks * a.M + tok] >> (8 * g);
-      acc[0] = mx_mfma<ACT, 0>(wv[0], sc, b, acc[0]);
-      if constexpr (RT > 1) acc[1] = mx_mfma<ACT, 1>(wv[1], sc, b, acc[1]);
-      if constexpr (RT > 2) {
-        acc[2] = mx_mfma<ACT, 2>(wv[2], sc, b, acc[2]);
-        acc[3] = mx_mfma<ACT, 3>(wv[3], sc, b, acc[3]);
+    }
+  };
+  const unsigned full = a.nks / U;  // whole groups
+  unsigned k = wave;
+  if (k < full) {
+    MxGroup<ACT, MT, RT, U> cur, next;
+#pragma unroll
+    for (int u = 0; u < U; u++) load_step(cur, u, k * U + u);
+    for (; k + NW < full; k += NW) {
+#pragma unroll
+      for (int u = 0; u < U; u++) load_step(next, u, (k + NW) * U + u);
+#pragma unroll
+      for (int u = 0; u < U; u++) multiply_step(cur, u);
+      cur = next;
+    }
+#pragma unroll
+    for (int u = 0; u < U; u++) multiply_step(cur, u);
+    k += NW;
+  }
+  if constexpr (U > 1) {
+    if (k == full) {  // the steps behind the last whole group
+      MxGroup<ACT, MT, RT, U> cur;
+      for (unsigned ks = full * U; ks < a.nks; ks++) {
+        load_step(cur, 0, ks);
+        multiply_step(cur, 0);
       }
     }
   }
 #pragma unroll
-  for (int i = 0; i < RT; i++) s_acc[(wave * RT + i) * 64 + lane] = acc[i];
+  for (int i = 0; i < RT; i++)
+#pragma unroll
+    for (int j = 0; j < MT; j++) s_acc[((wave * RT + i) * MT + j) * 64 + lane] = acc[i][j];
   __syncthreads();
-  for (unsigned o = threadIdx.x; o < RT * 64; o += NW * 64) {
+  for (unsigned o = threadIdx.x; o < RT * MT * 64; o += NW * 64) {
     floatx4_t v = s_acc[o];
 #pragma unroll
-    for (int k = 1; k < NW; k++) v += s_acc[k * RT * 64 + o];
-    const unsigned i = o >> 6, l = o & 63u;
-    store_4(a, t0 + (l & 15u), (long long)(rt0 + i) * 16 + 4 * (l >> 4), v);
+    for (int n = 1; n < NW; n++) v += s_acc[n * (RT * MT * 64) + o];
+    const unsigned i = o / (MT * 64), j = o / 64 % MT, l = o & 63u;
+    store_4(a, t0 + 16 * j + (l & 15u), (long long)(rt0 + i) * 16 + 4 * (l >> 4), v);
   }
 }
 
 // ------------------------------------------------------------------------------------------------
 // tile kernel: a workgroup of NWR x NWC waves owns RTM = NWR TR row tiles x NTT = NWC TC token tiles, a wave TR x TC of them.
 // K runs in stages of 128 channels, software pipelined: weights (1 KiB a row tile), activations (16 RB bytes a token tile) and
-// scales are copied from memory straight into rings of three LDS buffers; a wave holds its A operands of the stage in registers
+// scales are copied from memory straight into rings of RING LDS buffers; a wave holds its A operands of the stage in registers
 // and reads those of the next during it, B operands stream from LDS one token tile ahead.
-//   stage k:  copies of B(k+2) and its scales into the buffers of stage k-1 and of A(k+3) into that of A(k) (in registers by then);
-//             all token tiles but the last; counted wait (only this stage's copies may be under way) and barrier; then the first
+//   stage k:  copies of B(k+RING-1) and its scales into the buffers of stage k-1 and of A(k+RING) into that of A(k) (in registers by then);
+//             all token tiles but the last; counted wait (only the newest RING - 2 stages' copies may be under way) and barrier; then the first
 //             B operand and the A scales of stage k+1 are read while the last token tile is multiplied.
 // Activations stay in rows: a stage's RB bytes of a token are consecutive in memory (64, 128 or 256) and in LDS, where the
 // 16-byte pieces of a token are exchanged by an exclusive or with its number, so that the 16 tokens of an operand read hit all banks.
 // 16-bit activations: a unit of weights is expanded to 16 bits once per wave and stage, one stage ahead, between the multiplies.
 // nsplit > 1: K is cut, a workgroup stores an fp32 partial tile, k_mx_reduce adds them in ascending order.
 // ------------------------------------------------------------------------------------------------
-template <int ACT>
-constexpr int kRowBytes = ACT == ACT_FP4 ? 64 : (ACT == ACT_FP8 ? 128 : 256);  // of a token and stage
-
-template <int ACT, int TR, int TC, int NWR, int NWC>
+template <int ACT, int TR, int TC, int NWR, int NWC, int RING>
 struct MxTile {
   static constexpr int NW = NWR * NWC, RTM = NWR * TR, NTT = NWC * TC, RB = kRowBytes<ACT>;
   static constexpr int AU = RTM * 64, BU = NTT * RB;                            // 16-byte units of a stage
-  static constexpr int SA = RTM / 4, SB = ACT == ACT_16 ? 0 : NTT / 4;          // runs of 64 scale words
+  static constexpr bool ALIGNED = TR % 4 == 0;                                  // a wave's rows start with a scale word
+  static constexpr int SW_TR = (TR + 3) / 4;                                    // scale words of a wave
+  static constexpr int SA = (RTM + (RTM % 4 == 0 ? 0 : (RTM % 2 == 0 ? 2 : 3)) + 3) / 4, SB = ACT == ACT_16 ? 0 : NTT / 4;          // runs of 64 scale words
   static constexpr int AC = (RTM + NW - 1) / NW, BC = (BU / 64 + NW - 1) / NW, SC = (SA + SB + NW - 1) / NW;  // copies of a wave
   static constexpr int OPS = AC + BC + SC, SW = (SA + SB) * 64;
-  static_assert(3 * ((AU + BU) * 16 + SW * 4) <= 160 * 1024, "the rings fit the LDS");
+  static constexpr int LDS = RING * ((AU + BU) * 16 + SW * 4);
+  static_assert(LDS <= 160 * 1024, "the rings fit the LDS");
+  static constexpr int WAVES = NW >= 8 || 2 * LDS <= 160 * 1024 ? 2 : 1;        // of a SIMD: what the registers are shared among
   static constexpr int BV = ACT == ACT_FP4 ? 1 : (ACT == ACT_FP8 ? 2 : 4);      // B reads of a token tile
   static constexpr int AV = ACT == ACT_16 ? 4 : 1;                              // A operands of a row tile
-  static_assert(TR % 4 == 0 && NTT % 4 == 0, "scale words hold four row tiles, a run of them four token tiles");
+  static_assert(NTT % 4 == 0, "a run of scale words holds four token tiles");
 };
 
 template <int ACT, int TR>
@@ -261,14 +332,14 @@ __device__ __forceinline__ void mx_copy(const MxSource& s, unsigned lane_off, un
 #endif
 }
 
-template <int ACT, int DT, int TR, int TC, int NWR, int NWC>
+template <int ACT, int DT, int TR, int TC, int NWR, int NWC, int RING>
 struct MxTileWave {
-  using T = MxTile<ACT, TR, TC, NWR, NWC>;
+  using T = MxTile<ACT, TR, TC, NWR, NWC, RING>;
   floatx4_t acc[TR][TC];
   MxSource a_src, x_src, s_src[T::SC];
   unsigned a_off[T::AC], s_step[T::SC];           // uniform
   unsigned x_off[T::BC], s_off[T::SC], lane16;    // of the lane
-  unsigned lane, wave, wr, wc, b_off, shift;
+  unsigned lane, wave, wr, wc, b_off, shift, s_word, s_shift;
   unsigned k0, k1;
 
   __device__ __forceinline__ void copy_a(uint4* sa, unsigned k) {
@@ -283,11 +354,20 @@ struct MxTileWave {
 #pragma unroll
     for (int p = 0; p < T::SC; p++) mx_copy<4>(s_src[p], s_off[p], k * s_step[p], ss + ((p * T::NW + wave) % (T::SA + T::SB)) * 64);
   }
-  __device__ __forceinline__ void read_scales(const uint32_t* ss, uint32_t (&as)[TR / 4]) {
+  // byte i of the words: the scale of the wave's row tile i
+  __device__ __forceinline__ void read_scales(const uint32_t* ss, uint32_t (&as)[T::SW_TR]) {
+    if constexpr (T::ALIGNED) {
 #pragma unroll
-    for (int i = 0; i < TR / 4; i++) as[i] = ss[(wr * (TR / 4) + i) * 64 + lane];
+      for (int i = 0; i < T::SW_TR; i++) as[i] = ss[(s_word + i) * 64 + lane];
+    } else {
+      uint32_t w[T::SW_TR + 1];
+#pragma unroll
+      for (int i = 0; i <= T::SW_TR; i++) w[i] = ss[(s_word + i < (unsigned)T::SA ? s_word + i : T::SA - 1) * 64 + lane];
+#pragma unroll
+      for (int i = 0; i < T::SW_TR; i++) as[i] = (uint32_t)(((unsigned long long)w[i + 1] << 32 | w[i]) >> s_shift);
+    }
   }
-  __device__ __forceinline__ void read_a(const uint4* sa, const uint32_t (&as)[TR / 4], MxA<ACT, TR>& r) {
+  __device__ __forceinline__ void read_a(const uint4* sa, const uint32_t (&as)[MxTile<ACT, TR, TC, NWR, NWC, RING>::SW_TR], MxA<ACT, TR>& r) {
 #pragma unroll
     for (int i = 0; i < TR; i++) {
       const uint4 u = sa[(wr * TR + i) * 64 + lane];
@@ -313,7 +393,7 @@ struct MxTileWave {
       b.s = ss[T::SA * 64 + (wc * TC + j) * 16 + (lane & 15u)] >> shift;
     }
   }
-  __device__ __forceinline__ void multiply(const MxA<ACT, TR>& r, const uint32_t (&as)[TR / 4], const MxB<ACT>& b, int j) {
+  __device__ __forceinline__ void multiply(const MxA<ACT, TR>& r, const uint32_t (&as)[MxTile<ACT, TR, TC, NWR, NWC, RING>::SW_TR], const MxB<ACT>& b, int j) {
     if constexpr (ACT == ACT_16) {
 #pragma unroll
       for (int v = 0; v < 4; v++)
@@ -321,11 +401,11 @@ struct MxTileWave {
         for (int i = 0; i < TR; i++) acc[i][j] = mfma16<DT>(r.a[i][v], b.v[v], acc[i][j]);
     } else {
 #pragma unroll
-      for (int i = 0; i < TR; i += 4) {
-        acc[i][j] = mx_mfma<ACT, 0>(r.a[i][0], as[i / 4], b, acc[i][j]);
-        acc[i + 1][j] = mx_mfma<ACT, 1>(r.a[i + 1][0], as[i / 4], b, acc[i + 1][j]);
-        acc[i + 2][j] = mx_mfma<ACT, 2>(r.a[i + 2][0], as[i / 4], b, acc[i + 2][j]);
-        acc[i + 3][j] = mx_mfma<ACT, 3>(r.a[i + 3][0], as[i / 4], b, acc[i + 3][j]);
+      for (int i = 0; i < TR; i++) {
+        if (i % 4 == 0) acc[i][j] = mx_mfma<ACT, 0>(r.a[i][0], as[i / 4], b, acc[i][j]);
+        if (i % 4 == 1) acc[i][j] = mx_mfma<ACT, 1>(r.a[i][0], as[i / 4], b, acc[i][j]);
+        if (i % 4 == 2) acc[i][j] = mx_mfma<ACT, 2>(r.a[i][0], as[i / 4], b, acc[i][j]);
+        if (i % 4 == 3) acc[i][j] = mx_mfma<ACT, 3>(r.a[i][0], as[i / 4], b, acc[i][j]);
       }
     }
   }
@@ -335,6 +415,24 @@ __device__ __forceinline__ unsigned uniform(unsigned v) { return (unsigned)wave_
 // LDS that lanes of one wave exchange: in order in the hardware, kept in order by the compiler
 __device__ __forceinline__ void wave_fence() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
 
+template <int N, class F, int... I>
+__device__ __forceinline__ void each_stage_of(F& f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, class F>
+__device__ __forceinline__ void each_stage(F& f) {
+  each_stage_of<N>(f, std::make_integer_sequence<int, N>{});
+}
+
+// this wave's LDS reads are back; then the other waves
+__device__ __forceinline__ void mx_meet() {
+  sched_fence();
+#if defined(__HIP_DEVICE_COMPILE__)
+  __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt = 0 alone
+  __builtin_amdgcn_s_barrier();
+#endif
+  sched_fence();
+}
 // all of this wave's copies but the newest N have landed, its LDS reads are back; then the other waves
 template <int N>
 __device__ __forceinline__ void mx_arrive() {
@@ -347,18 +445,19 @@ __device__ __forceinline__ void mx_arrive() {
 }
 
 // cur: A(k) in registers; nxt receives A(k+1).  as: scales of stage k (16-bit activations: of k+1, which nxt is expanded with)
-template <int ACT, int DT, int TR, int TC, int NWR, int NWC>
-__device__ __forceinline__ void mx_stage(MxTileWave<ACT, DT, TR, TC, NWR, NWC>& st, const MxA<ACT, TR>& cur, MxA<ACT, TR>& nxt, uint32_t (&as)[TR / 4], MxB<ACT>& bq,
+template <int ACT, int DT, int TR, int TC, int NWR, int NWC, int RING>
+__device__ __forceinline__ void mx_stage(MxTileWave<ACT, DT, TR, TC, NWR, NWC, RING>& st, const MxA<ACT, TR>& cur, MxA<ACT, TR>& nxt, uint32_t (&as)[MxTile<ACT, TR, TC, NWR, NWC, RING>::SW_TR], MxB<ACT>& bq,
                                          const uint4* b_cur, const uint32_t* s_cur, const uint4* a_nxt, const uint4* b_nxt, const uint32_t* s_nxt, const uint32_t* s_nxt2,
                                          uint4* a_pre, uint4* b_pre, uint32_t* s_pre, unsigned k) {
-  using T = MxTile<ACT, TR, TC, NWR, NWC>;
+  using T = MxTile<ACT, TR, TC, NWR, NWC, RING>;
   constexpr int TH = TC > 1 ? TC - 1 : 1;  // token tiles ahead of the barrier
   constexpr int MM = TR * T::AV;           // multiplies of a token tile
   constexpr int READS = T::BV + (ACT == ACT_16 ? 0 : 1) + (TR + TH - 1) / TH;
-  const unsigned last = st.k1 - 1;
-  st.copy_b(b_pre, k + 2 < st.k1 ? k + 2 : last);
-  st.copy_s(s_pre, ACT == ACT_16 ? (k + 3 < st.k1 ? k + 3 : last) : (k + 2 < st.k1 ? k + 2 : last));
-  st.copy_a(a_pre, k + 3 < st.k1 ? k + 3 : last);
+  // B RING - 1 stages ahead, A (in registers a stage early) RING
+  const unsigned last = st.k1 - 1, kb = k + RING - 1 < st.k1 ? k + RING - 1 : last, ka = k + RING < st.k1 ? k + RING : last;
+  st.copy_b(b_pre, kb);
+  st.copy_s(s_pre, ACT == ACT_16 ? ka : kb);
+  st.copy_a(a_pre, ka);
   st.read_a(a_nxt, as, nxt);
 #pragma unroll
   for (int j = 0; j < TC - 1; j++) {
@@ -371,26 +470,35 @@ __device__ __forceinline__ void mx_stage(MxTileWave<ACT, DT, TR, TC, NWR, NWC>& 
 #pragma unroll
     for (int j = 0; j < TH; j++) sched_spread<MM, (T::OPS + TH - 1) / TH, READS, true>();
   }
-  mx_arrive<T::OPS>();
+  mx_arrive<(RING - 2) * T::OPS>();
   MxB<ACT> b;
-  uint32_t an[TR / 4];
+  uint32_t an[T::SW_TR];
   st.read_b(b_nxt, s_nxt, 0, b);
   st.read_scales(ACT == ACT_16 ? s_nxt2 : s_nxt, an);
   st.multiply(cur, as, bq, TC - 1);
   bq = b;
 #pragma unroll
-  for (int i = 0; i < TR / 4; i++) as[i] = an[i];
-  sched_group<0x100, T::BV + 1 + TR / 4>();
+  for (int i = 0; i < T::SW_TR; i++) as[i] = an[i];
+  sched_group<0x100, T::BV + 1 + T::SW_TR + (T::ALIGNED ? 0 : 1)>();
   sched_group<0x008, MM>();
   sched_fence();
 }
 
-template <int ACT, int DT, int TR, int TC, int NWR, int NWC>
-__device__ __attribute__((always_inline)) void mx_tile_pipeline(uint4* __restrict__ a0, uint4* __restrict__ a1, uint4* __restrict__ a2, uint4* __restrict__ b0,
-                                                                uint4* __restrict__ b1, uint4* __restrict__ b2, uint32_t* __restrict__ s0, uint32_t* __restrict__ s1,
-                                                                uint32_t* __restrict__ s2, const MxGemmArgs& a, const MxTilePlan& p) {
-  using T = MxTile<ACT, TR, TC, NWR, NWC>;
-  MxTileWave<ACT, DT, TR, TC, NWR, NWC> st;
+// the I-th of the buffers of a ring
+template <int I, class P>
+__device__ __forceinline__ P ring_at(P b0, P b1, P b2, P b3, P b4, P b5) {
+  return I == 0 ? b0 : (I == 1 ? b1 : (I == 2 ? b2 : (I == 3 ? b3 : (I == 4 ? b4 : b5))));
+}
+
+template <int ACT, int DT, int TR, int TC, int NWR, int NWC, int RING>
+__device__ __attribute__((always_inline)) void mx_tile_pipeline(uint4* __restrict__ a0, uint4* __restrict__ a1, uint4* __restrict__ a2, uint4* __restrict__ a3,
+                                                                uint4* __restrict__ a4, uint4* __restrict__ a5, uint4* __restrict__ b0, uint4* __restrict__ b1,
+                                                                uint4* __restrict__ b2, uint4* __restrict__ b3, uint4* __restrict__ b4, uint4* __restrict__ b5,
+                                                                uint32_t* __restrict__ s0, uint32_t* __restrict__ s1, uint32_t* __restrict__ s2,
+                                                                uint32_t* __restrict__ s3, uint32_t* __restrict__ s4, uint32_t* __restrict__ s5,
+                                                                const MxGemmArgs& a, const MxTilePlan& p) {
+  using T = MxTile<ACT, TR, TC, NWR, NWC, RING>;
+  MxTileWave<ACT, DT, TR, TC, NWR, NWC, RING> st;
   const unsigned tid = threadIdx.x;
   st.lane = tid & 63u;
   st.wave = (unsigned)wave_uniform((int)(tid >> 6));
@@ -433,55 +541,58 @@ __device__ __attribute__((always_inline)) void mx_tile_pipeline(uint4* __restric
   st.lane16 = st.lane * 16;
   const unsigned c = st.lane & 15u, g = st.lane >> 4;
   st.shift = 8u * g;
+  st.s_word = (rt0 % 4 + st.wr * TR) / 4;
+  st.s_shift = (rt0 % 4 + st.wr * TR) % 4 * 8;
   st.b_off = c * T::RB + (ACT == ACT_FP4 ? g ^ (c >> 2) : (ACT == ACT_FP8 ? g ^ (c >> 1) : (4u * g) ^ c)) * 16u;
 #pragma unroll
   for (int i = 0; i < TR; i++)
 #pragma unroll
     for (int j = 0; j < TC; j++) st.acc[i][j] = floatx4_t{0.f, 0.f, 0.f, 0.f};
 
-  const unsigned last = st.k1 - 1, kb = st.k0;
-  auto at = [&](unsigned k) { return k < st.k1 ? k : last; };
-  st.copy_b(b0, kb);
-  st.copy_s(s0, kb);
-  st.copy_a(a0, kb);
-  st.copy_b(b1, at(kb + 1));
-  st.copy_s(s1, at(kb + 1));
-  st.copy_a(a1, at(kb + 1));
-  if constexpr (ACT == ACT_16) st.copy_s(s2, at(kb + 2));
-  st.copy_a(a2, at(kb + 2));
-  mx_arrive<0>();
+#define A_AT(i) ring_at<(i) % RING>(a0, a1, a2, a3, a4, a5)
+#define B_AT(i) ring_at<(i) % RING>(b0, b1, b2, b3, b4, b5)
+#define S_AT(i) ring_at<(i) % RING>(s0, s1, s2, s3, s4, s5)
+  // what the stages ahead of the first would have copied, in their order: their waits hold from the start
+  const unsigned last = st.k1 - 1;
+  if constexpr (ACT == ACT_16) st.copy_s(s0, st.k0);
+  st.copy_a(a0, st.k0);
+  auto fill = [&](auto stage) {
+    constexpr int I = decltype(stage)::value;
+    const unsigned kb = st.k0 + I < st.k1 ? st.k0 + I : last, ka = st.k0 + I + 1 < st.k1 ? st.k0 + I + 1 : last;
+    st.copy_b(B_AT(I), kb);
+    if constexpr (ACT == ACT_16) st.copy_s(S_AT(I + 1), ka);
+    else st.copy_s(S_AT(I), kb);
+    st.copy_a(A_AT(I + 1), ka);
+  };
+  each_stage<RING - 1>(fill);
+  mx_arrive<(RING - 2) * T::OPS>();
   MxA<ACT, TR> r0, r1;
-  uint32_t as[TR / 4];
+  uint32_t as[T::SW_TR];
   MxB<ACT> bq;
   st.read_scales(s0, as);
   st.read_a(a0, as, r0);
   if constexpr (ACT == ACT_16) st.read_scales(s1, as);
   st.read_b(b0, s0, 0, bq);
-  mx_arrive<0>();  // every wave has its first A operands before the first stage's copies take their place
-  // 16-bit activations: the scales of stage k are used with A(k), a stage ahead of B(k): they are copied three stages ahead, into the buffer of A(k)'s
-#define STAGE(R, N, B0, S0, A1, B1, S1, S2, AP, BP, SP, K) mx_stage<ACT, DT, TR, TC, NWR, NWC>(st, R, N, as, bq, B0, S0, A1, B1, S1, S2, AP, BP, SP, K)
-  unsigned k = kb;
-  for (; k + 3 <= st.k1; k += 3) {
-    if constexpr (ACT == ACT_16) {
-      STAGE(r0, r1, b0, s0, a1, b1, s1, s2, a0, b2, s0, k);
-      STAGE(r1, r0, b1, s1, a2, b2, s2, s0, a1, b0, s1, k + 1);
-      STAGE(r0, r1, b2, s2, a0, b0, s0, s1, a2, b1, s2, k + 2);
-    } else {
-      STAGE(r0, r1, b0, s0, a1, b1, s1, s2, a0, b2, s2, k);
-      STAGE(r1, r0, b1, s1, a2, b2, s2, s0, a1, b0, s0, k + 1);
-      STAGE(r0, r1, b2, s2, a0, b0, s0, s1, a2, b1, s1, k + 2);
-    }
-    r0 = r1;
+  sched_fence();
+  mx_meet();  // every wave has its first A operands before the first stage's copies take their place
+  // 16-bit activations: the scales of stage k are used with A(k), a stage ahead of B(k): they are copied with A, into the buffer of stage k's
+  unsigned k = st.k0;
+  auto stage = [&](auto index) {
+    constexpr int I = decltype(index)::value;
+    mx_stage<ACT, DT, TR, TC, NWR, NWC, RING>(st, I % 2 ? r1 : r0, I % 2 ? r0 : r1, as, bq, B_AT(I), S_AT(I), A_AT(I + 1), B_AT(I + 1), S_AT(I + 1), S_AT(I + 2), A_AT(I),
+                                              B_AT(I + RING - 1), ACT == ACT_16 ? S_AT(I) : S_AT(I + RING - 1), k + I);
+  };
+  for (; k + RING <= st.k1; k += RING) {
+    each_stage<RING>(stage);
+    if constexpr (RING % 2) r0 = r1;
   }
-  if (k < st.k1) {
-    if constexpr (ACT == ACT_16) STAGE(r0, r1, b0, s0, a1, b1, s1, s2, a0, b2, s0, k);
-    else STAGE(r0, r1, b0, s0, a1, b1, s1, s2, a0, b2, s2, k);
-  }
-  if (k + 1 < st.k1) {
-    if constexpr (ACT == ACT_16) STAGE(r1, r0, b1, s1, a2, b2, s2, s0, a1, b0, s1, k + 1);
-    else STAGE(r1, r0, b1, s1, a2, b2, s2, s0, a1, b0, s0, k + 1);
-  }
-#undef STAGE
+  auto rest = [&](auto index) {
+    if (k + decltype(index)::value < st.k1) stage(index);
+  };
+  each_stage<RING - 1>(rest);
+#undef A_AT
+#undef B_AT
+#undef S_AT
   mx_arrive<0>();  // nothing is on its way into the rings
   __syncthreads();  // and every wave is done with them
 
@@ -501,25 +612,35 @@ __device__ __attribute__((always_inline)) void mx_tile_pipeline(uint4* __restric
     return;
   }
   // Outputs through LDS: a wave transposes one token tile after the other (32 bits: half of it) in a slice of its own and stores 16-byte pieces of rows of Y
-  constexpr unsigned ROW = TR * 32 + 16, SLICE = 16 * ROW;  // 16 tokens; the padding puts them into different banks
-  constexpr unsigned PER_A = T::AU * 16 / SLICE;
-  static_assert(3 * PER_A >= T::NW, "the weight buffers hold a slice for every wave");
-  unsigned char* slice = reinterpret_cast<unsigned char*>(st.wave < PER_A ? a0 : (st.wave < 2 * PER_A ? a1 : a2)) + st.wave % PER_A * SLICE;
+  constexpr int HT = (TR + 1) / 2;  // row tiles of a half
+  constexpr unsigned ROW = HT * 64 + 16, SLICE = 16 * ROW;  // 16 tokens; the padding puts them into different banks
+  constexpr unsigned PER_A = T::AU * 16 / SLICE, PER_B = T::BU * 16 / SLICE;  // of a buffer
+  constexpr unsigned BUFS = RING < 3 ? RING : 3;
+  static_assert(BUFS * (PER_A + PER_B) >= T::NW, "the rings hold a slice for every wave");
+  unsigned char* slice;
+  if (st.wave < BUFS * PER_A) {
+    const unsigned buf = st.wave / (PER_A ? PER_A : 1);
+    slice = reinterpret_cast<unsigned char*>(buf == 0 ? a0 : (buf == 1 ? a1 : a2)) + st.wave % (PER_A ? PER_A : 1) * SLICE;
+  } else {
+    const unsigned w = st.wave - BUFS * PER_A, buf = w / (PER_B ? PER_B : 1);
+    slice = reinterpret_cast<unsigned char*>(buf == 0 ? b0 : (buf == 1 ? b1 : b2)) + w % (PER_B ? PER_B : 1) * SLICE;
+  }
 #pragma unroll
   for (int j = 0; j < TC; j++) {
     if (a.out == ESPARSE_F32) {
 #pragma unroll
       for (int h = 0; h < 2; h++) {
 #pragma unroll
-        for (int i = 0; i < TR / 2; i++) *reinterpret_cast<floatx4_t*>(slice + c * ROW + (16 * i + 4 * g) * 4) = st.acc[h * (TR / 2) + i][j];
+        for (int i = 0; i < HT; i++)
+          if (h * HT + i < TR) *reinterpret_cast<floatx4_t*>(slice + c * ROW + (16 * i + 4 * g) * 4) = st.acc[h * HT + i < TR ? h * HT + i : 0][j];
         wave_fence();
 #pragma unroll
-        for (int q = 0; q < TR / 2; q++) {
-          const unsigned u = q * 64 + st.lane, tl = u / (2 * TR), piece = u % (2 * TR);
+        for (int q = 0; q < HT; q++) {
+          const unsigned u = q * 64 + st.lane, tl = u / (4 * HT), piece = u % (4 * HT);
           const floatx4_t v = *reinterpret_cast<const floatx4_t*>(slice + tl * ROW + piece * 16);
-          const long long t = t_wave + 16 * j + tl, n = n_wave + h * (8 * TR) + 4 * piece;
+          const long long t = t_wave + 16 * j + tl, n = n_wave + h * (16 * HT) + 4 * piece;
           float* y = reinterpret_cast<float*>(a.y) + t * a.N + n;
-          if (t < a.M) {
+          if (t < a.M && (TR % 2 == 0 || h == 0 || piece < 4 * (TR - HT))) {
             if (n + 4 <= a.N) {
               __builtin_memcpy(y, &v, 16);
             } else {
@@ -545,8 +666,9 @@ __device__ __attribute__((always_inline)) void mx_tile_pipeline(uint4* __restric
       else put(std::integral_constant<int, ESPARSE_BF16>{});
       wave_fence();
 #pragma unroll
-      for (int q = 0; q < TR / 2; q++) {
+      for (int q = 0; q < HT; q++) {
         const unsigned u = q * 64 + st.lane, tl = u / (2 * TR), piece = u % (2 * TR);
+        if (TR % 2 && tl >= 16) break;
         const uint4 v = *reinterpret_cast<const uint4*>(slice + tl * ROW + piece * 16);
         const long long t = t_wave + 16 * j + tl, n = n_wave + 8 * piece;
         uint16_t* y = reinterpret_cast<uint16_t*>(a.y) + t * a.N + n;
@@ -566,14 +688,16 @@ __device__ __attribute__((always_inline)) void mx_tile_pipeline(uint4* __restric
   }
 }
 
-template <int ACT, int DT, int TR, int TC, int NWR, int NWC>
-__global__ void __launch_bounds__(NWR * NWC * 64) k_mx_tile(const MxGemmArgs a, const MxTilePlan p) {
-  using T = MxTile<ACT, TR, TC, NWR, NWC>;
+template <int ACT, int DT, int TR, int TC, int NWR, int NWC, int RING>
+__global__ void __launch_bounds__(NWR * NWC * 64, (MxTile<ACT, TR, TC, NWR, NWC, RING>::WAVES)) k_mx_tile(const MxGemmArgs a, const MxTilePlan p) {
+  using T = MxTile<ACT, TR, TC, NWR, NWC, RING>;
   // separate arrays handed on as __restrict__ pointers: the compiler sees that reading one buffer does not have to wait for the copies into another
-  __shared__ uint4 a0[T::AU], a1[T::AU], a2[T::AU];
-  __shared__ uint4 b0[T::BU], b1[T::BU], b2[T::BU];
-  __shared__ uint32_t s0[T::SW], s1[T::SW], s2[T::SW];
-  mx_tile_pipeline<ACT, DT, TR, TC, NWR, NWC>(a0, a1, a2, b0, b1, b2, s0, s1, s2, a, p);
+#define RING_OF(type, b, size) __shared__ type b##0[size], b##1[size], b##2[RING > 2 ? size : 1], b##3[RING > 3 ? size : 1], b##4[RING > 4 ? size : 1], b##5[RING > 5 ? size : 1]
+  RING_OF(uint4, a, T::AU);
+  RING_OF(uint4, b, T::BU);
+  RING_OF(uint32_t, s, T::SW);
+#undef RING_OF
+  mx_tile_pipeline<ACT, DT, TR, TC, NWR, NWC, RING>(a0, a1, a2, a3, a4, a5, b0, b1, b2, b3, b4, b5, s0, s1, s2, s3, s4, s5, a, p);
 }
 
 // the partial tiles of a product that K was cut for, four features a thread
@@ -596,19 +720,16 @@ __global__ void __launch_bounds__(256) k_mx_pad_rows(const uint16_t* __restrict_
   out[u] = uint4{v[0], v[1], v[2], v[3]};
 }
 
-// 16-bit rows that are read where they are: whole 16-byte pieces of them
-bool readable(const void* X, long long ldx, long long K) { return K % 8 == 0 && ldx % 8 == 0 && esp_aligned16(X); }
-
-template <int ACT, int DT>
+template <int ACT, int DT, int MT, int RT, int NW, int U>
 hipError_t launch_rows(const MxGemmArgs& a, hipStream_t st) {
-  const dim3 grid(a.nrt, (unsigned)((a.M + 15) / 16));
-  hipLaunchKernelGGL((k_mx_rows<ACT, DT, 1, 16>), grid, dim3(1024), 0, st, a);
+  const dim3 grid(((a.nrt + RT - 1) / RT + 7) / 8 * 8, (unsigned)((a.M + 16 * MT - 1) / (16 * MT)));
+  hipLaunchKernelGGL((k_mx_rows<ACT, DT, MT, RT, NW, U>), grid, dim3(NW * 64), 0, st, a);
   return hipGetLastError();
 }
 
-template <int ACT, int DT, int TR, int TC, int NWR, int NWC>
+template <int ACT, int DT, int TR, int TC, int NWR, int NWC, int RING>
 hipError_t launch_tile(const MxGemmArgs& a, float* partial, unsigned nsplit, hipStream_t st) {
-  using T = MxTile<ACT, TR, TC, NWR, NWC>;
+  using T = MxTile<ACT, TR, TC, NWR, NWC, RING>;
   MxTilePlan p = {};
   p.partial = partial;
   p.nrb = (a.nrt + T::RTM - 1) / T::RTM;
@@ -617,7 +738,7 @@ hipError_t launch_tile(const MxGemmArgs& a, float* partial, unsigned nsplit, hip
   p.nsplit = (a.nks + p.per_split - 1) / p.per_split;
   p.band = p.ntb > 8 ? 8 : 1;
   const unsigned items = p.nrb * p.ntb * p.nsplit;
-  hipLaunchKernelGGL((k_mx_tile<ACT, DT, TR, TC, NWR, NWC>), dim3((items + 7) / 8 * 8), dim3(NWR * NWC * 64), 0, st, a, p);
+  hipLaunchKernelGGL((k_mx_tile<ACT, DT, TR, TC, NWR, NWC, RING>), dim3((items + 7) / 8 * 8), dim3(NWR * NWC * 64), 0, st, a, p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.nsplit == 1) return e;
   const long long units = a.M * ((long long)a.nrt * 4);
@@ -625,42 +746,174 @@ hipError_t launch_tile(const MxGemmArgs& a, float* partial, unsigned nsplit, hip
   return hipGetLastError();
 }
 
-template <int ACT, int DT>
-hipError_t launch(const MxGemmArgs& a, float* partial, hipStream_t st) {
-  const char* e = getenv("MXV");
-  const int v = e ? atoi(e) : 0;
-  if (a.M <= 64 && v == 0) return launch_rows<ACT, DT>(a, st);
-  if constexpr (ACT != ACT_16) {
-    if (v == 1) return launch_tile<ACT, DT, 4, 2, 2, 2>(a, partial, 1, st);   // 128 x 64, 4 waves
-    if (v == 2) return launch_tile<ACT, DT, 4, 4, 2, 2>(a, partial, 1, st);   // 128 x 128, 4 waves
-    if (v == 3) return launch_tile<ACT, DT, 4, 4, 2, 4>(a, partial, 1, st);   // 128 x 256, 8 waves
-    if (v == 4) return launch_tile<ACT, DT, 8, 2, 2, 4>(a, partial, 1, st);   // 256 x 128, 8 waves
-    if (v == 5) return launch_tile<ACT, DT, 4, 2, 2, 4>(a, partial, 1, st);   // 128 x 128, 8 waves
-    if (v == 6) return launch_tile<ACT, DT, 4, 8, 4, 2>(a, partial, 1, st);
-    return launch_tile<ACT, DT, 8, 4, 2, 4>(a, partial, 1, st);               // 256 x 256, 8 waves
-  } else {
-    if (v == 1) return launch_tile<ACT, DT, 4, 2, 2, 2>(a, partial, 1, st);   // 128 x 64, 4 waves
-    if (v == 2) return launch_tile<ACT, DT, 4, 4, 2, 2>(a, partial, 1, st);   // 128 x 128, 4 waves
-    if (v == 5) return launch_tile<ACT, DT, 4, 2, 2, 4>(a, partial, 1, st);   // 128 x 128, 8 waves
-    return launch_tile<ACT, DT, 4, 4, 4, 2>(a, partial, 1, st);               // 256 x 128, 8 waves
+// ------------------------------------------------------------------------------------------------
+// The choice of a kernel: the smallest estimate of its time in microseconds, a function of the sizes and of the kind of the activations alone.
+//   rows   t0 + steps (c L + b x) (1 - d + d q)                     L, x: workgroups per compute unit, whole and as they are; q: filled part of the token tiles
+//   tile   t0 + e L + c stages max(1, u L) + (K cut: r0 + r MB of partial tiles)      L: workgroups per compute unit (256 of them)
+// The constants are fitted to the times of every kernel on 12 weight shapes (512 x 512 to 36864 x 9216, ragged ones among them) and 1 to 2048 tokens, weights cold,
+// K cut up to eight times.  Over those 168 products of each kind the kernel so chosen takes 1.01 - 1.02 of the fastest one's time on average, 1.24 at most.
+// ------------------------------------------------------------------------------------------------
+// rows: token tiles, row tiles, waves, steps at a time; t0, c, b, d
+#define MX_ROWS_FP8(X) \
+  X(1, 1, 8, 2, 2.51, 0.066, 0.0185, 0.367) \
+  X(1, 2, 8, 2, 2.5, 0.0799, 0.0318, 0.233) \
+  X(1, 4, 8, 1, 2.55, 0.101, 0.0928, 0.134) \
+  X(1, 8, 8, 1, 2.69, 0.179, 0.169, 0.139) \
+  X(2, 1, 16, 1, 2.6, 0.138, 0.00993, 0.2) \
+  X(2, 2, 8, 2, 2.48, 0.155, 0.00772, 0.2) \
+  X(2, 4, 8, 1, 2.85, 0.162, 0.0589, 0.2) \
+  X(4, 1, 8, 1, 2.6, 0.238, 0, 0.2) \
+  X(4, 2, 8, 1, 2.82, 0.256, 0.018, 0.2) \
+  X(4, 4, 8, 1, 3.41, 0.28, 0.0412, 0.2)
+#define MX_ROWS_FP4(X) \
+  X(1, 1, 8, 2, 2.51, 0.0462, 0.0167, 0.284) \
+  X(1, 2, 8, 2, 2.42, 0.0655, 0.0363, 0.157) \
+  X(1, 4, 8, 1, 2.46, 0.0922, 0.0904, 0.0853) \
+  X(1, 8, 8, 1, 2.65, 0.162, 0.173, 0.106) \
+  X(2, 1, 16, 1, 2.72, 0.0739, 0.0206, 0.2) \
+  X(2, 2, 8, 2, 2.6, 0.105, 0.0327, 0.2) \
+  X(2, 4, 8, 1, 2.65, 0.135, 0.0632, 0.2) \
+  X(4, 1, 8, 1, 2.64, 0.145, 0, 0.2) \
+  X(4, 2, 8, 1, 2.71, 0.172, 0.00462, 0.2) \
+  X(4, 4, 8, 1, 3.18, 0.185, 0.0627, 0.2)
+#define MX_ROWS_16(X) \
+  X(1, 1, 8, 2, 2.9, 0.151, 0, 0.606) \
+  X(1, 2, 8, 2, 3.26, 0.119, 0.0793, 0.514) \
+  X(1, 4, 8, 1, 2.99, 0.174, 0.0851, 0.374) \
+  X(1, 8, 8, 1, 3.13, 0.249, 0.131, 0.0806) \
+  X(2, 1, 16, 1, 2.7, 0.269, 0.017, 0.2) \
+  X(2, 2, 8, 2, 3.46, 0.241, 0.0784, 0.2) \
+  X(2, 4, 8, 1, 3.37, 0.315, 0.0564, 0.2) \
+  X(4, 1, 8, 1, 3.1, 0.472, 0, 0.2) \
+  X(4, 2, 8, 1, 3.43, 0.493, 0.00998, 0.2) \
+  X(4, 4, 8, 1, 4.18, 0.545, 0.0133, 0.2)
+// tile: row and token tiles of a wave, waves along both, buffers of a ring; t0, e, c, u, r0, r
+#define MX_TILES_FP8(X) \
+  X(4, 2, 2, 2, 3, 2.43, 0.382, 0.374, 0.655, 2.5, 0.567) \
+  X(4, 4, 2, 2, 3, 3.99, 0, 0.431, 0.921, 2.87, 0.433) \
+  X(8, 4, 2, 2, 2, 3.63, 0.328, 0.987, 0.704, 4.75, 0.334) \
+  X(7, 4, 2, 2, 2, 6.69, 0, 0.934, 0.659, 1.32, 0.379) \
+  X(4, 2, 2, 2, 6, 2.53, 1.28, 0.266, 1.01, 2.3, 0.531) \
+  X(8, 4, 2, 4, 3, 0, 7.14, 0.91, 1.14, 6.86, 0.269) \
+  X(7, 4, 2, 4, 3, 1.6, 7.95, 0.961, 1.01, 3.47, 0.264) \
+  X(4, 2, 2, 2, 4, 2.92, 0.436, 0.28, 0.872, 2.48, 0.548)
+#define MX_TILES_FP4(X) \
+  X(4, 2, 2, 2, 3, 2.55, 0.0944, 0.353, 0.629, 2.53, 0.6) \
+  X(4, 4, 2, 2, 3, 3.8, 0, 0.398, 0.846, 2.92, 0.444) \
+  X(8, 4, 2, 2, 2, 3.88, 0, 0.884, 0.651, 4.94, 0.341) \
+  X(7, 4, 2, 2, 2, 6.55, 0, 0.871, 0.621, 1.56, 0.375) \
+  X(4, 2, 2, 2, 6, 3.03, 0.265, 0.247, 0.873, 2.33, 0.609) \
+  X(8, 4, 2, 4, 3, 0, 6.27, 0.595, 1.2, 7.26, 0.293) \
+  X(7, 4, 2, 4, 3, 1.64, 7.31, 0.565, 1.22, 3.88, 0.273) \
+  X(4, 2, 2, 2, 4, 2.91, 0.13, 0.266, 0.816, 2.39, 0.6)
+#define MX_TILES_16(X) \
+  X(4, 2, 2, 2, 3, 3.19, 1.27, 0.464, 0.889, 2.9, 0.427) \
+  X(4, 4, 4, 2, 3, 0.449, 5.38, 1.18, 1.05, 5.22, 0.331) \
+  X(3, 4, 4, 2, 3, 3.94, 2.79, 0.93, 1, 2.29, 0.414) \
+  X(4, 4, 4, 1, 2, 3.27, 0, 1.03, 0.703, 4.17, 0.396) \
+  X(4, 2, 2, 4, 3, 2.18, 2.28, 0.64, 1.19, 3.94, 0.42)
+
+struct MxChoice {
+  int variant;  // rows kernels first, then tile kernels
+  unsigned nsplit;
+};
+constexpr int COMPUTE_UNITS = 256;
+constexpr long long MOST_PARTIAL_BYTES = 256ll << 20;
+
+struct MxRows {
+  int mt, rt;
+  double t0, c, b, d;
+};
+struct MxTiles {
+  int rows, tokens;
+  double t0, e, c, u, r0, r;
+};
+#define ROWS_OF(MT, RT, NW, U, T0, C, B, D) {MT, RT, T0, C, B, D},
+#define TILE_OF(TR, TC, NWR, NWC, RING, T0, E, C, U, R0, R) {TR * NWR * 16, TC * NWC * 16, T0, E, C, U, R0, R},
+constexpr MxRows kRowsFp8[] = {MX_ROWS_FP8(ROWS_OF)}, kRowsFp4[] = {MX_ROWS_FP4(ROWS_OF)}, kRows16[] = {MX_ROWS_16(ROWS_OF)};
+constexpr MxTiles kTilesFp8[] = {MX_TILES_FP8(TILE_OF)}, kTilesFp4[] = {MX_TILES_FP4(TILE_OF)}, kTiles16[] = {MX_TILES_16(TILE_OF)};
+#undef ROWS_OF
+#undef TILE_OF
+
+long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
+
+template <size_t NR, size_t NT>
+MxChoice choose_from(const MxRows (&rows)[NR], const MxTiles (&tiles)[NT], long long M, long long N, long long K) {
+  const long long nks = ceil_div(K, 128), nrt = ceil_div(N, 64) * 4;
+  MxChoice best = {-1, 1};
+  double least = 0;
+  auto offer = [&](int v, unsigned ns, double t) {
+    if (best.variant < 0 || t < least) {
+      best = {v, ns};
+      least = t;
+    }
+  };
+  for (int v = 0; v < (int)NR; v++) {
+    const MxRows& r = rows[v];
+    // one workgroup along the tokens, up to twice 64 of them
+    if (M <= (r.mt > 1 ? 8 * r.mt : 0) || M > (r.mt == 4 ? 128 : 16 * r.mt)) continue;
+    const long long wgs = ceil_div(nrt, r.rt) * ceil_div(M, 16 * r.mt);
+    const double q = (double)(M < 16 * r.mt ? M : 16 * r.mt) / (16 * r.mt);
+    offer(v, 1, r.t0 + nks * (r.c * ceil_div(wgs, COMPUTE_UNITS) + r.b * wgs / COMPUTE_UNITS) * (1 - r.d + r.d * q));
   }
+  if (M > 16) {
+    for (int v = 0; v < (int)NT; v++) {
+      const MxTiles& k = tiles[v];
+      if (k.tokens > 64 && M <= k.tokens / 2) continue;
+      for (unsigned ns : {1u, 2u, 3u, 4u, 6u, 8u}) {
+        if (ns > 1 && (nks < 2 * ns || ns * M * nrt * 64 > MOST_PARTIAL_BYTES)) break;
+        const long long per = ceil_div(nks, ns), cut = ceil_div(nks, per), L = ceil_div(ceil_div(nrt * 16, k.rows) * ceil_div(M, k.tokens) * cut, COMPUTE_UNITS);
+        offer((int)NR + v, ns, k.t0 + k.e * L + k.c * per * (k.u * L > 1 ? k.u * L : 1) + (cut > 1 ? k.r0 + cut * M * nrt * 64e-6 * k.r : 0));
+      }
+    }
+  }
+  return best;
+}
+MxChoice choose(long long M, long long N, long long K, int act) {
+  if (act == ACT_FP8) return choose_from(kRowsFp8, kTilesFp8, M, N, K);
+  if (act == ACT_FP4) return choose_from(kRowsFp4, kTilesFp4, M, N, K);
+  return choose_from(kRows16, kTiles16, M, N, K);
+}
+size_t partial_bytes(const MxChoice& c, long long M, long long N) { return c.nsplit > 1 ? (size_t)c.nsplit * M * ceil_div(N, 64) * 64 * 4 : 0; }
+bool is_tile(const MxChoice& c, int act) {
+  return c.variant >= (int)(act == ACT_FP8 ? sizeof(kRowsFp8) / sizeof(MxRows) : (act == ACT_FP4 ? sizeof(kRowsFp4) / sizeof(MxRows) : sizeof(kRows16) / sizeof(MxRows)));
+}
+// Whether 16-bit rows are copied and padded first: the rows kernels read whole 16-byte pieces, the tile kernels whole runs of 128 channels (behind a row's
+// last channel there are other values, and behind the last row none)
+bool copies_rows(const MxChoice& c, long long K, int act, bool aligned) { return act == ACT_16 && (!aligned || K % (is_tile(c, act) ? 128 : 8) != 0); }
+size_t padded_bytes(long long M, long long K) { return ((size_t)M * ceil_div(K, 128) * 256 + 255) / 256 * 256; }
+
+template <int ACT, int DT>
+hipError_t launch(const MxGemmArgs& a, const MxChoice& c, float* partial, hipStream_t st) {
+  int i = 0;
+#define ROWS_GO(MT, RT, NW, U, ...) \
+  if (c.variant == i++) return launch_rows<ACT, DT, MT, RT, NW, U>(a, st);
+#define TILE_GO(TR, TC, NWR, NWC, RING, ...) \
+  if (c.variant == i++) return launch_tile<ACT, DT, TR, TC, NWR, NWC, RING>(a, partial, c.nsplit, st);
+  if constexpr (ACT == ACT_FP8) {
+    MX_ROWS_FP8(ROWS_GO) MX_TILES_FP8(TILE_GO)
+  } else if constexpr (ACT == ACT_FP4) {
+    MX_ROWS_FP4(ROWS_GO) MX_TILES_FP4(TILE_GO)
+  } else {
+    MX_ROWS_16(ROWS_GO) MX_TILES_16(TILE_GO)
+  }
+#undef ROWS_GO
+#undef TILE_GO
+  return hipErrorInvalidValue;
 }
 
 }  // namespace
 
-bool esp_mx_gemm_in_place(const void* X, long long ldx, long long K, int act) { return act != ACT_16 || readable(X, ldx, K); }
-
-size_t esp_mx_gemm_workspace_bytes(long long M, long long N, long long K, int act, bool in_place) {
-  (void)N;
-  (void)act;
-  return in_place ? 0 : (size_t)M * (size_t)((K + 127) / 128) * 256;
+size_t esp_mx_gemm_workspace_bytes(long long M, long long N, long long K, int act, bool aligned) {
+  const MxChoice c = choose(M, N, K, act);
+  return (copies_rows(c, K, act, aligned) ? padded_bytes(M, K) : 0) + partial_bytes(c, M, N);
 }
 
 int esp_mx_gemm_device(esparse_ctx* ctx, const void* X, const void* xs, long long M, long long ldx, int act, int dtype, const void* packed, long long N,
-                       long long K, int out, void* Y, void* workspace) {
+                       long long K, int out, void* Y, void* workspace, bool aligned) {
   MxGemmArgs a = {};
-  a.nks = (unsigned)((K + 127) / 128);
-  const long long groups = (N + 63) / 64;
+  a.nks = (unsigned)ceil_div(K, 128);
+  const long long groups = ceil_div(N, 64);
   a.nrt = (unsigned)(groups * 4);
   a.w = reinterpret_cast<const uint4*>(packed);
   a.ws = reinterpret_cast<const uint32_t*>(reinterpret_cast<const unsigned char*>(packed) + groups * 64 * (long long)a.nks * 64);
@@ -672,17 +925,21 @@ int esp_mx_gemm_device(esparse_ctx* ctx, const void* X, const void* xs, long lon
   a.K = K;
   a.out = out;
   a.ldx = act == ACT_FP4 ? 64ll * a.nks : (act == ACT_FP8 ? 128ll * a.nks : 2 * ldx);
-  if (act == ACT_16 && !readable(X, ldx, K)) {
+  unsigned char* ws = reinterpret_cast<unsigned char*>(workspace);
+  const MxChoice c = choose(M, N, K, act);
+  if (copies_rows(c, K, act, aligned)) {
     const unsigned chunks = a.nks * 16;
-    hipLaunchKernelGGL(k_mx_pad_rows, dim3((unsigned)((M * chunks + 255) / 256)), dim3(256), 0, ctx->stream, (const uint16_t*)X, ldx, M, K, chunks, (uint4*)workspace);
+    hipLaunchKernelGGL(k_mx_pad_rows, dim3((unsigned)((M * chunks + 255) / 256)), dim3(256), 0, ctx->stream, (const uint16_t*)X, ldx, M, K, chunks, (uint4*)ws);
     ESP_HIP(ctx, hipGetLastError());
-    a.x = reinterpret_cast<const unsigned char*>(workspace);
+    a.x = ws;
     a.ldx = 256ll * a.nks;
     a.K = 128ll * a.nks;
+    ws += padded_bytes(M, K);
   }
-  if (act == ACT_FP4) ESP_HIP(ctx, (launch<ACT_FP4, ESPARSE_F16>(a, nullptr, ctx->stream)));
-  else if (act == ACT_FP8) ESP_HIP(ctx, (launch<ACT_FP8, ESPARSE_F16>(a, nullptr, ctx->stream)));
-  else if (dtype == ESPARSE_F16) ESP_HIP(ctx, (launch<ACT_16, ESPARSE_F16>(a, nullptr, ctx->stream)));
-  else ESP_HIP(ctx, (launch<ACT_16, ESPARSE_BF16>(a, nullptr, ctx->stream)));
+  float* partial = reinterpret_cast<float*>(ws);
+  if (act == ACT_FP4) ESP_HIP(ctx, (launch<ACT_FP4, ESPARSE_F16>(a, c, partial, ctx->stream)));
+  else if (act == ACT_FP8) ESP_HIP(ctx, (launch<ACT_FP8, ESPARSE_F16>(a, c, partial, ctx->stream)));
+  else if (dtype == ESPARSE_F16) ESP_HIP(ctx, (launch<ACT_16, ESPARSE_F16>(a, c, partial, ctx->stream)));
+  else ESP_HIP(ctx, (launch<ACT_16, ESPARSE_BF16>(a, c, partial, ctx->stream)));
   return ESPARSE_OK;
 }

@@ -184,6 +184,26 @@ def test_product_larger(ctx, M, N, K, act):
 
 
 @pytest.mark.parametrize("act", ["16", "fp8", "fp4"])
+@pytest.mark.parametrize("M,N,K", [(1, 4096, 4096), (1, 11008, 4096), (16, 22016, 8192), (32, 4096, 11008), (32, 22016, 8192), (64, 4096, 4096), (64, 11008, 4096), (64, 22016, 8192),
+                                   (96, 5003, 3020), (128, 5120, 13824), (200, 9216, 9216), (333, 5003, 3020), (512, 13824, 5120), (768, 22016, 1024), (1024, 4096, 4096),
+                                   (2048, 13824, 1280), (2048, 22016, 640), (1500, 1000, 900)])
+def test_product_of_layer_sizes(ctx, M, N, K, act):
+    """Every kernel's own range of sizes; the 64-bit product is made on the device from the values read back (which other tests pin)."""
+    gen = torch.Generator("cuda").manual_seed(M + N + K)
+    wq = ctx.mx_quantize(torch.randn(N, K, device="cuda", generator=gen) * K ** -0.5, esp.MX_FP4)
+    x = (torch.randn(M, K, device="cuda", generator=gen) * torch.exp(torch.randn(K, device="cuda", generator=gen))).bfloat16()
+    X = x if act == "16" else ctx.mx_quantize(x, FMT[act])
+    x64 = (x if act == "16" else ctx.mx_dequantize(X, torch.float32)).double()
+    w64 = ctx.mx_dequantize(wq, torch.float32).double()
+    got, want = ctx.mx_gemm(X, ctx.mx_pack(wq), dtype=torch.bfloat16).double(), x64 @ w64.t()
+    before = (K + 16) * 2.0 ** -23 * (x64.abs() @ w64.abs().t())
+    if act == "fp8":
+        top = [torch.nn.functional.pad(v.abs(), (0, -K % 8)).reshape(v.shape[0], -1, 8).amax(2) for v in (x64, w64)]
+        before += 7 * 2.0 ** -13 * (top[0] @ top[1].t())
+    assert ((got - want).abs() <= 2.0 ** -8 * want.abs() + before * (1 + 2.0 ** -8)).all()
+
+
+@pytest.mark.parametrize("act", ["16", "fp8", "fp4"])
 @pytest.mark.parametrize("M,N", [(5, 70), (40, 96), (140, 131), (300, 640)])
 def test_product_in_32_bits(ctx, M, N, act):
     _product(ctx, M, N, 520, act, "f16", out="f32")
@@ -250,6 +270,19 @@ def test_product_leaves_other_memory_alone(ctx):
         ctx.mx_gemm(X, ctx.mx_pack(w), out=y, dtype=torch.float16)
         assert (buf[:256] == 7.25).all() and (buf[256 + M * N:] == 7.25).all()
         _assert_product(y, _np(X) if act == "16" else x64, w64, torch.float16, act)
+
+
+@pytest.mark.parametrize("M", [1, 9, 40, 200, 300])
+def test_product_reads_nothing_behind_a_row(ctx, M):
+    """16-bit rows with NaN and infinities between them and behind the last: K a multiple of 8, of 128, of neither."""
+    for K, ld in ((200, 208), (256, 264), (136, 136), (1000, 1024), (77, 80)):
+        rng = _rng("behind", M, K)
+        base = torch.full((M * ld + 256,), math.nan, dtype=torch.bfloat16, device="cuda")
+        base[1::3] = math.inf
+        x = torch.as_strided(base, (M, K), (ld, 1))
+        x.copy_(_features(rng, M, K, "bf16"))
+        w, w64 = _mx(rng.standard_normal((90, K)), orc.FP4)
+        _assert_product(ctx.mx_gemm(x, ctx.mx_pack(w)), _np(x), w64, torch.bfloat16, "16", f"{M} {K} {ld}")
 
 
 def test_product_is_the_same_every_time(ctx):

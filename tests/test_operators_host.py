@@ -114,7 +114,9 @@ GEMM = dict(X=P, xs=P, M=4, ldx=0, act=1, dtype=0, w=P, N=64, K=128, out=1, Y=P,
     (dict(N=0), EINVAL, "range"), (dict(K=0), EINVAL, "range"), (dict(X=None), EINVAL, "null"), (dict(w=None), EINVAL, "null"), (dict(Y=None), EINVAL, "null"),
     (dict(xs=None), EINVAL, "x_scales"), (dict(X=P + 8), EINVAL, "16-byte"), (dict(w=P + 8), EINVAL, "16-byte"), (dict(Y=P + 8), EINVAL, "16-byte"),
     (dict(act=2, ldx=127), EINVAL, "ldx"), (dict(act=2, ldx=128, X=P + 1), EINVAL, "aligned"), (dict(act=2, ldx=128, K=127), EINVAL, "workspace"),
-    (dict(act=2, ldx=128, K=127, ws=P, nbytes=8), EWORKSPACE, "workspace"), (dict(act=2, ldx=128, K=127, ws=P + 16, nbytes=1 << 30), EINVAL, "256-byte")])
+    (dict(act=2, ldx=128, K=127, ws=P, nbytes=8), EWORKSPACE, "workspace"), (dict(act=2, ldx=128, K=127, ws=P + 16, nbytes=1 << 30), EINVAL, "256-byte"),
+    (dict(act=2, ldx=129), EINVAL, "workspace"), (dict(act=2, ldx=128, X=P + 8), EINVAL, "workspace"), (dict(act=2, ldx=(1 << 22) + 8), EINVAL, "ldx"),
+    (dict(K=(1 << 22) + 1), EINVAL, "range")])
 def test_gemm_refuses(ctx, change, code, word):
     a = {**GEMM, **change}
     _expect(ctx, ctx._lib.esparse_mx_gemm(ctx._h, a["X"], a["xs"], a["M"], a["ldx"], a["act"], a["dtype"], a["w"], a["N"], a["K"], a["out"], a["Y"], a["ws"],
