@@ -577,57 +577,65 @@ class Context:
         self._check(self._lib.esparse_tune_load(self._h, path.encode()))
 
     # -- microscaled numbers and the steps around a product -------------------------------------
-    def _here(self, name: str, *tensors) -> None:
-        for t in tensors:
-            if t is not None and not (t.is_cuda and t.get_device() == self.device):
-                raise ValueError(f"{name}: a tensor is on {t.device}, the context on cuda:{self.device}")
+    def _away(self, name: str, *tensors):
+        where = ", ".join(str(t.device) for t in tensors)
+        raise ValueError(f"{name}: a tensor is on {where}, the context on cuda:{self.device}")
 
-    def _rows(self, name: str, t: torch.Tensor) -> int:
-        """Values from row to row of a matrix whose rows are contiguous."""
+    def _rows(self, name: str, t: torch.Tensor):
+        """(rows, values of a row, values from row to row) of a matrix on the context's device whose rows are contiguous."""
+        if t.get_device() != self.device:
+            self._away(name, t)
         if t.dim() != 2:
             raise ValueError(f"{name}: {t.dim()} dimensions instead of two")
         R, K = t.shape
+        if t.is_contiguous():
+            return R, K, K
         if K > 1 and t.stride(1) != 1:
             raise ValueError(f"{name}: the values of a row are {t.stride(1)} apart")
         if R > 1 and t.stride(0) < K:
             raise ValueError(f"{name}: rows overlap (stride {t.stride(0)} for {K} values)")
-        return t.stride(0) if R > 1 else K
+        return R, K, t.stride(0) if R > 1 else K
 
     def _check_mx(self, name: str, x: MX) -> int:
-        """The number of rows; the tensors' shapes are those of the format."""
-        R, steps = x.data.shape[0], (x.K + 127) // 128
+        """The number of rows; the tensors are on the context's device and of the format's shapes."""
+        data, scales = x.data, x.scales
+        if data.get_device() != self.device or scales.get_device() != self.device:
+            self._away(name, data, scales)
+        R, steps = data.shape[0], (x.K + 127) // 128
         if x.fmt not in (MX_FP4, MX_FP8):
             raise ValueError(f"{name}: format {x.fmt} is neither MX_FP4 nor MX_FP8")
-        if tuple(x.data.shape) != (R, steps * (64 if x.fmt == MX_FP4 else 128)) or tuple(x.scales.shape) != (steps, R, 4):
-            raise ValueError(f"{name}: data {tuple(x.data.shape)} and scales {tuple(x.scales.shape)} are not those of {R} rows of {x.K} channels")
-        if x.data.dtype != torch.uint8 or x.scales.dtype != torch.uint8 or not x.data.is_contiguous() or not x.scales.is_contiguous():
+        if data.shape != (R, steps * (64 if x.fmt == MX_FP4 else 128)) or scales.shape != (steps, R, 4):
+            raise ValueError(f"{name}: data {tuple(data.shape)} and scales {tuple(scales.shape)} are not those of {R} rows of {x.K} channels")
+        if data.dtype != torch.uint8 or scales.dtype != torch.uint8 or not data.is_contiguous() or not scales.is_contiguous():
             raise ValueError(f"{name}: data and scales are contiguous uint8 tensors")
         return R
 
-    def _empty_mx(self, R: int, K: int, fmt: int) -> MX:
+    @staticmethod
+    def _empty_mx(like: torch.Tensor, R: int, K: int, fmt: int) -> MX:
         if fmt not in (MX_FP4, MX_FP8):
             raise ValueError(f"format {fmt} is neither MX_FP4 nor MX_FP8")
-        steps, dev = (K + 127) // 128, f"cuda:{self.device}"
-        return MX(torch.empty((R, steps * (64 if fmt == MX_FP4 else 128)), dtype=torch.uint8, device=dev),
-                  torch.empty((steps, R, 4), dtype=torch.uint8, device=dev), K, fmt)
+        steps = (K + 127) // 128
+        return MX(like.new_empty((R, steps * (64 if fmt == MX_FP4 else 128)), dtype=torch.uint8),
+                  like.new_empty((steps, R, 4), dtype=torch.uint8), K, fmt)
 
     def mx_quantize(self, X: torch.Tensor, fmt: int) -> MX:
         """X[R, K] (f16, bf16, f32; rows may be apart) in microscaled 8 or 4 bits."""
-        code, ld = _code(X.dtype, "mx_quantize", f32=True), self._rows("mx_quantize", X)
-        self._here("mx_quantize", X)
-        R, K = X.shape
-        out = self._empty_mx(R, K, fmt)
+        code, (R, K, ld) = _code(X.dtype, "mx_quantize", f32=True), self._rows("mx_quantize", X)
+        out = self._empty_mx(X, R, K, fmt)
         self._sync_stream()
-        self._check(self._lib.esparse_mx_quantize(self._h, X.data_ptr(), R, K, ld, code, fmt, out.data.data_ptr(), out.scales.data_ptr()))
+        rc = self._lib.esparse_mx_quantize(self._h, X.data_ptr(), R, K, ld, code, fmt, out.data.data_ptr(), out.scales.data_ptr())
+        if rc:
+            self._check(rc)
         return out
 
     def mx_dequantize(self, x: MX, dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
         """The values [R, K] that x stands for."""
         code, R = _code(dtype, "mx_dequantize", f32=True), self._check_mx("mx_dequantize", x)
-        self._here("mx_dequantize", x.data, x.scales)
-        out = torch.empty((R, x.K), dtype=dtype, device=x.data.device)
+        out = x.data.new_empty((R, x.K), dtype=dtype)
         self._sync_stream()
-        self._check(self._lib.esparse_mx_dequantize(self._h, x.data.data_ptr(), x.scales.data_ptr(), R, x.K, x.fmt, code, out.data_ptr()))
+        rc = self._lib.esparse_mx_dequantize(self._h, x.data.data_ptr(), x.scales.data_ptr(), R, x.K, x.fmt, code, out.data_ptr())
+        if rc:
+            self._check(rc)
         return out
 
     def mx_pack(self, w: MX) -> MXWeight:
@@ -635,8 +643,7 @@ class Context:
         N = self._check_mx("mx_pack", w)
         if w.fmt != MX_FP4:
             raise ValueError("mx_pack: weights are in 4 bits (MX_FP4)")
-        self._here("mx_pack", w.data, w.scales)
-        packed = torch.empty(mx_packed_size(N, w.K), dtype=torch.uint8, device=w.data.device)
+        packed = w.data.new_empty(mx_packed_size(N, w.K))
         self._sync_stream()
         self._check(self._lib.esparse_mx_pack(self._h, w.data.data_ptr(), w.scales.data_ptr(), N, w.K, packed.data_ptr()))
         return MXWeight(packed, N, w.K)
@@ -644,31 +651,33 @@ class Context:
     def mx_gemm(self, X, w: MXWeight, *, dtype: Optional[torch.dtype] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """X . W^T in `dtype` (f16, bf16 or f32).  X: an MX of 8 or 4 bits (dtype: bf16 if not given), or a 16-bit matrix whose rows may be apart
         (dtype: its own), with which the weights alone are in 4 bits."""
+        packed, N = w.packed, w.N
         if isinstance(X, MX):
-            M, K, act, code, ld = self._check_mx("mx_gemm", X), X.K, X.fmt, 0, 0
-            self._here("mx_gemm", X.data, X.scales, w.packed)
+            M, K, act, code, ld, aligned = self._check_mx("mx_gemm", X), X.K, X.fmt, 0, 0, True
             x, scales, given = X.data.data_ptr(), X.scales.data_ptr(), torch.bfloat16
         else:
-            code, ld, act = _code(X.dtype, "mx_gemm"), self._rows("mx_gemm", X), _ACT_16
-            self._here("mx_gemm", X, w.packed)
-            (M, K), x, scales, given = X.shape, X.data_ptr(), None, X.dtype
-        N = w.N
+            given = X.dtype
+            code, (M, K, ld), act = _code(given, "mx_gemm"), self._rows("mx_gemm", X), _ACT_16
+            x, scales = X.data_ptr(), None
+            aligned = not (ld % 8 or x % 16)
         if K != w.K:
             raise ValueError(f"mx_gemm: activations of {K} channels, weights of {w.K}")
-        if w.packed.dtype != torch.uint8 or not w.packed.is_contiguous() or w.packed.numel() != _known_mx_packed_size(N, K):
+        if packed.get_device() != self.device:
+            self._away("mx_gemm", packed)
+        if packed.dtype != torch.uint8 or packed.numel() != _known_mx_packed_size(N, K) or not packed.is_contiguous():
             raise ValueError(f"mx_gemm: packed is not the weights of {N} x {K}")
         if out is None:
-            out = torch.empty((M, N), dtype=dtype or given, device=w.packed.device)
-        else:
-            self._here("mx_gemm", out)
-            if tuple(out.shape) != (M, N) or not out.is_contiguous() or (dtype is not None and out.dtype != dtype):
-                raise ValueError(f"mx_gemm: out is not a contiguous [{M}, {N}] of the type asked for")
+            out = packed.new_empty((M, N), dtype=dtype or given)
+        elif out.get_device() != self.device:
+            self._away("mx_gemm", out)
+        elif out.shape != (M, N) or not out.is_contiguous() or (dtype is not None and out.dtype != dtype):
+            raise ValueError(f"mx_gemm: out is not a contiguous [{M}, {N}] of the type asked for")
         out_code = _code(out.dtype, "mx_gemm", f32=True)
-        nbytes = _known_mx_gemm_workspace(M, N, K, act, act != _ACT_16 or not (ld % 8 or x % 16))
+        nbytes = _known_mx_gemm_workspace(M, N, K, act, aligned)
         # a block of its own for each call: calls on several streams and captured graphs do not share it
-        ws = torch.empty(nbytes, dtype=torch.uint8, device=out.device) if nbytes else None
+        ws = packed.new_empty(nbytes) if nbytes else None
         self._sync_stream()
-        rc = self._lib.esparse_mx_gemm(self._h, x, scales, M, ld, act, code, w.packed.data_ptr(), N, K, out_code, out.data_ptr(), _ptr(ws), nbytes)
+        rc = self._lib.esparse_mx_gemm(self._h, x, scales, M, ld, act, code, packed.data_ptr(), N, K, out_code, out.data_ptr(), _ptr(ws), nbytes)
         if rc:
             self._check(rc)
         return out
@@ -677,45 +686,58 @@ class Context:
                  fmt: Optional[int] = None, sum_out: Optional[torch.Tensor] = None):
         """(y, h): h = x + residual (h is x itself where there is no residual), y = h weight / sqrt(mean(h^2) + eps), in the type of x
         (fmt None) or as an MX.  sum_out: where to write h; x or residual for an update in place."""
-        code, ldx = _code(x.dtype, "rms_norm"), self._rows("rms_norm", x)
-        R, K = x.shape
-        self._here("rms_norm", x, weight, residual, sum_out)
-        if weight.dtype != x.dtype or tuple(weight.shape) != (K,) or not weight.is_contiguous():
+        dtype = x.dtype
+        code, (R, K, ldx) = _code(dtype, "rms_norm"), self._rows("rms_norm", x)
+        if weight.get_device() != self.device:
+            self._away("rms_norm", weight)
+        if weight.dtype != dtype or weight.shape != (K,) or not weight.is_contiguous():
             raise ValueError(f"rms_norm: weight is not a contiguous [{K}] of the type of x")
-        ldr = 0
+        r, ldr = None, 0
         if residual is not None:
-            if residual.dtype != x.dtype or residual.shape != x.shape:
+            rows, channels, ldr = self._rows("rms_norm", residual)
+            if residual.dtype != dtype or rows != R or channels != K:
                 raise ValueError("rms_norm: residual is not of the shape and type of x")
-            ldr = self._rows("rms_norm", residual)
+            r = residual.data_ptr()
             if sum_out is None:
-                sum_out = torch.empty((R, K), dtype=x.dtype, device=x.device)
-        if sum_out is not None and (sum_out.dtype != x.dtype or sum_out.shape != x.shape or not sum_out.is_contiguous()):
-            raise ValueError("rms_norm: sum_out is not a contiguous tensor of the shape and type of x")
+                sum_out = x.new_empty((R, K))
+        if sum_out is not None:
+            if sum_out.get_device() != self.device:
+                self._away("rms_norm", sum_out)
+            if sum_out.dtype != dtype or sum_out.shape != (R, K) or not sum_out.is_contiguous():
+                raise ValueError("rms_norm: sum_out is not a contiguous tensor of the shape and type of x")
+        h = None if sum_out is None else sum_out.data_ptr()
         if fmt is None:
-            y, q = torch.empty((R, K), dtype=x.dtype, device=x.device), None
+            y = x.new_empty((R, K))
+            to = y.data_ptr(), 0, None, None
         else:
-            y, q = None, self._empty_mx(R, K, fmt)
+            y = self._empty_mx(x, R, K, fmt)
+            to = None, fmt, y.data.data_ptr(), y.scales.data_ptr()
         self._sync_stream()
-        self._check(self._lib.esparse_rms_norm(self._h, x.data_ptr(), ldx, _ptr(residual), ldr, weight.data_ptr(), R, K, eps, code, _ptr(sum_out), _ptr(y),
-                                               fmt or 0, q.data.data_ptr() if q else None, q.scales.data_ptr() if q else None))
-        return (y if q is None else q), (x if sum_out is None else sum_out)
+        rc = self._lib.esparse_rms_norm(self._h, x.data_ptr(), ldx, r, ldr, weight.data_ptr(), R, K, eps, code, h, *to)
+        if rc:
+            self._check(rc)
+        return y, (x if sum_out is None else sum_out)
 
     def token_logprobs(self, logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, *, top: int = 0) -> TokenLogprobs:
         """Per row of logits[R, V] (f16, bf16, f32; rows may be apart): ln p of tokens[R] (int64; below 0: none, gives 0), the entropy, and the
         `top` most probable tokens in order."""
-        code, ld = _code(logits.dtype, "token_logprobs", f32=True), self._rows("token_logprobs", logits)
-        R, V = logits.shape
-        self._here("token_logprobs", logits, tokens)
-        if tokens is not None and (tokens.dtype != torch.int64 or tuple(tokens.shape) != (R,) or not tokens.is_contiguous()):
-            raise ValueError(f"token_logprobs: tokens is not a contiguous int64 [{R}]")
-        dev = logits.device
+        code, (R, V, ld) = _code(logits.dtype, "token_logprobs", f32=True), self._rows("token_logprobs", logits)
         nbytes = _known_logprobs_workspace(R, V, code, top)
-        ws = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
-        logprob = torch.empty(R, dtype=torch.float32, device=dev) if tokens is not None else None
-        entropy = torch.empty(R, dtype=torch.float32, device=dev)
-        ids = torch.empty((R, top), dtype=torch.int32, device=dev) if top else None
-        lps = torch.empty((R, top), dtype=torch.float32, device=dev) if top else None
+        logprob = ids = lps = tok = lp = ip = tp = None
+        if tokens is not None:
+            if tokens.get_device() != self.device:
+                self._away("token_logprobs", tokens)
+            if tokens.dtype != torch.int64 or tokens.shape != (R,) or not tokens.is_contiguous():
+                raise ValueError(f"token_logprobs: tokens is not a contiguous int64 [{R}]")
+            logprob = logits.new_empty(R, dtype=torch.float32)
+            tok, lp = tokens.data_ptr(), logprob.data_ptr()
+        entropy = logits.new_empty(R, dtype=torch.float32)
+        if top:
+            ids, lps = logits.new_empty((R, top), dtype=torch.int32), logits.new_empty((R, top), dtype=torch.float32)
+            ip, tp = ids.data_ptr(), lps.data_ptr()
+        ws = logits.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
         self._sync_stream()
-        self._check(self._lib.esparse_token_logprobs(self._h, logits.data_ptr(), R, V, ld, code, _ptr(tokens), top, _ptr(logprob), entropy.data_ptr(),
-                                                     _ptr(ids), _ptr(lps), _ptr(ws), nbytes))
+        rc = self._lib.esparse_token_logprobs(self._h, logits.data_ptr(), R, V, ld, code, tok, top, lp, entropy.data_ptr(), ip, tp, _ptr(ws), nbytes)
+        if rc:
+            self._check(rc)
         return TokenLogprobs(logprob, entropy, ids, lps)

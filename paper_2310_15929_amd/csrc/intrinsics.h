@@ -57,6 +57,20 @@ __device__ __forceinline__ uint4 load_stream_16(const uint4* p) {
   const esp_u32x4 v = __builtin_nontemporal_load(reinterpret_cast<const esp_u32x4*>(p));
   return uint4{v.x, v.y, v.z, v.w};
 }
+// 16 and 8 bytes to an address of any alignment of two, past the caches: a kernel that writes much more than the L2 holds and reads none of it again is
+// up to twice as fast with them (values read back from 4 bits, 11008 x 13824: 118 -> 57 us, 6.8 TB/s)
+typedef unsigned int esp_u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+typedef unsigned int esp_u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+__device__ __forceinline__ void store_stream_16(void* p, const void* v) {
+  esp_u32x4_any q;
+  __builtin_memcpy(&q, v, 16);
+  __builtin_nontemporal_store(q, reinterpret_cast<esp_u32x4_any*>(p));
+}
+__device__ __forceinline__ void store_stream_8(void* p, const void* v) {
+  esp_u32x2_any q;
+  __builtin_memcpy(&q, v, 8);
+  __builtin_nontemporal_store(q, reinterpret_cast<esp_u32x2_any*>(p));
+}
 __device__ __forceinline__ uint32_t load_stream_4(const uint32_t* p) { return __builtin_nontemporal_load(p); }
 __device__ __forceinline__ void sched_fence() {
 #if defined(__HIP_DEVICE_COMPILE__)

@@ -1,11 +1,12 @@
 // Log probabilities of given tokens, the entropy and the most probable alternatives of rows of logits.
 //   with m the row's largest logit, s = sum exp(x - m), t = sum (x - m) exp(x - m):
 //   log p(token) = x_token - m - ln s,   entropy = ln s - t / s,   all in fp32 (x - m is taken before it is scaled to base 2).
-// Bound by memory at many rows: a row, or one of the pieces that it is cut into where there are few rows, is read once into
-// registers; maximum, sums and the alternatives are taken there.  A second launch joins the pieces of a row.
-//   Alternatives: T = the k-th largest of the threads' own maxima is a lower bound of the k-th largest value, so only values
-// of at least T are looked at again - little more than k of them, unless many are equal: where their list overflows, k
-// rounds of a search for the next in order take its place.  Order: larger value first, then lower index.
+// Bound by memory, at 16 bits nearly by the vector unit too (about 11 issue slots a value: conversion, maximum, difference, exponential, two sums).
+// A row is read once: each thread keeps a running maximum with s and t relative to it, and brings them to a new maximum where four 16-byte pieces
+// hold one.  Where there are few rows a row is cut into pieces, a workgroup each; a second launch joins them.
+//   Alternatives: T = the k-th largest of the threads' own maxima is a lower bound of the k-th largest value, so only threads whose
+// maximum reaches T (about k of them) read their values a second time, and only values of at least T are looked at: little more than k, unless many
+// are equal: where their list overflows, k rounds of a search for the next in order take its place.  Order: larger value first, then lower index.
 #include <hip/hip_runtime.h>
 
 #include "common.h"
@@ -91,126 +92,175 @@ __device__ __forceinline__ void place_candidates(const unsigned long long* list,
   }
 }
 
-// A workgroup of NT threads holds `C` pieces of 16 bytes a thread.  PARTS: the row is cut, the results go to the workspace.
-template <int DT, int NT, int C, bool PARTS>
-__global__ void __launch_bounds__(NT) k_lp_row(const LpOut o, long long R, unsigned pieces, LpPartial* __restrict__ part, unsigned long long* __restrict__ part_top) {
-  constexpr int E = DT == ESPARSE_F32 ? 4 : 8, NW = NT / 64;
-  __shared__ float s_a[NW], s_b[NW];
+// One wave with C keys a lane: the largest 32-bit pattern that at least `top` of the keys reach, or one below it that at most half as many again and SLACK more do
+constexpr int SLACK = 8;  // fewer rounds of the search for a few values more to look at
+template <int C>
+__device__ __forceinline__ uint32_t key_bound(const uint32_t (&key)[C], int top) {
+  uint32_t bound = 0;
+  for (int bit = 31; bit >= 0; bit--) {
+    const uint32_t trial = bound | 1u << bit;
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < C; i++) n += __builtin_popcountll(__ballot(key[i] >= trial));
+    if (n >= top) {
+      bound = trial;
+      if (n <= top + top / 2 + SLACK) break;
+    }
+  }
+  return bound;
+}
+
+constexpr int NT = 256, NW = NT / 64;
+constexpr int AT_ONCE = 4;  // pieces of 16 bytes a thread reads at a time
+
+// values of a 16-byte unit; behind the row's end minus infinity
+template <int DT>
+struct LpUnit {
+  static constexpr int E = DT == ESPARSE_F32 ? 4 : 8;
+  uint32_t raw[4];
+  __device__ __forceinline__ void load(const void* row, long long at, long long V) {
+    const long long left = V - at;
+    if constexpr (DT == ESPARSE_F32) {
+      const float* p = reinterpret_cast<const float*>(row) + at;
+      if (left >= E) {
+        __builtin_memcpy(raw, p, 16);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; i++) raw[i] = 0xff800000u;
+        if (left > 0) {
+#pragma unroll
+          for (int i = 0; i < 4; i++) raw[i] = __builtin_bit_cast(uint32_t, p[i < left ? i : left - 1]);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; i++) raw[i] = i < left ? raw[i] : 0xff800000u;
+      }
+    } else {
+      const uint16_t* p = reinterpret_cast<const uint16_t*>(row) + at;
+      constexpr uint32_t low = DT == ESPARSE_F16 ? 0xfc00u : 0xff80u;
+      if (left >= E) {
+        __builtin_memcpy(raw, p, 16);
+      } else {
+        uint32_t t[8];
+#pragma unroll
+        for (int i = 0; i < 8; i++) t[i] = low;
+        if (left > 0) {  // all loads under way at once: places behind the last repeat it
+#pragma unroll
+          for (int i = 0; i < 8; i++) t[i] = p[i < left ? i : left - 1];
+        }
+#pragma unroll
+        for (int i = 0; i < 4; i++) raw[i] = (2 * i < left ? t[2 * i] : low) | (2 * i + 1 < left ? t[2 * i + 1] : low) << 16;
+      }
+    }
+  }
+  __device__ __forceinline__ float value(int i) const {
+    if constexpr (DT == ESPARSE_F32) return __builtin_bit_cast(float, raw[i]);
+    else return esp_to_float<DT>((uint16_t)(raw[i / 2] >> (16 * (i & 1))));
+  }
+};
+
+// One workgroup: `units` units of the row from unit `piece * units` on (PARTS: results to the workspace; otherwise the whole row).
+template <int DT, bool PARTS>
+__global__ void __launch_bounds__(NT) k_lp_row(const LpOut o, unsigned pieces, unsigned units, LpPartial* __restrict__ part, unsigned long long* __restrict__ part_top) {
+  using Unit = LpUnit<DT>;
+  constexpr int E = Unit::E;
+  __shared__ float s_m[NW], s_s[NW], s_t[NW];
   __shared__ uint32_t s_key[NT];
   __shared__ unsigned long long s_list[LIST];
   __shared__ unsigned long long s_next[NW];
   __shared__ uint32_t s_from;
-  __shared__ int s_n;
-  const long long row = PARTS ? blockIdx.x / pieces : blockIdx.x;
-  const unsigned piece = PARTS ? blockIdx.x % pieces : 0, tid = threadIdx.x, wave = tid >> 6;
-  const long long base = (long long)piece * (NT * C * E);
-  const long long V = o.V;
-  uint32_t raw[C][4];
-  // value i of this thread's piece j stands at base + (j NT + tid) E + i; behind the row's end there are minus infinities
+  __shared__ int s_n, s_threads;
+  const long long row = PARTS ? blockIdx.x / pieces : blockIdx.x, V = o.V;
+  const unsigned piece = PARTS ? blockIdx.x - (unsigned)row * pieces : 0, tid = threadIdx.x, wave = tid >> 6;
+  const unsigned all = (unsigned)((V + E - 1) / E), first = piece * units, end = first + units < all ? first + units : all;
+  const void* x = reinterpret_cast<const unsigned char*>(o.logits) + row * o.ld * (DT == ESPARSE_F32 ? 4 : 2);
+  float m = minus_infinity(), from = 0.f, s = 0.f, t = 0.f;  // from: m, 0 while there is none
+  auto take = [&](const Unit (&v)[AT_ONCE]) {
+    float top = m;
 #pragma unroll
-  for (int j = 0; j < C; j++) {
-    const long long at = base + (long long)(j * NT + tid) * E, left = V - at;
-    if (DT == ESPARSE_F32) {
-      const float* p = reinterpret_cast<const float*>(o.logits) + row * o.ld + at;
-      if (left >= E) {
-        __builtin_memcpy(raw[j], p, 16);
-      } else {
+    for (int j = 0; j < AT_ONCE; j++)
 #pragma unroll
-        for (int i = 0; i < 4; i++) raw[j][i] = i < left ? __builtin_bit_cast(uint32_t, p[i]) : 0xff800000u;
-      }
-    } else {
-      const uint16_t* p = reinterpret_cast<const uint16_t*>(o.logits) + row * o.ld + at;
-      constexpr uint32_t low = DT == ESPARSE_F16 ? 0xfc00u : 0xff80u;
-      if (left >= E) {
-        __builtin_memcpy(raw[j], p, 16);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-          uint32_t a = low, b = low;
-          if (2 * i < left) a = p[2 * i];
-          if (2 * i + 1 < left) b = p[2 * i + 1];
-          raw[j][i] = a | b << 16;
-        }
-      }
+      for (int i = 0; i < E; i++) top = __builtin_fmaxf(top, v[j].value(i));
+    if (top > m) {
+      const float d = from - top, f = natural_exp(d);
+      t = s == 0.f ? 0.f : f * __builtin_fmaf(s, __builtin_fmaxf(d, -128.f), t);
+      s = s == 0.f ? 0.f : s * f;  // (the first maximum may be so low that f is infinite)
+      m = from = top;
     }
-  }
-  auto value = [&](int j, int i) -> float {
-    if constexpr (DT == ESPARSE_F32) return __builtin_bit_cast(float, raw[j][i]);
-    else return esp_to_float<DT>((uint16_t)(raw[j][i / 2] >> (16 * (i & 1))));
+#pragma unroll
+    for (int j = 0; j < AT_ONCE; j++)
+#pragma unroll
+      for (int i = 0; i < E; i++) {
+        const float d = v[j].value(i) - from, p = natural_exp(d);
+        s += p;
+        t = __builtin_fmaf(p, __builtin_fmaxf(d, -128.f), t);  // (p is 0 far above that; minus infinity times 0 is none)
+      }
   };
-  float mine = minus_infinity();
+  // (a second set of registers for the next values: no faster, 32 instead of 31 us for 2048 x 32000; eight workgroups a compute unit take turns as it is)
+  for (unsigned u = first + tid; u < end; u += AT_ONCE * NT) {
+    Unit v[AT_ONCE];
 #pragma unroll
-  for (int j = 0; j < C; j++)
-#pragma unroll
-    for (int i = 0; i < E; i++) mine = __builtin_fmaxf(mine, value(j, i));
-  const float wm = wave_max(mine);
-  if ((tid & 63u) == 0) s_a[wave] = wm;
-  const bool any = base + (long long)tid * E < V;  // (a thread without values is below all others)
-  if (o.top) s_key[tid] = any ? order_key(mine) : 0u;
-  if (tid == 0) s_n = 0;
+    for (int j = 0; j < AT_ONCE; j++) v[j].load(x, u + j * NT < end ? (long long)(u + j * NT) * E : V, V);
+    take(v);
+  }
+  const float wm = wave_max(m);
+  if ((tid & 63u) == 0) s_m[wave] = wm;
+  const bool any = first + tid < end;  // (a thread without values is below all others)
+  if (o.top) s_key[tid] = any ? order_key(m) : 0u;
+  if (tid == 0) s_n = s_threads = 0;
   __syncthreads();
-  float m = s_a[0];
+  float row_m = s_m[0];
 #pragma unroll
-  for (int i = 1; i < NW; i++) m = __builtin_fmaxf(m, s_a[i]);
-  __syncthreads();
-  // (a row of minus infinities: taken from 0, so that its sum is 0; plus infinities and NaN make the sums NaN)
-  const float from = m == minus_infinity() ? 0.f : m;
-  float s = 0.f, t = 0.f;
-#pragma unroll
-  for (int j = 0; j < C; j++)
-#pragma unroll
-    for (int i = 0; i < E; i++) {
-      const float d = value(j, i) - from, p = natural_exp(d);
-      s += p;
-      t = __builtin_fmaf(p, __builtin_fmaxf(d, -128.f), t);  // (p is 0 far above that; minus infinity times 0 is none)
-    }
+  for (int i = 1; i < NW; i++) row_m = __builtin_fmaxf(row_m, s_m[i]);
+  {
+    const float to = row_m == minus_infinity() ? 0.f : row_m, d = from - to, f = natural_exp(d);
+    t = s == 0.f ? 0.f : f * __builtin_fmaf(s, __builtin_fmaxf(d, -128.f), t);
+    s = s == 0.f ? 0.f : s * f;
+  }
   s = wave_sum(s);
   t = wave_sum(t);
   if ((tid & 63u) == 0) {
-    s_a[wave] = s;
-    s_b[wave] = t;
+    s_s[wave] = s;
+    s_t[wave] = t;
   }
-  // T: the largest 32-bit pattern that at least `top` of the threads' maxima reach, to within twice as many (one wave)
   if (o.top && wave == 0) {
-    uint32_t from_key = 0;
-    for (int bit = 31; bit >= 0; bit--) {
-      const uint32_t trial = from_key | 1u << bit;
-      int n = 0;
+    uint32_t key[NW];
 #pragma unroll
-      for (int i = 0; i < NW; i++) n += __builtin_popcountll(__ballot(s_key[i * 64 + tid] >= trial));
-      if (n >= o.top) {
-        from_key = trial;
-        if (n <= o.top + o.top / 2) break;
-      }
-    }
-    if (tid == 0) s_from = from_key;
+    for (int i = 0; i < NW; i++) key[i] = s_key[i * 64 + tid];
+    const uint32_t bound = key_bound(key, o.top);
+    if (tid == 0) s_from = bound;
   }
   __syncthreads();
-  s = s_a[0];
-  t = s_b[0];
+  s = s_s[0];
+  t = s_t[0];
 #pragma unroll
   for (int i = 1; i < NW; i++) {
-    s += s_a[i];
-    t += s_b[i];
+    s += s_s[i];
+    t += s_t[i];
   }
   if (tid == 0) {
-    if (PARTS) part[row * pieces + piece] = LpPartial{m, s, t, 0.f};
-    else answer_row(o, row, m, s, t);
+    if (PARTS) part[row * pieces + piece] = LpPartial{row_m, s, t, 0.f};
+    else answer_row(o, row, row_m, s, t);
   }
   if (!o.top) return;
   const uint32_t from_key = s_from;
-  if (any && order_key(mine) >= from_key) {
+  // the threads that reach T, in any order; all threads look at those threads' units
+  if (any && order_key(m) >= from_key) s_key[atomicAdd(&s_threads, 1)] = tid;
+  __syncthreads();
+  const unsigned turns = (end - first + NT - 1) / NT, looks = (unsigned)s_threads * turns;
+  for (unsigned q = tid; q < looks; q += NT) {
+    const unsigned w = first + (q % turns) * NT + s_key[q / turns];
+    if (w >= end) continue;
+    Unit r;
+    r.load(x, (long long)w * E, V);
 #pragma unroll
-    for (int j = 0; j < C; j++)
-#pragma unroll
-      for (int i = 0; i < E; i++) {
-        const long long at = base + (long long)(j * NT + tid) * E + i;
-        const float x = value(j, i);
-        if (at < V && order_key(x) >= from_key) {
-          const int slot = atomicAdd(&s_n, 1);
-          if (slot < LIST) s_list[slot] = rank_key(x, (uint32_t)at);
-        }
+    for (int i = 0; i < E; i++) {
+      const long long at = (long long)w * E + i;
+      const float y = r.value(i);
+      if (at < V && order_key(y) >= from_key) {
+        const int slot = atomicAdd(&s_n, 1);
+        if (slot < LIST) s_list[slot] = rank_key(y, (uint32_t)at);
       }
+    }
   }
   __syncthreads();
   int n = s_n;
@@ -219,16 +269,18 @@ __global__ void __launch_bounds__(NT) k_lp_row(const LpOut o, long long R, unsig
     unsigned long long before = ~0ull;
     for (int k = 0; k < o.top; k++) {
       unsigned long long best = 0;
-#pragma unroll
-      for (int j = 0; j < C; j++)
+      for (unsigned w = first + tid; w < end; w += NT) {
+        Unit r;
+        r.load(x, (long long)w * E, V);
 #pragma unroll
         for (int i = 0; i < E; i++) {
-          const long long at = base + (long long)(j * NT + tid) * E + i;
+          const long long at = (long long)w * E + i;
           if (at < V) {
-            const unsigned long long key = rank_key(value(j, i), (uint32_t)at);
+            const unsigned long long key = rank_key(r.value(i), (uint32_t)at);
             if (key < before && key > best) best = key;
           }
         }
+      }
 #pragma unroll
       for (int w = 32; w; w >>= 1) {
         const unsigned long long other = __shfl_xor(best, w);
@@ -256,7 +308,7 @@ __global__ void __launch_bounds__(NT) k_lp_row(const LpOut o, long long R, unsig
     }
     for (int i = n + tid; i < o.top; i += NT) to[i] = 0;
   } else {
-    place_candidates(s_list, n, o.top, NT, o.top_ids + row * o.top, o.top_logprobs + row * o.top, m, s);
+    place_candidates(s_list, n, o.top, NT, o.top_ids + row * o.top, o.top_logprobs + row * o.top, row_m, s);
   }
 }
 
@@ -264,37 +316,33 @@ __global__ void __launch_bounds__(NT) k_lp_row(const LpOut o, long long R, unsig
 __global__ void __launch_bounds__(256) k_lp_join(const LpOut o, unsigned pieces, const LpPartial* __restrict__ part, const unsigned long long* __restrict__ part_top) {
   __shared__ float s_a[4], s_b[4];
   __shared__ unsigned long long s_list[LIST];
-  __shared__ unsigned long long s_low[4];
+  __shared__ uint32_t s_from;
   __shared__ int s_n;
   const long long row = blockIdx.x;
   const unsigned tid = threadIdx.x, wave = tid >> 6;
   const LpPartial* p = part + row * pieces;
   float m = minus_infinity();
-  unsigned long long low = 0;  // the largest of the pieces' last alternatives: nothing below it is among the row's
-  for (unsigned i = tid; i < pieces; i += 256) {
-    m = __builtin_fmaxf(m, p[i].m);
-    if (o.top) {
-      const unsigned long long k = part_top[(row * pieces + i + 1) * o.top - 1];
-      low = k > low ? k : low;
-    }
-  }
+  for (unsigned i = tid; i < pieces; i += 256) m = __builtin_fmaxf(m, p[i].m);
   m = wave_max(m);
-#pragma unroll
-  for (int w = 32; w; w >>= 1) {
-    const unsigned long long other = __shfl_xor(low, w);
-    low = other > low ? other : low;
-  }
-  if ((tid & 63u) == 0) {
-    s_a[wave] = m;
-    s_low[wave] = low;
-  }
+  if ((tid & 63u) == 0) s_a[wave] = m;
   if (tid == 0) s_n = 0;
+  // a bound of the row's last alternative among the pieces' ones (pieces * top <= LIST); 0: no value
+  const unsigned long long* lists = part_top + row * pieces * o.top;
+  const unsigned count = pieces * o.top;
+  if (o.top && wave == 3) {
+    uint32_t key[LIST / 64];
+#pragma unroll
+    for (int i = 0; i < LIST / 64; i++) {
+      const unsigned at = i * 64 + (tid & 63u);
+      key[i] = at < count ? (uint32_t)(lists[at] >> 32) : 0u;
+    }
+    const uint32_t bound = key_bound(key, o.top);
+    if ((tid & 63u) == 0) s_from = bound;
+  }
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < 4; i++) {
-    m = __builtin_fmaxf(m, s_a[i]);
-    low = s_low[i] > low ? s_low[i] : low;
-  }
+  for (int i = 0; i < 4; i++) m = __builtin_fmaxf(m, s_a[i]);
+  const uint32_t bound = o.top ? s_from : 0u;
   __syncthreads();
   const float from = m == minus_infinity() ? 0.f : m;
   float s = 0.f, t = 0.f;
@@ -317,49 +365,43 @@ __global__ void __launch_bounds__(256) k_lp_join(const LpOut o, unsigned pieces,
   t = s_b[0] + s_b[1] + s_b[2] + s_b[3];
   if (tid == 0) answer_row(o, row, m, s, t);
   if (!o.top) return;
-  const unsigned long long* lists = part_top + row * pieces * o.top;
-  for (unsigned i = tid; i < pieces * o.top; i += 256) {
+  for (unsigned i = tid; i < count; i += 256) {
     const unsigned long long k = lists[i];
-    if (k >= low && k) {
-      const int slot = atomicAdd(&s_n, 1);
-      if (slot < LIST) s_list[slot] = k;
-    }
+    if (k && (uint32_t)(k >> 32) >= bound) s_list[atomicAdd(&s_n, 1)] = k;
   }
   __syncthreads();
-  // (pieces * top <= LIST: the list holds them all)
   place_candidates(s_list, s_n, o.top, 256, o.top_ids + row * o.top, o.top_logprobs + row * o.top, m, s);
 }
 
-// How a row is cut: into pieces of 16 KiB of registers a workgroup of 256 threads where the rows alone leave compute units idle
+// Workgroups of a row: one where the rows fill the chip (1024 of them are four a compute unit; 1024 x 50048 16-bit: 25.2 us, cut in two 27.9), otherwise as many as
+// bring it there, of 512 units at least (two for each thread) or, with alternatives, whose lists have to be joined, 1024 (1 x 32000: 10.5 us, with 512 11.8)
 struct LpPlan {
-  int nt, c;         // threads of a workgroup, pieces of 16 bytes a thread
-  unsigned pieces;   // workgroups of a row
+  unsigned pieces, units;
 };
-constexpr int MAX_PIECES = LIST / ESPARSE_MAX_TOP;
+constexpr long long MAX_PIECES = LIST / ESPARSE_MAX_TOP;
 
-LpPlan plan(long long R, long long V, int dtype) {
+LpPlan plan(long long R, long long V, int dtype, int top) {
   const int e = dtype == ESPARSE_F32 ? 4 : 8;
   const long long units = (V + e - 1) / e;
-  (void)R;
-  static const int shapes[][2] = {{256, 1}, {256, 2}, {256, 4}, {256, 8}, {512, 8}, {1024, 8}, {1024, 16}};
-  for (auto& s : shapes)
-    if (units <= (long long)s[0] * s[1]) return {s[0], s[1], 1u};
-  return {1024, 16, (unsigned)((units + 16383) / 16384)};
+  long long pieces = (1024 + R - 1) / R;
+  if (pieces > units / (top ? 1024 : 512)) pieces = units / (top ? 1024 : 512);
+  if (pieces > MAX_PIECES) pieces = MAX_PIECES;
+  if (pieces < 1) pieces = 1;
+  const long long per = (units + pieces - 1) / pieces;
+  return {(unsigned)((units + per - 1) / per), (unsigned)per};
 }
 
 template <int DT>
 hipError_t launch(const LpOut& o, long long R, const LpPlan& p, void* ws, hipStream_t st) {
   LpPartial* part = reinterpret_cast<LpPartial*>(ws);
   unsigned long long* tops = reinterpret_cast<unsigned long long*>(part + R * p.pieces);
-#define GO(NT, C)                                                                                                                        \
-  if (p.nt == NT && p.c == C) {                                                                                                          \
-    if (p.pieces == 1) hipLaunchKernelGGL((k_lp_row<DT, NT, C, false>), dim3((unsigned)R), dim3(NT), 0, st, o, R, 1u, part, tops);       \
-    else hipLaunchKernelGGL((k_lp_row<DT, NT, C, true>), dim3((unsigned)(R * p.pieces)), dim3(NT), 0, st, o, R, p.pieces, part, tops);   \
+  if (p.pieces == 1) {
+    hipLaunchKernelGGL((k_lp_row<DT, false>), dim3((unsigned)R), dim3(NT), 0, st, o, 1u, p.units, part, tops);
+    return hipGetLastError();
   }
-  GO(256, 1) GO(256, 2) GO(256, 4) GO(256, 8) GO(512, 8) GO(1024, 8) GO(1024, 16)
-#undef GO
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || p.pieces == 1) return e;
+  hipLaunchKernelGGL((k_lp_row<DT, true>), dim3((unsigned)(R * p.pieces)), dim3(NT), 0, st, o, p.pieces, p.units, part, tops);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
   hipLaunchKernelGGL(k_lp_join, dim3((unsigned)R), dim3(256), 0, st, o, p.pieces, part, tops);
   return hipGetLastError();
 }
@@ -367,15 +409,14 @@ hipError_t launch(const LpOut& o, long long R, const LpPlan& p, void* ws, hipStr
 }  // namespace
 
 size_t esp_token_logprobs_workspace(long long R, long long V, int dtype, int top) {
-  const LpPlan p = plan(R, V, dtype);
+  const LpPlan p = plan(R, V, dtype, top);
   return p.pieces == 1 ? 0 : (size_t)R * p.pieces * (sizeof(LpPartial) + 8u * (size_t)top);
 }
-long long esp_token_logprobs_most(int dtype) { return (long long)MAX_PIECES * 16384 * (dtype == ESPARSE_F32 ? 4 : 8); }
 
 int esp_token_logprobs_device(esparse_ctx* ctx, const void* logits, long long R, long long V, long long ld, int dtype, const long long* tokens, int top,
                               float* logprob, float* entropy, int32_t* top_ids, float* top_logprobs, void* ws) {
   const LpOut o = {logits, tokens, logprob, entropy, top_ids, top_logprobs, V, ld, dtype, top};
-  const LpPlan p = plan(R, V, dtype);
+  const LpPlan p = plan(R, V, dtype, top);
   if (dtype == ESPARSE_F16) ESP_HIP(ctx, launch<ESPARSE_F16>(o, R, p, ws, ctx->stream));
   else if (dtype == ESPARSE_BF16) ESP_HIP(ctx, launch<ESPARSE_BF16>(o, R, p, ws, ctx->stream));
   else ESP_HIP(ctx, launch<ESPARSE_F32>(o, R, p, ws, ctx->stream));

@@ -5,7 +5,7 @@
 // The division and the rounding are one conversion instruction of gfx950 for two values, exact for every 16-bit input and
 // every scale (checked over all of them); it takes magnitudes beyond 464 of a scale to the NaN code of E4M3, hence mx_saturate_fp8.
 #pragma once
-#include "common.h"
+#include "intrinsics.h"
 
 typedef short esp_short2 __attribute__((ext_vector_type(2)));
 typedef _Float16 esp_half2 __attribute__((ext_vector_type(2)));
@@ -152,8 +152,8 @@ __device__ __forceinline__ uint32_t mx_scale_word(unsigned e, unsigned lane) {
 // stores a lane's codes (row: first byte of the row's data, chunk: number of the eight channels) and, from every 16th lane, the scale word
 template <int FMT>
 __device__ __forceinline__ void mx_store(unsigned char* row, unsigned chunk, MxCodes c, uint32_t* scale, unsigned e, unsigned lane) {
-  if constexpr (FMT == ESPARSE_MX_FP4) *reinterpret_cast<uint32_t*>(row + 4ull * chunk) = c.lo;
-  else *reinterpret_cast<uint2*>(row + 8ull * chunk) = uint2{c.lo, c.hi};
+  if constexpr (FMT == ESPARSE_MX_FP4) __builtin_nontemporal_store(c.lo, reinterpret_cast<uint32_t*>(row + 4ull * chunk));
+  else store_stream_8(row + 8ull * chunk, &c);
   const uint32_t w = mx_scale_word(e, lane);
   if ((lane & 15u) == 0u) *scale = w;
 }
@@ -165,12 +165,15 @@ __device__ __forceinline__ void load_8(const T* p, long long left, uint32_t (&v)
   if (left >= 8) {
     __builtin_memcpy(v, p, 16);
   } else {
+    // all eight loads under way at once: places behind the last repeat it
+    uint32_t t[8];
 #pragma unroll
-    for (int i = 0; i < 4; i++) {
-      uint32_t a = 0, b = 0;
-      if (2 * i < left) a = p[2 * i];
-      if (2 * i + 1 < left) b = p[2 * i + 1];
-      v[i] = a | b << 16;
+    for (int i = 0; i < 8; i++) t[i] = 0;
+    if (left > 0) {
+#pragma unroll
+      for (int i = 0; i < 8; i++) t[i] = p[i < left ? i : left - 1];
     }
+#pragma unroll
+    for (int i = 0; i < 4; i++) v[i] = (2 * i < left ? t[2 * i] : 0u) | (2 * i + 1 < left ? t[2 * i + 1] : 0u) << 16;
   }
 }

@@ -6,54 +6,52 @@
 
 namespace {
 
-// One workgroup of 256 threads takes 16 rows x 512 channels: 16 lanes hold 128 channels of a row (eight values a lane, four lanes a
-// block), a lane takes four such pieces, so that 64 bytes per lane are in flight and a row is read in runs of 1 KiB.  Rows change
-// fastest among the groups of 16 lanes: the scales [128 channels][row][4] leave in runs of 64 bytes.
+// One workgroup of 256 threads takes 16 rows x 512 channels: a wave 512 channels of one row (runs of 1 KiB are read, of 256 or 512 bytes written) and four
+// rows, 64 bytes a lane under way; 16 lanes hold 128 channels (eight values a lane, four lanes a block).  The scale words of the 16 rows meet in the L2.
 constexpr int TILE_ROWS = 16, TILE_STEPS = 4;
 
 template <int DT, int FMT>
 __global__ void __launch_bounds__(256) k_mx_quantize(const void* __restrict__ X, long long ldx, long long R, long long K, unsigned steps, unsigned spans,
                                                      unsigned char* __restrict__ data, uint32_t* __restrict__ scales) {
-  const unsigned tile = blockIdx.x / spans, span = blockIdx.x % spans, lane = threadIdx.x & 15u;
-  const long long row = (long long)tile * TILE_ROWS + (threadIdx.x >> 4);
-  if (row >= R) return;  // (whole groups of 16 lanes)
-  const unsigned s0 = span * TILE_STEPS;
-  unsigned char* out = data + row * ((long long)steps * (FMT == ESPARSE_MX_FP4 ? 64 : 128));
+  const unsigned tile = blockIdx.x / spans, span = blockIdx.x % spans, lane = threadIdx.x & 63u;
+  const long long row0 = (long long)tile * TILE_ROWS + (threadIdx.x >> 6);
+  const unsigned chunk = span * (TILE_STEPS * 16) + lane, step = chunk >> 4;
+  if (step >= steps) return;  // (whole groups of 16 lanes)
+  const long long at = (long long)chunk * 8, left = K - at;
+  const long long row_bytes = (long long)steps * (FMT == ESPARSE_MX_FP4 ? 64 : 128);
   if constexpr (DT == ESPARSE_F32) {
-    const float* x = reinterpret_cast<const float*>(X) + row * ldx;
-    float v[TILE_STEPS][8];
+    float v[TILE_ROWS / 4][8];
 #pragma unroll
-    for (int j = 0; j < TILE_STEPS; j++) {
-      const long long at = (long long)(s0 + j) * 128 + lane * 8, left = K - at;
+    for (int j = 0; j < TILE_ROWS / 4; j++) {
+      const float* x = reinterpret_cast<const float*>(X) + (row0 + 4 * j < R ? row0 + 4 * j : R - 1) * ldx + at;
       if (left >= 8) {
-        __builtin_memcpy(v[j], x + at, 32);
+        __builtin_memcpy(v[j], x, 32);
       } else {
 #pragma unroll
         for (int i = 0; i < 8; i++) {
           v[j][i] = 0.f;
-          if (i < left) v[j][i] = x[at + i];
+          if (i < left) v[j][i] = x[i];
         }
       }
     }
 #pragma unroll
-    for (int j = 0; j < TILE_STEPS; j++) {
-      if (s0 + j >= steps) break;
+    for (int j = 0; j < TILE_ROWS / 4; j++) {
+      const long long row = row0 + 4 * j;
+      if (row >= R) break;
       const unsigned e = mx_block_exponent<FMT>(v[j]);
-      mx_store<FMT>(out, (s0 + j) * 16 + lane, mx_encode<FMT>(v[j], e), scales + (long long)(s0 + j) * R + row, e, threadIdx.x);
+      mx_store<FMT>(data + row * row_bytes, chunk, mx_encode<FMT>(v[j], e), scales + (long long)step * R + row, e, lane);
     }
   } else {
-    const uint16_t* x = reinterpret_cast<const uint16_t*>(X) + row * ldx;
-    uint32_t v[TILE_STEPS][4];
+    uint32_t v[TILE_ROWS / 4][4];
 #pragma unroll
-    for (int j = 0; j < TILE_STEPS; j++) {
-      const long long at = (long long)(s0 + j) * 128 + lane * 8;
-      load_8(x + at, K - at, v[j]);
-    }
+    for (int j = 0; j < TILE_ROWS / 4; j++)
+      load_8(reinterpret_cast<const uint16_t*>(X) + (row0 + 4 * j < R ? row0 + 4 * j : R - 1) * ldx + at, left, v[j]);
 #pragma unroll
-    for (int j = 0; j < TILE_STEPS; j++) {
-      if (s0 + j >= steps) break;
+    for (int j = 0; j < TILE_ROWS / 4; j++) {
+      const long long row = row0 + 4 * j;
+      if (row >= R) break;
       const unsigned e = mx_block_exponent<DT, FMT>(v[j]);
-      mx_store<FMT>(out, (s0 + j) * 16 + lane, mx_encode<DT, FMT>(v[j], e), scales + (long long)(s0 + j) * R + row, e, threadIdx.x);
+      mx_store<FMT>(data + row * row_bytes, chunk, mx_encode<DT, FMT>(v[j], e), scales + (long long)step * R + row, e, lane);
     }
   }
 }
@@ -62,24 +60,25 @@ __global__ void __launch_bounds__(256) k_mx_quantize(const void* __restrict__ X,
 template <int FMT, int DT>
 __global__ void __launch_bounds__(256) k_mx_dequantize(const unsigned char* __restrict__ data, const unsigned char* __restrict__ scales, long long R,
                                                        long long K, unsigned steps, unsigned spans, void* __restrict__ out) {
-  const unsigned tile = blockIdx.x / spans, span = blockIdx.x % spans, lane = threadIdx.x & 15u;
-  const long long row = (long long)tile * TILE_ROWS + (threadIdx.x >> 4);
-  if (row >= R) return;
-  const unsigned s0 = span * TILE_STEPS;
-  const unsigned char* in = data + row * ((long long)steps * (FMT == ESPARSE_MX_FP4 ? 64 : 128));
-  uint32_t c[TILE_STEPS][2];
-  unsigned e[TILE_STEPS];
+  const unsigned tile = blockIdx.x / spans, span = blockIdx.x % spans, lane = threadIdx.x & 63u;
+  const long long row0 = (long long)tile * TILE_ROWS + (threadIdx.x >> 6);
+  const long long at = (long long)span * (TILE_STEPS * 128) + lane * 8, left = K - at;
+  if (left <= 0) return;
+  const unsigned step = span * TILE_STEPS + (lane >> 4);
+  const long long row_bytes = (long long)steps * (FMT == ESPARSE_MX_FP4 ? 64 : 128);
+  uint32_t c[TILE_ROWS / 4][2];
+  unsigned e[TILE_ROWS / 4];
 #pragma unroll
-  for (int j = 0; j < TILE_STEPS; j++) {
-    const unsigned s = s0 + j < steps ? s0 + j : steps - 1;
-    if constexpr (FMT == ESPARSE_MX_FP4) c[j][0] = *reinterpret_cast<const uint32_t*>(in + 4ull * (s * 16ull + lane));
-    else __builtin_memcpy(c[j], in + 8ull * (s * 16ull + lane), 8);
-    e[j] = scales[((long long)s * R + row) * 4 + (lane >> 2)];
+  for (int j = 0; j < TILE_ROWS / 4; j++) {
+    const long long row = row0 + 4 * j < R ? row0 + 4 * j : R - 1;
+    if constexpr (FMT == ESPARSE_MX_FP4) c[j][0] = *reinterpret_cast<const uint32_t*>(data + row * row_bytes + at / 2);
+    else __builtin_memcpy(c[j], data + row * row_bytes + at, 8);
+    e[j] = scales[((long long)step * R + row) * 4 + ((lane >> 2) & 3u)];
   }
 #pragma unroll
-  for (int j = 0; j < TILE_STEPS; j++) {
-    const long long at = (long long)(s0 + j) * 128 + lane * 8, left = K - at;
-    if (left <= 0) break;
+  for (int j = 0; j < TILE_ROWS / 4; j++) {
+    const long long row = row0 + 4 * j;
+    if (row >= R) break;
     float f[8];
 #if defined(__HIP_DEVICE_COMPILE__)
     const float s = mx_scale(e[j]);
@@ -109,7 +108,8 @@ __global__ void __launch_bounds__(256) k_mx_dequantize(const unsigned char* __re
     if constexpr (DT == ESPARSE_F32) {
       float* o = reinterpret_cast<float*>(out) + row * K + at;
       if (left >= 8) {
-        __builtin_memcpy(o, f, 32);
+        store_stream_16(o, f);
+        store_stream_16(o + 4, f + 4);
       } else {
 #pragma unroll
         for (int i = 0; i < 8; i++)
@@ -121,7 +121,7 @@ __global__ void __launch_bounds__(256) k_mx_dequantize(const unsigned char* __re
 #pragma unroll
       for (int i = 0; i < 8; i++) h[i] = esp_from_float<DT>(f[i]);
       if (left >= 8) {
-        __builtin_memcpy(o, h, 16);
+        store_stream_16(o, h);
       } else {
 #pragma unroll
         for (int i = 0; i < 8; i++)

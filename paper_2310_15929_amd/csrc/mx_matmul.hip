@@ -674,7 +674,7 @@ __device__ __attribute__((always_inline)) void mx_tile_pipeline(uint4* __restric
         uint16_t* y = reinterpret_cast<uint16_t*>(a.y) + t * a.N + n;
         if (t < a.M) {
           if (n + 8 <= a.N) {
-            __builtin_memcpy(y, &v, 16);
+            store_stream_16(y, &v);
           } else {
             const uint32_t d[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll

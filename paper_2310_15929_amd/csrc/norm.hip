@@ -31,7 +31,7 @@ __device__ __forceinline__ uint32_t add_pair(uint32_t a, uint32_t b) {
 }
 __device__ __forceinline__ void store_8(uint16_t* p, long long left, const uint32_t (&v)[4]) {
   if (left >= 8) {
-    __builtin_memcpy(p, v, 16);
+    store_stream_16(p, v);
   } else {
 #pragma unroll
     for (int i = 0; i < 8; i++)

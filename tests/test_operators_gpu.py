@@ -466,6 +466,29 @@ def test_no_rows(ctx):
     assert r.logprob.shape == (0,) and r.top_ids.shape == (0, 3)
 
 
+# ---- refusals of the binding --------------------------------------------------------------------------
+def test_binding_refuses(ctx):
+    x = torch.zeros(4, 64, dtype=torch.bfloat16, device="cuda")
+    mx = ctx.mx_quantize(x, esp.MX_FP4)
+    w = ctx.mx_pack(mx)
+    tok = torch.zeros(4, dtype=torch.int64, device="cuda")
+    for call in (lambda: ctx.mx_quantize(x.t(), 0), lambda: ctx.mx_quantize(x[0], 0), lambda: ctx.mx_quantize(x[:1].expand(4, 64), 0), lambda: ctx.mx_quantize(x, 2),
+                 lambda: ctx.mx_dequantize(esp.MX(mx.data, mx.scales, 200, 0)), lambda: ctx.mx_dequantize(esp.MX(mx.data, mx.scales, 64, 1)),
+                 lambda: ctx.mx_dequantize(esp.MX(mx.data.char(), mx.scales, 64, 0)), lambda: ctx.mx_dequantize(esp.MX(mx.data, mx.scales, 64, 5)),
+                 lambda: ctx.mx_dequantize(esp.MX(mx.data, mx.scales.transpose(0, 1), 64, 0)), lambda: ctx.mx_pack(ctx.mx_quantize(x, esp.MX_FP8)),
+                 lambda: ctx.mx_gemm(x[:, :32], w), lambda: ctx.mx_gemm(x, esp.MXWeight(w.packed[:-1], 4, 64)), lambda: ctx.mx_gemm(x, esp.MXWeight(w.packed, 4, 200)),
+                 lambda: ctx.mx_gemm(x, w, out=x), lambda: ctx.mx_gemm(x, w, out=x[:, :4]), lambda: ctx.mx_gemm(x, w, out=torch.empty(4, 4, device="cuda"), dtype=torch.float16),
+                 lambda: ctx.rms_norm(x, x[0, :32]), lambda: ctx.rms_norm(x, x[0].float()), lambda: ctx.rms_norm(x, x[0], residual=x[:2]), lambda: ctx.rms_norm(x, x[0], fmt=3),
+                 lambda: ctx.rms_norm(x, x[0], sum_out=torch.zeros(4, 128, dtype=torch.bfloat16, device="cuda")[:, :64]),
+                 lambda: ctx.token_logprobs(x, tok.int()), lambda: ctx.token_logprobs(x, tok[:3]), lambda: ctx.rms_norm(x, x[0].cpu()), lambda: ctx.token_logprobs(x, tok.cpu())):
+        with pytest.raises(ValueError):
+            call()
+    for call in (lambda: ctx.token_logprobs(x, tok, top=33), lambda: ctx.token_logprobs(x, tok, top=-1), lambda: ctx.token_logprobs(x[:, :4], tok, top=5),
+                 lambda: ctx.rms_norm(x, x[0], math.nan), lambda: ctx.rms_norm(x, x[0], -1.0)):
+        with pytest.raises(esp.EsparseError):
+            call()
+
+
 # ---- together, as they are used -----------------------------------------------------------------------
 def _run_together(ctx, x, residual, norm_w, layer, head, tokens):
     """Residual and norm into 8 bits, a 4-bit layer, norm, the vocabulary's product in 32 bits, log probabilities."""

@@ -172,14 +172,9 @@ def test_binding_refuses(ctx):
     w = esp.MXWeight(torch.zeros(esp.mx_packed_size(64, 64), dtype=torch.uint8), 64, 64)
     for call in (lambda: ctx.mx_quantize(x, esp.MX_FP4), lambda: ctx.mx_dequantize(mx), lambda: ctx.mx_pack(mx), lambda: ctx.mx_gemm(mx, w), lambda: ctx.mx_gemm(x, w),
                  lambda: ctx.rms_norm(x, x[0]), lambda: ctx.token_logprobs(x)):
-        with pytest.raises(ValueError, match="is on cpu"):
+        with pytest.raises(ValueError, match="on cpu, "):
             call()
     for call in (lambda: ctx.mx_quantize(x.double(), 0), lambda: ctx.mx_dequantize(mx, torch.float64), lambda: ctx.mx_gemm(x.float(), w),
                  lambda: ctx.rms_norm(x.float(), x[0]), lambda: ctx.token_logprobs(x.double())):
         with pytest.raises(TypeError):
-            call()
-    for call in (lambda: ctx.mx_quantize(x.t(), 0), lambda: ctx.mx_quantize(x[0], 0), lambda: ctx.mx_quantize(x[:1].expand(4, 64), 0),
-                 lambda: ctx.mx_dequantize(esp.MX(mx.data, mx.scales, 200, 0)), lambda: ctx.mx_dequantize(esp.MX(mx.data, mx.scales, 64, 1)),
-                 lambda: ctx.mx_dequantize(esp.MX(mx.data.char(), mx.scales, 64, 0)), lambda: ctx.mx_dequantize(esp.MX(mx.data, mx.scales, 64, 5))):
-        with pytest.raises(ValueError):
             call()
