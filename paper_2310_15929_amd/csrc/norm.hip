@@ -50,31 +50,38 @@ __device__ __forceinline__ float squares(const uint32_t (&v)[4]) {
   return s;
 }
 
-// the sum over the NT threads of a row; every thread gets it.  `buf`: one float per wave
+// 1 / sqrt(mean of the squares + eps) from the threads' sums, added in 64 bits, as the sum of two floats; every thread of the row gets it.  A product
+// h w of two 16-bit numbers is exact in fp32, so that y = h w (hi + lo) is rounded once: an output in 8 or 4 bits lies on the other side of the middle
+// between two of its numbers less often than with the three roundings of (h * inv) * w.  `buf`: one double per wave
 template <int NT>
-__device__ __forceinline__ float row_sum(float v, float* buf) {
+__device__ __forceinline__ float2 row_inverse(float own, double* buf, long long K, float eps) {
+  double v = own;
 #pragma unroll
   for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
   if constexpr (NT > 64) {
     const int wave = threadIdx.x >> 6;
     if ((threadIdx.x & 63) == 0) buf[wave] = v;
     __syncthreads();
-    v = 0.f;
+    v = 0.;
 #pragma unroll
     for (int i = 0; i < NT / 64; i++) v += buf[i];
   }
-  return v;
+  const double inv = 1. / __builtin_sqrt(v / (double)K + (double)eps);
+  const float hi = (float)inv;
+  return float2{hi, __builtin_isfinite(hi) ? (float)(inv - (double)hi) : 0.f};
 }
 
 // output of one piece of eight channels.  Lanes of pieces behind the row's last channel take part (zeros in the padding of a
 // microscaled row); `chunk` differs by one between neighbouring lanes and starts at a multiple of 16
 template <int DT, int OUT>
-__device__ __forceinline__ void norm_out(const NormArgs& a, long long row, unsigned chunk, const uint32_t (&h)[4], const uint32_t (&w)[4], float inv) {
+__device__ __forceinline__ void norm_out(const NormArgs& a, long long row, unsigned chunk, const uint32_t (&h)[4], const uint32_t (&w)[4], float2 inv) {
   float v[8];
 #pragma unroll
   for (int i = 0; i < 4; i++) {
-    v[2 * i] = esp_to_float<DT>((uint16_t)h[i]) * inv * esp_to_float<DT>((uint16_t)w[i]);
-    v[2 * i + 1] = esp_to_float<DT>((uint16_t)(h[i] >> 16)) * inv * esp_to_float<DT>((uint16_t)(w[i] >> 16));
+    const float lo = esp_to_float<DT>((uint16_t)h[i]) * esp_to_float<DT>((uint16_t)w[i]);
+    const float hi = esp_to_float<DT>((uint16_t)(h[i] >> 16)) * esp_to_float<DT>((uint16_t)(w[i] >> 16));
+    v[2 * i] = __builtin_fmaf(lo, inv.x, lo * inv.y);
+    v[2 * i + 1] = __builtin_fmaf(hi, inv.x, hi * inv.y);
   }
   if constexpr (OUT == OUT_16) {
     uint32_t o[4];
@@ -95,7 +102,7 @@ __device__ __forceinline__ void norm_out(const NormArgs& a, long long row, unsig
 template <int DT, int OUT, int NT, int C>
 __global__ void __launch_bounds__(NT < 256 ? 256 : NT) k_rms_norm(const NormArgs a) {
   constexpr int ROWS = NT < 256 ? 256 / NT : 1;
-  __shared__ float buf[NT > 64 ? NT / 64 : 1];
+  __shared__ double buf[NT > 64 ? NT / 64 : 1];
   const unsigned t = threadIdx.x % NT;
   const long long row = (long long)blockIdx.x * ROWS + threadIdx.x / NT;
   if (row >= a.R) return;  // (whole waves, and no barrier where a workgroup has several rows)
@@ -118,7 +125,7 @@ __global__ void __launch_bounds__(NT < 256 ? 256 : NT) k_rms_norm(const NormArgs
     if (a.sum_out) store_8(a.sum_out + row * a.K + (long long)(j * NT + t) * 8, a.K - (long long)(j * NT + t) * 8, h[j]);
     s += squares<DT>(h[j]);
   }
-  const float inv = 1.f / __builtin_sqrtf(row_sum<NT>(s, buf) / (float)a.K + a.eps);
+  const float2 inv = row_inverse<NT>(s, buf, a.K, a.eps);
 #pragma unroll
   for (int j = 0; j < C; j++) norm_out<DT, OUT>(a, row, j * NT + t, h[j], w[j], inv);
 }
@@ -126,7 +133,7 @@ __global__ void __launch_bounds__(NT < 256 ? 256 : NT) k_rms_norm(const NormArgs
 // rows that do not fit the registers of a workgroup are read twice
 template <int DT, int OUT>
 __global__ void __launch_bounds__(1024) k_rms_norm_long(const NormArgs a) {
-  __shared__ float buf[16];
+  __shared__ double buf[16];
   const long long row = blockIdx.x;
   const unsigned chunks = a.steps * 16, t = threadIdx.x;
   float s = 0.f;
@@ -142,7 +149,7 @@ __global__ void __launch_bounds__(1024) k_rms_norm_long(const NormArgs a) {
     if (a.sum_out) store_8(a.sum_out + row * a.K + at, left, h);
     s += squares<DT>(h);
   }
-  const float inv = 1.f / __builtin_sqrtf(row_sum<1024>(s, buf) / (float)a.K + a.eps);
+  const float2 inv = row_inverse<1024>(s, buf, a.K, a.eps);
   for (unsigned c0 = 0; c0 < chunks; c0 += 1024) {
     const unsigned c = c0 + t;
     const long long at = (long long)c * 8, left = a.K - at;
