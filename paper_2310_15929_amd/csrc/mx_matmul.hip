@@ -412,8 +412,13 @@ struct MxTileWave {
 };
 
 __device__ __forceinline__ unsigned uniform(unsigned v) { return (unsigned)wave_uniform((int)v); }
-// LDS that lanes of one wave exchange: in order in the hardware, kept in order by the compiler
-__device__ __forceinline__ void wave_fence() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
+// LDS that the lanes of one wave exchange: the hardware keeps its order, the fences keep the compiler's, and the barrier (no instruction) keeps all lanes
+// together: with fences alone the lanes that skip the conditional stores between two passes were sent ahead to write the next one
+__device__ __forceinline__ void wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
 
 template <int N, class F, int... I>
 __device__ __forceinline__ void each_stage_of(F& f, std::integer_sequence<int, I...>) {
@@ -777,41 +782,39 @@ hipError_t launch_tile(const MxGemmArgs& a, float* partial, unsigned nsplit, hip
   X(4, 2, 8, 1, 2.71, 0.172, 0.00462, 0.2) \
   X(4, 4, 8, 1, 3.18, 0.185, 0.0627, 0.2)
 #define MX_ROWS_16(X) \
-  X(1, 1, 8, 2, 2.9, 0.151, 0, 0.606) \
-  X(1, 2, 8, 2, 3.26, 0.119, 0.0793, 0.514) \
-  X(1, 4, 8, 1, 2.99, 0.174, 0.0851, 0.374) \
-  X(1, 8, 8, 1, 3.13, 0.249, 0.131, 0.0806) \
-  X(2, 1, 16, 1, 2.7, 0.269, 0.017, 0.2) \
-  X(2, 2, 8, 2, 3.46, 0.241, 0.0784, 0.2) \
-  X(2, 4, 8, 1, 3.37, 0.315, 0.0564, 0.2) \
-  X(4, 1, 8, 1, 3.1, 0.472, 0, 0.2) \
-  X(4, 2, 8, 1, 3.43, 0.493, 0.00998, 0.2) \
-  X(4, 4, 8, 1, 4.18, 0.545, 0.0133, 0.2)
+  X(1, 1, 8, 2, 2.91, 0.15, 0, 0.605) \
+  X(1, 2, 8, 2, 3.26, 0.122, 0.0739, 0.514) \
+  X(1, 4, 8, 1, 3.05, 0.168, 0.0945, 0.371) \
+  X(1, 8, 8, 1, 3.2, 0.246, 0.132, 0.0795) \
+  X(2, 1, 16, 1, 2.72, 0.269, 0.0162, 0.2) \
+  X(2, 2, 8, 2, 3.5, 0.239, 0.0803, 0.2) \
+  X(2, 4, 8, 1, 3.38, 0.313, 0.0566, 0.2) \
+  X(4, 1, 8, 1, 3.11, 0.47, 0, 0.2)
 // tile: row and token tiles of a wave, waves along both, buffers of a ring; t0, e, c, u, r0, r
 #define MX_TILES_FP8(X) \
-  X(4, 2, 2, 2, 3, 2.43, 0.382, 0.374, 0.655, 2.5, 0.567) \
-  X(4, 4, 2, 2, 3, 3.99, 0, 0.431, 0.921, 2.87, 0.433) \
-  X(8, 4, 2, 2, 2, 3.63, 0.328, 0.987, 0.704, 4.75, 0.334) \
-  X(7, 4, 2, 2, 2, 6.69, 0, 0.934, 0.659, 1.32, 0.379) \
-  X(4, 2, 2, 2, 6, 2.53, 1.28, 0.266, 1.01, 2.3, 0.531) \
-  X(8, 4, 2, 4, 3, 0, 7.14, 0.91, 1.14, 6.86, 0.269) \
-  X(7, 4, 2, 4, 3, 1.6, 7.95, 0.961, 1.01, 3.47, 0.264) \
-  X(4, 2, 2, 2, 4, 2.92, 0.436, 0.28, 0.872, 2.48, 0.548)
+  X(4, 2, 2, 2, 3, 2.38, 0.387, 0.376, 0.637, 2.52, 0.576) \
+  X(4, 4, 2, 2, 3, 3.86, 0, 0.439, 0.905, 2.94, 0.433) \
+  X(8, 4, 2, 2, 2, 2.85, 0.961, 0.995, 0.695, 4.96, 0.321) \
+  X(7, 4, 2, 2, 2, 6, 0, 0.947, 0.662, 1.96, 0.374) \
+  X(4, 2, 2, 2, 6, 2.28, 1.51, 0.269, 0.974, 2.35, 0.523) \
+  X(8, 4, 2, 4, 3, 0, 7.45, 0.628, 1.66, 6.6, 0.263) \
+  X(7, 4, 2, 4, 3, 0, 9.21, 0.605, 1.63, 4.04, 0.243) \
+  X(4, 2, 2, 2, 4, 2.73, 0.557, 0.281, 0.841, 2.54, 0.55)
 #define MX_TILES_FP4(X) \
-  X(4, 2, 2, 2, 3, 2.55, 0.0944, 0.353, 0.629, 2.53, 0.6) \
-  X(4, 4, 2, 2, 3, 3.8, 0, 0.398, 0.846, 2.92, 0.444) \
-  X(8, 4, 2, 2, 2, 3.88, 0, 0.884, 0.651, 4.94, 0.341) \
-  X(7, 4, 2, 2, 2, 6.55, 0, 0.871, 0.621, 1.56, 0.375) \
-  X(4, 2, 2, 2, 6, 3.03, 0.265, 0.247, 0.873, 2.33, 0.609) \
-  X(8, 4, 2, 4, 3, 0, 6.27, 0.595, 1.2, 7.26, 0.293) \
-  X(7, 4, 2, 4, 3, 1.64, 7.31, 0.565, 1.22, 3.88, 0.273) \
-  X(4, 2, 2, 2, 4, 2.91, 0.13, 0.266, 0.816, 2.39, 0.6)
+  X(4, 2, 2, 2, 3, 2.58, 0, 0.354, 0.613, 2.54, 0.617) \
+  X(4, 4, 2, 2, 3, 3.62, 0, 0.404, 0.835, 3.03, 0.447) \
+  X(8, 4, 2, 2, 2, 3.57, 0, 0.892, 0.647, 5.19, 0.341) \
+  X(7, 4, 2, 2, 2, 5.69, 0, 0.885, 0.62, 2.34, 0.372) \
+  X(4, 2, 2, 2, 6, 2.92, 0.305, 0.248, 0.839, 2.37, 0.618) \
+  X(8, 4, 2, 4, 3, 0, 6.64, 0.686, 1.04, 7.02, 0.288) \
+  X(7, 4, 2, 4, 3, 0, 8.64, 0.696, 1.01, 4.41, 0.253) \
+  X(4, 2, 2, 2, 4, 2.82, 0.137, 0.267, 0.79, 2.44, 0.609)
 #define MX_TILES_16(X) \
-  X(4, 2, 2, 2, 3, 3.19, 1.27, 0.464, 0.889, 2.9, 0.427) \
-  X(4, 4, 4, 2, 3, 0.449, 5.38, 1.18, 1.05, 5.22, 0.331) \
-  X(3, 4, 4, 2, 3, 3.94, 2.79, 0.93, 1, 2.29, 0.414) \
-  X(4, 4, 4, 1, 2, 3.27, 0, 1.03, 0.703, 4.17, 0.396) \
-  X(4, 2, 2, 4, 3, 2.18, 2.28, 0.64, 1.19, 3.94, 0.42)
+  X(4, 4, 4, 2, 3, 0, 6.04, 1.22, 1.02, 5.52, 0.285) \
+  X(3, 4, 4, 2, 3, 1.33, 5.28, 0.901, 1.03, 3.44, 0.279) \
+  X(4, 4, 4, 1, 2, 3.5, 0, 1.02, 0.702, 4.14, 0.387) \
+  X(4, 2, 2, 4, 3, 1.69, 3.11, 0.687, 1.1, 4.09, 0.335) \
+  X(2, 4, 4, 1, 3, 3.41, 0.769, 0.444, 0.915, 3.01, 0.429)
 
 struct MxChoice {
   int variant;  // rows kernels first, then tile kernels

@@ -204,7 +204,7 @@ def test_product_of_layer_sizes(ctx, M, N, K, act):
 
 
 @pytest.mark.parametrize("act", ["16", "fp8", "fp4"])
-@pytest.mark.parametrize("M,N", [(5, 70), (40, 96), (140, 131), (300, 640)])
+@pytest.mark.parametrize("M,N", [(5, 70), (40, 96), (140, 131), (300, 640), (200, 640), (513, 1000), (1030, 2100), (2050, 4100)])
 def test_product_in_32_bits(ctx, M, N, act):
     _product(ctx, M, N, 520, act, "f16", out="f32")
 
