@@ -714,6 +714,12 @@ class DeviceOfCall {
 
 static bool aligned_to(const void* p, size_t q) { return reinterpret_cast<uintptr_t>(p) % q == 0; }
 static size_t dtype_bytes(int dtype) { return dtype == ESPARSE_F32 ? 4 : 2; }
+// whether two stretches of memory share a byte (null: no)
+static bool overlap(const void* a, size_t a_bytes, const void* b, size_t b_bytes) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return a && b && x < y + b_bytes && y < x + a_bytes;
+}
+static size_t rows_bytes(long long R, long long K, long long ld, size_t each) { return ((size_t)(R - 1) * (size_t)ld + (size_t)K) * each; }
 
 static int check_dtype_or_f32(esparse_ctx* ctx, int dtype) {
   ESP_REQUIRE(ctx, dtype == ESPARSE_F16 || dtype == ESPARSE_BF16 || dtype == ESPARSE_F32, ESPARSE_EUNSUPPORTED, "dtype %d is not f16 / bf16 / f32", dtype);
@@ -751,6 +757,11 @@ int esparse_mx_quantize(esparse_ctx* ctx, const void* X, long long R, long long 
   ESP_REQUIRE(ctx, ldx >= K, ESPARSE_EINVAL, "ldx = %lld is less than K = %lld", ldx, K);
   ESP_REQUIRE(ctx, aligned_to(X, dtype_bytes(dtype)), ESPARSE_EINVAL, "X is not aligned to its type");
   ESP_REQUIRE(ctx, esp_aligned16(data) && esp_aligned16(scales), ESPARSE_EINVAL, "data / scales is not 16-byte aligned");
+  size_t data_bytes = 0, scale_bytes = 0;
+  (void)esparse_mx_size(R, K, format, &data_bytes, &scale_bytes);
+  const size_t x_bytes = rows_bytes(R, K, ldx, dtype_bytes(dtype));
+  ESP_REQUIRE(ctx, !overlap(X, x_bytes, data, data_bytes) && !overlap(X, x_bytes, scales, scale_bytes) && !overlap(data, data_bytes, scales, scale_bytes), ESPARSE_EINVAL,
+              "data or scales overlaps X or the other");
   const DeviceOfCall device(ctx->device);
   ESP_HIP(ctx, device.error());
   return esp_mx_quantize_device(ctx, X, R, K, ldx, dtype, format, data, scales);
@@ -765,6 +776,10 @@ int esparse_mx_dequantize(esparse_ctx* ctx, const void* data, const void* scales
   ESP_REQUIRE(ctx, data && scales && out, ESPARSE_EINVAL, "data / scales / out is null");
   ESP_REQUIRE(ctx, aligned_to(out, dtype_bytes(dtype)), ESPARSE_EINVAL, "out is not aligned to its type");
   ESP_REQUIRE(ctx, esp_aligned16(data) && esp_aligned16(scales), ESPARSE_EINVAL, "data / scales is not 16-byte aligned");
+  size_t data_bytes = 0, scale_bytes = 0;
+  (void)esparse_mx_size(R, K, format, &data_bytes, &scale_bytes);
+  const size_t out_bytes = rows_bytes(R, K, K, dtype_bytes(dtype));
+  ESP_REQUIRE(ctx, !overlap(out, out_bytes, data, data_bytes) && !overlap(out, out_bytes, scales, scale_bytes), ESPARSE_EINVAL, "out overlaps data or scales");
   const DeviceOfCall device(ctx->device);
   ESP_HIP(ctx, device.error());
   return esp_mx_dequantize_device(ctx, data, scales, R, K, format, dtype, out);
@@ -819,11 +834,21 @@ int esparse_mx_gemm(esparse_ctx* ctx, const void* X, const void* x_scales, long 
     ESP_REQUIRE(ctx, esp_aligned16(X) && esp_aligned16(x_scales), ESPARSE_EINVAL, "X / x_scales is not 16-byte aligned");
   }
   ESP_REQUIRE(ctx, esp_aligned16(packed_w) && esp_aligned16(Y), ESPARSE_EINVAL, "packed_w / Y is not 16-byte aligned");
+  size_t x_bytes = 0, xs_bytes = 0, w_bytes = 0;
+  if (act == ESPARSE_MX_ACT_16) x_bytes = rows_bytes(M, K, ldx, 2);
+  else (void)esparse_mx_size(M, K, act == ESPARSE_MX_ACT_FP4 ? ESPARSE_MX_FP4 : ESPARSE_MX_FP8, &x_bytes, &xs_bytes);
+  (void)esparse_mx_packed_size(N, K, &w_bytes);
+  const size_t y_bytes = rows_bytes(M, N, N, dtype_bytes(out_dtype));
+  ESP_REQUIRE(ctx, !overlap(Y, y_bytes, X, x_bytes) && !overlap(Y, y_bytes, x_scales, xs_bytes) && !overlap(Y, y_bytes, packed_w, w_bytes), ESPARSE_EINVAL,
+              "Y overlaps an operand");
   const bool aligned = act != ESPARSE_MX_ACT_16 || (esp_aligned16(X) && ldx % 8 == 0);
   const size_t need = esp_mx_gemm_workspace_bytes(M, N, K, act, aligned);
   ESP_REQUIRE(ctx, need == 0 || workspace, ESPARSE_EINVAL, "workspace is null, %zu bytes needed", need);
   ESP_REQUIRE(ctx, need == 0 || workspace_bytes >= need, ESPARSE_EWORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, need);
   ESP_REQUIRE(ctx, need == 0 || aligned_to(workspace, 256), ESPARSE_EINVAL, "workspace is not 256-byte aligned");
+  ESP_REQUIRE(ctx, need == 0 || (!overlap(workspace, need, Y, y_bytes) && !overlap(workspace, need, X, x_bytes) && !overlap(workspace, need, x_scales, xs_bytes) &&
+                                 !overlap(workspace, need, packed_w, w_bytes)),
+              ESPARSE_EINVAL, "workspace overlaps an operand or Y");
   const DeviceOfCall device(ctx->device);
   ESP_HIP(ctx, device.error());
   return esp_mx_gemm_device(ctx, X, x_scales, M, ldx, act, dtype, packed_w, N, K, out_dtype, Y, workspace, aligned);
@@ -844,22 +869,20 @@ int esparse_rms_norm(esparse_ctx* ctx, const void* x, long long ldx, const void*
               "a pointer is not aligned to its type");
   ESP_REQUIRE(ctx, esp_aligned16(data) && esp_aligned16(scales), ESPARSE_EINVAL, "data / scales is not 16-byte aligned");
   // in place: element by element, or not at all
-  auto apart = [&](const void* out, size_t out_bytes, const void* in, long long ld, bool may_be_same) {
-    if (!out || !in || (may_be_same && out == in && (ld == K || R == 1))) return true;
-    const uintptr_t o = reinterpret_cast<uintptr_t>(out), i = reinterpret_cast<uintptr_t>(in), in_bytes = 2 * ((size_t)(R - 1) * (size_t)ld + (size_t)K);
-    return o + out_bytes <= i || i + in_bytes <= o;
-  };
-  const size_t bytes16 = 2 * (size_t)R * (size_t)K;
-  ESP_REQUIRE(ctx, apart(sum_out, bytes16, x, ldx, true) && apart(sum_out, bytes16, residual, ldr, true), ESPARSE_EINVAL,
+  const size_t bytes16 = rows_bytes(R, K, K, 2), x_bytes = rows_bytes(R, K, ldx, 2), r_bytes = residual ? rows_bytes(R, K, ldr, 2) : 0;
+  auto same = [&](const void* in, long long ld) { return in == sum_out && (ld == K || R == 1); };
+  ESP_REQUIRE(ctx, (same(x, ldx) || !overlap(sum_out, bytes16, x, x_bytes)) && (same(residual, ldr) || !overlap(sum_out, bytes16, residual, r_bytes)), ESPARSE_EINVAL,
               "sum_out overlaps x or residual without being the same rows");
-  const void* out = y ? y : data;
   size_t out_bytes = bytes16, scale_bytes = 0;
   if (!y) (void)esparse_mx_size(R, K, format, &out_bytes, &scale_bytes);
-  for (const void* in : {x, residual, (const void*)sum_out}) {
-    const long long ld = in == x ? ldx : (in == residual ? ldr : K);
-    ESP_REQUIRE(ctx, apart(out, out_bytes, in, ld, false) && (y || apart(scales, scale_bytes, in, ld, false)), ESPARSE_EINVAL,
-                "the output overlaps an input or sum_out");
-  }
+  const struct {
+    const void* p;
+    size_t bytes;
+  } outs[] = {{y ? y : data, out_bytes}, {scales, scale_bytes}}, ins[] = {{x, x_bytes}, {residual, r_bytes}, {sum_out, bytes16}, {weight, 2 * (size_t)K}};
+  for (const auto& o : outs)
+    for (const auto& i : ins) ESP_REQUIRE(ctx, !overlap(o.p, o.bytes, i.p, i.bytes), ESPARSE_EINVAL, "the output overlaps an input or sum_out");
+  ESP_REQUIRE(ctx, !overlap(sum_out, bytes16, weight, 2 * (size_t)K) && !overlap(outs[0].p, out_bytes, scales, scale_bytes), ESPARSE_EINVAL,
+              "sum_out overlaps weight, or data overlaps scales");
   const DeviceOfCall device(ctx->device);
   ESP_HIP(ctx, device.error());
   return esp_rms_norm_device(ctx, x, ldx, residual, ldr, weight, R, K, eps, dtype, sum_out, y, format, data, scales);

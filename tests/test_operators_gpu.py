@@ -449,10 +449,45 @@ def test_logprobs_without_tokens(ctx):
 
 
 def test_logprobs_do_not_depend_on_other_rows(ctx):
-    x = torch.randn(700, 3000, device="cuda", generator=torch.Generator("cuda").manual_seed(2))
-    t = torch.arange(700, device="cuda")
-    many, one = ctx.token_logprobs(x, t, top=5), ctx.token_logprobs(x[:700].clone(), t, top=5)
-    assert torch.equal(many.logprob, one.logprob) and torch.equal(many.entropy, one.entropy) and torch.equal(many.top_ids, one.top_ids)
+    gen = torch.Generator("cuda").manual_seed(2)
+    for R, V in ((700, 3000), (5, 40000)):
+        x = torch.randn(R, V, device="cuda", generator=gen)
+        t = torch.arange(R, device="cuda")
+        first = ctx.token_logprobs(x, t, top=5)
+        x[1::2] = torch.randn(R // 2, V, device="cuda", generator=gen) * 50
+        x[1, 3] = math.nan
+        second = ctx.token_logprobs(x, t, top=5)
+        for a, b in zip((first.logprob, first.entropy, first.top_ids, first.top_logprobs), (second.logprob, second.entropy, second.top_ids, second.top_logprobs)):
+            assert torch.equal(a[::2], b[::2])
+
+
+# ---- beyond 32 bits -----------------------------------------------------------------------------------
+def test_offsets_beyond_32_bits(ctx):
+    """The last rows of matrices with more than 2^32 bytes and values are those of a call on these rows alone."""
+    gen = torch.Generator("cuda").manual_seed(9)
+    R, K, last = 70000, 65536, 5
+    x = torch.empty(R, K, dtype=torch.bfloat16, device="cuda")
+    x.normal_(generator=gen)
+    tail = x[-last:].clone()
+    for fmt in FMT.values():
+        q, part = ctx.mx_quantize(x, fmt), ctx.mx_quantize(tail, fmt)
+        assert torch.equal(q.data[-last:], part.data) and torch.equal(q.scales[:, -last:], part.scales)
+        assert torch.equal(ctx.mx_dequantize(q, torch.bfloat16)[-last:], ctx.mx_dequantize(part, torch.bfloat16))
+    w = torch.ones(K, dtype=torch.bfloat16, device="cuda")
+    y, h = ctx.rms_norm(x, w, residual=x)
+    y2, h2 = ctx.rms_norm(tail, w, residual=tail)
+    assert torch.equal(y[-last:], y2) and torch.equal(h[-last:], h2)
+    del y, h, q
+    big, small = ctx.token_logprobs(x, torch.arange(R, device="cuda"), top=3), ctx.token_logprobs(tail, torch.arange(R - last, R, device="cuda") % K, top=3)
+    assert torch.equal(big.top_ids[-last:], small.top_ids) and torch.allclose(big.entropy[-last:], small.entropy, rtol=1e-5)
+    # outputs of a product beyond 2^32: 70000 tokens x 65600 features of 128 channels
+    a, b = ctx.mx_quantize(x[:, :128], esp.MX_FP8), ctx.mx_quantize(x[:65600, 128:256], esp.MX_FP4)
+    packed = ctx.mx_pack(b)
+    out = ctx.mx_gemm(a, packed)
+    alone = ctx.mx_gemm(ctx.mx_quantize(tail[:, :128], esp.MX_FP8), packed)
+    assert torch.equal(out[-last:], alone)
+    out = ctx.mx_gemm(x[:, :128], packed)
+    assert torch.allclose(out[-last:].float(), ctx.mx_gemm(tail[:, :128].contiguous(), packed).float(), rtol=2.0 ** -7, atol=1e-3)
 
 
 # ---- empty inputs -------------------------------------------------------------------------------------

@@ -88,14 +88,17 @@ def _expect(ctx, rc, code, word):
     ((P, 2, 8, 8, 0, 0, None, P), EINVAL, "null"), ((P, 2, 8, 8, 0, 0, P, None), EINVAL, "null"), ((P, 2, 8, 7, 0, 0, P, P), EINVAL, "ldx"),
     ((P, -1, 8, 8, 0, 0, P, P), EINVAL, "rows"), ((P, 1 << 22, 8, 8, 0, 0, P, P), EINVAL, "rows"), ((P, 2, 0, 8, 0, 0, P, P), EINVAL, "range"),
     ((P + 1, 2, 8, 8, 0, 0, P, P), EINVAL, "aligned"), ((P + 2, 2, 8, 8, 2, 0, P, P), EINVAL, "aligned"), ((P, 2, 8, 8, 0, 0, P + 8, P), EINVAL, "16-byte"),
-    ((P, 1 << 21, 1 << 20, 1 << 20, 0, 0, P, P), EINVAL, "2^34")])
+    ((P, 1 << 21, 1 << 20, 1 << 20, 0, 0, P, P), EINVAL, "2^34"),
+    ((P, 2, 8, 8, 0, 0, P, P << 4), EINVAL, "overlaps"), ((P, 2, 8, 8, 0, 0, P << 4, P), EINVAL, "overlaps"), ((P, 2, 8, 8, 0, 0, P << 4, (P << 4) + 64), EINVAL, "overlaps"),
+    ((P, 9, 8, 800, 2, 1, P + 20000, P << 4), EINVAL, "overlaps")])
 def test_quantize_refuses(ctx, args, code, word):
     _expect(ctx, ctx._lib.esparse_mx_quantize(ctx._h, *args), code, word)
 
 
 @pytest.mark.parametrize("args,code,word", [
     ((P, P, 2, 8, 0, 4, P), EUNSUPPORTED, "dtype"), ((P, P, 2, 8, 3, 0, P), EUNSUPPORTED, "format"), ((None, P, 2, 8, 0, 0, P), EINVAL, "null"),
-    ((P, P, 2, 8, 0, 0, None), EINVAL, "null"), ((P, P + 4, 2, 8, 0, 0, P), EINVAL, "16-byte"), ((P, P, 2, 8, 0, 2, P + 2), EINVAL, "aligned")])
+    ((P, P, 2, 8, 0, 0, None), EINVAL, "null"), ((P, P + 4, 2, 8, 0, 0, P), EINVAL, "16-byte"), ((P, P, 2, 8, 0, 2, P + 2), EINVAL, "aligned"), ((P, P << 4, 2, 8, 0, 0, P + 16), EINVAL, "overlaps"),
+    ((P << 4, P, 2, 8, 0, 0, P), EINVAL, "overlaps")])
 def test_dequantize_refuses(ctx, args, code, word):
     _expect(ctx, ctx._lib.esparse_mx_dequantize(ctx._h, *args), code, word)
 
@@ -106,7 +109,7 @@ def test_pack_refuses(ctx, args, code, word):
 
 
 #         X, scales, M, ldx, act, dtype, w, N, K, out, Y, ws, bytes
-GEMM = dict(X=P, xs=P, M=4, ldx=0, act=1, dtype=0, w=P, N=64, K=128, out=1, Y=P, ws=None, nbytes=0)
+GEMM = dict(X=P, xs=P << 4, M=4, ldx=0, act=1, dtype=0, w=P << 5, N=64, K=128, out=1, Y=P << 8, ws=None, nbytes=0)
 
 
 @pytest.mark.parametrize("change,code,word", [
@@ -114,16 +117,18 @@ GEMM = dict(X=P, xs=P, M=4, ldx=0, act=1, dtype=0, w=P, N=64, K=128, out=1, Y=P,
     (dict(N=0), EINVAL, "range"), (dict(K=0), EINVAL, "range"), (dict(X=None), EINVAL, "null"), (dict(w=None), EINVAL, "null"), (dict(Y=None), EINVAL, "null"),
     (dict(xs=None), EINVAL, "x_scales"), (dict(X=P + 8), EINVAL, "16-byte"), (dict(w=P + 8), EINVAL, "16-byte"), (dict(Y=P + 8), EINVAL, "16-byte"),
     (dict(act=2, ldx=127), EINVAL, "ldx"), (dict(act=2, ldx=128, X=P + 1), EINVAL, "aligned"), (dict(act=2, ldx=128, K=127), EINVAL, "workspace"),
-    (dict(act=2, ldx=128, K=127, ws=P, nbytes=8), EWORKSPACE, "workspace"), (dict(act=2, ldx=128, K=127, ws=P + 16, nbytes=1 << 30), EINVAL, "256-byte"),
+    (dict(act=2, ldx=128, K=127, ws=P, nbytes=8), EWORKSPACE, "workspace"), (dict(act=2, ldx=128, K=127, ws=(P << 9) + 16, nbytes=1 << 30), EINVAL, "256-byte"),
     (dict(act=2, ldx=129), EINVAL, "workspace"), (dict(act=2, ldx=128, X=P + 8), EINVAL, "workspace"), (dict(act=2, ldx=(1 << 22) + 8), EINVAL, "ldx"),
-    (dict(K=(1 << 22) + 1), EINVAL, "range")])
+    (dict(K=(1 << 22) + 1), EINVAL, "range"), (dict(Y=P), EINVAL, "overlaps"), (dict(Y=P << 4), EINVAL, "overlaps"),
+    (dict(Y=(P << 5) + 4096), EINVAL, "overlaps"), (dict(act=2, ldx=127, K=127, ws=P << 8, nbytes=1 << 30), EINVAL, "overlaps"),
+    (dict(act=2, ldx=127, K=127, ws=P, nbytes=1 << 30), EINVAL, "overlaps")])
 def test_gemm_refuses(ctx, change, code, word):
     a = {**GEMM, **change}
     _expect(ctx, ctx._lib.esparse_mx_gemm(ctx._h, a["X"], a["xs"], a["M"], a["ldx"], a["act"], a["dtype"], a["w"], a["N"], a["K"], a["out"], a["Y"], a["ws"],
                                           a["nbytes"]), code, word)
 
 
-NORM = dict(x=P, ldx=64, r=None, ldr=0, w=P, R=2, K=64, eps=1e-6, dtype=1, s=None, y=1 << 20, fmt=0, data=None, scales=None)
+NORM = dict(x=P, ldx=64, r=None, ldr=0, w=P << 3, R=2, K=64, eps=1e-6, dtype=1, s=None, y=1 << 20, fmt=0, data=None, scales=None)
 
 
 @pytest.mark.parametrize("change,code,word", [
@@ -131,7 +136,7 @@ NORM = dict(x=P, ldx=64, r=None, ldr=0, w=P, R=2, K=64, eps=1e-6, dtype=1, s=Non
     (dict(x=None), EINVAL, "null"), (dict(w=None), EINVAL, "null"), (dict(y=None), EINVAL, "either"), (dict(data=P << 12, scales=P << 13), EINVAL, "either"),
     (dict(y=None, data=P << 12), EINVAL, "either"), (dict(y=None, data=P << 12, scales=P << 13, fmt=7), EUNSUPPORTED, "format"), (dict(ldx=63), EINVAL, "ldx"),
     (dict(r=P << 12, ldr=3), EINVAL, "ldr"), (dict(x=P + 1), EINVAL, "aligned"), (dict(y=P), EINVAL, "overlaps"), (dict(s=P + 2), EINVAL, "overlaps"),
-    (dict(s=P, ldx=65), EINVAL, "overlaps"), (dict(s=1 << 20), EINVAL, "overlaps"), (dict(y=None, data=P + 128, scales=P << 13), EINVAL, "overlaps"),
+    (dict(s=P, ldx=65), EINVAL, "overlaps"), (dict(s=1 << 20), EINVAL, "overlaps"), (dict(y=(P << 3) + 2), EINVAL, "overlaps"), (dict(s=(P << 3) - 2), EINVAL, "overlaps"), (dict(y=None, data=P << 12, scales=P << 12), EINVAL, "overlaps"), (dict(y=None, data=P + 128, scales=P << 13), EINVAL, "overlaps"),
     (dict(y=None, data=(P << 12) + 8, scales=P << 13), EINVAL, "16-byte")])
 def test_norm_refuses(ctx, change, code, word):
     a = {**NORM, **change}
