@@ -768,8 +768,7 @@ hipError_t launch_tile(const MxGemmArgs& a, float* partial, unsigned nsplit, hip
   X(2, 2, 8, 2, 2.48, 0.155, 0.00772, 0.2) \
   X(2, 4, 8, 1, 2.85, 0.162, 0.0589, 0.2) \
   X(4, 1, 8, 1, 2.6, 0.238, 0, 0.2) \
-  X(4, 2, 8, 1, 2.82, 0.256, 0.018, 0.2) \
-  X(4, 4, 8, 1, 3.41, 0.28, 0.0412, 0.2)
+  X(4, 2, 8, 1, 2.82, 0.256, 0.018, 0.2)
 #define MX_ROWS_FP4(X) \
   X(1, 1, 8, 2, 2.51, 0.0462, 0.0167, 0.284) \
   X(1, 2, 8, 2, 2.42, 0.0655, 0.0363, 0.157) \
