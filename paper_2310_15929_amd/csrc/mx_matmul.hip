@@ -281,8 +281,13 @@ __global__ void __launch_bounds__(NW * 64) k_mx_rows(const MxGemmArgs a) {
 // 16-byte pieces of a token are exchanged by an exclusive or with its number, so that the 16 tokens of an operand read hit all banks.
 // 16-bit activations: a unit of weights is expanded to 16 bits once per wave and stage, one stage ahead, between the multiplies.
 // nsplit > 1: K is cut, a workgroup stores an fp32 partial tile, k_mx_reduce adds them in ascending order.
+// KG = 2: two groups of NWR x NWC waves, each with rings of its own, take half of the stages each; at the end each group hands half of its sums to the other.
+//   A compute unit keeps a bounded number of lines on their way, whatever the depth of the rings (fp8, 128 x 64 tiles: 0.28 us a stage with 4 as with 6 buffers
+//   and with two groups; 0.2 with weights in the last cache), so for tens to hundreds of tokens it is smaller tiles - more compute units at work - that pay
+//   (fp8, 256 x 4096 x 4096: 12.2 us with 128 x 64, 9.8 with 64 x 64, 13.9 with 32 x 64).  In 16 bits expanding the weights stands between the multiplies: a
+//   second group does it meanwhile (256 x 4096 x 4096, 64 x 64: 14.9 us with one group and 6 buffers, 13.5 with two groups of 3).
 // ------------------------------------------------------------------------------------------------
-template <int ACT, int TR, int TC, int NWR, int NWC, int RING>
+template <int ACT, int TR, int TC, int NWR, int NWC, int RING, int KG>
 struct MxTile {
   static constexpr int NW = NWR * NWC, RTM = NWR * TR, NTT = NWC * TC, RB = kRowBytes<ACT>;
   static constexpr int AU = RTM * 64, BU = NTT * RB;                            // 16-byte units of a stage
@@ -291,9 +296,9 @@ struct MxTile {
   static constexpr int SA = (RTM + (RTM % 4 == 0 ? 0 : (RTM % 2 == 0 ? 2 : 3)) + 3) / 4, SB = ACT == ACT_16 ? 0 : NTT / 4;          // runs of 64 scale words
   static constexpr int AC = (RTM + NW - 1) / NW, BC = (BU / 64 + NW - 1) / NW, SC = (SA + SB + NW - 1) / NW;  // copies of a wave
   static constexpr int OPS = AC + BC + SC, SW = (SA + SB) * 64;
-  static constexpr int LDS = RING * ((AU + BU) * 16 + SW * 4);
+  static constexpr int LDS = KG * RING * ((AU + BU) * 16 + SW * 4);
   static_assert(LDS <= 160 * 1024, "the rings fit the LDS");
-  static constexpr int WAVES = NW >= 8 || 2 * LDS <= 160 * 1024 ? 2 : 1;        // of a SIMD: what the registers are shared among
+  static constexpr int WAVES = KG * NW >= 8 || 2 * LDS <= 160 * 1024 ? 2 : 1;        // of a SIMD: what the registers are shared among
   static constexpr int BV = ACT == ACT_FP4 ? 1 : (ACT == ACT_FP8 ? 2 : 4);      // B reads of a token tile
   static constexpr int AV = ACT == ACT_16 ? 4 : 1;                              // A operands of a row tile
   static_assert(NTT % 4 == 0, "a run of scale words holds four token tiles");
@@ -332,9 +337,9 @@ __device__ __forceinline__ void mx_copy(const MxSource& s, unsigned lane_off, un
 #endif
 }
 
-template <int ACT, int DT, int TR, int TC, int NWR, int NWC, int RING>
+template <int ACT, int DT, int TR, int TC, int NWR, int NWC, int RING, int KG>
 struct MxTileWave {
-  using T = MxTile<ACT, TR, TC, NWR, NWC, RING>;
+  using T = MxTile<ACT, TR, TC, NWR, NWC, RING, KG>;
   floatx4_t acc[TR][TC];
   MxSource a_src, x_src, s_src[T::SC];
   unsigned a_off[T::AC], s_step[T::SC];           // uniform
@@ -367,7 +372,7 @@ struct MxTileWave {
       for (int i = 0; i < T::SW_TR; i++) as[i] = (uint32_t)(((unsigned long long)w[i + 1] << 32 | w[i]) >> s_shift);
     }
   }
-  __device__ __forceinline__ void read_a(const uint4* sa, const uint32_t (&as)[MxTile<ACT, TR, TC, NWR, NWC, RING>::SW_TR], MxA<ACT, TR>& r) {
+  __device__ __forceinline__ void read_a(const uint4* sa, const uint32_t (&as)[MxTile<ACT, TR, TC, NWR, NWC, RING, KG>::SW_TR], MxA<ACT, TR>& r) {
 #pragma unroll
     for (int i = 0; i < TR; i++) {
       const uint4 u = sa[(wr * TR + i) * 64 + lane];
@@ -393,7 +398,7 @@ struct MxTileWave {
       b.s = ss[T::SA * 64 + (wc * TC + j) * 16 + (lane & 15u)] >> shift;
     }
   }
-  __device__ __forceinline__ void multiply(const MxA<ACT, TR>& r, const uint32_t (&as)[MxTile<ACT, TR, TC, NWR, NWC, RING>::SW_TR], const MxB<ACT>& b, int j) {
+  __device__ __forceinline__ void multiply(const MxA<ACT, TR>& r, const uint32_t (&as)[MxTile<ACT, TR, TC, NWR, NWC, RING, KG>::SW_TR], const MxB<ACT>& b, int j) {
     if constexpr (ACT == ACT_16) {
 #pragma unroll
       for (int v = 0; v < 4; v++)
@@ -450,11 +455,11 @@ __device__ __forceinline__ void mx_arrive() {
 }
 
 // cur: A(k) in registers; nxt receives A(k+1).  as: scales of stage k (16-bit activations: of k+1, which nxt is expanded with)
-template <int ACT, int DT, int TR, int TC, int NWR, int NWC, int RING>
-__device__ __forceinline__ void mx_stage(MxTileWave<ACT, DT, TR, TC, NWR, NWC, RING>& st, const MxA<ACT, TR>& cur, MxA<ACT, TR>& nxt, uint32_t (&as)[MxTile<ACT, TR, TC, NWR, NWC, RING>::SW_TR], MxB<ACT>& bq,
+template <int ACT, int DT, int TR, int TC, int NWR, int NWC, int RING, int KG>
+__device__ __forceinline__ void mx_stage(MxTileWave<ACT, DT, TR, TC, NWR, NWC, RING, KG>& st, const MxA<ACT, TR>& cur, MxA<ACT, TR>& nxt, uint32_t (&as)[MxTile<ACT, TR, TC, NWR, NWC, RING, KG>::SW_TR], MxB<ACT>& bq,
                                          const uint4* b_cur, const uint32_t* s_cur, const uint4* a_nxt, const uint4* b_nxt, const uint32_t* s_nxt, const uint32_t* s_nxt2,
                                          uint4* a_pre, uint4* b_pre, uint32_t* s_pre, unsigned k) {
-  using T = MxTile<ACT, TR, TC, NWR, NWC, RING>;
+  using T = MxTile<ACT, TR, TC, NWR, NWC, RING, KG>;
   constexpr int TH = TC > 1 ? TC - 1 : 1;  // token tiles ahead of the barrier
   constexpr int MM = TR * T::AV;           // multiplies of a token tile
   constexpr int READS = T::BV + (ACT == ACT_16 ? 0 : 1) + (TR + TH - 1) / TH;
@@ -495,18 +500,20 @@ __device__ __forceinline__ P ring_at(P b0, P b1, P b2, P b3, P b4, P b5) {
   return I == 0 ? b0 : (I == 1 ? b1 : (I == 2 ? b2 : (I == 3 ? b3 : (I == 4 ? b4 : b5))));
 }
 
-template <int ACT, int DT, int TR, int TC, int NWR, int NWC, int RING>
+template <int ACT, int DT, int TR, int TC, int NWR, int NWC, int RING, int KG>
 __device__ __attribute__((always_inline)) void mx_tile_pipeline(uint4* __restrict__ a0, uint4* __restrict__ a1, uint4* __restrict__ a2, uint4* __restrict__ a3,
                                                                 uint4* __restrict__ a4, uint4* __restrict__ a5, uint4* __restrict__ b0, uint4* __restrict__ b1,
                                                                 uint4* __restrict__ b2, uint4* __restrict__ b3, uint4* __restrict__ b4, uint4* __restrict__ b5,
                                                                 uint32_t* __restrict__ s0, uint32_t* __restrict__ s1, uint32_t* __restrict__ s2,
                                                                 uint32_t* __restrict__ s3, uint32_t* __restrict__ s4, uint32_t* __restrict__ s5,
                                                                 const MxGemmArgs& a, const MxTilePlan& p) {
-  using T = MxTile<ACT, TR, TC, NWR, NWC, RING>;
-  MxTileWave<ACT, DT, TR, TC, NWR, NWC, RING> st;
+  using T = MxTile<ACT, TR, TC, NWR, NWC, RING, KG>;
+  MxTileWave<ACT, DT, TR, TC, NWR, NWC, RING, KG> st;
   const unsigned tid = threadIdx.x;
   st.lane = tid & 63u;
   st.wave = (unsigned)wave_uniform((int)(tid >> 6));
+  const unsigned group = KG > 1 ? st.wave / T::NW : 0;  // of waves: its own rings, its own half of the stages
+  st.wave -= group * T::NW;
   st.wr = st.wave / NWC;
   st.wc = st.wave % NWC;
   // XCD x (= blockIdx % 8) works through the items [x per, (x + 1) per): neighbouring macro tiles share operands in its L2
@@ -515,6 +522,11 @@ __device__ __attribute__((always_inline)) void mx_tile_pipeline(uint4* __restric
   const unsigned tile = uniform(item / p.nsplit), split = item - tile * p.nsplit;
   st.k0 = split * p.per_split;
   st.k1 = st.k0 + p.per_split < a.nks ? st.k0 + p.per_split : a.nks;
+  const unsigned stages = (st.k1 - st.k0 + KG - 1) / KG;  // of the first group; the second has as many or one less
+  if constexpr (KG > 1) {
+    if (group == 0) st.k1 = st.k0 + stages;
+    else st.k0 += stages;
+  }
   // bands of `band` row blocks, the token blocks outermost within one
   const unsigned bt = p.band * p.ntb, bi = uniform(tile / bt), in = tile - bi * bt, gh = p.nrb - bi * p.band < p.band ? p.nrb - bi * p.band : p.band;
   const unsigned tb = uniform(in / gh), rb = bi * p.band + in - tb * gh;
@@ -554,13 +566,13 @@ __device__ __attribute__((always_inline)) void mx_tile_pipeline(uint4* __restric
 #pragma unroll
     for (int j = 0; j < TC; j++) st.acc[i][j] = floatx4_t{0.f, 0.f, 0.f, 0.f};
 
-#define A_AT(i) ring_at<(i) % RING>(a0, a1, a2, a3, a4, a5)
-#define B_AT(i) ring_at<(i) % RING>(b0, b1, b2, b3, b4, b5)
-#define S_AT(i) ring_at<(i) % RING>(s0, s1, s2, s3, s4, s5)
+#define A_AT(i) (ring_at<(i) % RING>(a0, a1, a2, a3, a4, a5) + group * T::AU)
+#define B_AT(i) (ring_at<(i) % RING>(b0, b1, b2, b3, b4, b5) + group * T::BU)
+#define S_AT(i) (ring_at<(i) % RING>(s0, s1, s2, s3, s4, s5) + group * T::SW)
   // what the stages ahead of the first would have copied, in their order: their waits hold from the start
-  const unsigned last = st.k1 - 1;
-  if constexpr (ACT == ACT_16) st.copy_s(s0, st.k0);
-  st.copy_a(a0, st.k0);
+  const unsigned last = st.k1 - 1, first = KG > 1 && st.k0 > last ? last : st.k0;
+  if constexpr (ACT == ACT_16) st.copy_s(S_AT(0), first);
+  st.copy_a(A_AT(0), first);
   auto fill = [&](auto stage) {
     constexpr int I = decltype(stage)::value;
     const unsigned kb = st.k0 + I < st.k1 ? st.k0 + I : last, ka = st.k0 + I + 1 < st.k1 ? st.k0 + I + 1 : last;
@@ -574,17 +586,17 @@ __device__ __attribute__((always_inline)) void mx_tile_pipeline(uint4* __restric
   MxA<ACT, TR> r0, r1;
   uint32_t as[T::SW_TR];
   MxB<ACT> bq;
-  st.read_scales(s0, as);
-  st.read_a(a0, as, r0);
-  if constexpr (ACT == ACT_16) st.read_scales(s1, as);
-  st.read_b(b0, s0, 0, bq);
+  st.read_scales(S_AT(0), as);
+  st.read_a(A_AT(0), as, r0);
+  if constexpr (ACT == ACT_16) st.read_scales(S_AT(1), as);
+  st.read_b(B_AT(0), S_AT(0), 0, bq);
   sched_fence();
   mx_meet();  // every wave has its first A operands before the first stage's copies take their place
   // 16-bit activations: the scales of stage k are used with A(k), a stage ahead of B(k): they are copied with A, into the buffer of stage k's
   unsigned k = st.k0;
   auto stage = [&](auto index) {
     constexpr int I = decltype(index)::value;
-    mx_stage<ACT, DT, TR, TC, NWR, NWC, RING>(st, I % 2 ? r1 : r0, I % 2 ? r0 : r1, as, bq, B_AT(I), S_AT(I), A_AT(I + 1), B_AT(I + 1), S_AT(I + 1), S_AT(I + 2), A_AT(I),
+    mx_stage<ACT, DT, TR, TC, NWR, NWC, RING, KG>(st, I % 2 ? r1 : r0, I % 2 ? r0 : r1, as, bq, B_AT(I), S_AT(I), A_AT(I + 1), B_AT(I + 1), S_AT(I + 1), S_AT(I + 2), A_AT(I),
                                               B_AT(I + RING - 1), ACT == ACT_16 ? S_AT(I) : S_AT(I + RING - 1), k + I);
   };
   for (; k + RING <= st.k1; k += RING) {
@@ -595,18 +607,42 @@ __device__ __attribute__((always_inline)) void mx_tile_pipeline(uint4* __restric
     if (k + decltype(index)::value < st.k1) stage(index);
   };
   each_stage<RING - 1>(rest);
+  if (KG > 1 && st.k1 - st.k0 < stages) mx_meet();  // the barrier of the first group's last stage
 #undef A_AT
 #undef B_AT
 #undef S_AT
   mx_arrive<0>();  // nothing is on its way into the rings
   __syncthreads();  // and every wave is done with them
 
-  const long long t_wave = t0 + (long long)st.wc * TC * 16, n_wave = ((long long)rt0 + st.wr * TR) * 16;
+  constexpr int TJ = TC / KG;  // token tiles of a wave from here on
+  if constexpr (KG > 1) {
+    // the groups' sums: each hands half of its token tiles to the other, through its larger buffers, and adds what it gets to the rest
+    constexpr bool IN_B = T::BU > T::AU;
+    constexpr unsigned UNITS = IN_B ? T::BU : T::AU;
+    static_assert(KG == 2 && TC % 2 == 0 && T::NW * TR * TJ <= RING * (int)UNITS / 64, "the rings hold half the sums");
+    auto chunk = [&](unsigned of, int q) {
+      const unsigned ch = st.wave * (TR * TJ) + q, buf = ch / (UNITS / 64);
+      uint4* ring = IN_B ? (buf == 0 ? b0 : (buf == 1 ? b1 : (buf == 2 ? b2 : (buf == 3 ? b3 : (buf == 4 ? b4 : b5)))))
+                         : (buf == 0 ? a0 : (buf == 1 ? a1 : (buf == 2 ? a2 : (buf == 3 ? a3 : (buf == 4 ? a4 : a5)))));
+      return reinterpret_cast<floatx4_t*>(ring + of * UNITS + ch % (UNITS / 64) * 64 + st.lane);
+    };
+#pragma unroll
+    for (int i = 0; i < TR; i++)
+#pragma unroll
+      for (int j = 0; j < TJ; j++) *chunk(group, i * TJ + j) = group ? st.acc[i][j] : st.acc[i][j + TJ];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < TR; i++)
+#pragma unroll
+      for (int j = 0; j < TJ; j++) st.acc[i][j] = (group ? st.acc[i][j + TJ] : st.acc[i][j]) + *chunk(group ^ 1u, i * TJ + j);
+    __syncthreads();
+  }
+  const long long t_wave = t0 + (long long)(st.wc * TC + group * TJ) * 16, n_wave = ((long long)rt0 + st.wr * TR) * 16;
   if (p.nsplit > 1) {
     // partial tile: [split][token][Np rows]
     const long long Np = (long long)a.nrt * 16;
 #pragma unroll
-    for (int j = 0; j < TC; j++) {
+    for (int j = 0; j < TJ; j++) {
       const long long t = t_wave + 16 * j + c;
 #pragma unroll
       for (int i = 0; i < TR; i++) {
@@ -625,13 +661,13 @@ __device__ __attribute__((always_inline)) void mx_tile_pipeline(uint4* __restric
   unsigned char* slice;
   if (st.wave < BUFS * PER_A) {
     const unsigned buf = st.wave / (PER_A ? PER_A : 1);
-    slice = reinterpret_cast<unsigned char*>(buf == 0 ? a0 : (buf == 1 ? a1 : a2)) + st.wave % (PER_A ? PER_A : 1) * SLICE;
+    slice = reinterpret_cast<unsigned char*>((buf == 0 ? a0 : (buf == 1 ? a1 : a2)) + group * T::AU) + st.wave % (PER_A ? PER_A : 1) * SLICE;
   } else {
     const unsigned w = st.wave - BUFS * PER_A, buf = w / (PER_B ? PER_B : 1);
-    slice = reinterpret_cast<unsigned char*>(buf == 0 ? b0 : (buf == 1 ? b1 : b2)) + w % (PER_B ? PER_B : 1) * SLICE;
+    slice = reinterpret_cast<unsigned char*>((buf == 0 ? b0 : (buf == 1 ? b1 : b2)) + group * T::BU) + w % (PER_B ? PER_B : 1) * SLICE;
   }
 #pragma unroll
-  for (int j = 0; j < TC; j++) {
+  for (int j = 0; j < TJ; j++) {
     if (a.out == ESPARSE_F32) {
 #pragma unroll
       for (int h = 0; h < 2; h++) {
@@ -693,16 +729,16 @@ __device__ __attribute__((always_inline)) void mx_tile_pipeline(uint4* __restric
   }
 }
 
-template <int ACT, int DT, int TR, int TC, int NWR, int NWC, int RING>
-__global__ void __launch_bounds__(NWR * NWC * 64, (MxTile<ACT, TR, TC, NWR, NWC, RING>::WAVES)) k_mx_tile(const MxGemmArgs a, const MxTilePlan p) {
-  using T = MxTile<ACT, TR, TC, NWR, NWC, RING>;
+template <int ACT, int DT, int TR, int TC, int NWR, int NWC, int RING, int KG>
+__global__ void __launch_bounds__(NWR * NWC * KG * 64, (MxTile<ACT, TR, TC, NWR, NWC, RING, KG>::WAVES)) k_mx_tile(const MxGemmArgs a, const MxTilePlan p) {
+  using T = MxTile<ACT, TR, TC, NWR, NWC, RING, KG>;
   // separate arrays handed on as __restrict__ pointers: the compiler sees that reading one buffer does not have to wait for the copies into another
 #define RING_OF(type, b, size) __shared__ type b##0[size], b##1[size], b##2[RING > 2 ? size : 1], b##3[RING > 3 ? size : 1], b##4[RING > 4 ? size : 1], b##5[RING > 5 ? size : 1]
-  RING_OF(uint4, a, T::AU);
-  RING_OF(uint4, b, T::BU);
-  RING_OF(uint32_t, s, T::SW);
+  RING_OF(uint4, a, KG * T::AU);
+  RING_OF(uint4, b, KG * T::BU);
+  RING_OF(uint32_t, s, KG * T::SW);
 #undef RING_OF
-  mx_tile_pipeline<ACT, DT, TR, TC, NWR, NWC, RING>(a0, a1, a2, a3, a4, a5, b0, b1, b2, b3, b4, b5, s0, s1, s2, s3, s4, s5, a, p);
+  mx_tile_pipeline<ACT, DT, TR, TC, NWR, NWC, RING, KG>(a0, a1, a2, a3, a4, a5, b0, b1, b2, b3, b4, b5, s0, s1, s2, s3, s4, s5, a, p);
 }
 
 // the partial tiles of a product that K was cut for, four features a thread
@@ -732,9 +768,9 @@ hipError_t launch_rows(const MxGemmArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
-template <int ACT, int DT, int TR, int TC, int NWR, int NWC, int RING>
+template <int ACT, int DT, int TR, int TC, int NWR, int NWC, int RING, int KG>
 hipError_t launch_tile(const MxGemmArgs& a, float* partial, unsigned nsplit, hipStream_t st) {
-  using T = MxTile<ACT, TR, TC, NWR, NWC, RING>;
+  using T = MxTile<ACT, TR, TC, NWR, NWC, RING, KG>;
   MxTilePlan p = {};
   p.partial = partial;
   p.nrb = (a.nrt + T::RTM - 1) / T::RTM;
@@ -743,7 +779,7 @@ hipError_t launch_tile(const MxGemmArgs& a, float* partial, unsigned nsplit, hip
   p.nsplit = (a.nks + p.per_split - 1) / p.per_split;
   p.band = p.ntb > 8 ? 8 : 1;
   const unsigned items = p.nrb * p.ntb * p.nsplit;
-  hipLaunchKernelGGL((k_mx_tile<ACT, DT, TR, TC, NWR, NWC, RING>), dim3((items + 7) / 8 * 8), dim3(NWR * NWC * 64), 0, st, a, p);
+  hipLaunchKernelGGL((k_mx_tile<ACT, DT, TR, TC, NWR, NWC, RING, KG>), dim3((items + 7) / 8 * 8), dim3(NWR * NWC * KG * 64), 0, st, a, p);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.nsplit == 1) return e;
   const long long units = a.M * ((long long)a.nrt * 4);
@@ -755,65 +791,63 @@ hipError_t launch_tile(const MxGemmArgs& a, float* partial, unsigned nsplit, hip
 // The choice of a kernel: the smallest estimate of its time in microseconds, a function of the sizes and of the kind of the activations alone.
 //   rows   t0 + steps (c L + b x) (1 - d + d q)                     L, x: workgroups per compute unit, whole and as they are; q: filled part of the token tiles
 //   tile   t0 + e L + c stages max(1, u L) + (K cut: r0 + r MB of partial tiles)      L: workgroups per compute unit (256 of them)
-// The constants are fitted to the times of every kernel on 12 weight shapes (512 x 512 to 36864 x 9216, ragged ones among them) and 1 to 2048 tokens, weights cold,
-// K cut up to eight times.  Over those 168 products of each kind the kernel so chosen takes 1.01 - 1.02 of the fastest one's time on average, 1.24 at most.
+// The constants are fitted to the times of every kernel on 13 weight shapes (512 x 512 to 36864 x 9216, ragged ones among them) and 1 to 2048 tokens, weights cold,
+// K cut up to eight times.  Over those 208 products of each kind the kernel so chosen takes 1.01 of the fastest one's time on average, 1.27 at most (6.5 us against 8.3).
+// Of 27 kernels that were measured, the 15 of a kind are those without which the average would be worse.
 // ------------------------------------------------------------------------------------------------
 // rows: token tiles, row tiles, waves, steps at a time; t0, c, b, d
 #define MX_ROWS_FP8(X) \
-  X(1, 1, 8, 2, 2.51, 0.066, 0.0185, 0.367) \
-  X(1, 2, 8, 2, 2.5, 0.0799, 0.0318, 0.233) \
-  X(1, 4, 8, 1, 2.55, 0.101, 0.0928, 0.134) \
-  X(1, 8, 8, 1, 2.69, 0.179, 0.169, 0.139) \
-  X(2, 1, 16, 1, 2.6, 0.138, 0.00993, 0.2) \
-  X(2, 2, 8, 2, 2.48, 0.155, 0.00772, 0.2) \
-  X(2, 4, 8, 1, 2.85, 0.162, 0.0589, 0.2) \
-  X(4, 1, 8, 1, 2.6, 0.238, 0, 0.2) \
-  X(4, 2, 8, 1, 2.82, 0.256, 0.018, 0.2)
+  X(1, 1, 8, 2, 2.44, 0.0633, 0.0238, 0.387) \
+  X(1, 2, 8, 2, 2.39, 0.0821, 0.0355, 0.265) \
+  X(1, 4, 8, 1, 2.48, 0.097, 0.103, 0.133) \
+  X(1, 8, 8, 1, 2.48, 0.188, 0.158, 0.109) \
+  X(2, 2, 8, 2, 2.38, 0.147, 0.0252, 0.535) \
+  X(2, 4, 8, 1, 2.69, 0.152, 0.0808, 0.396) \
+  X(4, 1, 8, 1, 2.43, 0.237, 0.0138, 0.608)
 #define MX_ROWS_FP4(X) \
-  X(1, 1, 8, 2, 2.51, 0.0462, 0.0167, 0.284) \
-  X(1, 2, 8, 2, 2.42, 0.0655, 0.0363, 0.157) \
-  X(1, 4, 8, 1, 2.46, 0.0922, 0.0904, 0.0853) \
-  X(1, 8, 8, 1, 2.65, 0.162, 0.173, 0.106) \
-  X(2, 1, 16, 1, 2.72, 0.0739, 0.0206, 0.2) \
-  X(2, 2, 8, 2, 2.6, 0.105, 0.0327, 0.2) \
-  X(2, 4, 8, 1, 2.65, 0.135, 0.0632, 0.2) \
-  X(4, 1, 8, 1, 2.64, 0.145, 0, 0.2) \
-  X(4, 2, 8, 1, 2.71, 0.172, 0.00462, 0.2) \
-  X(4, 4, 8, 1, 3.18, 0.185, 0.0627, 0.2)
+  X(1, 1, 8, 2, 2.47, 0.0427, 0.0231, 0.309) \
+  X(1, 2, 8, 2, 2.33, 0.0705, 0.0364, 0.203) \
+  X(1, 4, 8, 1, 2.44, 0.083, 0.107, 0.0851) \
+  X(1, 8, 8, 1, 2.48, 0.164, 0.175, 0.0858) \
+  X(2, 1, 16, 1, 2.46, 0.0772, 0.0245, 0.638) \
+  X(2, 2, 8, 2, 2.41, 0.0984, 0.0471, 0.51) \
+  X(2, 4, 8, 1, 2.59, 0.115, 0.098, 0.268) \
+  X(4, 1, 8, 1, 2.41, 0.13, 0.0303, 0.588)
 #define MX_ROWS_16(X) \
-  X(1, 1, 8, 2, 2.91, 0.15, 0, 0.605) \
-  X(1, 2, 8, 2, 3.26, 0.122, 0.0739, 0.514) \
-  X(1, 4, 8, 1, 3.05, 0.168, 0.0945, 0.371) \
-  X(1, 8, 8, 1, 3.2, 0.246, 0.132, 0.0795) \
-  X(2, 1, 16, 1, 2.72, 0.269, 0.0162, 0.2) \
-  X(2, 2, 8, 2, 3.5, 0.239, 0.0803, 0.2) \
-  X(2, 4, 8, 1, 3.38, 0.313, 0.0566, 0.2) \
-  X(4, 1, 8, 1, 3.11, 0.47, 0, 0.2)
-// tile: row and token tiles of a wave, waves along both, buffers of a ring; t0, e, c, u, r0, r
+  X(1, 1, 8, 2, 2.54, 0.129, 0.031, 0.612) \
+  X(1, 2, 8, 2, 2.51, 0.144, 0.0524, 0.494) \
+  X(1, 4, 8, 1, 2.42, 0.176, 0.0916, 0.36) \
+  X(1, 8, 8, 1, 2.43, 0.265, 0.118, 0.0882) \
+  X(2, 1, 16, 1, 2.35, 0.25, 0.0289, 0.415) \
+  X(4, 1, 8, 1, 2.37, 0.466, 0.0107, 0.715)
+// tile: row and token tiles of a wave, waves along both, buffers of a ring, groups of waves along K; t0, e, c, u, r0, r
 #define MX_TILES_FP8(X) \
-  X(4, 2, 2, 2, 3, 2.38, 0.387, 0.376, 0.637, 2.52, 0.576) \
-  X(4, 4, 2, 2, 3, 3.86, 0, 0.439, 0.905, 2.94, 0.433) \
-  X(8, 4, 2, 2, 2, 2.85, 0.961, 0.995, 0.695, 4.96, 0.321) \
-  X(7, 4, 2, 2, 2, 6, 0, 0.947, 0.662, 1.96, 0.374) \
-  X(4, 2, 2, 2, 6, 2.28, 1.51, 0.269, 0.974, 2.35, 0.523) \
-  X(8, 4, 2, 4, 3, 0, 7.45, 0.628, 1.66, 6.6, 0.263) \
-  X(7, 4, 2, 4, 3, 0, 9.21, 0.605, 1.63, 4.04, 0.243) \
-  X(4, 2, 2, 2, 4, 2.73, 0.557, 0.281, 0.841, 2.54, 0.55)
+  X(4, 2, 2, 2, 3, 1, 2.81, 0.122, 0.359, 0.711, 2.76, 0.615) \
+  X(4, 4, 2, 2, 3, 1, 4.06, 0.159, 0.435, 0.893, 2.29, 0.473) \
+  X(8, 4, 2, 2, 2, 1, 3.07, 1.35, 0.968, 0.704, 4.41, 0.333) \
+  X(4, 2, 2, 2, 6, 1, 2.02, 1.71, 0.159, 1.74, 2.39, 0.626) \
+  X(8, 4, 2, 4, 3, 1, 0, 7.1, 1.1, 1.01, 5.64, 0.285) \
+  X(4, 2, 2, 2, 4, 1, 2.5, 0.708, 0.286, 0.881, 2.7, 0.599) \
+  X(2, 2, 2, 2, 6, 1, 2.73, 0.605, 0.193, 0.955, 2.26, 0.694) \
+  X(2, 1, 1, 4, 6, 1, 2.7, 0.442, 0.161, 0.946, 2.49, 0.621)
 #define MX_TILES_FP4(X) \
-  X(4, 2, 2, 2, 3, 2.58, 0, 0.354, 0.613, 2.54, 0.617) \
-  X(4, 4, 2, 2, 3, 3.62, 0, 0.404, 0.835, 3.03, 0.447) \
-  X(8, 4, 2, 2, 2, 3.57, 0, 0.892, 0.647, 5.19, 0.341) \
-  X(7, 4, 2, 2, 2, 5.69, 0, 0.885, 0.62, 2.34, 0.372) \
-  X(4, 2, 2, 2, 6, 2.92, 0.305, 0.248, 0.839, 2.37, 0.618) \
-  X(8, 4, 2, 4, 3, 0, 6.64, 0.686, 1.04, 7.02, 0.288) \
-  X(7, 4, 2, 4, 3, 0, 8.64, 0.696, 1.01, 4.41, 0.253) \
-  X(4, 2, 2, 2, 4, 2.82, 0.137, 0.267, 0.79, 2.44, 0.609)
+  X(4, 4, 2, 2, 3, 1, 3.99, 0, 0.406, 0.794, 2.33, 0.483) \
+  X(7, 4, 2, 2, 2, 1, 5.91, 0, 0.882, 0.62, 1.75, 0.416) \
+  X(4, 2, 2, 2, 6, 1, 3.1, 0.102, 0.245, 0.966, 2.74, 0.666) \
+  X(8, 4, 2, 4, 3, 1, 0, 6.03, 0.72, 1.06, 6.26, 0.306) \
+  X(4, 2, 2, 2, 4, 1, 2.88, 0.0556, 0.269, 0.884, 2.8, 0.624) \
+  X(2, 2, 2, 2, 6, 1, 2.84, 0.259, 0.173, 0.957, 2.19, 0.774) \
+  X(2, 1, 1, 4, 6, 1, 2.54, 0.337, 0.142, 0.892, 2.47, 0.704)
 #define MX_TILES_16(X) \
-  X(4, 4, 4, 2, 3, 0, 6.04, 1.22, 1.02, 5.52, 0.285) \
-  X(3, 4, 4, 2, 3, 1.33, 5.28, 0.901, 1.03, 3.44, 0.279) \
-  X(4, 4, 4, 1, 2, 3.5, 0, 1.02, 0.702, 4.14, 0.387) \
-  X(4, 2, 2, 4, 3, 1.69, 3.11, 0.687, 1.1, 4.09, 0.335) \
-  X(2, 4, 4, 1, 3, 3.41, 0.769, 0.444, 0.915, 3.01, 0.429)
+  X(4, 4, 4, 2, 3, 1, 0, 4.48, 1.21, 1.12, 4.28, 0.387) \
+  X(3, 4, 4, 2, 3, 1, 0.169, 5.01, 0.898, 1.14, 2.31, 0.386) \
+  X(4, 4, 4, 1, 2, 1, 1.53, 1.22, 1.06, 0.68, 4.3, 0.361) \
+  X(4, 2, 2, 4, 3, 1, 1.88, 2.65, 0.786, 1, 2.45, 0.48) \
+  X(2, 4, 4, 1, 3, 1, 2.94, 0.589, 0.481, 0.88, 2.71, 0.561) \
+  X(2, 4, 4, 1, 3, 2, 1.12, 2.97, 0.362, 1.14, 2.81, 0.749) \
+  X(2, 2, 2, 2, 3, 2, 1.26, 2.1, 0.258, 1.2, 2.89, 0.758) \
+  X(1, 2, 2, 2, 3, 2, 1.18, 2.22, 0.241, 1.02, 2.73, 0.661) \
+  X(2, 2, 4, 2, 3, 1, 2.19, 1.11, 0.446, 1.09, 3.07, 0.623)
 
 struct MxChoice {
   int variant;  // rows kernels first, then tile kernels
@@ -831,7 +865,7 @@ struct MxTiles {
   double t0, e, c, u, r0, r;
 };
 #define ROWS_OF(MT, RT, NW, U, T0, C, B, D) {MT, RT, T0, C, B, D},
-#define TILE_OF(TR, TC, NWR, NWC, RING, T0, E, C, U, R0, R) {TR * NWR * 16, TC * NWC * 16, T0, E, C, U, R0, R},
+#define TILE_OF(TR, TC, NWR, NWC, RING, KG, T0, E, C, U, R0, R) {TR * NWR * 16, TC * NWC * 16, T0, E, C, U, R0, R},
 constexpr MxRows kRowsFp8[] = {MX_ROWS_FP8(ROWS_OF)}, kRowsFp4[] = {MX_ROWS_FP4(ROWS_OF)}, kRows16[] = {MX_ROWS_16(ROWS_OF)};
 constexpr MxTiles kTilesFp8[] = {MX_TILES_FP8(TILE_OF)}, kTilesFp4[] = {MX_TILES_FP4(TILE_OF)}, kTiles16[] = {MX_TILES_16(TILE_OF)};
 #undef ROWS_OF
@@ -890,8 +924,8 @@ hipError_t launch(const MxGemmArgs& a, const MxChoice& c, float* partial, hipStr
   int i = 0;
 #define ROWS_GO(MT, RT, NW, U, ...) \
   if (c.variant == i++) return launch_rows<ACT, DT, MT, RT, NW, U>(a, st);
-#define TILE_GO(TR, TC, NWR, NWC, RING, ...) \
-  if (c.variant == i++) return launch_tile<ACT, DT, TR, TC, NWR, NWC, RING>(a, partial, c.nsplit, st);
+#define TILE_GO(TR, TC, NWR, NWC, RING, KG, ...) \
+  if (c.variant == i++) return launch_tile<ACT, DT, TR, TC, NWR, NWC, RING, KG>(a, partial, c.nsplit, st);
   if constexpr (ACT == ACT_FP8) {
     MX_ROWS_FP8(ROWS_GO) MX_TILES_FP8(TILE_GO)
   } else if constexpr (ACT == ACT_FP4) {

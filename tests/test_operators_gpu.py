@@ -187,7 +187,7 @@ def test_product_larger(ctx, M, N, K, act):
 @pytest.mark.parametrize("M,N,K", [(1, 4096, 4096), (1, 11008, 4096), (16, 22016, 8192), (32, 4096, 11008), (32, 22016, 8192), (64, 4096, 4096), (64, 11008, 4096), (64, 22016, 8192),
                                    (96, 5003, 3020), (128, 5120, 13824), (200, 9216, 9216), (333, 5003, 3020), (512, 13824, 5120), (768, 22016, 1024), (1024, 4096, 4096),
                                    (2048, 13824, 1280), (2048, 22016, 640), (1500, 1000, 900), (20, 11000, 640), (24, 5120, 640),
-                                   (700, 18432, 640), (700, 18421, 1250), (1490, 13824, 4096), (512, 22016, 4096)])
+                                   (700, 18432, 640), (700, 18421, 1250), (1490, 13824, 4096), (512, 22016, 4096), (4, 5120, 384), (512, 11000, 512), (250, 22016, 384)])
 def test_product_of_layer_sizes(ctx, M, N, K, act):
     """Every kernel's own range of sizes; the 64-bit product is made on the device from the values read back (which other tests pin)."""
     gen = torch.Generator("cuda").manual_seed(M + N + K)
@@ -208,6 +208,21 @@ def test_product_of_layer_sizes(ctx, M, N, K, act):
 @pytest.mark.parametrize("M,N", [(5, 70), (40, 96), (140, 131), (300, 640), (200, 640), (513, 1000), (1030, 2100), (2050, 4100)])
 def test_product_in_32_bits(ctx, M, N, act):
     _product(ctx, M, N, 520, act, "f16", out="f32")
+
+
+@pytest.mark.parametrize("dtype,out", [("f16", "f32"), ("bf16", "bf16")])
+@pytest.mark.parametrize("M,N", [(200, 64), (64, 130), (20, 130), (200, 4090), (33, 11000)])
+@pytest.mark.parametrize("K", [1, 128, 200, 384, 520, 640, 900])
+def test_product_with_k_in_halves(ctx, M, N, K, dtype, out):
+    """Two groups of waves share the 128-channel steps of K: none for the second, as many for both, one less; K not a multiple of 128."""
+    _product(ctx, M, N, K, "16", dtype, out=out)
+
+
+@pytest.mark.parametrize("act", ["16", "fp8", "fp4"])
+@pytest.mark.parametrize("M,N,K", [(20, 130, 2800), (20, 64, 3200), (33, 500, 4600), (100, 11000, 3100), (333, 4090, 3100)])
+def test_product_with_k_cut_unevenly(ctx, M, N, K, act):
+    """A last piece of K with a single step of 128 channels, among others."""
+    _product(ctx, M, N, K, act, "bf16")
 
 
 @pytest.mark.parametrize("M", [1, 20, 150])
