@@ -1,6 +1,6 @@
 // The norm in front of a linear layer: h = x + residual (rounded to the type, as it is kept for the next layer), y = h w / sqrt(mean(h^2) + eps),
 // y rounded once, to 16 bits or to microscaled 8 or 4 bits as the product of csrc/mx_matmul.hip takes them.
-// Bound by memory: a row stays in registers between the sum of its squares (fp32) and its output, so that every value is read and written
+// Bound by memory: a row stays in registers between the sum of its squares (64 bits) and its output, so that every value is read and written
 // once.  NT threads work on a row, C pieces of eight channels each; 64 threads (a wave) need no barrier.
 #include <hip/hip_runtime.h>
 
@@ -38,23 +38,21 @@ __device__ __forceinline__ void store_8(uint16_t* p, long long left, const uint3
       if (i < left) p[i] = (uint16_t)(v[i / 2] >> (16 * (i & 1)));
   }
 }
+// s + the squares of eight values, in 64 bits: rows of 16-bit numbers of any size, sums that no output can tell from exact ones
 template <int DT>
-__device__ __forceinline__ float squares(const uint32_t (&v)[4]) {
-  float s = 0.f;
+__device__ __forceinline__ double squares(const uint32_t (&v)[4], double s) {
 #pragma unroll
   for (int i = 0; i < 4; i++) {
-    const float lo = esp_to_float<DT>((uint16_t)v[i]), hi = esp_to_float<DT>((uint16_t)(v[i] >> 16));
-    s = __builtin_fmaf(lo, lo, s);
-    s = __builtin_fmaf(hi, hi, s);
+    const double lo = esp_to_float<DT>((uint16_t)v[i]), hi = esp_to_float<DT>((uint16_t)(v[i] >> 16));
+    s = __builtin_fma(lo, lo, s);
+    s = __builtin_fma(hi, hi, s);
   }
   return s;
 }
 
-// 1 / sqrt(mean of the squares + eps) from the threads' sums, added in 64 bits, as the sum of two floats; every thread of the row gets it.  A product
-// h w of two 16-bit numbers is exact in fp32, so that y = h w (hi + lo) is rounded once: an output in 8 or 4 bits lies on the other side of the middle
-// between two of its numbers less often than with the three roundings of (h * inv) * w.  `buf`: one double per wave
+// 1 / sqrt(mean of the squares + eps) from the threads' sums, as the sum of two floats; every thread of the row gets it.  `buf`: one double per wave
 template <int NT>
-__device__ __forceinline__ float2 row_inverse(float own, double* buf, long long K, float eps) {
+__device__ __forceinline__ float2 row_inverse(double own, double* buf, long long K, float eps) {
   double v = own;
 #pragma unroll
   for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
@@ -71,17 +69,44 @@ __device__ __forceinline__ float2 row_inverse(float own, double* buf, long long 
   return float2{hi, __builtin_isfinite(hi) ? (float)(inv - (double)hi) : 0.f};
 }
 
-// output of one piece of eight channels.  Lanes of pieces behind the row's last channel take part (zeros in the padding of a
-// microscaled row); `chunk` differs by one between neighbouring lanes and starts at a multiple of 16
+// p (hi + lo), rounded once
+__device__ __forceinline__ float times(float p, float2 by) {
+  return __builtin_copysignf(__builtin_fmaf(p, by.x, p * by.y), p);  // (-0 (hi + lo) with lo < 0 would be +0)
+}
+// v = times(p, by) to an odd last bit where it is not exact: rounding that again to 8 or 4 bits gives what rounding the exact value would
+__device__ __forceinline__ float to_odd(float v, float p, float2 by) {
+  const float rest = __builtin_fmaf(p, by.y, __builtin_fmaf(p, by.x, -v));
+  const uint32_t b = __builtin_bit_cast(uint32_t, v);
+  if ((b & 1u) || (b << 1) == 0u || !(rest < 0.f || rest > 0.f)) return v;
+  return __builtin_bit_cast(float, (rest > 0.f) == ((int)b >= 0) ? b + 1u : b - 1u);
+}
+
+// output of one piece of eight channels (a product h w of two 16-bit numbers is exact in fp32: y = h w / sqrt(..) is rounded once).  Lanes of pieces
+// behind the row's last channel take part (zeros in the padding of a microscaled row); `chunk` differs by one between neighbouring lanes and starts at a
+// multiple of 16
 template <int DT, int OUT>
 __device__ __forceinline__ void norm_out(const NormArgs& a, long long row, unsigned chunk, const uint32_t (&h)[4], const uint32_t (&w)[4], float2 inv) {
-  float v[8];
+  float v[8], p[8];
 #pragma unroll
   for (int i = 0; i < 4; i++) {
-    const float lo = esp_to_float<DT>((uint16_t)h[i]) * esp_to_float<DT>((uint16_t)w[i]);
-    const float hi = esp_to_float<DT>((uint16_t)(h[i] >> 16)) * esp_to_float<DT>((uint16_t)(w[i] >> 16));
-    v[2 * i] = __builtin_fmaf(lo, inv.x, lo * inv.y);
-    v[2 * i + 1] = __builtin_fmaf(hi, inv.x, hi * inv.y);
+    p[2 * i] = esp_to_float<DT>((uint16_t)h[i]) * esp_to_float<DT>((uint16_t)w[i]);
+    p[2 * i + 1] = esp_to_float<DT>((uint16_t)(h[i] >> 16)) * esp_to_float<DT>((uint16_t)(w[i] >> 16));
+  }
+#pragma unroll
+  for (int i = 0; i < 8; i++) v[i] = times(p[i], inv);
+  if constexpr (OUT != OUT_16) {
+    // The middle between two codes, and a power of two, has at most five of the 24 significant bits: only a value with the others zero can have been
+    // rounded onto one (one in 2^19, so that the test costs less than rounding all of them to odd: 2048 x 8192 to 8 bits 26.6 us against 28.2)
+    uint32_t low = ~0u;
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+      const uint32_t b = __builtin_bit_cast(uint32_t, v[i]) << 13;
+      low = b < low ? b : low;
+    }
+    if (low == 0u) {
+#pragma unroll
+      for (int i = 0; i < 8; i++) v[i] = to_odd(v[i], p[i], inv);
+    }
   }
   if constexpr (OUT == OUT_16) {
     uint32_t o[4];
@@ -115,7 +140,7 @@ __global__ void __launch_bounds__(NT < 256 ? 256 : NT) k_rms_norm(const NormArgs
   }
 #pragma unroll
   for (int j = 0; j < C; j++) load_8(a.weight + (long long)(j * NT + t) * 8, a.K - (long long)(j * NT + t) * 8, w[j]);
-  float s = 0.f;
+  double s = 0.;
 #pragma unroll
   for (int j = 0; j < C; j++) {
     if (a.residual) {
@@ -123,7 +148,7 @@ __global__ void __launch_bounds__(NT < 256 ? 256 : NT) k_rms_norm(const NormArgs
       for (int i = 0; i < 4; i++) h[j][i] = add_pair<DT>(h[j][i], r[j][i]);
     }
     if (a.sum_out) store_8(a.sum_out + row * a.K + (long long)(j * NT + t) * 8, a.K - (long long)(j * NT + t) * 8, h[j]);
-    s += squares<DT>(h[j]);
+    s = squares<DT>(h[j], s);
   }
   const float2 inv = row_inverse<NT>(s, buf, a.K, a.eps);
 #pragma unroll
@@ -136,7 +161,7 @@ __global__ void __launch_bounds__(1024) k_rms_norm_long(const NormArgs a) {
   __shared__ double buf[16];
   const long long row = blockIdx.x;
   const unsigned chunks = a.steps * 16, t = threadIdx.x;
-  float s = 0.f;
+  double s = 0.;
   uint32_t h[4], r[4], w[4];
   for (unsigned c = t; c < chunks; c += 1024) {
     const long long at = (long long)c * 8, left = a.K - at;
@@ -147,7 +172,7 @@ __global__ void __launch_bounds__(1024) k_rms_norm_long(const NormArgs a) {
       for (int i = 0; i < 4; i++) h[i] = add_pair<DT>(h[i], r[i]);
     }
     if (a.sum_out) store_8(a.sum_out + row * a.K + at, left, h);
-    s += squares<DT>(h);
+    s = squares<DT>(h, s);
   }
   const float2 inv = row_inverse<1024>(s, buf, a.K, a.eps);
   for (unsigned c0 = 0; c0 < chunks; c0 += 1024) {

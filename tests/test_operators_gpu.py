@@ -331,6 +331,33 @@ def test_norm(ctx, R, K, residual, dtype):
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
 @pytest.mark.parametrize("fmt", ["fp4", "fp8"])
+@pytest.mark.parametrize("R,K", [(300, 4096), (70, 8192), (900, 1000), (20, 33000)])
+def test_norm_to_mx_rounds_once(ctx, R, K, fmt, dtype):
+    """The codes of the exact norm, all of them: sums in 64 bits, and results that are not exact kept off the middles between two codes
+    (eps is a power of two: it is the same number in 32 bits and in 64)."""
+    rng = _rng("norm once", R, K)
+    x, r = _features(rng, R, K, dtype), _features(rng, R, K, dtype)
+    w = torch.from_numpy(rng.standard_normal(K)).to(TORCH[dtype])
+    q, _ = ctx.rms_norm(x.cuda(), w.cuda(), 2.0 ** -17, residual=r.cuda(), fmt=FMT[fmt])
+    h64 = (x.double() + r.double()).to(TORCH[dtype]).double().numpy()
+    _assert_mx(q, orc.rms_norm(h64, w.double().numpy(), 2.0 ** -17), FMT[fmt])
+
+
+@pytest.mark.parametrize("fmt", [None, "fp4", "fp8"])
+def test_norm_of_rows_whose_squares_pass_32_bits(ctx, fmt):
+    rng, K = _rng("norm far"), 520
+    x = (_features(rng, 6, K, "f16").double() * 2.0 ** torch.tensor([[0.0], [64], [100], [-70], [-100], [30]], dtype=torch.float64)).bfloat16()
+    w = torch.from_numpy(rng.standard_normal(K)).bfloat16()
+    want = orc.rms_norm(x.double().numpy(), w.double().numpy(), 2.0 ** -17)
+    y, _ = ctx.rms_norm(x.cuda(), w.cuda(), 2.0 ** -17, fmt=fmt and FMT[fmt])
+    if fmt:
+        _assert_mx(y, want, FMT[fmt])
+    else:
+        assert (np.abs(_np(y) - want) <= _norm_bound(want, 0, HALF[torch.bfloat16], TINY[torch.bfloat16])).all()
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("fmt", ["fp4", "fp8"])
 @pytest.mark.parametrize("R,K", [(1, 1), (5, 33), (3, 512), (70, 515), (20, 4096), (3, 4097), (2, 13824), (2, 33000)])
 def test_norm_to_mx(ctx, R, K, fmt, dtype):
     """The codes are those of the exact norm, but where the sum's rounding moves a value across the middle of two of them or a block's largest across a power of two."""
