@@ -9,7 +9,7 @@
 // are equal: where their list overflows, k rounds of a search for the next in order take its place.  Order: larger value first, then lower index.
 #include <hip/hip_runtime.h>
 
-#include "common.h"
+#include "intrinsics.h"
 
 namespace {
 
@@ -71,25 +71,60 @@ __device__ __forceinline__ float log_prob(float x, float m, float s) {
   if (s == 0.f) return minus_infinity();
   return (x - m) - __builtin_logf(s);
 }
-__device__ __forceinline__ void answer_row(const LpOut& o, long long row, float m, float s, float t) {
-  if (o.tokens && o.logprob) {
-    const long long id = o.tokens[row];
-    o.logprob[row] = id < 0 ? 0.f : (id >= o.V ? __builtin_nanf("") : log_prob(logit_at(o, row, id), m, s));
-  }
+// the row's token (asked for early: its logit is another trip to memory) and that logit
+__device__ __forceinline__ long long token_of(const LpOut& o, long long row) { return o.tokens && o.logprob ? o.tokens[row] : -1; }
+__device__ __forceinline__ float token_logit(const LpOut& o, long long row, long long id) { return id >= 0 && id < o.V ? logit_at(o, row, id) : 0.f; }
+__device__ __forceinline__ void answer_row(const LpOut& o, long long row, long long id, float x, float m, float s, float t) {
+  if (o.tokens && o.logprob) o.logprob[row] = id < 0 ? 0.f : (id >= o.V ? __builtin_nanf("") : log_prob(x, m, s));
   if (o.entropy) o.entropy[row] = s == 0.f ? 0.f : __builtin_logf(s) - t / s;
 }
 
-// The first `top` of n candidates (n >= top, all different) to their places: a candidate's place is the number of those before it.
-__device__ __forceinline__ void place_candidates(const unsigned long long* list, int n, int top, int nt, int32_t* ids, float* lps, float m, float s) {
-  for (int i = threadIdx.x; i < n; i += nt) {
-    const unsigned long long k = list[i];
-    int place = 0;
-    for (int j = 0; j < n; j++) place += list[j] > k;
-    if (place < top) {
-      ids[place] = s != s ? -1 : (int32_t)~(uint32_t)k;
-      lps[place] = s != s ? s : log_prob(key_value((uint32_t)(k >> 32)), m, s);
+constexpr int NT = 256, NW = NT / 64;
+
+// The first `top` of n candidates (all different, at most 64 C) to put(place, candidate): a candidate's place is the number of those before it.  Every wave
+// holds all of them and counts for each NW-th (each thread in a loop over the list in shared memory: 1 x 32000 with 20 alternatives 13.2 instead of 10.6 us;
+// more than 128 candidates are rare, and registers for them would cost the kernels an eighth of their waves)
+template <int C, class Put>
+__device__ __forceinline__ void place_from(const unsigned long long* list, int n, int top, const Put& put) {
+  const int lane = threadIdx.x & 63, wave = wave_uniform((int)(threadIdx.x >> 6));
+  unsigned long long own[C];
+  int place[C];
+#pragma unroll
+  for (int c = 0; c < C; c++) {
+    own[c] = c * 64 + lane < n ? list[c * 64 + lane] : 0ull;
+    place[c] = top;
+  }
+#pragma unroll
+  for (int c = 0; c < C; c++)
+    for (int l = wave; l < 64 && c * 64 + l < n; l += NW) {
+      const unsigned long long k = (unsigned long long)(uint32_t)__builtin_amdgcn_readlane((int)(own[c] >> 32), l) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)own[c], l);
+      int before = 0;
+#pragma unroll
+      for (int d = 0; d < C; d++) before += __builtin_popcountll(__ballot(own[d] > k));
+      place[c] = lane == l ? before : place[c];
+    }
+#pragma unroll
+  for (int c = 0; c < C; c++)
+    if (place[c] < top) put(place[c], own[c]);
+}
+template <class Put>
+__device__ __forceinline__ void place_candidates(const unsigned long long* list, int n, int top, const Put& put) {
+  if (n <= 64) {
+    place_from<1>(list, n, top, put);
+  } else if (n <= 128) {
+    place_from<2>(list, n, top, put);
+  } else {
+    for (int i = threadIdx.x; i < n; i += NT) {
+      const unsigned long long k = list[i];
+      int place = 0;
+      for (int j = 0; j < n; j++) place += list[j] > k;
+      if (place < top) put(place, k);
     }
   }
+}
+__device__ __forceinline__ void answer_place(const LpOut& o, long long row, int place, unsigned long long k, float m, float s) {
+  o.top_ids[row * o.top + place] = s != s ? -1 : (int32_t)~(uint32_t)k;
+  o.top_logprobs[row * o.top + place] = s != s ? s : log_prob(key_value((uint32_t)(k >> 32)), m, s);
 }
 
 // One wave with C keys a lane: the largest 32-bit pattern that at least `top` of the keys reach, or one below it that at most half as many again and SLACK more do
@@ -110,7 +145,6 @@ __device__ __forceinline__ uint32_t key_bound(const uint32_t (&key)[C], int top)
   return bound;
 }
 
-constexpr int NT = 256, NW = NT / 64;
 constexpr int AT_ONCE = 4;  // pieces of 16 bytes a thread reads at a time
 
 // values of a 16-byte unit; behind the row's end minus infinity
@@ -173,6 +207,7 @@ __global__ void __launch_bounds__(NT) k_lp_row(const LpOut o, unsigned pieces, u
   const unsigned piece = PARTS ? blockIdx.x - (unsigned)row * pieces : 0, tid = threadIdx.x, wave = tid >> 6;
   const unsigned all = (unsigned)((V + E - 1) / E), first = piece * units, end = first + units < all ? first + units : all;
   const void* x = reinterpret_cast<const unsigned char*>(o.logits) + row * o.ld * (DT == ESPARSE_F32 ? 4 : 2);
+  const long long id = !PARTS && tid == 0 ? token_of(o, row) : -1;
   float m = minus_infinity(), from = 0.f, s = 0.f, t = 0.f;  // from: m, 0 while there is none
   auto take = [&](const Unit (&v)[AT_ONCE]) {
     float top = m;
@@ -202,6 +237,7 @@ __global__ void __launch_bounds__(NT) k_lp_row(const LpOut o, unsigned pieces, u
     for (int j = 0; j < AT_ONCE; j++) v[j].load(x, u + j * NT < end ? (long long)(u + j * NT) * E : V, V);
     take(v);
   }
+  const float x_id = !PARTS && tid == 0 ? token_logit(o, row, id) : 0.f;
   const float wm = wave_max(m);
   if ((tid & 63u) == 0) s_m[wave] = wm;
   const bool any = first + tid < end;  // (a thread without values is below all others)
@@ -239,7 +275,7 @@ __global__ void __launch_bounds__(NT) k_lp_row(const LpOut o, unsigned pieces, u
   }
   if (tid == 0) {
     if (PARTS) part[row * pieces + piece] = LpPartial{row_m, s, t, 0.f};
-    else answer_row(o, row, row_m, s, t);
+    else answer_row(o, row, id, x_id, row_m, s, t);
   }
   if (!o.top) return;
   const uint32_t from_key = s_from;
@@ -300,77 +336,56 @@ __global__ void __launch_bounds__(NT) k_lp_row(const LpOut o, unsigned pieces, u
   if (PARTS) {
     // this piece's first `top`, in order; a piece with fewer values ends in zeros
     unsigned long long* to = part_top + (row * pieces + piece) * o.top;
-    for (int i = tid; i < n; i += NT) {
-      const unsigned long long k = s_list[i];
-      int place = 0;
-      for (int j = 0; j < n; j++) place += s_list[j] > k;
-      if (place < o.top) to[place] = k;
-    }
+    place_candidates(s_list, n, o.top, [&](int place, unsigned long long k) { to[place] = k; });
     for (int i = n + tid; i < o.top; i += NT) to[i] = 0;
   } else {
-    place_candidates(s_list, n, o.top, NT, o.top_ids + row * o.top, o.top_logprobs + row * o.top, row_m, s);
+    place_candidates(s_list, n, o.top, [&](int place, unsigned long long k) { answer_place(o, row, place, k, row_m, s); });
   }
 }
 
-// joins the pieces of a row: one workgroup a row
-__global__ void __launch_bounds__(256) k_lp_join(const LpOut o, unsigned pieces, const LpPartial* __restrict__ part, const unsigned long long* __restrict__ part_top) {
-  __shared__ float s_a[4], s_b[4];
+constexpr int MAX_PIECES = LIST / ESPARSE_MAX_TOP;
+static_assert(MAX_PIECES <= 64 && LIST % NT == 0, "a lane for every piece");
+
+// Joins the pieces of a row: one workgroup a row.  Bound by its trips to memory one after the other, so all that does not depend on another answer is read at
+// the start and each wave joins the sums for itself (8 rows of 131072 with 20 alternatives, the whole call: 10.8 us; with the pieces, the lists and the token
+// read one after the other and a search for the bound bit by bit 13.3)
+__global__ void __launch_bounds__(NT) k_lp_join(const LpOut o, unsigned pieces, const LpPartial* __restrict__ part, const unsigned long long* __restrict__ part_top) {
   __shared__ unsigned long long s_list[LIST];
-  __shared__ uint32_t s_from;
   __shared__ int s_n;
   const long long row = blockIdx.x;
-  const unsigned tid = threadIdx.x, wave = tid >> 6;
-  const LpPartial* p = part + row * pieces;
-  float m = minus_infinity();
-  for (unsigned i = tid; i < pieces; i += 256) m = __builtin_fmaxf(m, p[i].m);
-  m = wave_max(m);
-  if ((tid & 63u) == 0) s_a[wave] = m;
-  if (tid == 0) s_n = 0;
-  // a bound of the row's last alternative among the pieces' ones (pieces * top <= LIST); 0: no value
+  const unsigned tid = threadIdx.x, lane = tid & 63u;
+  const LpPartial p = lane < pieces ? part[row * pieces + lane] : LpPartial{minus_infinity(), 0.f, 0.f, 0.f};
   const unsigned long long* lists = part_top + row * pieces * o.top;
   const unsigned count = pieces * o.top;
-  if (o.top && wave == 3) {
-    uint32_t key[LIST / 64];
+  unsigned long long mine[LIST / NT];
 #pragma unroll
-    for (int i = 0; i < LIST / 64; i++) {
-      const unsigned at = i * 64 + (tid & 63u);
-      key[i] = at < count ? (uint32_t)(lists[at] >> 32) : 0u;
-    }
-    const uint32_t bound = key_bound(key, o.top);
-    if ((tid & 63u) == 0) s_from = bound;
-  }
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < 4; i++) m = __builtin_fmaxf(m, s_a[i]);
-  const uint32_t bound = o.top ? s_from : 0u;
-  __syncthreads();
-  const float from = m == minus_infinity() ? 0.f : m;
-  float s = 0.f, t = 0.f;
-  for (unsigned i = tid; i < pieces; i += 256) {
-    const float pm = p[i].m == minus_infinity() ? 0.f : p[i].m, d = pm - from;
-    if (p[i].s != 0.f) {  // (its sums are taken from another maximum)
-      const float f = natural_exp(d);
-      s += p[i].s * f;
-      t += f * __builtin_fmaf(p[i].s, __builtin_fmaxf(d, -128.f), p[i].t);
-    }
-  }
-  s = wave_sum(s);
-  t = wave_sum(t);
-  if ((tid & 63u) == 0) {
-    s_a[wave] = s;
-    s_b[wave] = t;
-  }
-  __syncthreads();
-  s = s_a[0] + s_a[1] + s_a[2] + s_a[3];
-  t = s_b[0] + s_b[1] + s_b[2] + s_b[3];
-  if (tid == 0) answer_row(o, row, m, s, t);
+  for (int i = 0; i < LIST / NT; i++) mine[i] = i * NT + tid < count ? lists[i * NT + tid] : 0ull;
+  const unsigned jth = o.top ? (o.top + pieces - 1) / pieces : 1;
+  const uint32_t share = o.top && lane < pieces ? (uint32_t)(lists[lane * o.top + jth - 1] >> 32) : 0u;
+  const long long id = tid == 0 ? token_of(o, row) : -1;
+  const float x_id = tid == 0 ? token_logit(o, row, id) : 0.f;
+  if (tid == 0) s_n = 0;
+  const float m = wave_max(p.m), from = m == minus_infinity() ? 0.f : m, d = (p.m == minus_infinity() ? 0.f : p.m) - from, f = natural_exp(d);
+  const bool some = p.s != 0.f;  // (its sums are taken from another maximum)
+  const float s = wave_sum(some ? p.s * f : 0.f), t = wave_sum(some ? f * __builtin_fmaf(p.s, __builtin_fmaxf(d, -128.f), p.t) : 0.f);
+  if (tid == 0) answer_row(o, row, id, x_id, m, s, t);
   if (!o.top) return;
-  for (unsigned i = tid; i < count; i += 256) {
-    const unsigned long long k = lists[i];
-    if (k && (uint32_t)(k >> 32) >= bound) s_list[atomicAdd(&s_n, 1)] = k;
+  // A key that at least `top` alternatives reach: the lists are in order, and of their j-th (j pieces >= top) the q-th largest (q j >= top) is reached by j of q
+  // lists each (0: no value)
+  const unsigned qth = (o.top + jth - 1) / jth;
+  unsigned before = 0;
+  for (unsigned l = 0; l < pieces; l++) {
+    const uint32_t k = (uint32_t)__builtin_amdgcn_readlane((int)share, (int)l);
+    before += k > share || (k == share && l < lane);
   }
+  const unsigned long long who = __ballot(lane < pieces && before == qth - 1);
+  const uint32_t bound = (uint32_t)__builtin_amdgcn_readlane((int)share, (int)__builtin_ctzll(who));
   __syncthreads();
-  place_candidates(s_list, s_n, o.top, 256, o.top_ids + row * o.top, o.top_logprobs + row * o.top, m, s);
+#pragma unroll
+  for (int i = 0; i < LIST / NT; i++)
+    if (mine[i] && (uint32_t)(mine[i] >> 32) >= bound) s_list[atomicAdd(&s_n, 1)] = mine[i];
+  __syncthreads();
+  place_candidates(s_list, s_n, o.top, [&](int place, unsigned long long k) { answer_place(o, row, place, k, m, s); });
 }
 
 // Workgroups of a row: one where the rows fill the chip (1024 of them are four a compute unit; 1024 x 50048 16-bit: 25.2 us, cut in two 27.9), otherwise as many as
@@ -378,7 +393,6 @@ __global__ void __launch_bounds__(256) k_lp_join(const LpOut o, unsigned pieces,
 struct LpPlan {
   unsigned pieces, units;
 };
-constexpr long long MAX_PIECES = LIST / ESPARSE_MAX_TOP;
 
 LpPlan plan(long long R, long long V, int dtype, int top) {
   const int e = dtype == ESPARSE_F32 ? 4 : 8;
