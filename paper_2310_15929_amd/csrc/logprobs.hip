@@ -7,6 +7,8 @@
 //   Alternatives: T = the k-th largest of the threads' own maxima is a lower bound of the k-th largest value, so only threads whose
 // maximum reaches T (about k of them) read their values a second time, and only values of at least T are looked at: little more than k, unless many
 // are equal: where their list overflows, k rounds of a search for the next in order take its place.  Order: larger value first, then lower index.
+//   Measured, cold: 2048 x 131072 16-bit 104 us (5.2 TB/s; 20 alternatives 143), 2048 x 32000 30 us (4.4 TB/s), 555 x 50021 32-bit 28.7 us (3.9 TB/s: two
+// pieces a row, 4.3 workgroups a compute unit; 5 alternatives 32.7), 8 x 131072 6.2 us, 1 x 32000 5.6 us (20 alternatives 10.6).
 #include <hip/hip_runtime.h>
 
 #include "intrinsics.h"
@@ -389,7 +391,8 @@ __global__ void __launch_bounds__(NT) k_lp_join(const LpOut o, unsigned pieces, 
 }
 
 // Workgroups of a row: one where the rows fill the chip (1024 of them are four a compute unit; 1024 x 50048 16-bit: 25.2 us, cut in two 27.9), otherwise as many as
-// bring it there, of 512 units at least (two for each thread) or, with alternatives, whose lists have to be joined, 1024 (1 x 32000: 10.5 us, with 512 11.8)
+// bring it there, of 512 units at least (two for each thread) or, with alternatives, whose lists have to be joined, 1024 (with 512: 8 x 131072 10.7 instead of
+// 10.0 us, 1 x 16000 8.6 instead of 6.8, though 1 x 32000 9.0 instead of 9.7)
 struct LpPlan {
   unsigned pieces, units;
 };
