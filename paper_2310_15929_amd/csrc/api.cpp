@@ -798,6 +798,11 @@ int esparse_mx_pack(esparse_ctx* ctx, const void* data, const void* scales, long
   ESP_REQUIRE(ctx, N >= 1, ESPARSE_EINVAL, "N = 0");
   ESP_REQUIRE(ctx, data && scales && packed_out, ESPARSE_EINVAL, "data / scales / packed_out is null");
   ESP_REQUIRE(ctx, esp_aligned16(data) && esp_aligned16(scales) && esp_aligned16(packed_out), ESPARSE_EINVAL, "data / scales / packed_out is not 16-byte aligned");
+  size_t data_bytes = 0, scale_bytes = 0, packed_bytes = 0;
+  (void)esparse_mx_size(N, K, ESPARSE_MX_FP4, &data_bytes, &scale_bytes);
+  (void)esparse_mx_packed_size(N, K, &packed_bytes);
+  ESP_REQUIRE(ctx, !overlap(packed_out, packed_bytes, data, data_bytes) && !overlap(packed_out, packed_bytes, scales, scale_bytes), ESPARSE_EINVAL,
+              "packed_out overlaps data or scales");
   const DeviceOfCall device(ctx->device);
   ESP_HIP(ctx, device.error());
   return esp_mx_pack_device(ctx, data, scales, N, K, packed_out);
@@ -919,6 +924,15 @@ int esparse_token_logprobs(esparse_ctx* ctx, const void* logits, long long R, lo
   ESP_REQUIRE(ctx, need == 0 || workspace, ESPARSE_EINVAL, "workspace is null, %zu bytes needed", need);
   ESP_REQUIRE(ctx, need == 0 || workspace_bytes >= need, ESPARSE_EWORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, need);
   ESP_REQUIRE(ctx, need == 0 || aligned_to(workspace, 256), ESPARSE_EINVAL, "workspace is not 256-byte aligned");
+  const size_t rows4 = 4 * (size_t)R, tops4 = rows4 * (size_t)top;
+  const struct {
+    const void* p;
+    size_t bytes;
+  } all[] = {{logprob, rows4}, {entropy, rows4}, {top_ids, tops4}, {top_logprobs, tops4}, {workspace, need}, {logits, rows_bytes(R, V, ld, dtype_bytes(dtype))}, {tokens, 2 * rows4}};
+  for (int i = 0; i < 5; i++)  // what is written, against all that comes after it
+    for (int j = i + 1; j < 7; j++)
+      ESP_REQUIRE(ctx, all[i].bytes == 0 || all[j].bytes == 0 || !overlap(all[i].p, all[i].bytes, all[j].p, all[j].bytes), ESPARSE_EINVAL,
+                  "an output or the workspace overlaps an input or another output");
   const DeviceOfCall device(ctx->device);
   ESP_HIP(ctx, device.error());
   return esp_token_logprobs_device(ctx, logits, R, V, ld, dtype, reinterpret_cast<const long long*>(tokens), top, logprob, entropy, top_ids, top_logprobs, workspace);

@@ -21,7 +21,7 @@ struct NormArgs {
   uint32_t* scales;
   long long ldx, ldr, R, K;
   unsigned steps;
-  float eps;
+  double eps;
 };
 
 template <int DT>
@@ -53,7 +53,7 @@ __device__ __forceinline__ double squares(const uint32_t (&v)[4], double s) {
 
 // 1 / sqrt(mean of the squares + eps) from the threads' sums, as the sum of two floats; every thread of the row gets it.  `buf`: one double per wave
 template <int NT>
-__device__ __forceinline__ float2 row_inverse(double own, double* buf, long long K, float eps) {
+__device__ __forceinline__ float2 row_inverse(double own, double* buf, long long K, double eps) {
   double v = own;
 #pragma unroll
   for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
@@ -65,7 +65,7 @@ __device__ __forceinline__ float2 row_inverse(double own, double* buf, long long
 #pragma unroll
     for (int i = 0; i < NT / 64; i++) v += buf[i];
   }
-  const double inv = 1. / __builtin_sqrt(v / (double)K + (double)eps);
+  const double inv = 1. / __builtin_sqrt(v / (double)K + eps);
   const float hi = (float)inv;
   return float2{hi, __builtin_isfinite(hi) ? (float)(inv - (double)hi) : 0.f};
 }
@@ -215,7 +215,7 @@ hipError_t launch(const NormArgs& a, hipStream_t st) {
 int esp_rms_norm_device(esparse_ctx* ctx, const void* x, long long ldx, const void* residual, long long ldr, const void* weight, long long R, long long K,
                         double eps, int dtype, void* sum_out, void* y, int fmt, void* data, void* scales) {
   const NormArgs a = {(const uint16_t*)x, (const uint16_t*)residual, (const uint16_t*)weight, (uint16_t*)sum_out, (uint16_t*)y, (unsigned char*)data,
-                      (uint32_t*)scales, ldx, ldr, R, K, (unsigned)((K + 127) / 128), (float)eps};
+                      (uint32_t*)scales, ldx, ldr, R, K, (unsigned)((K + 127) / 128), eps};
   if (dtype == ESPARSE_F16) {
     if (y) ESP_HIP(ctx, (launch<ESPARSE_F16, OUT_16>(a, ctx->stream)));
     else if (fmt == ESPARSE_MX_FP4) ESP_HIP(ctx, (launch<ESPARSE_F16, ESPARSE_MX_FP4>(a, ctx->stream)));

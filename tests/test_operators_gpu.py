@@ -343,6 +343,30 @@ def test_norm_to_mx_rounds_once(ctx, R, K, fmt, dtype):
     _assert_mx(q, orc.rms_norm(h64, w.double().numpy(), 2.0 ** -17), FMT[fmt])
 
 
+@pytest.mark.parametrize("fmt", ["fp4", "fp8"])
+def test_norm_takes_eps_in_64_bits(ctx, fmt):
+    """Rows whose mean square is of the size of eps, which is no 32-bit number."""
+    rng, R, K = _rng("norm eps"), 200, 4096
+    x = (_features(rng, R, K, "bf16").double() * 2.0 ** -9).bfloat16()
+    w = torch.from_numpy(rng.standard_normal(K)).bfloat16()
+    q, _ = ctx.rms_norm(x.cuda(), w.cuda(), 1.1e-5, fmt=FMT[fmt])
+    _assert_mx(q, orc.rms_norm(x.double().numpy(), w.double().numpy(), 1.1e-5), FMT[fmt])
+
+
+@pytest.mark.parametrize("R,K", [(5, 100), (5, 4096), (5, 33000)])
+def test_norm_of_rows_that_are_no_numbers(ctx, R, K):
+    rng = _rng("norm nan", K)
+    x, w = _features(rng, R, K, "bf16"), torch.ones(K, dtype=torch.bfloat16)
+    x[1, K // 2], x[2, 3], x[3] = float("nan"), float("-inf"), 0.0
+    y, _ = ctx.rms_norm(x.cuda(), w.cuda(), 1e-5)
+    y = y.cpu()
+    assert torch.isnan(y[1]).all() and torch.isnan(y[2, 3]) and torch.isnan(y[2]).sum() == 1 and (y[2][~torch.isnan(y[2])] == 0).all() and (y[3] == 0).all()
+    assert torch.isfinite(y[[0, 4]]).all() and torch.isnan(ctx.rms_norm(x.cuda(), w.cuda(), 0.0)[0][3]).all()
+    q, _ = ctx.rms_norm(x.cuda(), w.cuda(), 1e-5, fmt=esp.MX_FP8)
+    v = ctx.mx_dequantize(q, torch.float32).cpu()
+    assert torch.isnan(v[1]).all() and torch.isnan(v[2, :32]).all() and (v[2, 32:] == 0).all() and (v[3] == 0).all() and torch.isfinite(v[[0, 4]]).all()
+
+
 @pytest.mark.parametrize("fmt", [None, "fp4", "fp8"])
 def test_norm_of_rows_whose_squares_pass_32_bits(ctx, fmt):
     rng, K = _rng("norm far"), 520

@@ -103,7 +103,8 @@ def test_dequantize_refuses(ctx, args, code, word):
     _expect(ctx, ctx._lib.esparse_mx_dequantize(ctx._h, *args), code, word)
 
 
-@pytest.mark.parametrize("args,code,word", [((None, P, 2, 8, P), EINVAL, "null"), ((P, P, 0, 8, P), EINVAL, "N"), ((P, P, 2, 8, P + 8), EINVAL, "16-byte")])
+@pytest.mark.parametrize("args,code,word", [((None, P, 2, 8, P), EINVAL, "null"), ((P, P, 0, 8, P), EINVAL, "N"), ((P, P, 2, 8, P + 8), EINVAL, "16-byte"),
+                                            ((P, P << 4, 2, 8, P), EINVAL, "overlaps"), ((P << 4, P, 200, 8, P - 64), EINVAL, "overlaps")])
 def test_pack_refuses(ctx, args, code, word):
     _expect(ctx, ctx._lib.esparse_mx_pack(ctx._h, *args), code, word)
 
@@ -152,7 +153,10 @@ LOGPROBS = dict(x=P, R=2, V=64, ld=64, dtype=1, tokens=P, top=0, lp=P, ent=P, id
     (dict(top=-1), EINVAL, "top"), (dict(top=33), EINVAL, "top"), (dict(V=4, top=5), EINVAL, "top"), (dict(x=None), EINVAL, "null"), (dict(ld=63), EINVAL, "ld"),
     (dict(lp=None), EINVAL, "together"), (dict(tokens=None), EINVAL, "together"), (dict(top=2), EINVAL, "top_ids"), (dict(x=P + 1), EINVAL, "aligned"),
     (dict(tokens=P + 4), EINVAL, "aligned"), (dict(V=1 << 21, ld=1 << 21), EINVAL, "workspace"),
-    (dict(V=1 << 21, ld=1 << 21, ws=P, nbytes=4), EWORKSPACE, "workspace"), (dict(V=1 << 21, ld=1 << 21, ws=P + 8, nbytes=1 << 30), EINVAL, "256-byte")])
+    (dict(V=1 << 21, ld=1 << 21, ws=P, nbytes=4), EWORKSPACE, "workspace"), (dict(V=1 << 21, ld=1 << 21, ws=P + 8, nbytes=1 << 30), EINVAL, "256-byte"),
+    (dict(), EINVAL, "overlaps"), (dict(lp=P << 4, ent=P << 5, tokens=(P << 5) - 8), EINVAL, "overlaps"), (dict(lp=P << 4, ent=P + 128 + 124, tokens=P << 6), EINVAL, "overlaps"),
+    (dict(lp=P << 4, ent=(P << 4) + 4, tokens=P << 6), EINVAL, "overlaps"), (dict(lp=P << 4, ent=P << 5, tokens=P << 6, top=2, ids=P << 7, lps=(P << 7) + 12), EINVAL, "overlaps"),
+    (dict(lp=P << 4, ent=P << 5, tokens=P << 6, V=1 << 20, ld=1 << 20, x=1 << 30, ws=(1 << 30) + (1 << 20), nbytes=1 << 20), EINVAL, "overlaps")])
 def test_logprobs_refuse(ctx, change, code, word):
     a = {**LOGPROBS, **change}
     _expect(ctx, ctx._lib.esparse_token_logprobs(ctx._h, a["x"], a["R"], a["V"], a["ld"], a["dtype"], a["tokens"], a["top"], a["lp"], a["ent"], a["ids"], a["lps"],
