@@ -699,7 +699,7 @@ class Context:
                 raise ValueError("rms_norm: residual is not of the shape and type of x")
             r = residual.data_ptr()
             if sum_out is None:
-                sum_out = x.new_empty((R, K))
+                sum_out = torch.empty_like(residual) if ldr == K else x.new_empty((R, K))  # (0.3 us less on the host)
         if sum_out is not None:
             if sum_out.get_device() != self.device:
                 self._away("rms_norm", sum_out)
@@ -707,7 +707,7 @@ class Context:
                 raise ValueError("rms_norm: sum_out is not a contiguous tensor of the shape and type of x")
         h = None if sum_out is None else sum_out.data_ptr()
         if fmt is None:
-            y = x.new_empty((R, K))
+            y = torch.empty_like(x) if ldx == K else x.new_empty((R, K))
             to = y.data_ptr(), 0, None, None
         else:
             y = self._empty_mx(x, R, K, fmt)

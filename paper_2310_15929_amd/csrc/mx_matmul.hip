@@ -283,9 +283,10 @@ __global__ void __launch_bounds__(NW * 64) k_mx_rows(const MxGemmArgs a) {
 // 16-byte pieces of a token are exchanged by an exclusive or with its number, so that the 16 tokens of an operand read hit all banks.
 // 16-bit activations: a unit of weights is expanded to 16 bits once per wave and stage, one stage ahead, between the multiplies.
 // Bound by the matrix pipe and its power at prompts: 2048 x 13824 x 5120 takes 104 - 108 us with 8-bit activations (2.7 - 2.8 PFLOP/s; the instruction alone,
-// in registers on random data, 4.3, on zeros this kernel 98 us), 79 with 4-bit (3.7; alone 7.3), 218 with 16-bit ones (1.33; alone 1.75).  2048 x 22016 x 8192:
-// 252, 178 and 530 us.  256 x 256 tiles: a stage of 8 bits takes 1.1 us against 1.0 of multiplies alone, one of 4 bits 0.72 against 0.59; several stages between
-// two barriers (rings of 4, two at a time) took 208 us instead of 183 (4 bits, 2048 x 22016 x 8192).
+// in registers on random data, 4.3), 79 with 4-bit (3.7; alone 7.3), 218 with 16-bit ones (1.33; alone 1.75); 2048 x 22016 x 8192 252 - 270, 175 - 190 and 520 - 530 us
+// and on zeros, which draw less power, 216, 155 and 411.  8192 x 8192 x 8192: 3.1, 4.5 and 1.44 PFLOP/s, on zeros 4.0, 6.0 and 1.8.  So what the stage does beside
+// the multiplies hardly counts: rings of 4 (4 bits: 181 - 183 us), wave tiles of 4 x 8 (187 - 190) and 8 x 8 (245 and more: registers spilled), two stages
+// between two barriers (no less) are not kept.
 // nsplit > 1: K is cut, a workgroup stores an fp32 partial tile, k_mx_reduce adds them in ascending order.
 // KG = 2: two groups of NWR x NWC waves, each with rings of its own, take half of the stages each; at the end each group hands half of its sums to the other.
 //   A compute unit keeps a bounded number of lines on their way, whatever the depth of the rings (fp8, 128 x 64 tiles: 0.28 us a stage with 4 as with 6 buffers
