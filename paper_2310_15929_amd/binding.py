@@ -125,6 +125,9 @@ def _dtype_code(t: torch.Tensor) -> int:
 _CODES = {torch.float16: F16, torch.bfloat16: BF16, torch.float32: F32}
 
 
+_EMPTY = torch.empty_strided
+
+
 def _code(dtype: torch.dtype, name: str, f32: bool = False) -> int:
     """The library's number of a type that a call takes."""
     code = _CODES.get(dtype)
@@ -308,6 +311,7 @@ class Context:
         if rc:
             raise EsparseError(rc, "esparse_create")
         self.device = device
+        self._on = torch.device("cuda", device)
         self._ws = None
         self._ws_at, self._ws_room = 0, -1  # the workspace's first aligned address and the bytes from there (-1: no workspace yet)
         self._stream = None              # the stream the library knows
@@ -610,18 +614,21 @@ class Context:
             raise ValueError(f"{name}: data and scales are contiguous uint8 tensors")
         return R
 
-    @staticmethod
-    def _empty_mx(like: torch.Tensor, R: int, K: int, fmt: int) -> MX:
+    def _empty(self, rows: int, columns: int, dtype: torch.dtype) -> torch.Tensor:
+        # (small calls wait for the host: 1.3 us with the strides given, 1.6 with new_empty, 1.2 with empty_like where a tensor of the shape is at hand)
+        return _EMPTY((rows, columns), (columns, 1), dtype=dtype, device=self._on)
+
+    def _empty_mx(self, R: int, K: int, fmt: int) -> MX:
         if fmt not in (MX_FP4, MX_FP8):
             raise ValueError(f"format {fmt} is neither MX_FP4 nor MX_FP8")
         steps = (K + 127) // 128
-        return MX(like.new_empty((R, steps * (64 if fmt == MX_FP4 else 128)), dtype=torch.uint8),
-                  like.new_empty((steps, R, 4), dtype=torch.uint8), K, fmt)
+        return MX(self._empty(R, steps * (64 if fmt == MX_FP4 else 128), torch.uint8),
+                  _EMPTY((steps, R, 4), (4 * R, 4, 1), dtype=torch.uint8, device=self._on), K, fmt)
 
     def mx_quantize(self, X: torch.Tensor, fmt: int) -> MX:
         """X[R, K] (f16, bf16, f32; rows may be apart) in microscaled 8 or 4 bits."""
         code, (R, K, ld) = _code(X.dtype, "mx_quantize", f32=True), self._rows("mx_quantize", X)
-        out = self._empty_mx(X, R, K, fmt)
+        out = self._empty_mx(R, K, fmt)
         self._sync_stream()
         rc = self._lib.esparse_mx_quantize(self._h, X.data_ptr(), R, K, ld, code, fmt, out.data.data_ptr(), out.scales.data_ptr())
         if rc:
@@ -631,7 +638,7 @@ class Context:
     def mx_dequantize(self, x: MX, dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
         """The values [R, K] that x stands for."""
         code, R = _code(dtype, "mx_dequantize", f32=True), self._check_mx("mx_dequantize", x)
-        out = x.data.new_empty((R, x.K), dtype=dtype)
+        out = self._empty(R, x.K, dtype)
         self._sync_stream()
         rc = self._lib.esparse_mx_dequantize(self._h, x.data.data_ptr(), x.scales.data_ptr(), R, x.K, x.fmt, code, out.data_ptr())
         if rc:
@@ -667,7 +674,7 @@ class Context:
         if packed.dtype != torch.uint8 or packed.numel() != _known_mx_packed_size(N, K) or not packed.is_contiguous():
             raise ValueError(f"mx_gemm: packed is not the weights of {N} x {K}")
         if out is None:
-            out = packed.new_empty((M, N), dtype=dtype or given)
+            out = self._empty(M, N, dtype or given)
         elif out.get_device() != self.device:
             self._away("mx_gemm", out)
         elif out.shape != (M, N) or not out.is_contiguous() or (dtype is not None and out.dtype != dtype):
@@ -699,7 +706,7 @@ class Context:
                 raise ValueError("rms_norm: residual is not of the shape and type of x")
             r = residual.data_ptr()
             if sum_out is None:
-                sum_out = torch.empty_like(residual) if ldr == K else x.new_empty((R, K))  # (0.3 us less on the host)
+                sum_out = torch.empty_like(residual) if ldr == K else self._empty(R, K, dtype)
         if sum_out is not None:
             if sum_out.get_device() != self.device:
                 self._away("rms_norm", sum_out)
@@ -707,10 +714,10 @@ class Context:
                 raise ValueError("rms_norm: sum_out is not a contiguous tensor of the shape and type of x")
         h = None if sum_out is None else sum_out.data_ptr()
         if fmt is None:
-            y = torch.empty_like(x) if ldx == K else x.new_empty((R, K))
+            y = torch.empty_like(x) if ldx == K else self._empty(R, K, dtype)
             to = y.data_ptr(), 0, None, None
         else:
-            y = self._empty_mx(x, R, K, fmt)
+            y = self._empty_mx(R, K, fmt)
             to = None, fmt, y.data.data_ptr(), y.scales.data_ptr()
         self._sync_stream()
         rc = self._lib.esparse_rms_norm(self._h, x.data_ptr(), ldx, r, ldr, weight.data_ptr(), R, K, eps, code, h, *to)
@@ -729,13 +736,13 @@ class Context:
                 self._away("token_logprobs", tokens)
             if tokens.dtype != torch.int64 or tokens.shape != (R,) or not tokens.is_contiguous():
                 raise ValueError(f"token_logprobs: tokens is not a contiguous int64 [{R}]")
-            logprob = logits.new_empty(R, dtype=torch.float32)
+            logprob = _EMPTY((R,), (1,), dtype=torch.float32, device=self._on)
             tok, lp = tokens.data_ptr(), logprob.data_ptr()
-        entropy = logits.new_empty(R, dtype=torch.float32)
+        entropy = _EMPTY((R,), (1,), dtype=torch.float32, device=self._on)
         if top:
-            ids, lps = logits.new_empty((R, top), dtype=torch.int32), logits.new_empty((R, top), dtype=torch.float32)
+            ids, lps = self._empty(R, top, torch.int32), self._empty(R, top, torch.float32)
             ip, tp = ids.data_ptr(), lps.data_ptr()
-        ws = logits.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
+        ws = _EMPTY((nbytes,), (1,), dtype=torch.uint8, device=self._on) if nbytes else None
         self._sync_stream()
         rc = self._lib.esparse_token_logprobs(self._h, logits.data_ptr(), R, V, ld, code, tok, top, lp, entropy.data_ptr(), ip, tp, _ptr(ws), nbytes)
         if rc:
