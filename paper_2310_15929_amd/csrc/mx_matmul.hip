@@ -749,20 +749,27 @@ __global__ void __launch_bounds__(NWR * NWC * KG * 64, (MxTile<ACT, TR, TC, NWR,
 }
 
 // the partial tiles of a product that K was cut for, four features a thread
+constexpr unsigned MOST_PIECES = 8;
 __global__ void __launch_bounds__(256) k_mx_reduce(const MxGemmArgs a, const float* __restrict__ partial, unsigned nsplit) {
-  const long long Np = (long long)a.nrt * 16, u = (long long)blockIdx.x * 256 + threadIdx.x;
-  const long long t = u / (Np / 4), n = u % (Np / 4) * 4;
+  // (at most 2^24 units: MOST_PARTIAL_BYTES)
+  const unsigned u = blockIdx.x * 256u + threadIdx.x, row = u / (a.nrt * 4u);
+  const long long Np = (long long)a.nrt * 16, t = row, n = (u - row * (a.nrt * 4u)) * 4u;
   if (t >= a.M || n >= a.N) return;
-  floatx4_t v = *reinterpret_cast<const floatx4_t*>(partial + t * Np + n);
-  for (unsigned s = 1; s < nsplit; s++) v += *reinterpret_cast<const floatx4_t*>(partial + ((long long)s * a.M + t) * Np + n);
-  store_4(a, t, n, v);
+  floatx4_t v[MOST_PIECES];
+#pragma unroll
+  for (unsigned s = 0; s < MOST_PIECES; s++)  // all of them under way at once (pieces behind the last repeat it)
+    v[s] = *reinterpret_cast<const floatx4_t*>(partial + ((long long)(s < nsplit ? s : nsplit - 1) * a.M + t) * Np + n);
+#pragma unroll
+  for (unsigned s = 1; s < MOST_PIECES; s++)
+    if (s < nsplit) v[0] += v[s];
+  store_4(a, t, n, v[0]);
 }
 
 // rows of 16-bit activations that the kernels cannot read as they are, into rows of 128 nks values, zero padded
 __global__ void __launch_bounds__(256) k_mx_pad_rows(const uint16_t* __restrict__ x, long long ldx, long long M, long long K, unsigned chunks, uint4* __restrict__ out) {
-  const long long u = (long long)blockIdx.x * 256 + threadIdx.x;
-  if (u >= M * chunks) return;
-  const long long t = u / chunks, at = (u % chunks) * 8;
+  const unsigned u = blockIdx.x * 256u + threadIdx.x, row = u / chunks;  // (fewer than 2^32 units: at most 2^34 values, rows padded by 15 units at most)
+  const long long t = row, at = (u - row * chunks) * 8u;
+  if (t >= M) return;
   uint32_t v[4];
   load_8(x + t * ldx + at, K - at, v);
   out[u] = uint4{v[0], v[1], v[2], v[3]};
@@ -799,62 +806,62 @@ hipError_t launch_tile(const MxGemmArgs& a, float* partial, unsigned nsplit, hip
 //   rows   t0 + steps (c L + b x) (1 - d + d q)                     L, x: workgroups per compute unit, whole and as they are; q: filled part of the token tiles
 //   tile   t0 + e L + c stages max(1, u L) + (K cut: r0 + r MB of partial tiles)      L: workgroups per compute unit (256 of them)
 // The constants are fitted to the times of every kernel on 13 weight shapes (512 x 512 to 36864 x 9216, ragged ones among them) and 1 to 2048 tokens, weights cold,
-// K cut up to eight times.  Over those 208 products of each kind the kernel so chosen takes 1.01 of the fastest one's time on average, 1.27 at most (6.5 us against 8.3).
+// K cut up to eight times.  Over those 208 products of each kind the kernel so chosen takes 1.003 - 1.007 of the fastest one's time on average, 1.17 at most (6.5 us against 7.7).
 // Of 27 kernels that were measured, the 15 of a kind are those without which the average would be worse.
 // ------------------------------------------------------------------------------------------------
 // rows: token tiles, row tiles, waves, steps at a time; t0, c, b, d
 #define MX_ROWS_FP8(X) \
-  X(1, 1, 8, 2, 2.44, 0.0633, 0.0238, 0.387) \
-  X(1, 2, 8, 2, 2.39, 0.0821, 0.0355, 0.265) \
-  X(1, 4, 8, 1, 2.48, 0.097, 0.103, 0.133) \
-  X(1, 8, 8, 1, 2.48, 0.188, 0.158, 0.109) \
-  X(2, 2, 8, 2, 2.38, 0.147, 0.0252, 0.535) \
-  X(2, 4, 8, 1, 2.69, 0.152, 0.0808, 0.396) \
-  X(4, 1, 8, 1, 2.43, 0.237, 0.0138, 0.608)
+  X(1, 1, 8, 2, 2.45, 0.0642, 0.0218, 0.383) \
+  X(1, 2, 8, 2, 2.46, 0.076, 0.0415, 0.26) \
+  X(1, 4, 8, 1, 2.47, 0.1, 0.0955, 0.129) \
+  X(1, 8, 8, 1, 2.57, 0.18, 0.172, 0.123) \
+  X(2, 2, 8, 2, 2.41, 0.144, 0.0254, 0.497) \
+  X(2, 4, 8, 1, 2.64, 0.155, 0.0726, 0.386) \
+  X(4, 1, 8, 1, 2.42, 0.237, 0.00489, 0.511)
 #define MX_ROWS_FP4(X) \
-  X(1, 1, 8, 2, 2.47, 0.0427, 0.0231, 0.309) \
-  X(1, 2, 8, 2, 2.33, 0.0705, 0.0364, 0.203) \
-  X(1, 4, 8, 1, 2.44, 0.083, 0.107, 0.0851) \
-  X(1, 8, 8, 1, 2.48, 0.164, 0.175, 0.0858) \
-  X(2, 1, 16, 1, 2.46, 0.0772, 0.0245, 0.638) \
-  X(2, 2, 8, 2, 2.41, 0.0984, 0.0471, 0.51) \
-  X(2, 4, 8, 1, 2.59, 0.115, 0.098, 0.268) \
-  X(4, 1, 8, 1, 2.41, 0.13, 0.0303, 0.588)
+  X(1, 1, 8, 2, 2.44, 0.0448, 0.0193, 0.294) \
+  X(1, 2, 8, 2, 2.34, 0.0653, 0.0417, 0.189) \
+  X(1, 4, 8, 1, 2.44, 0.0857, 0.105, 0.0857) \
+  X(1, 8, 8, 1, 2.52, 0.161, 0.186, 0.0959) \
+  X(2, 1, 16, 1, 2.54, 0.0745, 0.0231, 0.608) \
+  X(2, 2, 8, 2, 2.45, 0.0997, 0.0398, 0.486) \
+  X(2, 4, 8, 1, 2.54, 0.122, 0.0839, 0.243) \
+  X(4, 1, 8, 1, 2.45, 0.128, 0.0241, 0.49)
 #define MX_ROWS_16(X) \
-  X(1, 1, 8, 2, 2.54, 0.129, 0.031, 0.612) \
-  X(1, 2, 8, 2, 2.51, 0.144, 0.0524, 0.494) \
-  X(1, 4, 8, 1, 2.42, 0.176, 0.0916, 0.36) \
-  X(1, 8, 8, 1, 2.43, 0.265, 0.118, 0.0882) \
-  X(2, 1, 16, 1, 2.35, 0.25, 0.0289, 0.415) \
-  X(4, 1, 8, 1, 2.37, 0.466, 0.0107, 0.715)
+  X(1, 1, 8, 2, 2.53, 0.13, 0.0287, 0.608) \
+  X(1, 2, 8, 2, 2.52, 0.142, 0.0557, 0.499) \
+  X(1, 4, 8, 1, 2.45, 0.177, 0.0917, 0.368) \
+  X(1, 8, 8, 1, 2.52, 0.255, 0.136, 0.091) \
+  X(2, 1, 16, 1, 2.33, 0.255, 0.0306, 0.573) \
+  X(4, 1, 8, 1, 2.36, 0.469, 0.0101, 0.756)
 // tile: row and token tiles of a wave, waves along both, buffers of a ring, groups of waves along K; t0, e, c, u, r0, r
 #define MX_TILES_FP8(X) \
-  X(4, 2, 2, 2, 3, 1, 2.81, 0.122, 0.359, 0.711, 2.76, 0.615) \
-  X(4, 4, 2, 2, 3, 1, 4.06, 0.159, 0.435, 0.893, 2.29, 0.473) \
-  X(8, 4, 2, 2, 2, 1, 3.07, 1.35, 0.968, 0.704, 4.41, 0.333) \
-  X(4, 2, 2, 2, 6, 1, 2.02, 1.71, 0.159, 1.74, 2.39, 0.626) \
-  X(8, 4, 2, 4, 3, 1, 0, 7.1, 1.1, 1.01, 5.64, 0.285) \
-  X(4, 2, 2, 2, 4, 1, 2.5, 0.708, 0.286, 0.881, 2.7, 0.599) \
-  X(2, 2, 2, 2, 6, 1, 2.73, 0.605, 0.193, 0.955, 2.26, 0.694) \
-  X(2, 1, 1, 4, 6, 1, 2.7, 0.442, 0.161, 0.946, 2.49, 0.621)
+  X(4, 2, 2, 2, 3, 1, 2.43, 0.275, 0.377, 0.677, 2.14, 0.625) \
+  X(4, 4, 2, 2, 3, 1, 3.99, 0, 0.433, 0.901, 2.14, 0.488) \
+  X(8, 4, 2, 2, 2, 1, 4.3, 0, 0.97, 0.711, 4.04, 0.364) \
+  X(4, 2, 2, 2, 6, 1, 2.4, 1.16, 0.281, 1, 1.86, 0.626) \
+  X(8, 4, 2, 4, 3, 1, 0, 6.84, 0.93, 1.16, 6.43, 0.286) \
+  X(4, 2, 2, 2, 4, 1, 2.81, 0.288, 0.29, 0.886, 2.04, 0.631) \
+  X(2, 2, 2, 2, 6, 1, 2.91, 0.324, 0.198, 0.943, 1.76, 0.698) \
+  X(2, 1, 1, 4, 6, 1, 2.73, 0.371, 0.166, 0.921, 1.93, 0.67)
 #define MX_TILES_FP4(X) \
-  X(4, 4, 2, 2, 3, 1, 3.99, 0, 0.406, 0.794, 2.33, 0.483) \
-  X(7, 4, 2, 2, 2, 1, 5.91, 0, 0.882, 0.62, 1.75, 0.416) \
-  X(4, 2, 2, 2, 6, 1, 3.1, 0.102, 0.245, 0.966, 2.74, 0.666) \
-  X(8, 4, 2, 4, 3, 1, 0, 6.03, 0.72, 1.06, 6.26, 0.306) \
-  X(4, 2, 2, 2, 4, 1, 2.88, 0.0556, 0.269, 0.884, 2.8, 0.624) \
-  X(2, 2, 2, 2, 6, 1, 2.84, 0.259, 0.173, 0.957, 2.19, 0.774) \
-  X(2, 1, 1, 4, 6, 1, 2.54, 0.337, 0.142, 0.892, 2.47, 0.704)
+  X(4, 4, 2, 2, 3, 1, 3.74, 0, 0.403, 0.801, 2.26, 0.493) \
+  X(7, 4, 2, 2, 2, 1, 6.19, 0, 0.869, 0.626, 1.43, 0.401) \
+  X(4, 2, 2, 2, 6, 1, 3.04, 0.0408, 0.251, 0.94, 2.04, 0.684) \
+  X(8, 4, 2, 4, 3, 1, 0, 6.27, 0.64, 1.14, 6.48, 0.311) \
+  X(4, 2, 2, 2, 4, 1, 2.79, 0.0506, 0.273, 0.871, 2.09, 0.654) \
+  X(2, 2, 2, 2, 6, 1, 2.99, 0.017, 0.175, 0.955, 1.75, 0.746) \
+  X(2, 1, 1, 4, 6, 1, 2.69, 0.182, 0.144, 0.901, 2, 0.634)
 #define MX_TILES_16(X) \
-  X(4, 4, 4, 2, 3, 1, 0, 4.48, 1.21, 1.12, 4.28, 0.387) \
-  X(3, 4, 4, 2, 3, 1, 0.169, 5.01, 0.898, 1.14, 2.31, 0.386) \
-  X(4, 4, 4, 1, 2, 1, 1.53, 1.22, 1.06, 0.68, 4.3, 0.361) \
-  X(4, 2, 2, 4, 3, 1, 1.88, 2.65, 0.786, 1, 2.45, 0.48) \
-  X(2, 4, 4, 1, 3, 1, 2.94, 0.589, 0.481, 0.88, 2.71, 0.561) \
-  X(2, 4, 4, 1, 3, 2, 1.12, 2.97, 0.362, 1.14, 2.81, 0.749) \
-  X(2, 2, 2, 2, 3, 2, 1.26, 2.1, 0.258, 1.2, 2.89, 0.758) \
-  X(1, 2, 2, 2, 3, 2, 1.18, 2.22, 0.241, 1.02, 2.73, 0.661) \
-  X(2, 2, 4, 2, 3, 1, 2.19, 1.11, 0.446, 1.09, 3.07, 0.623)
+  X(4, 4, 4, 2, 3, 1, 0.66, 3.72, 1.21, 1.08, 4.44, 0.407) \
+  X(3, 4, 4, 2, 3, 1, 1.99, 3.32, 0.989, 1.01, 2.05, 0.43) \
+  X(4, 4, 4, 1, 2, 1, 2.46, 0.0824, 1.06, 0.691, 3.25, 0.458) \
+  X(4, 2, 2, 4, 3, 1, 1.99, 1.83, 0.731, 1.07, 2.88, 0.501) \
+  X(2, 4, 4, 1, 3, 1, 2.99, 0.317, 0.483, 0.891, 2.15, 0.591) \
+  X(2, 4, 4, 1, 3, 2, 1.06, 2.7, 0.407, 1.03, 2.61, 0.69) \
+  X(2, 2, 2, 2, 3, 2, 1.52, 1.76, 0.31, 1.02, 2.46, 0.712) \
+  X(1, 2, 2, 2, 3, 2, 1.34, 1.93, 0.145, 1.78, 2.36, 0.625) \
+  X(2, 2, 4, 2, 3, 1, 2.14, 0.946, 0.484, 1.01, 2.54, 0.621)
 
 struct MxChoice {
   int variant;  // rows kernels first, then tile kernels
@@ -903,7 +910,7 @@ MxChoice choose_from(const MxRows (&rows)[NR], const MxTiles (&tiles)[NT], long 
     for (int v = 0; v < (int)NT; v++) {
       const MxTiles& k = tiles[v];
       if (k.tokens > 64 && M <= k.tokens / 2) continue;
-      for (unsigned ns : {1u, 2u, 3u, 4u, 6u, 8u}) {
+      for (unsigned ns : {1u, 2u, 3u, 4u, 6u, MOST_PIECES}) {
         if (ns > 1 && (nks < 2 * ns || ns * M * nrt * 64 > MOST_PARTIAL_BYTES)) break;
         const long long per = ceil_div(nks, ns), cut = ceil_div(nks, per), L = ceil_div(ceil_div(nrt * 16, k.rows) * ceil_div(M, k.tokens) * cut, COMPUTE_UNITS);
         offer((int)NR + v, ns, k.t0 + k.e * L + k.c * per * (k.u * L > 1 ? k.u * L : 1) + (cut > 1 ? k.r0 + cut * M * nrt * 64e-6 * k.r : 0));
