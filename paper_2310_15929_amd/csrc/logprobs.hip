@@ -7,9 +7,11 @@
 //   Alternatives: T = the k-th largest of the threads' own maxima is a lower bound of the k-th largest value, so only threads whose
 // maximum reaches T (about k of them) read their values a second time, and only values of at least T are looked at: little more than k, unless many
 // are equal: where their list overflows, k rounds of a search for the next in order take its place.  Order: larger value first, then lower index.
-//   Measured, cold: 2048 x 131072 16-bit 104 us (5.2 TB/s; 20 alternatives 143), 2048 x 32000 30 us (4.4 TB/s), 555 x 50021 32-bit 28.7 us (3.9 TB/s: two
-// pieces a row, 4.3 workgroups a compute unit; 5 alternatives 32.7), 8 x 131072 6.2 us, 1 x 32000 5.6 us (20 alternatives 10.6).
+//   Measured, cold: 2048 x 131072 16-bit 104 us (5.2 TB/s; 20 alternatives 143), 2048 x 32000 30 us (4.4 TB/s), 555 x 50021 32-bit 27.4 us (4.1 TB/s: two
+// pieces a row, 4.3 workgroups a compute unit; 5 alternatives 31.9), 8 x 131072 6.2 us, 1 x 32000 5.6 us (20 alternatives 10.6).
 #include <hip/hip_runtime.h>
+
+#include <type_traits>
 
 #include "intrinsics.h"
 
@@ -211,10 +213,11 @@ __global__ void __launch_bounds__(NT) k_lp_row(const LpOut o, unsigned pieces, u
   const void* x = reinterpret_cast<const unsigned char*>(o.logits) + row * o.ld * (DT == ESPARSE_F32 ? 4 : 2);
   const long long id = !PARTS && tid == 0 ? token_of(o, row) : -1;
   float m = minus_infinity(), from = 0.f, s = 0.f, t = 0.f;  // from: m, 0 while there is none
-  auto take = [&](const Unit (&v)[AT_ONCE]) {
+  auto take = [&](const Unit* v, auto count) {
+    constexpr int N = decltype(count)::value;
     float top = m;
 #pragma unroll
-    for (int j = 0; j < AT_ONCE; j++)
+    for (int j = 0; j < N; j++)
 #pragma unroll
       for (int i = 0; i < E; i++) top = __builtin_fmaxf(top, v[j].value(i));
     if (top > m) {
@@ -224,7 +227,7 @@ __global__ void __launch_bounds__(NT) k_lp_row(const LpOut o, unsigned pieces, u
       m = from = top;
     }
 #pragma unroll
-    for (int j = 0; j < AT_ONCE; j++)
+    for (int j = 0; j < N; j++)
 #pragma unroll
       for (int i = 0; i < E; i++) {
         const float d = v[j].value(i) - from, p = natural_exp(d);
@@ -233,11 +236,22 @@ __global__ void __launch_bounds__(NT) k_lp_row(const LpOut o, unsigned pieces, u
       }
   };
   // (a second set of registers for the next values: no faster, 32 instead of 31 us for 2048 x 32000; eight workgroups a compute unit take turns as it is)
-  for (unsigned u = first + tid; u < end; u += AT_ONCE * NT) {
+  unsigned u = first + tid, of_wave = first + (unsigned)wave_uniform((int)(tid & ~63u));
+  for (; of_wave + (AT_ONCE - 1) * NT + 63 < end; u += AT_ONCE * NT, of_wave += AT_ONCE * NT) {
     Unit v[AT_ONCE];
 #pragma unroll
-    for (int j = 0; j < AT_ONCE; j++) v[j].load(x, u + j * NT < end ? (long long)(u + j * NT) * E : V, V);
-    take(v);
+    for (int j = 0; j < AT_ONCE; j++) v[j].load(x, (long long)(u + j * NT) * E, V);
+    take(v, std::integral_constant<int, AT_ONCE>{});
+  }
+  // the last ones, as many as there are: a place without a value costs the vector unit as much as one with (100 x 131072: 13.7 us in whole turns, 12.1 so)
+  if (of_wave < end) {
+    Unit v[AT_ONCE];
+#pragma unroll
+    for (int j = 0; j < AT_ONCE; j++)
+      if (of_wave + j * NT < end) v[j].load(x, u + j * NT < end ? (long long)(u + j * NT) * E : V, V);
+#pragma unroll
+    for (int j = 0; j < AT_ONCE; j++)
+      if (of_wave + j * NT < end) take(v + j, std::integral_constant<int, 1>{});
   }
   const float x_id = !PARTS && tid == 0 ? token_logit(o, row, id) : 0.f;
   const float wm = wave_max(m);
