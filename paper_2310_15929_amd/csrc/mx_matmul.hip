@@ -806,27 +806,29 @@ hipError_t launch_tile(const MxGemmArgs& a, float* partial, unsigned nsplit, hip
 //   rows   t0 + steps (c L + b x) (1 - d + d q)                     L, x: workgroups per compute unit, whole and as they are; q: filled part of the token tiles
 //   tile   t0 + e L + c stages max(1, u L) + (K cut: r0 + r MB of partial tiles)      L: workgroups per compute unit (256 of them)
 // The constants are fitted to the times of every kernel on 13 weight shapes (512 x 512 to 36864 x 9216, ragged ones among them) and 1 to 2048 tokens, weights cold,
-// K cut up to eight times.  Over those 208 products of each kind the kernel so chosen takes 1.003 - 1.007 of the fastest one's time on average, 1.17 at most (6.5 us against 7.7).
-// Of 27 kernels that were measured, the 15 of a kind are those without which the average would be worse.
+// K cut up to eight times.  Over those 234 products of each kind the kernel so chosen takes 1.005 - 1.011 of the fastest one's time on average, 1.23 at most (8.1 us
+// against 6.6).  Of 32 kernels that were measured, the 15 of a kind are those without which the average would be worse.
 // ------------------------------------------------------------------------------------------------
 // rows: token tiles, row tiles, waves, steps at a time; t0, c, b, d
 #define MX_ROWS_FP8(X) \
-  X(1, 1, 8, 2, 2.45, 0.0642, 0.0218, 0.383) \
-  X(1, 2, 8, 2, 2.46, 0.076, 0.0415, 0.26) \
-  X(1, 4, 8, 1, 2.47, 0.1, 0.0955, 0.129) \
-  X(1, 8, 8, 1, 2.57, 0.18, 0.172, 0.123) \
-  X(2, 2, 8, 2, 2.41, 0.144, 0.0254, 0.497) \
-  X(2, 4, 8, 1, 2.64, 0.155, 0.0726, 0.386) \
-  X(4, 1, 8, 1, 2.42, 0.237, 0.00489, 0.511)
+  X(1, 1, 8, 2, 2.4, 0.0662, 0.0161, 0.378) \
+  X(1, 2, 8, 2, 2.41, 0.0777, 0.0334, 0.243) \
+  X(1, 8, 8, 1, 2.48, 0.181, 0.152, 0.0962) \
+  X(2, 2, 8, 2, 2.41, 0.147, 0.0175, 0.495) \
+  X(2, 4, 8, 1, 2.71, 0.155, 0.0691, 0.403) \
+  X(4, 1, 8, 1, 2.44, 0.233, 0.00552, 0.495) \
+  X(1, 4, 8, 2, 2.39, 0.108, 0.0843, 0.178) \
+  X(1, 1, 16, 1, 2.55, 0.0609, 0.0206, 0.411)
 #define MX_ROWS_FP4(X) \
-  X(1, 1, 8, 2, 2.44, 0.0448, 0.0193, 0.294) \
-  X(1, 2, 8, 2, 2.34, 0.0653, 0.0417, 0.189) \
-  X(1, 4, 8, 1, 2.44, 0.0857, 0.105, 0.0857) \
-  X(1, 8, 8, 1, 2.52, 0.161, 0.186, 0.0959) \
-  X(2, 1, 16, 1, 2.54, 0.0745, 0.0231, 0.608) \
-  X(2, 2, 8, 2, 2.45, 0.0997, 0.0398, 0.486) \
-  X(2, 4, 8, 1, 2.54, 0.122, 0.0839, 0.243) \
-  X(4, 1, 8, 1, 2.45, 0.128, 0.0241, 0.49)
+  X(1, 1, 8, 2, 2.44, 0.0434, 0.0199, 0.296) \
+  X(1, 2, 8, 2, 2.4, 0.0573, 0.0456, 0.161) \
+  X(1, 8, 8, 1, 2.4, 0.163, 0.159, 0.0476) \
+  X(2, 1, 16, 1, 2.49, 0.0717, 0.0241, 0.509) \
+  X(2, 2, 8, 2, 2.4, 0.104, 0.0319, 0.509) \
+  X(2, 4, 8, 1, 2.51, 0.123, 0.0803, 0.279) \
+  X(4, 1, 8, 1, 2.41, 0.127, 0.0242, 0.511) \
+  X(1, 4, 8, 2, 2.36, 0.0917, 0.0959, 0.131) \
+  X(1, 1, 16, 2, 2.63, 0.0381, 0.0268, 0.335)
 #define MX_ROWS_16(X) \
   X(1, 1, 8, 2, 2.53, 0.13, 0.0287, 0.608) \
   X(1, 2, 8, 2, 2.52, 0.142, 0.0557, 0.499) \
@@ -836,22 +838,20 @@ hipError_t launch_tile(const MxGemmArgs& a, float* partial, unsigned nsplit, hip
   X(4, 1, 8, 1, 2.36, 0.469, 0.0101, 0.756)
 // tile: row and token tiles of a wave, waves along both, buffers of a ring, groups of waves along K; t0, e, c, u, r0, r
 #define MX_TILES_FP8(X) \
-  X(4, 2, 2, 2, 3, 1, 2.43, 0.275, 0.377, 0.677, 2.14, 0.625) \
-  X(4, 4, 2, 2, 3, 1, 3.99, 0, 0.433, 0.901, 2.14, 0.488) \
-  X(8, 4, 2, 2, 2, 1, 4.3, 0, 0.97, 0.711, 4.04, 0.364) \
-  X(4, 2, 2, 2, 6, 1, 2.4, 1.16, 0.281, 1, 1.86, 0.626) \
-  X(8, 4, 2, 4, 3, 1, 0, 6.84, 0.93, 1.16, 6.43, 0.286) \
-  X(4, 2, 2, 2, 4, 1, 2.81, 0.288, 0.29, 0.886, 2.04, 0.631) \
-  X(2, 2, 2, 2, 6, 1, 2.91, 0.324, 0.198, 0.943, 1.76, 0.698) \
-  X(2, 1, 1, 4, 6, 1, 2.73, 0.371, 0.166, 0.921, 1.93, 0.67)
+  X(4, 2, 2, 2, 3, 1, 2.69, 0.0319, 0.374, 0.675, 2.09, 0.64) \
+  X(4, 4, 2, 2, 3, 1, 3.87, 0, 0.427, 0.887, 2.36, 0.47) \
+  X(8, 4, 2, 2, 2, 1, 4.26, 0, 0.954, 0.695, 4.18, 0.364) \
+  X(4, 2, 2, 2, 6, 1, 2.61, 0.968, 0.265, 1.04, 1.85, 0.634) \
+  X(8, 4, 2, 4, 3, 1, 0, 6.88, 0.849, 1.21, 6.94, 0.27) \
+  X(2, 2, 2, 2, 6, 1, 2.99, 0.28, 0.193, 0.934, 1.66, 0.72) \
+  X(2, 1, 1, 4, 6, 1, 2.68, 0.424, 0.164, 0.913, 1.88, 0.654)
 #define MX_TILES_FP4(X) \
-  X(4, 4, 2, 2, 3, 1, 3.74, 0, 0.403, 0.801, 2.26, 0.493) \
-  X(7, 4, 2, 2, 2, 1, 6.19, 0, 0.869, 0.626, 1.43, 0.401) \
-  X(4, 2, 2, 2, 6, 1, 3.04, 0.0408, 0.251, 0.94, 2.04, 0.684) \
-  X(8, 4, 2, 4, 3, 1, 0, 6.27, 0.64, 1.14, 6.48, 0.311) \
-  X(4, 2, 2, 2, 4, 1, 2.79, 0.0506, 0.273, 0.871, 2.09, 0.654) \
-  X(2, 2, 2, 2, 6, 1, 2.99, 0.017, 0.175, 0.955, 1.75, 0.746) \
-  X(2, 1, 1, 4, 6, 1, 2.69, 0.182, 0.144, 0.901, 2, 0.634)
+  X(4, 4, 2, 2, 3, 1, 3.74, 0, 0.401, 0.793, 2.26, 0.494) \
+  X(7, 4, 2, 2, 2, 1, 6.32, 0, 0.858, 0.617, 1.38, 0.403) \
+  X(4, 2, 2, 2, 6, 1, 3.1, 0, 0.25, 0.934, 2.09, 0.681) \
+  X(8, 4, 2, 4, 3, 1, 0, 6.2, 0.703, 1.02, 7.27, 0.265) \
+  X(2, 2, 2, 2, 6, 1, 3.01, 0, 0.174, 0.942, 1.78, 0.754) \
+  X(2, 1, 1, 4, 6, 1, 2.72, 0.185, 0.143, 0.895, 1.99, 0.654)
 #define MX_TILES_16(X) \
   X(4, 4, 4, 2, 3, 1, 0.66, 3.72, 1.21, 1.08, 4.44, 0.407) \
   X(3, 4, 4, 2, 3, 1, 1.99, 3.32, 0.989, 1.01, 2.05, 0.43) \

@@ -187,7 +187,8 @@ def test_product_larger(ctx, M, N, K, act):
 @pytest.mark.parametrize("M,N,K", [(1, 4096, 4096), (1, 11008, 4096), (16, 22016, 8192), (32, 4096, 11008), (32, 22016, 8192), (64, 4096, 4096), (64, 11008, 4096), (64, 22016, 8192),
                                    (96, 5003, 3020), (128, 5120, 13824), (200, 9216, 9216), (333, 5003, 3020), (512, 13824, 5120), (768, 22016, 1024), (1024, 4096, 4096),
                                    (2048, 13824, 1280), (2048, 22016, 640), (1500, 1000, 900), (20, 11000, 640), (24, 5120, 640),
-                                   (700, 18432, 640), (700, 18421, 1250), (1490, 13824, 4096), (512, 22016, 4096), (4, 5120, 384), (512, 11000, 512), (250, 22016, 384)])
+                                   (700, 18432, 640), (700, 18421, 1250), (1490, 13824, 4096), (512, 22016, 4096), (4, 5120, 384), (512, 11000, 512), (250, 22016, 384), (1, 1000, 4096), (2, 18432, 4000), (8, 22016, 640),
+                                   (1, 4096, 11008)])
 def test_product_of_layer_sizes(ctx, M, N, K, act):
     """Every kernel's own range of sizes; the 64-bit product is made on the device from the values read back (which other tests pin)."""
     gen = torch.Generator("cuda").manual_seed(M + N + K)
