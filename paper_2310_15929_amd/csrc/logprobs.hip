@@ -127,8 +127,15 @@ __device__ __forceinline__ void place_candidates(const unsigned long long* list,
   }
 }
 __device__ __forceinline__ void answer_place(const LpOut& o, long long row, int place, unsigned long long k, float m, float s) {
-  o.top_ids[row * o.top + place] = s != s ? -1 : (int32_t)~(uint32_t)k;
-  o.top_logprobs[row * o.top + place] = s != s ? s : log_prob(key_value((uint32_t)(k >> 32)), m, s);
+  o.top_ids[row * o.top + place] = (int32_t)~(uint32_t)k;
+  o.top_logprobs[row * o.top + place] = log_prob(key_value((uint32_t)(k >> 32)), m, s);
+}
+// a row with a NaN or an infinite logit: none of its values is looked at (a NaN has no place in the order: one with its sign set is below minus infinity)
+__device__ __forceinline__ void answer_no_places(const LpOut& o, long long row) {
+  for (int i = threadIdx.x; i < o.top; i += NT) {
+    o.top_ids[row * o.top + i] = -1;
+    o.top_logprobs[row * o.top + i] = __builtin_nanf("");
+  }
 }
 
 // One wave with C keys a lane: the largest 32-bit pattern that at least `top` of the keys reach, or one below it that at most half as many again and SLACK more do
@@ -294,6 +301,14 @@ __global__ void __launch_bounds__(NT) k_lp_row(const LpOut o, unsigned pieces, u
     else answer_row(o, row, id, x_id, row_m, s, t);
   }
   if (!o.top) return;
+  if (s != s) {  // (the same for all threads)
+    if constexpr (PARTS) {
+      for (int i = tid; i < o.top; i += NT) part_top[(row * pieces + piece) * o.top + i] = 0;
+    } else {
+      answer_no_places(o, row);
+    }
+    return;
+  }
   const uint32_t from_key = s_from;
   // the threads that reach T, in any order; all threads look at those threads' units
   if (any && order_key(m) >= from_key) s_key[atomicAdd(&s_threads, 1)] = tid;
@@ -386,6 +401,10 @@ __global__ void __launch_bounds__(NT) k_lp_join(const LpOut o, unsigned pieces, 
   const float s = wave_sum(some ? p.s * f : 0.f), t = wave_sum(some ? f * __builtin_fmaf(p.s, __builtin_fmaxf(d, -128.f), p.t) : 0.f);
   if (tid == 0) answer_row(o, row, id, x_id, m, s, t);
   if (!o.top) return;
+  if (s != s) {
+    answer_no_places(o, row);
+    return;
+  }
   // A key that at least `top` alternatives reach: the lists are in order, and of their j-th (j pieces >= top) the q-th largest (q j >= top) is reached by j of q
   // lists each (0: no value)
   const unsigned qth = (o.top + jth - 1) / jth;

@@ -495,6 +495,28 @@ def test_logprobs_of_masked_rows(ctx, V):
         _assert_logprobs(ctx, x.cuda(), [t - 1 if 0 < t < V else t for t in tokens], 1, f"{V} {dtype}")
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("R,V", [(1, 7), (3, 40), (2, 5000), (1100, 3000), (3, 70000), (2, 140000)])
+def test_logprobs_of_rows_of_negative_nan(ctx, R, V, dtype):
+    """A NaN of either sign makes the row NaN and all its ids -1, however few other values there are: outputs that held something else before."""
+    bits = {"f16": -0x200, "bf16": -0x40, "f32": -0x400000}[dtype]   # the quiet NaN with the sign set
+    for finite in (0, 1, 3, V - 1):
+        x = torch.full((R, V), bits, dtype=torch.int32 if dtype == "f32" else torch.int16).view(TORCH[dtype]).clone()
+        x[0, V - finite:] = torch.arange(finite).to(TORCH[dtype]) / 8
+        assert torch.isnan(x[:, 0]).all() and torch.signbit(x[:, 0]).all()
+        for top in {1, min(5, V), min(32, V)}:
+            code = {"f16": esp.F16, "bf16": esp.BF16, "f32": esp.F32}[dtype]
+            nbytes = esp.token_logprobs_workspace(R, V, code, top)
+            ws = torch.zeros(nbytes + 1, dtype=torch.uint8, device="cuda")
+            dev, tok = x.cuda(), torch.full((R,), V - 1, device="cuda")
+            ids, tops, lp, ent = (torch.full(shape, 777, dtype=t, device="cuda")
+                                  for shape, t in (((R, top), torch.int32), ((R, top), torch.float32), ((R,), torch.float32), ((R,), torch.float32)))
+            ctx._sync_stream()
+            assert ctx._lib.esparse_token_logprobs(ctx._h, dev.data_ptr(), R, V, V, code, tok.data_ptr(), top, lp.data_ptr(), ent.data_ptr(), ids.data_ptr(), tops.data_ptr(),
+                                                   ws.data_ptr(), nbytes) == 0
+            assert (ids == -1).all() and torch.isnan(tops).all() and torch.isnan(lp).all() and torch.isnan(ent).all(), (finite, top)
+
+
 def test_logprobs_far_from_zero(ctx):
     """A common offset of the logits takes no precision beyond that of the logits themselves."""
     rng = _rng("far")
