@@ -74,11 +74,12 @@ __device__ __forceinline__ float2 row_inverse(double own, double* buf, long long
 __device__ __forceinline__ float times(float p, float2 by) {
   return __builtin_copysignf(__builtin_fmaf(p, by.x, p * by.y), p);  // (-0 (hi + lo) with lo < 0 would be +0)
 }
-// v = times(p, by) to an odd last bit where it is not exact: rounding that again to 8 or 4 bits gives what rounding the exact value would
+// v = times(p, by) to an odd last bit where it is not exact: rounding that again to 8 or 4 bits gives what rounding the exact value would.  The factor is
+// right to 2^-47, so a value as near to v as that is taken to be v: rows of one magnitude, and others with a rational norm, put results right on a middle
 __device__ __forceinline__ float to_odd(float v, float p, float2 by) {
   const float rest = __builtin_fmaf(p, by.y, __builtin_fmaf(p, by.x, -v));
   const uint32_t b = __builtin_bit_cast(uint32_t, v);
-  if ((b & 1u) || (b << 1) == 0u || !(rest < 0.f || rest > 0.f)) return v;
+  if ((b & 1u) || (b << 1) == 0u || !(__builtin_fabsf(rest) > 0x1p-44f * __builtin_fabsf(v))) return v;
   return __builtin_bit_cast(float, (rest > 0.f) == ((int)b >= 0) ? b + 1u : b - 1u);
 }
 

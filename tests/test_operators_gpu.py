@@ -345,6 +345,31 @@ def test_norm_to_mx_rounds_once(ctx, R, K, fmt, dtype):
 
 
 @pytest.mark.parametrize("fmt", ["fp4", "fp8"])
+@pytest.mark.parametrize("K", [64, 512, 4096, 33024])
+def test_norm_right_on_the_middle_of_two_codes(ctx, K, fmt):
+    """Rows whose norm is rational and no power of two: y is exact there, and the weights put it on the middles between codes, beside them, and on powers of two."""
+    rng = _rng("norm middle", K)
+    mid = np.array([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 1.0, 2.0, 4.0, 6.0, 1.0078125, 0.99609375, 2.515625, 2.484375])
+    if fmt == "fp8":
+        mid = np.concatenate([mid, np.array([(2 * m + 1) / 16 * 2.0 ** e for m in range(8, 16) for e in (-2, 0, 3)])])
+    w = torch.from_numpy(mid[rng.integers(0, len(mid), K)] * np.where(rng.random(K) < 0.5, -1.0, 1.0)).bfloat16()
+    sign = np.where(rng.random((40, K)) < 0.5, -1.0, 1.0)
+    size = np.array([1.0, 3, 5, 7, 11, 13, 49, 77, 101, 127])[np.arange(40) % 10] * np.array([1.0, 0.125, 2.0 ** 12, 2.0 ** -13])[np.arange(40) // 10]
+    x = torch.from_numpy(sign * size[:, None]).bfloat16()
+    want = orc.rms_norm(x.double().numpy(), w.double().numpy(), 0.0)
+    assert np.array_equal(np.abs(want), np.broadcast_to(np.abs(w.double().numpy()), want.shape))   # exact in 64 bits
+    _assert_mx(ctx.rms_norm(x.cuda(), w.cuda(), 0.0, fmt=FMT[fmt])[0], want, FMT[fmt])
+    # several magnitudes: of 64 channels 15 are 3, one is 21: a mean square of 9 (15 + 49) / 64 = 9
+    pattern = np.zeros(64)
+    pattern[3::4] = 3.0
+    pattern[7] = 21.0
+    x = torch.from_numpy(np.tile(pattern, K // 64)[None] * sign[:3]).bfloat16()
+    want = orc.rms_norm(x.double().numpy(), w.double().numpy(), 0.0)
+    assert np.array_equal(want, x.double().numpy() / 3 * w.double().numpy())
+    _assert_mx(ctx.rms_norm(x.cuda(), w.cuda(), 0.0, fmt=FMT[fmt])[0], want, FMT[fmt])
+
+
+@pytest.mark.parametrize("fmt", ["fp4", "fp8"])
 def test_norm_takes_eps_in_64_bits(ctx, fmt):
     """Rows whose mean square is of the size of eps, which is no 32-bit number."""
     rng, R, K = _rng("norm eps"), 200, 4096
