@@ -51,9 +51,14 @@ __device__ __forceinline__ double squares(const uint32_t (&v)[4], double s) {
   return s;
 }
 
-// 1 / sqrt(mean of the squares + eps) from the threads' sums, as the sum of two floats; every thread of the row gets it.  `buf`: one double per wave
+// mean of the squares + eps, and 1 / its root as hi + lo (right to 2^-47)
+struct RowInverse {
+  float hi, lo;
+  double mean;
+};
+// ... from the threads' sums; every thread of the row gets it.  `buf`: one double per wave
 template <int NT>
-__device__ __forceinline__ float2 row_inverse(double own, double* buf, long long K, double eps) {
+__device__ __forceinline__ RowInverse row_inverse(double own, double* buf, long long K, double eps) {
   double v = own;
 #pragma unroll
   for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
@@ -65,29 +70,30 @@ __device__ __forceinline__ float2 row_inverse(double own, double* buf, long long
 #pragma unroll
     for (int i = 0; i < NT / 64; i++) v += buf[i];
   }
-  const double inv = 1. / __builtin_sqrt(v / (double)K + eps);
+  const double mean = v / (double)K + eps, inv = 1. / __builtin_sqrt(mean);
   const float hi = (float)inv;
-  return float2{hi, __builtin_isfinite(hi) ? (float)(inv - (double)hi) : 0.f};
+  return RowInverse{hi, __builtin_isfinite(hi) ? (float)(inv - (double)hi) : 0.f, mean};
 }
 
 // p (hi + lo), rounded once
-__device__ __forceinline__ float times(float p, float2 by) {
-  return __builtin_copysignf(__builtin_fmaf(p, by.x, p * by.y), p);  // (-0 (hi + lo) with lo < 0 would be +0)
+__device__ __forceinline__ float times(float p, const RowInverse& by) {
+  return __builtin_copysignf(__builtin_fmaf(p, by.hi, p * by.lo), p);  // (-0 (hi + lo) with lo < 0 would be +0)
 }
-// v = times(p, by) to an odd last bit where it is not exact: rounding that again to 8 or 4 bits gives what rounding the exact value would.  The factor is
-// right to 2^-47, so a value as near to v as that is taken to be v: rows of one magnitude, and others with a rational norm, put results right on a middle
-__device__ __forceinline__ float to_odd(float v, float p, float2 by) {
-  const float rest = __builtin_fmaf(p, by.y, __builtin_fmaf(p, by.x, -v));
+// v = times(p, by), not 0, to an odd last bit where it is not exact: rounding that again to 8 or 4 bits gives what rounding the exact value would.  Which side of v the
+// exact value is on, or whether it is v (rows of one magnitude, and others with a rational norm, put results right on the middle of two codes), the squares tell
+// without a root: those of p and v are exact in 64 bits
+__device__ __forceinline__ float to_odd(float v, float p, const RowInverse& by) {
+  const double rest = __builtin_fma(-(double)v * (double)v, by.mean, (double)p * (double)p);
   const uint32_t b = __builtin_bit_cast(uint32_t, v);
-  if ((b & 1u) || (b << 1) == 0u || !(__builtin_fabsf(rest) > 0x1p-44f * __builtin_fabsf(v))) return v;
-  return __builtin_bit_cast(float, (rest > 0.f) == ((int)b >= 0) ? b + 1u : b - 1u);
+  if ((b & 1u) || !(rest < 0. || rest > 0.)) return v;
+  return __builtin_bit_cast(float, rest > 0. ? b + 1u : b - 1u);
 }
 
 // output of one piece of eight channels (a product h w of two 16-bit numbers is exact in fp32: y = h w / sqrt(..) is rounded once).  Lanes of pieces
 // behind the row's last channel take part (zeros in the padding of a microscaled row); `chunk` differs by one between neighbouring lanes and starts at a
 // multiple of 16
 template <int DT, int OUT>
-__device__ __forceinline__ void norm_out(const NormArgs& a, long long row, unsigned chunk, const uint32_t (&h)[4], const uint32_t (&w)[4], float2 inv) {
+__device__ __forceinline__ void norm_out(const NormArgs& a, long long row, unsigned chunk, const uint32_t (&h)[4], const uint32_t (&w)[4], const RowInverse& inv) {
   float v[8], p[8];
 #pragma unroll
   for (int i = 0; i < 4; i++) {
@@ -98,16 +104,29 @@ __device__ __forceinline__ void norm_out(const NormArgs& a, long long row, unsig
   for (int i = 0; i < 8; i++) v[i] = times(p[i], inv);
   if constexpr (OUT != OUT_16) {
     // The middle between two codes, and a power of two, has at most five of the 24 significant bits: only a value with the others zero can have been
-    // rounded onto one (one in 2^19, so that the test costs less than rounding all of them to odd: 2048 x 8192 to 8 bits 26.6 us against 28.2)
+    // rounded onto one (one in 2^19)
     uint32_t low = ~0u;
 #pragma unroll
     for (int i = 0; i < 8; i++) {
       const uint32_t b = __builtin_bit_cast(uint32_t, v[i]) << 13;
       low = b < low ? b : low;
     }
-    if (low == 0u) {
+    if (low == 0u) {  // (those of the eight, one after the other: all eight in a row are so much code that 2048 x 4096 to 8 bits takes 15.1 us instead of 13.9)
+      unsigned todo = 0;
 #pragma unroll
-      for (int i = 0; i < 8; i++) v[i] = to_odd(v[i], p[i], inv);
+      for (int i = 0; i < 8; i++) todo |= (__builtin_bit_cast(uint32_t, v[i]) << 13 == 0u && v[i] != 0.f ? 1u : 0u) << i;
+      for (; todo; todo &= todo - 1u) {
+        const unsigned at = (unsigned)__builtin_ctz(todo);
+        float one = v[0], of = p[0];
+#pragma unroll
+        for (unsigned i = 1; i < 8; i++) {
+          one = at == i ? v[i] : one;
+          of = at == i ? p[i] : of;
+        }
+        one = to_odd(one, of, inv);
+#pragma unroll
+        for (unsigned i = 0; i < 8; i++) v[i] = at == i ? one : v[i];
+      }
     }
   }
   if constexpr (OUT == OUT_16) {
@@ -152,7 +171,7 @@ __global__ void __launch_bounds__(NT < 256 ? 256 : NT) k_rms_norm(const NormArgs
     if (a.sum_out) store_8(a.sum_out + row * a.K + (long long)(j * NT + t) * 8, a.K - (long long)(j * NT + t) * 8, h[j]);
     s = squares<DT>(h[j], s);
   }
-  const float2 inv = row_inverse<NT>(s, buf, a.K, a.eps);
+  const RowInverse inv = row_inverse<NT>(s, buf, a.K, a.eps);
 #pragma unroll
   for (int j = 0; j < C; j++) norm_out<DT, OUT>(a, row, j * NT + t, h[j], w[j], inv);
 }
@@ -176,7 +195,7 @@ __global__ void __launch_bounds__(1024) k_rms_norm_long(const NormArgs a) {
     if (a.sum_out) store_8(a.sum_out + row * a.K + at, left, h);
     s = squares<DT>(h, s);
   }
-  const float2 inv = row_inverse<1024>(s, buf, a.K, a.eps);
+  const RowInverse inv = row_inverse<1024>(s, buf, a.K, a.eps);
   for (unsigned c0 = 0; c0 < chunks; c0 += 1024) {
     const unsigned c = c0 + t;
     const long long at = (long long)c * 8, left = a.K - at;

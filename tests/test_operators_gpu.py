@@ -370,6 +370,21 @@ def test_norm_right_on_the_middle_of_two_codes(ctx, K, fmt):
 
 
 @pytest.mark.parametrize("fmt", ["fp4", "fp8"])
+@pytest.mark.parametrize("K", [64, 520, 4096, 33000])
+def test_norm_beside_the_middle_of_two_codes(ctx, K, fmt):
+    """Rows of ones with an eps that takes y as little as 2^-51 below weights that are on middles and powers of two; of 3 with an eps for the same."""
+    rng = _rng("norm beside", K)
+    mid = np.array([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 1.0, 2.0, 4.0, 6.0] + ([(2 * m + 1) / 16 for m in range(8, 16)] if fmt == "fp8" else []))
+    w = torch.from_numpy(mid[rng.integers(0, len(mid), K)] * np.where(rng.random(K) < 0.5, -1.0, 1.0)).bfloat16()
+    for size in (1.0, 3.0):
+        x = torch.from_numpy(size * np.where(rng.random((5, K)) < 0.5, -1.0, 1.0)).bfloat16()
+        for bits in (30, 40, 44, 47, 50):
+            want = orc.rms_norm(x.double().numpy(), w.double().numpy(), size * size * 2.0 ** -bits)
+            assert (np.abs(want) < np.abs(w.double().numpy())).all()
+            _assert_mx(ctx.rms_norm(x.cuda(), w.cuda(), size * size * 2.0 ** -bits, fmt=FMT[fmt])[0], want, FMT[fmt], f"{size} {bits}")
+
+
+@pytest.mark.parametrize("fmt", ["fp4", "fp8"])
 def test_norm_takes_eps_in_64_bits(ctx, fmt):
     """Rows whose mean square is of the size of eps, which is no 32-bit number."""
     rng, R, K = _rng("norm eps"), 200, 4096
