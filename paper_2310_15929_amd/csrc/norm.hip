@@ -51,12 +51,15 @@ __device__ __forceinline__ double squares(const uint32_t (&v)[4], double s) {
   return s;
 }
 
-// mean of the squares + eps, and 1 / its root as hi + lo (right to 2^-47)
+// mean of the squares + eps, times 2^(2 up), and 1 / its root as hi + lo (right to 2^-47)
 struct RowInverse {
   float hi, lo;
+  int up;
   double mean;
 };
-// ... from the threads' sums; every thread of the row gets it.  `buf`: one double per wave
+// ... from the threads' sums; every thread of the row gets it.  `buf`: one double per wave.  hi is from 1 to 2, or 0, infinite or NaN with up = 0: rows of bf16
+// numbers (and an eps of any size) have inverses from far below to 2^149, and h weight may pass fp32 where y does not, so that h takes the factor 2^up before the
+// weight (in all rows: a test for those that need it costs as much, 0.1 us a launch)
 template <int NT>
 __device__ __forceinline__ RowInverse row_inverse(double own, double* buf, long long K, double eps) {
   double v = own;
@@ -70,9 +73,17 @@ __device__ __forceinline__ RowInverse row_inverse(double own, double* buf, long 
 #pragma unroll
     for (int i = 0; i < NT / 64; i++) v += buf[i];
   }
-  const double mean = v / (double)K + eps, inv = 1. / __builtin_sqrt(mean);
+  const double mean = v / (double)K + eps;
+  double inv = 1. / __builtin_sqrt(mean);
+  const unsigned long long bits = __builtin_bit_cast(unsigned long long, inv);
+  const unsigned top = (unsigned)(bits >> 32), exponent = top >> 20;
+  int up = 0;
+  if (exponent - 1u < 2046u) {
+    up = (int)exponent - 1023;
+    inv = __builtin_bit_cast(double, (unsigned long long)((top & 0xfffffu) | 0x3ff00000u) << 32 | (unsigned)bits);
+  }
   const float hi = (float)inv;
-  return RowInverse{hi, __builtin_isfinite(hi) ? (float)(inv - (double)hi) : 0.f, mean};
+  return RowInverse{hi, __builtin_isfinite(hi) ? (float)(inv - (double)hi) : 0.f, up, __builtin_ldexp(mean, 2 * up)};
 }
 
 // p (hi + lo), rounded once
@@ -89,7 +100,8 @@ __device__ __forceinline__ float to_odd(float v, float p, const RowInverse& by) 
   return __builtin_bit_cast(float, rest > 0. ? b + 1u : b - 1u);
 }
 
-// output of one piece of eight channels (a product h w of two 16-bit numbers is exact in fp32: y = h w / sqrt(..) is rounded once).  Lanes of pieces
+// output of one piece of eight channels (a product of two 16-bit numbers and a power of two is exact within fp32: y = h w / sqrt(..) is
+// rounded once).  Lanes of pieces
 // behind the row's last channel take part (zeros in the padding of a microscaled row); `chunk` differs by one between neighbouring lanes and starts at a
 // multiple of 16
 template <int DT, int OUT>
@@ -97,8 +109,8 @@ __device__ __forceinline__ void norm_out(const NormArgs& a, long long row, unsig
   float v[8], p[8];
 #pragma unroll
   for (int i = 0; i < 4; i++) {
-    p[2 * i] = esp_to_float<DT>((uint16_t)h[i]) * esp_to_float<DT>((uint16_t)w[i]);
-    p[2 * i + 1] = esp_to_float<DT>((uint16_t)(h[i] >> 16)) * esp_to_float<DT>((uint16_t)(w[i] >> 16));
+    p[2 * i] = __builtin_ldexpf(esp_to_float<DT>((uint16_t)h[i]), inv.up) * esp_to_float<DT>((uint16_t)w[i]);
+    p[2 * i + 1] = __builtin_ldexpf(esp_to_float<DT>((uint16_t)(h[i] >> 16)), inv.up) * esp_to_float<DT>((uint16_t)(w[i] >> 16));
   }
 #pragma unroll
   for (int i = 0; i < 8; i++) v[i] = times(p[i], inv);

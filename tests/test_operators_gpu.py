@@ -421,6 +421,42 @@ def test_norm_of_rows_whose_squares_pass_32_bits(ctx, fmt):
         assert (np.abs(_np(y) - want) <= _norm_bound(want, 0, HALF[torch.bfloat16], TINY[torch.bfloat16])).all()
 
 
+@pytest.mark.parametrize("fmt", [None, "fp4", "fp8"])
+@pytest.mark.parametrize("K", [64, 520, 4100, 8200, 33000])
+def test_norm_of_rows_whose_inverse_passes_32_bits(ctx, K, fmt):
+    """Rows from the smallest bf16 numbers to the largest, eps 0 or of their size: 1 / rms up to 2^133, down to 2^-127, and h weight beyond fp32 in either direction."""
+    rng = _rng("norm inverse", K)
+    for row_exp, w_exp, eps in ((-133, 0, 0.0), (-129, 0, 0.0), (-127, 3, 2.0 ** -260), (-100, -30, 0.0), (-61, -90, 0.0), (-59, 0, 0.0), (59, 0, 0.0), (61, 60, 0.0), (110, 100, 0.0), (125, 0, 0.0), (125, 2, 2.0 ** 300)):
+        x = torch.from_numpy(rng.integers(1, 8, (3, K)) * np.where(rng.random((3, K)) < 0.5, -1.0, 1.0) * 2.0 ** (row_exp - (0 if row_exp < 0 else 2))).bfloat16()
+        w = torch.from_numpy((1 + rng.random(K)) * 2.0 ** w_exp).bfloat16()
+        assert (x != 0).all() and torch.isfinite(x).all()
+        want = orc.rms_norm(x.double().numpy(), w.double().numpy(), eps)
+        y, _ = ctx.rms_norm(x.cuda(), w.cuda(), eps, fmt=fmt and FMT[fmt])
+        if fmt:
+            _assert_mx(y, want, FMT[fmt], f"{row_exp} {w_exp}")
+        else:  # one rounding of a value that is right to 2^-23
+            bound = np.abs(want) * (HALF[torch.bfloat16] + 2.0 ** -23) + TINY[torch.bfloat16]
+            assert (np.abs(_np(y) - want) <= bound).all(), (row_exp, w_exp)
+    # f16 rows with an eps that takes y below every f16 number, but not below every scale
+    x = torch.from_numpy(rng.standard_normal((2, K))).half()
+    w = torch.from_numpy(1 + rng.random(K)).half()
+    y, _ = ctx.rms_norm(x.cuda(), w.cuda(), 2.0 ** 140, fmt=fmt and FMT[fmt])
+    if fmt:
+        _assert_mx(y, orc.rms_norm(x.double().numpy(), w.double().numpy(), 2.0 ** 140), FMT[fmt])
+    else:
+        assert (y == 0).all()
+    # one value that is no zero among many: 1 / rms above it by the root of K
+    x = torch.zeros(2, K, dtype=torch.bfloat16)
+    x[0, K // 2], x[1, 1] = 2.0 ** -133, -2.0 ** 127
+    w = torch.full((K,), 1.5, dtype=torch.bfloat16)
+    want = orc.rms_norm(x.double().numpy(), w.double().numpy(), 0.0)
+    y, _ = ctx.rms_norm(x.cuda(), w.cuda(), 0.0, fmt=fmt and FMT[fmt])
+    if fmt:
+        _assert_mx(y, want, FMT[fmt])
+    else:
+        assert (np.abs(_np(y) - want) <= np.abs(want) * (HALF[torch.bfloat16] + 2.0 ** -23)).all()
+
+
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
 @pytest.mark.parametrize("fmt", ["fp4", "fp8"])
 @pytest.mark.parametrize("R,K", [(1, 1), (5, 33), (3, 512), (70, 515), (20, 4096), (3, 4097), (2, 13824), (2, 33000)])
