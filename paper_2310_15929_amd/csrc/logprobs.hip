@@ -6,7 +6,9 @@
 // hold one.  Where there are few rows a row is cut into pieces, a workgroup each; a second launch joins them.
 //   Alternatives: T = the k-th largest of the threads' own maxima is a lower bound of the k-th largest value, so only threads whose
 // maximum reaches T (about k of them) read their values a second time, and only values of at least T are looked at: little more than k, unless many
-// are equal: where their list overflows, k rounds of a search for the next in order take its place.  Order: larger value first, then lower index.
+// are equal, as where a mask leaves fewer values than alternatives.  There the list overflows: the values above T are listed, then the first ones that are T
+// itself, in order (8 x 131072 with 20 alternatives where a mask leaves 5 values: 25 us, 2048 rows of them 261; with k rounds of a search for the next in order
+// 82 and 2250).  If a few threads hold so many values above T that this list overflows too, those rounds take its place.  Order: larger value first, then lower index.
 //   Measured, cold: 2048 x 131072 16-bit 104 us (5.2 TB/s; 20 alternatives 143), 2048 x 32000 30 us (4.4 TB/s), 555 x 50021 32-bit 27.4 us (4.1 TB/s: two
 // pieces a row, 4.3 workgroups a compute unit; 5 alternatives 31.9), 8 x 131072 6.2 us, 1 x 32000 5.6 us (20 alternatives 10.6).
 #include <hip/hip_runtime.h>
@@ -314,24 +316,76 @@ __global__ void __launch_bounds__(NT) k_lp_row(const LpOut o, unsigned pieces, u
   if (any && order_key(m) >= from_key) s_key[atomicAdd(&s_threads, 1)] = tid;
   __syncthreads();
   const unsigned turns = (end - first + NT - 1) / NT, looks = (unsigned)s_threads * turns;
-  for (unsigned q = tid; q < looks; q += NT) {
-    const unsigned w = first + (q % turns) * NT + s_key[q / turns];
-    if (w >= end) continue;
-    Unit r;
-    r.load(x, (long long)w * E, V);
+  // the values of at least `least` of those threads; where there are too many for the list, a second time those above `tie`
+  uint32_t least = from_key, tie = 0;
+  int n = 0;
+  for (bool again = false;; again = true) {
+    int slot = 0;
+    for (unsigned q = tid; q < looks && slot < LIST; q += NT) {
+      const unsigned w = first + (q % turns) * NT + s_key[q / turns];
+      if (w >= end) continue;
+      Unit r;
+      r.load(x, (long long)w * E, V);
 #pragma unroll
-    for (int i = 0; i < E; i++) {
-      const long long at = (long long)w * E + i;
-      const float y = r.value(i);
-      if (at < V && order_key(y) >= from_key) {
-        const int slot = atomicAdd(&s_n, 1);
-        if (slot < LIST) s_list[slot] = rank_key(y, (uint32_t)at);
+      for (int i = 0; i < E; i++) {
+        const long long at = (long long)w * E + i;
+        const float y = r.value(i);
+        if (at < V && order_key(y) >= least) {
+          slot = atomicAdd(&s_n, 1);
+          if (slot < LIST) s_list[slot] = rank_key(y, (uint32_t)at);
+        }
       }
     }
+    __syncthreads();
+    n = s_n;
+    if (__builtin_expect(n <= LIST || again, 1)) break;
+    // the lowest of the maxima that reach T.  At least `top` threads have it or more, so the values above it and the first equal ones are enough
+    tie = any && order_key(m) >= from_key ? order_key(m) : ~0u;
+#pragma unroll
+    for (int w = 32; w; w >>= 1) {
+      const uint32_t other = __shfl_xor(tie, w);
+      tie = other < tie ? other : tie;
+    }
+    if ((tid & 63u) == 0) s_next[wave] = tie;
+    __syncthreads();
+    tie = (uint32_t)s_next[0];
+#pragma unroll
+    for (int i = 1; i < NW; i++) tie = (uint32_t)s_next[i] < tie ? (uint32_t)s_next[i] : tie;
+    least = tie + 1u;  // (no maximum is NaN: there is a key above it)
+    if (tid == 0) s_n = 0;
+    __syncthreads();
   }
-  __syncthreads();
-  int n = s_n;
-  if (n > LIST) {  // many equal values: the next in order, again and again
+  if (__builtin_expect(tie != 0u && n < o.top, 0)) {  // the first values that are `tie`, NT units at a time: a thread's are behind those of the threads before it
+    for (unsigned w0 = first; n < o.top && w0 < end; w0 += NT) {
+      Unit r;
+      unsigned equal = 0;
+      const unsigned w = w0 + tid;
+      if (w < end) {
+        r.load(x, (long long)w * E, V);
+#pragma unroll
+        for (int i = 0; i < E; i++) equal |= (unsigned)((long long)w * E + i < V && order_key(r.value(i)) == tie) << i;
+      }
+      int place = __builtin_popcount(equal);
+#pragma unroll
+      for (int d = 1; d < 64; d <<= 1) {
+        const int lower = __shfl_up(place, d);
+        place += (int)(tid & 63u) >= d ? lower : 0;
+      }
+      if ((tid & 63u) == 63u) s_next[wave] = (unsigned long long)place;
+      place += n - __builtin_popcount(equal);
+      __syncthreads();
+#pragma unroll
+      for (unsigned i = 0; i < NW; i++) {
+        const int count = (int)s_next[i];
+        place += i < wave ? count : 0;
+        n += count;
+      }
+      for (; equal && place < o.top; equal &= equal - 1u) s_list[place++] = (unsigned long long)tie << 32 | (uint32_t)~(w * E + (unsigned)__builtin_ctz(equal));
+      __syncthreads();
+    }
+    n = n < o.top ? n : o.top;
+  }
+  if (__builtin_expect(n > LIST, 0)) {  // the next in order, again and again
     __syncthreads();
     unsigned long long before = ~0ull;
     for (int k = 0; k < o.top; k++) {

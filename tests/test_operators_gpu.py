@@ -593,6 +593,31 @@ def test_logprobs_of_rows_of_negative_nan(ctx, R, V, dtype):
             assert (ids == -1).all() and torch.isnan(tops).all() and torch.isnan(lp).all() and torch.isnan(ent).all(), (finite, top)
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("R,V", [(13, 300), (13, 5000), (13, 16376), (13, 70001), (1050, 9001), (13, 140000)])
+def test_logprobs_of_rows_with_many_equal_values(ctx, R, V, dtype):
+    """Rows in which a mask leaves none to 40 values (minus infinity, the type's lowest number, a large negative one), rows of two and three values, ties between the alternatives,
+    and a few threads' values above all others: more of them than a workgroup lists."""
+    rng = _rng("equal", R, V)
+    low = {"f16": -65504.0, "bf16": float(torch.finfo(torch.bfloat16).min), "f32": float(torch.finfo(torch.float32).min)}[dtype]
+    x = np.full((13, V), -math.inf)
+    for r, (fill, count) in enumerate(((-math.inf, 1), (-math.inf, 5), (-math.inf, 19), (-math.inf, 40), (low, 0), (low, 5), (low, 33), (-10000.0, 3), (-10000.0, 21))):
+        x[r] = fill
+        x[r, rng.permutation(V)[:count]] = rng.standard_normal(count) * 3
+    x[9] = np.where(rng.random(V) < 0.3, 1.0, 0.5)                                          # thousands tie for the first places
+    x[10] = np.where(rng.random(V) < 12 / V, 2.0, np.where(rng.random(V) < 0.4, -1.0, -3.0))  # a dozen first, then ties
+    x[11] = np.where(np.arange(V) // (4 if dtype == "f32" else 8) % 256 < 31, rng.standard_normal(V), -5.0)   # 31 threads of 256 hold all but one value
+    x[12] = np.where(np.arange(V) < V - 7, -2.5, 1.0)                                       # the last ones first, then from the start
+    x = torch.from_numpy(x).to(TORCH[dtype])
+    x = torch.cat((x, x[torch.arange(R - 13) % 13])).cuda()
+    tokens = torch.arange(R, device="cuda") * 7919 % V
+    for top in (1, 5, 20, 32):
+        _assert_logprobs(ctx, x[:13], [int(t) for t in tokens[:13]], top, f"{dtype} {top}")
+        if R > 13:   # one workgroup a row
+            few, many = ctx.token_logprobs(x[:13], tokens[:13], top=top), ctx.token_logprobs(x, tokens, top=top)
+            assert all(torch.equal(many.top_ids[i:i + 13], few.top_ids) for i in range(0, R - 13, 13))
+
+
 def test_logprobs_far_from_zero(ctx):
     """A common offset of the logits takes no precision beyond that of the logits themselves."""
     rng = _rng("far")
