@@ -336,7 +336,8 @@ int esparse_rms_norm(esparse_ctx* ctx, const void* x, long long ldx, const void*
  * logprob (with tokens) and entropy may be NULL; top = 0: no alternatives.  Logits of minus infinity have probability 0; a row that holds nothing else gives
  * logprob and alternatives of minus infinity and entropy 0.  A row with a NaN or plus infinity gives NaN throughout and ids of -1.
  * top <= ESPARSE_MAX_TOP and <= V, V <= ESPARSE_MAX_VOCABULARY.  workspace as above.  Outputs and workspace may not overlap each other or an input.  R = 0 is a no-op.  Does not synchronise.
- * Results depend neither on the values of other rows nor on chance (no floating-point atomics); the order of a row's sums follows from R, V and the type.
+ * Results depend neither on the values of other rows nor on chance (no floating-point atomics); the order of a row's sums follows from R, V, the type and whether
+ * alternatives are asked for (top > 0; how many makes no difference).
  * Errors: EINVAL, EUNSUPPORTED (dtype, V), EWORKSPACE, EHIP. */
 #define ESPARSE_MAX_TOP 32
 #define ESPARSE_MAX_VOCABULARY (1ll << 21)

@@ -652,6 +652,21 @@ def test_logprobs_do_not_depend_on_other_rows(ctx):
             assert torch.equal(a[::2], b[::2])
 
 
+@pytest.mark.parametrize("R,V,dtype", [(8, 131072, "bf16"), (1, 8192, "f16"), (1, 32000, "bf16"), (3, 70000, "f32"), (2000, 3000, "f16")])
+def test_logprobs_order_of_the_sums(ctx, R, V, dtype):
+    """How many alternatives are asked for does not change a row's sums; whether any are may, in the last bits."""
+    x = torch.from_numpy(_rng("order", R, V).standard_normal((R, V)) * 3).to(TORCH[dtype]).cuda()
+    tokens = torch.arange(R, device="cuda")
+    results = [ctx.token_logprobs(x, tokens, top=top) for top in (0, 1, 5, 32)]
+    for r in results[2:]:
+        assert torch.equal(r.logprob, results[1].logprob) and torch.equal(r.entropy, results[1].entropy)
+        assert torch.equal(r.top_ids[:, :1], results[1].top_ids) and torch.equal(r.top_logprobs[:, :1], results[1].top_logprobs)
+    _assert_logprobs(ctx, x[:8], list(range(min(R, 8))), 0)
+    # both are within the bound of test_logprobs for a row's sum of the exact value
+    s_err = 2.0 ** -21 + (128 + 2 * math.log2(V + 1)) * 2.0 ** -24
+    assert ((results[0].logprob - results[1].logprob).abs() <= 2 * (s_err + 4 * 2.0 ** -24 * (results[0].logprob.abs() + 32))).all()
+
+
 # ---- beyond 32 bits -----------------------------------------------------------------------------------
 def test_offsets_beyond_32_bits(ctx):
     """The last rows of matrices with more than 2^32 bytes and values are those of a call on these rows alone."""
