@@ -300,8 +300,9 @@ int esparse_mx_dequantize(esparse_ctx* ctx, const void* data, const void* scales
  * act says what X is:
  *   ESPARSE_MX_ACT_FP4, ESPARSE_MX_ACT_FP8  MX rows (X: data, x_scales: scales of the layout above; dtype and ldx are ignored): the scaled matrix instruction
  *   ESPARSE_MX_ACT_16  16-bit values (dtype f16 or bf16; ldx values from row to row, x_scales ignored): the weights alone are in 4 bits.  Their scaled numbers are
- *     brought to the type of X in registers (bf16: exact; f16: exact for scales from 2^-23 to 2^13, rounded and limited to f16 beyond) for the
- *     16-bit matrix instruction.
+ *     brought to the type of X in registers, as a conversion to that type gives them, for the 16-bit matrix instruction.  bf16: exact for scales up to 2^125.
+ *     f16: exact for scales from 2^-23 to 2^13; below, rounded to multiples of 2^-24; a weight beyond 65504 is infinite (and NaN opposite a 0 of X): such weights need
+ *     bf16 or MX activations.
  * workspace: DEVICE scratch of esparse_mx_gemm_workspace bytes (host only; may be 0), 256-byte aligned, overwritten.  aligned: 1 where X is 16-byte aligned and ldx a multiple of 8,
  * or X is MX; 0 otherwise (then 16-bit rows are copied into the workspace first, as they are for some K).  K and ldx: at most 2^22. M = 0 is a no-op.  A block of W or X with scale 255
  * makes the outputs it takes part in NaN.  Y and the workspace may not overlap an operand.  With ESPARSE_MX_ACT_FP8 the instruction adds the products of eight consecutive channels after it has cut each to a multiple

@@ -83,8 +83,8 @@ __device__ __forceinline__ floatx4_t mx_mfma(uint4 a, uint32_t as, const MxB<ACT
 // The scale of the widening conversions, from the low byte of e: they take its exponent alone (tested for all 256), with 0 for 2^-127 and 255 for NaN
 __device__ __forceinline__ float mx_widen_scale(uint32_t e) { return __builtin_bit_cast(float, e << 23); }
 
-// one 32-bit word of a weight unit (eight channels) as the A operand of the 16-bit instruction, times 2^(E - 127).  bf16: exact.  f16: rounded
-// where the scaled number is no f16 (below 2^-24 or beyond 65504)
+// one 32-bit word of a weight unit (eight channels) as the A operand of the 16-bit instruction, times 2^(E - 127).  bf16: exact up to the
+// type's largest number.  f16: rounded to even where the scaled number is none (no multiple of 2^-24), infinite beyond 65504
 template <int DT>
 __device__ __forceinline__ uint4 mx_widen(uint32_t w, float s) {
   uint4 r = {0u, 0u, 0u, 0u};

@@ -276,6 +276,45 @@ def test_product_with_wide_scales(ctx):
     _assert_product(ctx.mx_gemm(xt.cuda(), ctx.mx_pack(wq), dtype=torch.float32), xt.double().numpy(), w64, torch.float32, "16", "16")
 
 
+@pytest.mark.parametrize("act", ["f16", "bf16", "fp8", "fp4"])
+@pytest.mark.parametrize("M", [1, 16, 50, 200, 600])
+def test_product_of_every_code_and_scale(ctx, M, act):
+    """Weights of one number a row, all codes with all scales, times 1: in 16 bits the weight as a conversion to that type gives it (f16: exact for scales of 2^-23 to 2^13,
+    rounded to even below, infinite beyond 65504), with microscaled activations as fp32 holds it."""
+    K = 256
+    E = np.repeat(np.arange(255, dtype=np.uint8), 16)[:, None].repeat(K // 32, 1)
+    code = np.zeros((len(E), K), np.uint8)
+    code[np.arange(len(E)), np.arange(len(E)) * 37 % K] = np.tile(np.arange(16, dtype=np.uint8), 255)
+    w = orc.mx_values(code, E, orc.FP4).sum(1)
+    packed = ctx.mx_pack(esp.MX(_dev(orc.mx_data(code, orc.FP4)), _dev(orc.mx_scales(E)), K, esp.MX_FP4))
+    ones = torch.ones(M, K, dtype=TORCH[act] if act in TORCH else torch.float32, device="cuda")
+    y = ctx.mx_gemm(ones if act in TORCH else ctx.mx_quantize(ones, FMT[act]), packed, dtype=torch.float32).cpu()
+    want = torch.from_numpy(w).to(TORCH.get(act, torch.float32)).float()
+    if act == "f16":
+        s = np.repeat(np.arange(255) - 127, 16)
+        inside = torch.from_numpy((s >= -23) & (s <= 13))
+        assert torch.equal(want[inside].double(), torch.from_numpy(w)[inside]) and torch.isinf(want[(np.abs(w) > 65504).nonzero()[0]]).all()
+    assert torch.equal(y, want.expand(M, -1))
+
+
+@pytest.mark.parametrize("M", [1, 16, 200])
+def test_product_of_weights_beyond_f16(ctx, M):
+    """A weight beyond 65504 is infinite for f16 activations: the output of its row is infinite, NaN opposite a zero; bf16 activations take it as it is; other rows stay as they are."""
+    rng, K, N = _rng("beyond f16", M), 256, 80
+    w = rng.standard_normal((N, K))
+    w[7, 100] = 98304.0     # 6 x 2^14
+    x = rng.standard_normal((M, K))
+    x[0, 100] = 0.0
+    x[1:, 100] = 0.5 + np.abs(x[1:, 100])
+    wq, w64 = _mx(w, orc.FP4)
+    xt = torch.from_numpy(x)
+    y = ctx.mx_gemm(xt.half().cuda(), ctx.mx_pack(wq), dtype=torch.float32)
+    assert torch.isnan(y[0, 7]) and (y[1:, 7] == math.inf).all()
+    keep = np.arange(N) != 7
+    _assert_product(y[:, torch.from_numpy(keep).cuda()], xt.half().double().numpy(), w64[keep], torch.float32, "16")
+    _assert_product(ctx.mx_gemm(xt.bfloat16().cuda(), ctx.mx_pack(wq), dtype=torch.float32), xt.bfloat16().double().numpy(), w64, torch.float32, "16")
+
+
 def test_product_leaves_other_memory_alone(ctx):
     """Guards around the output and behind the workspace keep their pattern, whatever part of a tile is used."""
     for M, N, K, act in [(1, 5, 40, "16"), (19, 33, 130, "fp8"), (70, 129, 300, "16"), (150, 257, 256, "fp4"), (260, 300, 1000, "fp8"), (300, 1001, 333, "16")]:
