@@ -315,6 +315,21 @@ def test_product_of_weights_beyond_f16(ctx, M):
     _assert_product(ctx.mx_gemm(xt.bfloat16().cuda(), ctx.mx_pack(wq), dtype=torch.float32), xt.bfloat16().double().numpy(), w64, torch.float32, "16")
 
 
+@pytest.mark.parametrize("M,N,K", [(1, 300, 4096), (16, 512, 2048), (40, 1000, 1100), (333, 1003, 620), (700, 2100, 1100)])
+def test_product_of_8_bit_activations_with_full_sums(ctx, M, N, K):
+    """MX 8-bit values are exact in bf16: read back and multiplied as 16-bit activations they give the sums in fp32 that the scaled instruction cuts (its products of eight
+    consecutive channels at 2^-13 of the largest)."""
+    rng = _rng("full sums", M, N)
+    w, w64 = _mx(rng.standard_normal((N, K)) * K ** -0.5, orc.FP4)
+    x = rng.standard_normal((M, K)) * np.exp(2 * rng.standard_normal(K))
+    X, x64 = _mx(x, orc.FP8)
+    packed = ctx.mx_pack(w)
+    back = ctx.mx_dequantize(X, torch.bfloat16)
+    assert np.array_equal(_np(back), x64)
+    _assert_product(ctx.mx_gemm(X, packed, dtype=torch.float32), x64, w64, torch.float32, "fp8")
+    _assert_product(ctx.mx_gemm(back, packed, dtype=torch.float32), x64, w64, torch.float32, "16")
+
+
 def test_product_leaves_other_memory_alone(ctx):
     """Guards around the output and behind the workspace keep their pattern, whatever part of a tile is used."""
     for M, N, K, act in [(1, 5, 40, "16"), (19, 33, 130, "fp8"), (70, 129, 300, "16"), (150, 257, 256, "fp4"), (260, 300, 1000, "fp8"), (300, 1001, 333, "16")]:
