@@ -714,10 +714,10 @@ class DeviceOfCall {
 
 static bool aligned_to(const void* p, size_t q) { return reinterpret_cast<uintptr_t>(p) % q == 0; }
 static size_t dtype_bytes(int dtype) { return dtype == ESPARSE_F32 ? 4 : 2; }
-// whether two stretches of memory share a byte (null: no)
+// whether two stretches of memory share a byte (null, or of no bytes: no)
 static bool overlap(const void* a, size_t a_bytes, const void* b, size_t b_bytes) {
   const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return a && b && x < y + b_bytes && y < x + a_bytes;
+  return a && b && a_bytes && b_bytes && x < y + b_bytes && y < x + a_bytes;
 }
 static size_t rows_bytes(long long R, long long K, long long ld, size_t each) { return ((size_t)(R - 1) * (size_t)ld + (size_t)K) * each; }
 
@@ -931,7 +931,7 @@ int esparse_token_logprobs(esparse_ctx* ctx, const void* logits, long long R, lo
   } all[] = {{logprob, rows4}, {entropy, rows4}, {top_ids, tops4}, {top_logprobs, tops4}, {workspace, need}, {logits, rows_bytes(R, V, ld, dtype_bytes(dtype))}, {tokens, 2 * rows4}};
   for (int i = 0; i < 5; i++)  // what is written, against all that comes after it
     for (int j = i + 1; j < 7; j++)
-      ESP_REQUIRE(ctx, all[i].bytes == 0 || all[j].bytes == 0 || !overlap(all[i].p, all[i].bytes, all[j].p, all[j].bytes), ESPARSE_EINVAL,
+      ESP_REQUIRE(ctx, !overlap(all[i].p, all[i].bytes, all[j].p, all[j].bytes), ESPARSE_EINVAL,
                   "an output or the workspace overlaps an input or another output");
   const DeviceOfCall device(ctx->device);
   ESP_HIP(ctx, device.error());

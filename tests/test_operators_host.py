@@ -129,6 +129,14 @@ def test_gemm_refuses(ctx, change, code, word):
                                           a["nbytes"]), code, word)
 
 
+def test_gemm_ignores_scales_of_16_bit_activations(ctx):
+    """x_scales inside Y or the workspace: no overlap with activations that have none (the call gets as far as the missing workspace)."""
+    for change in (dict(xs=(P << 8) + 64), dict(xs=(P << 9) + 64, ws=P << 9, nbytes=8)):
+        a = {**GEMM, "act": 2, "ldx": 127, "K": 127, **change}
+        _expect(ctx, ctx._lib.esparse_mx_gemm(ctx._h, a["X"], a["xs"], a["M"], a["ldx"], a["act"], a["dtype"], a["w"], a["N"], a["K"], a["out"], a["Y"], a["ws"],
+                                              a["nbytes"]), EWORKSPACE if a["ws"] else EINVAL, "workspace")
+
+
 NORM = dict(x=P, ldx=64, r=None, ldr=0, w=P << 3, R=2, K=64, eps=1e-6, dtype=1, s=None, y=1 << 20, fmt=0, data=None, scales=None)
 
 
