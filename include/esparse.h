@@ -283,7 +283,7 @@ int esparse_output_error(esparse_ctx* ctx, const void* Yref, const void* Y, long
  * esparse_mx_size: the bytes of both (host only).  esparse_mx_quantize: X[R,K] (f16, bf16, f32) with ldx values from row to row
  * (ldx >= K; X and its rows need only the alignment of one value).  esparse_mx_dequantize: out[R,K] (f16, bf16, f32) contiguous, each value rounded once
  * to the type (bf16 and f32 hold every value within their range exactly).  data and scales: 16-byte aligned.  R = 0 is a no-op.  Outputs may not overlap inputs.  Neither synchronises.
- * Here and in the calls below matrices have fewer than 2^22 rows and at most 2^34 values.
+ * Here and in the calls below matrices have fewer than 2^22 rows and at most 2^34 values, and rows that are apart end within 2^38 values.
  * Errors: EINVAL, EUNSUPPORTED (dtype, format), EHIP. */
 typedef enum { ESPARSE_MX_FP4 = 0, ESPARSE_MX_FP8 = 1 } esparse_mx_format;
 int esparse_mx_size(long long R, long long K, esparse_mx_format format, size_t* data_bytes, size_t* scale_bytes);
@@ -333,7 +333,7 @@ int esparse_rms_norm(esparse_ctx* ctx, const void* x, long long ldx, const void*
                      void* data, void* scales);
 
 /* ---- Behind the last product: log probabilities, entropy, alternatives -----------------------------------
- * logits[R,V] (f16, bf16, f32) with ld values from row to row (>= V, the alignment of one value).  Per row, in fp32 (natural logarithms):
+ * logits[R,V] (f16, bf16, f32) with ld values from row to row (V <= ld < 2^31, the alignment of one value).  Per row, in fp32 (natural logarithms):
  *   logprob[r]  ln softmax(logits[r])[tokens[r]]; tokens DEVICE int64[R]: one below 0 marks a row without a token (0.0 is written), one of V or more gives NaN
  *   entropy[r]  -sum p ln p
  *   top_ids[r][top] (int32), top_logprobs[r][top]  the `top` largest logits: larger first, equal ones by the lower index

@@ -738,6 +738,13 @@ static int check_rows(esparse_ctx* ctx, long long R, long long K, const char* k_
   return ESPARSE_OK;
 }
 
+// the distance of rows: the last of them within 2^38 values (more than a GPU holds; what follows is computed in 64 bits)
+static int check_stride(esparse_ctx* ctx, long long R, long long K, long long ld, const char* name) {
+  ESP_REQUIRE(ctx, ld >= K, ESPARSE_EINVAL, "%s = %lld is less than K = %lld", name, ld, K);
+  ESP_REQUIRE(ctx, R <= 1 || ld <= (1ll << 38) / (R - 1), ESPARSE_EINVAL, "%lld rows that are %s = %lld values apart are out of range", R, name, ld);
+  return ESPARSE_OK;
+}
+
 int esparse_mx_size(long long R, long long K, esparse_mx_format format, size_t* data_bytes, size_t* scale_bytes) {
   if (format != ESPARSE_MX_FP4 && format != ESPARSE_MX_FP8) return ESPARSE_EUNSUPPORTED;
   if (R < 0 || R > kMaxRows || K < 1 || K >= (1ll << 31) || R * K > kMaxValues) return ESPARSE_EINVAL;
@@ -754,7 +761,7 @@ int esparse_mx_quantize(esparse_ctx* ctx, const void* X, long long R, long long 
   if (rc || (rc = check_format(ctx, format)) || (rc = check_rows(ctx, R, K, "K"))) return rc;
   if (R == 0) return ESPARSE_OK;
   ESP_REQUIRE(ctx, X && data && scales, ESPARSE_EINVAL, "X / data / scales is null");
-  ESP_REQUIRE(ctx, ldx >= K, ESPARSE_EINVAL, "ldx = %lld is less than K = %lld", ldx, K);
+  if ((rc = check_stride(ctx, R, K, ldx, "ldx"))) return rc;
   ESP_REQUIRE(ctx, aligned_to(X, dtype_bytes(dtype)), ESPARSE_EINVAL, "X is not aligned to its type");
   ESP_REQUIRE(ctx, esp_aligned16(data) && esp_aligned16(scales), ESPARSE_EINVAL, "data / scales is not 16-byte aligned");
   size_t data_bytes = 0, scale_bytes = 0;
@@ -869,7 +876,7 @@ int esparse_rms_norm(esparse_ctx* ctx, const void* x, long long ldx, const void*
   ESP_REQUIRE(ctx, x && weight, ESPARSE_EINVAL, "x / weight is null");
   ESP_REQUIRE(ctx, y ? !data && !scales : data && scales, ESPARSE_EINVAL, "the output is either y or data and scales");
   if (!y && (rc = check_format(ctx, format))) return rc;
-  ESP_REQUIRE(ctx, ldx >= K && (!residual || ldr >= K), ESPARSE_EINVAL, "ldx = %lld or ldr = %lld is less than K = %lld", ldx, ldr, K);
+  if ((rc = check_stride(ctx, R, K, ldx, "ldx")) || (residual && (rc = check_stride(ctx, R, K, ldr, "ldr")))) return rc;
   ESP_REQUIRE(ctx, aligned_to(x, 2) && aligned_to(residual, 2) && aligned_to(weight, 2) && aligned_to(sum_out, 2) && aligned_to(y, 2), ESPARSE_EINVAL,
               "a pointer is not aligned to its type");
   ESP_REQUIRE(ctx, esp_aligned16(data) && esp_aligned16(scales), ESPARSE_EINVAL, "data / scales is not 16-byte aligned");

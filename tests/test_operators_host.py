@@ -153,6 +153,16 @@ def test_norm_refuses(ctx, change, code, word):
                                            a["data"], a["scales"]), code, word)
 
 
+def test_rows_too_far_apart_are_refused(ctx):
+    """Distances whose products with the rows pass 64 bits: a stretch of memory that seemed short before the check of overlaps."""
+    for ld in ((1 << 62), (1 << 63) - 1, (1 << 38) + 1):
+        _expect(ctx, ctx._lib.esparse_mx_quantize(ctx._h, P, 3, 8, ld, 0, 0, P << 4, P << 5), EINVAL, "out of range")
+        for change in (dict(ldx=ld), dict(r=P << 12, ldr=ld)):
+            a = {**NORM, "R": 3, **change}
+            _expect(ctx, ctx._lib.esparse_rms_norm(ctx._h, a["x"], a["ldx"], a["r"], a["ldr"], a["w"], a["R"], a["K"], a["eps"], a["dtype"], a["s"], a["y"], a["fmt"],
+                                                   a["data"], a["scales"]), EINVAL, "out of range")
+
+
 LOGPROBS = dict(x=P, R=2, V=64, ld=64, dtype=1, tokens=P, top=0, lp=P, ent=P, ids=None, lps=None, ws=None, nbytes=0)
 
 
