@@ -205,6 +205,37 @@ def test_product_of_layer_sizes(ctx, M, N, K, act):
     assert ((got - want).abs() <= 2.0 ** -8 * want.abs() + before * (1 + 2.0 ** -8)).all()
 
 
+# a size for each kernel of the product, in the order of the tables in csrc/mx_matmul.hip, with odd numbers of features where that leaves the choice as it is
+KERNEL_SIZES = {
+    "fp8": [(1, 63, 128), (1, 4113, 128), (16, 20469, 133), (18, 61, 128), (24, 8267, 263), (33, 65, 128), (1, 8237, 128), (1, 63, 3604),
+            (136, 67, 128), (587, 23365, 129), (1473, 13583, 129), (65, 8613, 1031), (534, 19621, 1033), (65, 4133, 392), (131, 63, 130)],
+    "fp4": [(1, 64, 257), (1, 63, 129), (6, 16407, 129), (28, 61, 265), (17, 63, 128), (24, 8207, 129), (33, 63, 128), (1, 61, 128), (1, 64, 4612),
+            (386, 23430, 129), (515, 22043, 1555), (66, 8253, 131), (518, 20397, 513), (2054, 193, 130), (130, 63, 133)],
+    "16": [(1, 63, 129), (1, 4125, 129), (1, 63, 128), (6, 16415, 134), (18, 63, 129), (33, 65, 128),
+           (274, 19750, 1430), (129, 22145, 672), (66, 16583, 128), (65, 17203, 515), (67, 1355, 2573), (17, 16653, 1161), (2059, 193, 129), (131, 65, 128), (65, 4197, 128)]}
+
+
+@pytest.mark.parametrize("out", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("act,kernel", [(act, k) for act in KERNEL_SIZES for k in range(len(KERNEL_SIZES[act]))])
+def test_product_of_each_kernel(ctx, act, kernel, dtype, out):
+    """Every kernel with activations of both types (from both, if microscaled) and outputs of the three."""
+    M, N, K = KERNEL_SIZES[act][kernel]
+    gen = torch.Generator("cuda").manual_seed(M + N + K)
+    wq = ctx.mx_quantize(torch.randn(N, K, device="cuda", generator=gen) * K ** -0.5, esp.MX_FP4)
+    x = (torch.randn(M, K, device="cuda", generator=gen) * torch.exp(torch.randn(K, device="cuda", generator=gen))).to(TORCH[dtype])
+    X = x if act == "16" else ctx.mx_quantize(x, FMT[act])
+    x64 = (x if act == "16" else ctx.mx_dequantize(X, torch.float32)).double()
+    w64 = ctx.mx_dequantize(wq, torch.float32).double()
+    got, want = ctx.mx_gemm(X, ctx.mx_pack(wq), dtype=TORCH[out]), x64 @ w64.t()
+    before = (K + 16) * 2.0 ** -23 * (x64.abs() @ w64.abs().t())
+    if act == "fp8":
+        top = [torch.nn.functional.pad(v.abs(), (0, -K % 8)).reshape(v.shape[0], -1, 8).amax(2) for v in (x64, w64)]
+        before += 7 * 2.0 ** -13 * (top[0] @ top[1].t())
+    half = HALF[TORCH[out]]
+    assert got.dtype == TORCH[out] and ((got.double() - want).abs() <= half * want.abs() + before * (1 + half) + TINY[TORCH[out]]).all()
+
+
 @pytest.mark.parametrize("act", ["16", "fp8", "fp4"])
 @pytest.mark.parametrize("M,N", [(5, 70), (40, 96), (140, 131), (300, 640), (200, 640), (513, 1000), (1030, 2100), (2050, 4100)])
 def test_product_in_32_bits(ctx, M, N, act):
