@@ -805,9 +805,10 @@ hipError_t launch_tile(const MxGemmArgs& a, float* partial, unsigned nsplit, hip
 // The choice of a kernel: the smallest estimate of its time in microseconds, a function of the sizes and of the kind of the activations alone.
 //   rows   t0 + steps (c L + b x) (1 - d + d q)                     L, x: workgroups per compute unit, whole and as they are; q: filled part of the token tiles
 //   tile   t0 + e L + c stages max(1, u L) + (K cut: r0 + r MB of partial tiles)      L: workgroups per compute unit (256 of them)
-// The constants are fitted to the times of every kernel on 13 weight shapes (512 x 512 to 36864 x 9216, ragged ones among them) and 1 to 2048 tokens, weights cold,
-// K cut up to eight times.  Over those 234 products of each kind the kernel so chosen takes 1.005 - 1.011 of the fastest one's time on average, 1.23 at most (8.1 us
-// against 6.6).  Of 32 kernels that were measured, the 15 of a kind are those without which the average would be worse.
+// The constants are a least-squares fit of the logarithm of estimate / time, kernels near the fastest weighted most, to the times of 20 kernels of each kind on 13 weight
+// shapes (512 x 512 to 36864 x 9216, ragged ones among them) and 1 to 2048 tokens, weights cold, K cut up to eight times.  Over those 234 products of each kind the kernel so
+// chosen takes 1.007 (8 bits), 1.011 (4 bits) and 1.005 (16 bits) of the fastest one's time on average, 1.22 at most (8.1 us against 6.6); without any one of the 15 kernels
+// the average would be worse.  (profiles/mx_kernel_choice.py makes these figures from the tables below and profiles/mx_kernel_choice_times.csv)
 // ------------------------------------------------------------------------------------------------
 // rows: token tiles, row tiles, waves, steps at a time; t0, c, b, d
 #define MX_ROWS_FP8(X) \
