@@ -41,6 +41,22 @@ def estimate(kernel, constants, M, N, K, cut):
     return t0 + e * load + c * per * max(1, u * load) + (r0 + pieces * M * row_tiles * 64e-6 * r if pieces > 1 else 0)
 
 
+def choose(kernels, M, N, K):
+    """(kernel, cut) as the library chooses among those that it offers for a size"""
+    steps, row_tiles = ceil_div(K, 128), ceil_div(N, 64) * 4
+    offers = []
+    for kernel, constants in kernels.items():
+        if kernel[0] == "rows":
+            t = kernel[1]
+            if (8 * t if t > 1 else 0) < M <= (128 if t == 4 else 16 * t):
+                offers.append((kernel, 1))
+        elif M > 16:
+            tokens = kernel[2] * kernel[4] * 16
+            if tokens <= 64 or M > tokens // 2:
+                offers += [(kernel, cut) for cut in CUTS if cut == 1 or (steps >= 2 * cut and cut * M * row_tiles * 64 <= 256 << 20)]
+    return min(offers, key=lambda o: estimate(o[0], kernels[o[0]], M, N, K, o[1]))
+
+
 def read_times():
     """{act: {(M, N, K): {(kernel, cut): us}}}"""
     times, names = {}, []
@@ -59,8 +75,9 @@ def ratios(cases, kernels):
     """(ratio to the fastest of all kernels, product, chosen, its time, the fastest time), largest first"""
     out = []
     for product, cells in cases.items():
-        offered = [k for k in cells if k[0] in kernels]
-        chosen = min(offered, key=lambda k: estimate(k[0], kernels[k[0]], *product, k[1]))
+        chosen = choose(kernels, *product)
+        if chosen not in cells:  # (without one of the kernels, a cut of K that was not timed)
+            chosen = min((k for k in cells if k[0] in kernels), key=lambda k: estimate(k[0], kernels[k[0]], *product, k[1]))
         best = min(cells.values())
         out.append((cells[chosen] / best, product, chosen, cells[chosen], best))
     return sorted(out, reverse=True)

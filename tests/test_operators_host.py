@@ -1,6 +1,8 @@
 """The operators around a 4-bit linear layer without a GPU: pins of the oracle, size queries, refusals."""
 import ctypes as C
+import importlib.util
 import math
+import os
 
 import numpy as np
 import pytest
@@ -75,6 +77,34 @@ def test_sizes(R, K):
 def test_size_queries_refuse(call):
     with pytest.raises(esp.EsparseError):
         call()
+
+
+# ---- the choice of a kernel of the product ----------------------------------------------------------
+@pytest.fixture(scope="module")
+def choice():
+    spec = importlib.util.spec_from_file_location("mx_kernel_choice", os.path.join(os.path.dirname(__file__), "..", "profiles", "mx_kernel_choice.py"))
+    module = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(module)
+    return module
+
+
+@pytest.mark.parametrize("act", ["fp8", "fp4", "16"])
+def test_choice_is_near_the_fastest_kernel(choice, act):
+    """What the source says of its tables, from the times beside them."""
+    source, cases = open(choice.SOURCE).read(), choice.read_times()[act]
+    kernels = {**choice.table(source, "rows", act), **choice.table(source, "tile", act)}
+    assert len(kernels) == 15 and len(cases) == 234
+    ratios = [cells[choice.choose(kernels, *product)] / min(cells.values()) for product, cells in cases.items()]
+    assert np.mean(ratios) <= 1.0115 and max(ratios) <= 1.23
+
+
+def test_sizes_of_the_gpu_tests_reach_every_kernel(choice):
+    """The sizes of test_operators_gpu.KERNEL_SIZES, in the order of the tables."""
+    from test_operators_gpu import KERNEL_SIZES
+    source = open(choice.SOURCE).read()
+    for act, sizes in KERNEL_SIZES.items():
+        kernels = {**choice.table(source, "rows", act), **choice.table(source, "tile", act)}
+        assert [choice.choose(kernels, *size)[0] for size in sizes] == list(kernels), act
 
 
 # ---- refusals of the C calls (before any device call) -----------------------------------------------
