@@ -324,8 +324,8 @@ int esparse_mx_gemm(esparse_ctx* ctx, const void* X, const void* x_scales, long 
  * h = x + residual (rounded to dtype; residual NULL: h = x), y = h weight / sqrt(mean(h^2) + eps), sums in 64 bits, y rounded once (h / sqrt(..) and y within fp32).
  * x[R,K], residual[R,K] with ldx / ldr values from row to row (>= K), weight[K]; f16 or bf16.  sum_out[R,K] receives h (NULL: not kept); it may be x or residual
  * (then with rows of K values).  The output is either y[R,K] in dtype (data and scales NULL) or MX rows of `format` in data and scales (y NULL), from
- * the exact values, as esparse_mx_gemm takes them.  A NaN in a row makes the row NaN (so does a row of zeros with eps = 0), an infinity gives NaN in its place and 0
- * elsewhere.  The output may not overlap the inputs or sum_out.  R = 0 is a no-op.  Does not synchronise.
+ * the exact values, as esparse_mx_gemm takes them.  A NaN in a row makes the row NaN (so does a row of zeros with eps = 0), an infinity gives NaN in its place
+ * (as MX: in its block) and 0 elsewhere.  The output may not overlap the inputs or sum_out.  R = 0 is a no-op.  Does not synchronise.
  * x, residual, weight, sum_out, y need only the alignment of one value.
  * Errors: EINVAL, EUNSUPPORTED (dtype, format), EHIP. */
 int esparse_rms_norm(esparse_ctx* ctx, const void* x, long long ldx, const void* residual, long long ldr, const void* weight,

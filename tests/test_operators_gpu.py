@@ -237,6 +237,30 @@ def test_product_of_each_kernel(ctx, act, kernel, dtype, out):
 
 
 @pytest.mark.parametrize("act", ["16", "fp8", "fp4"])
+@pytest.mark.parametrize("M", [1, 40, 300])
+def test_product_of_the_most_channels(ctx, M, act):
+    """K = 2^22, rows of 16 bits 2^23 bytes apart: offsets within a tile beyond 2^31.  200 channels of a token are no zeros, so that the bound of the sums stays small."""
+    gen = torch.Generator("cuda").manual_seed(M)
+    N, K, n = 40, 1 << 22, 200
+    wq = ctx.mx_quantize(torch.randn(N, K, device="cuda", generator=gen).bfloat16(), esp.MX_FP4)
+    at = (torch.arange(n, device="cuda") * 20971 + torch.arange(M, device="cuda")[:, None] * 977) % K
+    at[:, 0], at[:, 1] = 0, K - 1
+    assert (at.sort(1).values.diff(dim=1) > 0).all()
+    x = torch.zeros(M, K, dtype=torch.bfloat16, device="cuda").scatter_(1, at, torch.randn(M, n, device="cuda", generator=gen).bfloat16())
+    X = x if act == "16" else ctx.mx_quantize(x, FMT[act])
+    got = ctx.mx_gemm(X, ctx.mx_pack(wq), dtype=torch.float32).double()
+    values = (x if act == "16" else ctx.mx_dequantize(X, torch.bfloat16)).gather(1, at).double()
+    w = ctx.mx_dequantize(wq, torch.float32)
+    want, size = torch.empty(M, N, dtype=torch.float64, device="cuda"), torch.empty(M, N, dtype=torch.float64, device="cuda")
+    for m in range(M):
+        p = w[:, at[m]].double() * values[m]
+        want[m], size[m] = p.sum(1), p.abs().sum(1)
+    # sums of n products (zeros add nothing); 8 bits: a product alone among its eight channels is not cut, one beside a larger one by less than 2^-13 of that
+    before = (n + 16) * 2.0 ** -23 * size + (7 * 2.0 ** -13 * size if act == "fp8" else 0)
+    assert ((got - want).abs() <= before * (1 + HALF[torch.float32]) + HALF[torch.float32] * want.abs()).all()
+
+
+@pytest.mark.parametrize("act", ["16", "fp8", "fp4"])
 @pytest.mark.parametrize("M,N", [(5, 70), (40, 96), (140, 131), (300, 640), (200, 640), (513, 1000), (1030, 2100), (2050, 4100)])
 def test_product_in_32_bits(ctx, M, N, act):
     _product(ctx, M, N, 520, act, "f16", out="f32")
@@ -582,6 +606,22 @@ def test_norm_in_place_and_rows_apart(ctx):
         ctx.rms_norm(x[:-1], w, residual=r[:-1], sum_out=x[1:])
 
 
+@pytest.mark.parametrize("fmt", [None, "fp8"])
+@pytest.mark.parametrize("K", [64, 700, 33000])
+def test_norm_without_a_residual_keeps_its_input(ctx, K, fmt):
+    """sum_out without a residual receives x; x itself may be it."""
+    rng = _rng("copy", K)
+    x, w = _features(rng, 5, K, "f16").cuda(), torch.from_numpy(rng.standard_normal(K)).half().cuda()
+    wide = torch.zeros(5, K + 3, dtype=torch.float16, device="cuda")
+    wide[:, 1:K + 1] = x
+    y, h = ctx.rms_norm(x, w, fmt=fmt and FMT[fmt])
+    kept, same = torch.full_like(x, 7.0), x.clone()
+    for y2, h2 in (ctx.rms_norm(wide[:, 1:K + 1], w, fmt=fmt and FMT[fmt], sum_out=kept), ctx.rms_norm(same, w, fmt=fmt and FMT[fmt], sum_out=same)):
+        assert torch.equal(h2, x) and h is x
+        assert torch.equal(y2.data, y.data) and torch.equal(y2.scales, y.scales) if fmt else torch.equal(y2, y)
+    assert h2 is same and torch.equal(kept, x)
+
+
 def test_norm_of_extreme_rows(ctx):
     w = torch.ones(256, dtype=torch.bfloat16, device="cuda")
     x = torch.ones(5, 256, dtype=torch.bfloat16, device="cuda")
@@ -701,6 +741,27 @@ def test_logprobs_of_rows_with_many_equal_values(ctx, R, V, dtype):
         if R > 13:   # one workgroup a row
             few, many = ctx.token_logprobs(x[:13], tokens[:13], top=top), ctx.token_logprobs(x, tokens, top=top)
             assert all(torch.equal(many.top_ids[i:i + 13], few.top_ids) for i in range(0, R - 13, 13))
+
+
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+@pytest.mark.parametrize("R", [1, 40, 1100])
+def test_logprobs_of_the_largest_vocabulary(ctx, R, dtype):
+    """V = 2^21: rows cut into 32 pieces, into 25, and not at all."""
+    V = 1 << 21
+    x = torch.randn(min(R, 3), V, device="cuda", generator=torch.Generator("cuda").manual_seed(R)).mul_(3).to(TORCH[dtype])
+    x[0, -1], x[0, 0], x[-1, V // 2:] = 20.0, 20.0, -math.inf
+    tokens = [V - 1] + [V // 2 - 1] * (R - 1)
+    if R > 3:
+        first = _np(x)
+        r = ctx.token_logprobs(x[torch.arange(R, device="cuda") % 3], torch.tensor(tokens, device="cuda"), top=32)
+        lp, ent, ids, tops = orc.token_logprobs(first, tokens[:3], 32)
+        s_err = 2.0 ** -21 + (128 + 2 * 21) * 2.0 ** -24
+        for row in (0, 1, 2, R - 3, R - 2, R - 1):
+            assert np.array_equal(r.top_ids[row].cpu().numpy(), ids[row % 3])
+            assert (np.abs(_np(r.top_logprobs[row]) - tops[row % 3]) <= s_err + 4 * 2.0 ** -24 * (np.abs(tops[row % 3]) + 32)).all()
+            assert abs(float(r.entropy[row]) - ent[row % 3]) <= s_err * (3 + 2 * math.log(V)) + 4 * 2.0 ** -24 * (ent[row % 3] + 32)
+    else:
+        _assert_logprobs(ctx, x, tokens, 32)
 
 
 def test_logprobs_far_from_zero(ctx):
