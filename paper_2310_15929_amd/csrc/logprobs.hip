@@ -9,8 +9,8 @@
 // are equal, as where a mask leaves fewer values than alternatives.  There the list overflows: the values above T are listed, then the first ones that are T
 // itself, in order (8 x 131072 with 20 alternatives where a mask leaves 5 values: 25 us, 2048 rows of them 261; with k rounds of a search for the next in order
 // 82 and 2250).  If a few threads hold so many values above T that this list overflows too, those rounds take its place.  Order: larger value first, then lower index.
-//   Measured, cold: 2048 x 131072 16-bit 104 us (5.2 TB/s; 20 alternatives 143), 2048 x 32000 30 us (4.4 TB/s), 555 x 50021 32-bit 27.4 us (4.1 TB/s: two
-// pieces a row, 4.3 workgroups a compute unit; 5 alternatives 31.9), 8 x 131072 6.2 us, 1 x 32000 5.6 us (20 alternatives 10.6).
+//   Measured, cold, captured: 2048 x 131072 16-bit 103 us (5.2 TB/s; 20 alternatives 143: the second read), 2048 x 32000 31 us (4.2 TB/s), 555 x 50021 32-bit 27.6 us (4.0 TB/s:
+// two pieces a row, 4.3 workgroups a compute unit; 5 alternatives 32.4), 8 x 131072 5.8 us (20 alternatives 10.7), 1 x 32000 5.7 us (20 alternatives 9.9).
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -432,8 +432,8 @@ constexpr int MAX_PIECES = LIST / ESPARSE_MAX_TOP;
 static_assert(MAX_PIECES <= 64 && LIST % NT == 0, "a lane for every piece");
 
 // Joins the pieces of a row: one workgroup a row.  Bound by its trips to memory one after the other, so all that does not depend on another answer is read at
-// the start and each wave joins the sums for itself (8 rows of 131072 with 20 alternatives, the whole call: 10.8 us; with the pieces, the lists and the token
-// read one after the other and a search for the bound bit by bit 13.3)
+// the start and each wave joins the sums for itself (8 rows of 131072 with 20 alternatives, both launches, captured: 10.7 us; with the pieces, the lists and the
+// token read one after the other and a search for the bound bit by bit 13.3)
 __global__ void __launch_bounds__(NT) k_lp_join(const LpOut o, unsigned pieces, const LpPartial* __restrict__ part, const unsigned long long* __restrict__ part_top) {
   __shared__ unsigned long long s_list[LIST];
   __shared__ int s_n;

@@ -1,8 +1,8 @@
 // The norm in front of a linear layer: h = x + residual (rounded to the type, as it is kept for the next layer), y = h w / sqrt(mean(h^2) + eps),
 // y rounded once, to 16 bits or to microscaled 8 or 4 bits as the product of csrc/mx_matmul.hip takes them.
 // Bound by memory: a row stays in registers between the sum of its squares (64 bits) and its output, so that every value is read and written
-// once.  NT threads work on a row, C pieces of eight channels each; 64 threads (a wave) need no barrier.  Measured, cold, with a residual: 1 x 4096 3.2 us,
-// 2048 x 4096 12.1 us (5.6 TB/s), to 8 bits 14.3, 2048 x 8192 26.2 us (5.1 TB/s), to 8 bits 26.6 (4.4 TB/s), without a residual 12.7 (5.3 TB/s).
+// once.  NT threads work on a row, C pieces of eight channels each; 64 threads (a wave) need no barrier.  Measured, cold, with a residual: 1 x 4096 3.4 us,
+// 2048 x 4096 12.3 us (5.5 TB/s), to 8 bits 14.0, 2048 x 8192 27.7 us (4.8 TB/s), to 8 bits 26.5 (4.4 TB/s), without a residual 12.7 (5.3 TB/s).
 #include <hip/hip_runtime.h>
 
 #include "mx.h"
