@@ -51,11 +51,11 @@ __device__ __forceinline__ double squares(const uint32_t (&v)[4], double s) {
   return s;
 }
 
-// mean of the squares + eps, times 2^(2 up), and 1 / its root as hi + lo (right to 2^-47)
+// 1 / sqrt(mean of the squares + eps) = (hi + lo) 2^up, right to 2^-47, and K times the mean and eps, times 2^(2 up)
 struct RowInverse {
   float hi, lo;
   int up;
-  double mean;
+  double sum;
 };
 // ... from the threads' sums; every thread of the row gets it.  `buf`: one double per wave.  hi is from 1 to 2, or 0, infinite or NaN with up = 0: rows of bf16
 // numbers (and an eps of any size) have inverses from far below to 2^149, and h weight may pass fp32 where y does not, so that h takes the factor 2^up before the
@@ -73,8 +73,7 @@ __device__ __forceinline__ RowInverse row_inverse(double own, double* buf, long 
 #pragma unroll
     for (int i = 0; i < NT / 64; i++) v += buf[i];
   }
-  const double mean = v / (double)K + eps;
-  double inv = 1. / __builtin_sqrt(mean);
+  double inv = 1. / __builtin_sqrt(v / (double)K + eps);
   const unsigned long long bits = __builtin_bit_cast(unsigned long long, inv);
   const unsigned top = (unsigned)(bits >> 32), exponent = top >> 20;
   int up = 0;
@@ -83,7 +82,7 @@ __device__ __forceinline__ RowInverse row_inverse(double own, double* buf, long 
     inv = __builtin_bit_cast(double, (unsigned long long)((top & 0xfffffu) | 0x3ff00000u) << 32 | (unsigned)bits);
   }
   const float hi = (float)inv;
-  return RowInverse{hi, __builtin_isfinite(hi) ? (float)(inv - (double)hi) : 0.f, up, __builtin_ldexp(mean, 2 * up)};
+  return RowInverse{hi, __builtin_isfinite(hi) ? (float)(inv - (double)hi) : 0.f, up, __builtin_ldexp(__builtin_fma(eps, (double)K, v), 2 * up)};
 }
 
 // p (hi + lo), rounded once
@@ -92,9 +91,9 @@ __device__ __forceinline__ float times(float p, const RowInverse& by) {
 }
 // v = times(p, by), not 0, to an odd last bit where it is not exact: rounding that again to 8 or 4 bits gives what rounding the exact value would.  Which side of v the
 // exact value is on, or whether it is v (rows of one magnitude, and others with a rational norm, put results right on the middle of two codes), the squares tell
-// without a root: those of p and v are exact in 64 bits
-__device__ __forceinline__ float to_odd(float v, float p, const RowInverse& by) {
-  const double rest = __builtin_fma(-(double)v * (double)v, by.mean, (double)p * (double)p);
+// without a root or a division: those of p (times K, below 2^21) and of v are exact in 64 bits
+__device__ __forceinline__ float to_odd(float v, float p, const RowInverse& by, long long K) {
+  const double rest = __builtin_fma(-(double)v * (double)v, by.sum, (double)p * (double)p * (double)K);
   const uint32_t b = __builtin_bit_cast(uint32_t, v);
   if ((b & 1u) || !(rest < 0. || rest > 0.)) return v;
   return __builtin_bit_cast(float, rest > 0. ? b + 1u : b - 1u);
@@ -135,7 +134,7 @@ __device__ __forceinline__ void norm_out(const NormArgs& a, long long row, unsig
           one = at == i ? v[i] : one;
           of = at == i ? p[i] : of;
         }
-        one = to_odd(one, of, inv);
+        one = to_odd(one, of, inv, a.K);
 #pragma unroll
         for (unsigned i = 0; i < 8; i++) v[i] = at == i ? one : v[i];
       }

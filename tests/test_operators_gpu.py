@@ -494,6 +494,24 @@ def test_norm_beside_the_middle_of_two_codes(ctx, K, fmt):
 
 
 @pytest.mark.parametrize("fmt", ["fp4", "fp8"])
+@pytest.mark.parametrize("K", [100, 225, 900, 4500, 14400, 40000])
+def test_norm_right_on_the_middle_where_the_mean_is_no_number_of_64_bits(ctx, K, fmt):
+    """36 or 64 of 100 channels of one magnitude, the others 0: a root mean square of 0.6 or 0.8 of it, and weights that put weight / 0.6 or weight / 0.8 on middles."""
+    rng = _rng("norm fraction", K)
+    for part, (num, den) in ((0.36, (5, 3)), (0.64, (5, 4))):
+        on = np.arange(K) < round(K * part)
+        sign = np.where(rng.random((9, K)) < 0.5, -1.0, 1.0) * rng.permuted(np.broadcast_to(on, (9, K)), axis=1)
+        base = np.array([1.0, 1.25, 1.625, 0.5, 2.0, 4.0, 1.9375]) * (den / 4 if den == 4 else 0.75)
+        w = base[rng.integers(0, len(base), K)] * np.where(rng.random(K) < 0.5, -1.0, 1.0)
+        x = sign * np.array([1.0, 3, 5, 7, 11, 2.0 ** -9, 96, 13, 0.625])[:, None]
+        want = np.abs(sign) * sign * (w * num / den)[None]    # in numbers of a few bits: exact
+        xt, wt = torch.from_numpy(x).bfloat16(), torch.from_numpy(w).bfloat16()
+        assert np.array_equal(xt.double().numpy(), x) and np.array_equal(wt.double().numpy(), w) and (want * 1024 % 1 == 0).all()
+        assert np.allclose(want, orc.rms_norm(x, w, 0.0), rtol=1e-14, atol=0)
+        _assert_mx(ctx.rms_norm(xt.cuda(), wt.cuda(), 0.0, fmt=FMT[fmt])[0], want, FMT[fmt])
+
+
+@pytest.mark.parametrize("fmt", ["fp4", "fp8"])
 def test_norm_takes_eps_in_64_bits(ctx, fmt):
     """Rows whose mean square is of the size of eps, which is no 32-bit number."""
     rng, R, K = _rng("norm eps"), 200, 4096
