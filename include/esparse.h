@@ -36,8 +36,8 @@ extern "C" {
 
 typedef struct esparse_ctx esparse_ctx; /* opaque: device, stream, scratch, last error */
 
-/* ESPARSE_F32: logits of esparse_token_logprobs, input of esparse_mx_quantize, output of esparse_mx_dequantize and esparse_mx_gemm;
- * EUNSUPPORTED elsewhere. */
+/* ESPARSE_F32: logits of esparse_token_logprobs and esparse_sample, input of esparse_mx_quantize, output of esparse_mx_dequantize, esparse_mx_gemm and
+ * esparse_cache_read; EUNSUPPORTED elsewhere. */
 typedef enum { ESPARSE_F16 = 0, ESPARSE_BF16 = 1, ESPARSE_F32 = 2 } esparse_dtype;
 
 typedef enum {
@@ -349,6 +349,74 @@ int esparse_token_logprobs_workspace(long long R, long long V, esparse_dtype dty
 int esparse_token_logprobs(esparse_ctx* ctx, const void* logits, long long R, long long V, long long ld, esparse_dtype dtype,
                            const int64_t* tokens, int top, float* logprob, float* entropy, int32_t* top_ids, float* top_logprobs,
                            void* workspace, size_t workspace_bytes);
+
+/* ---- Heads behind the q/k/v products: norm, rotation, the cache in 4 bits -------------------------------
+ * A cache holds keys and values in MX 4 bits (the codes and scales of ESPARSE_MX_FP4 above) in pages of `page` tokens (a power of two, 16..1024), each kind in
+ *   data    uint8[pages][heads][page][row / 2]    row = 64, 128 or 256: head_dim (1..256) rounded up, the channels from head_dim on 0
+ *   scales  uint8[pages][heads][page][row / 32]
+ * of esparse_cache_size bytes (host only); 16-byte aligned.  Slot s is place s % page of page s / page; pages * page < 2^31.
+ * The struct is HOST memory, read during the call.
+ *
+ * esparse_rotate_heads: T tokens with positions[T] (int32).  q[T][q_heads][head_dim], k and v[T][kv_heads][head_dim] (f16 or bf16) with ldq / ldk / ldv values from token to
+ * token, the heads of a token one behind the other, each with the alignment of one value.  q or k may be NULL (none).
+ *   y = x weight / sqrt(mean(x^2) + eps) over the head_dim channels of a head (weight[head_dim] of type dtype; NULL: y = x);
+ *   then pairs (a, b) of its first `rotary` channels (even, 0..head_dim) become (a cos t - b sin t, b cos t + a sin t), t = position frequencies[i] (f32[rotary / 2]),
+ *   i < rotary / 2: channels i and i + rotary / 2, or with paired = 1 channels 2 i and 2 i + 1.
+ * In 64 bits up to one rounding.  q_out[T][q_heads][head_dim]; keys to k_out[T][kv_heads][head_dim] (may be NULL with a cache) and, with a cache, keys and v to the places
+ * slots[T] (int32).  A token whose slot is no place of the cache is not kept; of tokens given the same slot the last is.
+ * NaN and infinities as in esparse_rms_norm; a rotated channel is NaN with its partner.  In the cache a block of 32 channels that holds one reads as NaN.  (Numbers beyond 2^130
+ * are limited to 6 x 2^127.)  Outputs and the cache may not overlap inputs or each other.  T = 0 is a no-op.  Does not synchronise; can be captured.
+ *
+ * esparse_cache_read: the numbers of places slots[T] as k_out, v_out[T][heads][head_dim] (f16, bf16 or f32, either may be NULL), each rounded once.  A slot that is no place gives zeros.
+ * Errors: EINVAL, EUNSUPPORTED (dtype), EHIP. */
+typedef struct {
+  void *k_data, *k_scales, *v_data, *v_scales; /* DEVICE */
+  long long pages;
+  int page, heads, head_dim;
+} esparse_cache;
+typedef struct {
+  int q_heads, kv_heads, head_dim, rotary;
+  int paired; /* 0: channels i and i + rotary / 2, 1: neighbours */
+  double eps;
+} esparse_heads;
+int esparse_cache_size(long long pages, int page, int heads, int head_dim, size_t* data_bytes, size_t* scale_bytes);
+int esparse_rotate_heads(esparse_ctx* ctx, const esparse_heads* heads, long long T, esparse_dtype dtype, const void* q, long long ldq, const void* q_weight,
+                         const void* k, long long ldk, const void* k_weight, const int32_t* positions, const float* frequencies, void* q_out, void* k_out,
+                         const void* v, long long ldv, const esparse_cache* cache, const int32_t* slots);
+int esparse_cache_read(esparse_ctx* ctx, const esparse_cache* cache, const int32_t* slots, long long T, esparse_dtype dtype, void* k_out, void* v_out);
+
+/* ---- Attention over the cache ----------------------------------------------------------------------------
+ * out[T][q_heads][head_dim] = softmax(scale q . k) v over cached tokens; q as in esparse_rotate_heads, q_heads a multiple of the cache's heads: query head h reads head
+ * h / (q_heads / heads).  B sequences: tokens of sequence b are lengths[b] (int32) places, the j-th in page table[b][j / page] (int32 [B][width]), place j % page.
+ * Its queries are its last tokens: rows starts[b] .. starts[b + 1] - 1 of q (int32 [B + 1], ascending), or with starts NULL row b alone (then T = B); the last of them sees all
+ * tokens, the one before it one fewer and so on.  A query that sees none gives 0.  lse[T][q_heads] (f32, may be NULL): ln of the sum of exp(scale q . k) (minus infinity if none).
+ * Negative lengths count as 0, longer ones than the table has room for as that; tokens in a page outside [0, pages) are left out, as are all rows of q that belong to no sequence: those rows of
+ * out and lse are left as they were.  Tokens that a query does not see do not touch it, whatever their places hold.
+ * Keys, probabilities and values take part in the 16 bits of dtype, which hold the cache's numbers as said at esparse_mx_gemm; sums and statistics are in 32 bits.
+ * q must be finite; a key without number (scale 255) makes the queries that see it NaN, such a block of a value its channels.
+ * workspace: DEVICE scratch of esparse_cache_attention_workspace bytes (host only; may be 0; it reads the cache's sizes alone; ragged: 1 with starts, else 0), 256-byte aligned, overwritten.
+ * Outputs and workspace may not overlap inputs or each other.  T = 0 or B = 0 is a no-op.  The order of a row's sums follows from the sizes and the sequence's length.
+ * Does not synchronise; can be captured, and replayed with other contents of table, lengths and starts.  Errors: EINVAL, EUNSUPPORTED (dtype), EWORKSPACE, EHIP. */
+int esparse_cache_attention_workspace(const esparse_cache* cache, long long T, int B, int q_heads, long long width, int ragged, size_t* bytes);
+int esparse_cache_attention(esparse_ctx* ctx, const void* q, long long ldq, long long T, int q_heads, esparse_dtype dtype, const esparse_cache* cache,
+                            const int32_t* table, long long width, const int32_t* lengths, const int32_t* starts, int B, double scale, void* out, float* lse,
+                            void* workspace, size_t workspace_bytes);
+
+/* ---- A token from each row of logits ---------------------------------------------------------------------
+ * logits[R,V] as in esparse_token_logprobs.  Per row, w_i = exp((x_i - max x) / temperature) in 64 bits, in the order of the logits, larger ones first and equal ones by the lower index:
+ *   top_k (int32[R])  the first top_k are kept (0 or less: all)
+ *   top_p (f32[R])    of these, the ones before which less than top_p of the sum of all of them has come (the first always; 1 or more, NaN: all)
+ *   min_p (f32[R])    of these, the ones with w_i >= min_p (the largest always; NaN: all)
+ * tokens[r] (int64) is the first, by index, up to which more than u[r] (f32, [0, 1); others count as the nearest, NaN as 0) of the kept sum has come; logprob[r] (f32, may be NULL)
+ * ln(w / kept sum).  temperature (f32[R]) 0: the largest logit, the lowest index of equal ones, logprob 0.
+ * temperature, top_k, top_p, min_p may be NULL (1, all, all, all).  Logits of minus infinity are never drawn.  A row with a NaN or plus infinity, with nothing but minus infinity, or whose
+ * temperature is negative, infinite or NaN gives -1 and NaN.  Sums are exact to 2^-40 of the largest weight and do not depend on chance.
+ * workspace: DEVICE scratch of esparse_sample_workspace bytes (host only), 256-byte aligned, overwritten.  Outputs and workspace may not overlap inputs or each other.
+ * R = 0 is a no-op.  Does not synchronise; can be captured.  Errors: EINVAL, EUNSUPPORTED (dtype, V), EWORKSPACE, EHIP. */
+int esparse_sample_workspace(long long R, long long V, size_t* bytes);
+int esparse_sample(esparse_ctx* ctx, const void* logits, long long R, long long V, long long ld, esparse_dtype dtype, const float* temperature,
+                   const int32_t* top_k, const float* top_p, const float* min_p, const float* u, int64_t* tokens, float* logprob, void* workspace,
+                   size_t workspace_bytes);
 
 /* ---- Measurement aid: what the matrix pipes sustain on this chip -------------------------------
  * Not a step of the method: the ceiling its product kernels (Section 4) are compared with, beside the published

@@ -36,6 +36,15 @@ class _Opts(C.Structure):
                 ("alpha", C.c_double), ("flags", C.c_uint), ("max_swaps", C.c_longlong)]
 
 
+class _Cache(C.Structure):
+    _fields_ = [("k_data", C.c_void_p), ("k_scales", C.c_void_p), ("v_data", C.c_void_p), ("v_scales", C.c_void_p),
+                ("pages", C.c_longlong), ("page", C.c_int), ("heads", C.c_int), ("head_dim", C.c_int)]
+
+
+class _Heads(C.Structure):
+    _fields_ = [("q_heads", C.c_int), ("kv_heads", C.c_int), ("head_dim", C.c_int), ("rotary", C.c_int), ("paired", C.c_int), ("eps", C.c_double)]
+
+
 def load_library():
     """Load libesparse.so (built by __graft_entry__.build()).  Raises if it is not there."""
     global _lib
@@ -91,6 +100,13 @@ def load_library():
         "esparse_rms_norm": (i32, [vp, vp, ll, vp, ll, vp, ll, ll, C.c_double, i32, vp, vp, i32, vp, vp]),
         "esparse_token_logprobs_workspace": (i32, [ll, ll, i32, i32, P(sz)]),
         "esparse_token_logprobs": (i32, [vp, vp, ll, ll, ll, i32, vp, i32, vp, vp, vp, vp, vp, sz]),
+        "esparse_cache_size": (i32, [ll, i32, i32, i32, P(sz), P(sz)]),
+        "esparse_rotate_heads": (i32, [vp, P(_Heads), ll, i32, vp, ll, vp, vp, ll, vp, vp, vp, vp, vp, vp, ll, P(_Cache), vp]),
+        "esparse_cache_read": (i32, [vp, P(_Cache), vp, ll, i32, vp, vp]),
+        "esparse_cache_attention_workspace": (i32, [P(_Cache), ll, i32, i32, ll, i32, P(sz)]),
+        "esparse_cache_attention": (i32, [vp, vp, ll, ll, i32, i32, P(_Cache), vp, ll, vp, vp, i32, C.c_double, vp, vp, vp, sz]),
+        "esparse_sample_workspace": (i32, [ll, ll, P(sz)]),
+        "esparse_sample": (i32, [vp, vp, ll, ll, ll, i32, vp, vp, vp, vp, vp, vp, vp, vp, sz]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -111,7 +127,8 @@ EXPORTED = ["esparse_create", "esparse_destroy", "esparse_set_stream", "esparse_
             "esparse_dense_pack", "esparse_dense_gemm", "esparse_tune", "esparse_tune_group", "esparse_tune_save",
             "esparse_tune_load", "esparse_mx_size", "esparse_mx_quantize", "esparse_mx_dequantize", "esparse_mx_packed_size",
             "esparse_mx_pack", "esparse_mx_gemm_workspace", "esparse_mx_gemm", "esparse_rms_norm",
-            "esparse_token_logprobs_workspace", "esparse_token_logprobs"]
+            "esparse_token_logprobs_workspace", "esparse_token_logprobs", "esparse_cache_size", "esparse_rotate_heads", "esparse_cache_read",
+            "esparse_cache_attention_workspace", "esparse_cache_attention", "esparse_sample_workspace", "esparse_sample"]
 
 
 def _dtype_code(t: torch.Tensor) -> int:
@@ -207,6 +224,32 @@ def token_logprobs_workspace(R: int, V: int, dtype: int, top: int) -> int:
     return a.value
 
 
+def cache_size(pages: int, page: int, heads: int, head_dim: int):
+    """(bytes of the codes, bytes of the scales) of the keys, or of the values, of a cache."""
+    a, b = C.c_size_t(), C.c_size_t()
+    rc = load_library().esparse_cache_size(pages, page, heads, head_dim, C.byref(a), C.byref(b))
+    if rc:
+        raise EsparseError(rc, f"esparse_cache_size: {pages} pages of {page} tokens, {heads} heads of {head_dim} channels")
+    return a.value, b.value
+
+
+def cache_attention_workspace(pages: int, page: int, heads: int, head_dim: int, T: int, B: int, q_heads: int, width: int, ragged: bool) -> int:
+    a = C.c_size_t()
+    cache = _Cache(None, None, None, None, pages, page, heads, head_dim)
+    rc = load_library().esparse_cache_attention_workspace(C.byref(cache), T, B, q_heads, width, int(ragged), C.byref(a))
+    if rc:
+        raise EsparseError(rc, f"esparse_cache_attention_workspace: T = {T}, B = {B}, {q_heads} heads on {heads}, width {width}")
+    return a.value
+
+
+def sample_workspace(R: int, V: int) -> int:
+    a = C.c_size_t()
+    rc = load_library().esparse_sample_workspace(R, V, C.byref(a))
+    if rc:
+        raise EsparseError(rc, f"esparse_sample_workspace: R = {R}, V = {V}")
+    return a.value
+
+
 # for the calls: sizes asked for before, a function of their arguments alone (typed: 16.0 is not the 16 that was asked for)
 _known_size = functools.lru_cache(4096, typed=True)(compressed_size)
 _known_workspace = functools.lru_cache(4096, typed=True)(spmm_workspace)
@@ -214,6 +257,8 @@ _known_group_workspace = functools.lru_cache(4096, typed=True)(_group_workspace)
 _known_mx_packed_size = functools.lru_cache(4096, typed=True)(mx_packed_size)
 _known_mx_gemm_workspace = functools.lru_cache(4096, typed=True)(mx_gemm_workspace)
 _known_logprobs_workspace = functools.lru_cache(4096, typed=True)(token_logprobs_workspace)
+_known_attention_workspace = functools.lru_cache(4096, typed=True)(cache_attention_workspace)
+_known_sample_workspace = functools.lru_cache(4096, typed=True)(sample_workspace)
 
 
 def dense_packed_size(N: int, K: int) -> int:
@@ -292,6 +337,16 @@ class TokenLogprobs:
     entropy: torch.Tensor                 # float32 [R]
     top_ids: Optional[torch.Tensor]       # int32 [R, top]
     top_logprobs: Optional[torch.Tensor]  # float32 [R, top]
+
+
+@dataclass
+class KVCache:
+    """Keys and values in microscaled 4 bits, in pages (include/esparse.h)."""
+    k_data: torch.Tensor    # uint8 [pages, heads, page, row / 2], row = 64, 128 or 256: head_dim rounded up
+    k_scales: torch.Tensor  # uint8 [pages, heads, page, row / 32]
+    v_data: torch.Tensor
+    v_scales: torch.Tensor
+    head_dim: int
 
 
 def _raw_stream(device: int) -> int:
@@ -748,3 +803,175 @@ class Context:
         if rc:
             self._check(rc)
         return TokenLogprobs(logprob, entropy, ids, lps)
+
+    # -- heads, the cache in 4 bits, attention over it, tokens drawn ------------------------------
+    def _heads(self, name: str, t: torch.Tensor):
+        """(tokens, heads, channels, values from token to token) of heads [T, H, D] whose tokens are contiguous."""
+        if t.get_device() != self.device:
+            self._away(name, t)
+        if t.dim() != 3:
+            raise ValueError(f"{name}: {t.dim()} dimensions instead of three")
+        T, H, D = t.shape
+        if t.is_contiguous():
+            return T, H, D, H * D
+        if (D > 1 and t.stride(2) != 1) or (H > 1 and t.stride(1) != D):
+            raise ValueError(f"{name}: the heads of a token are not one behind the other (strides {t.stride()})")
+        if T > 1 and t.stride(0) < H * D:
+            raise ValueError(f"{name}: tokens overlap (stride {t.stride(0)} for {H * D} values)")
+        return T, H, D, t.stride(0) if T > 1 else H * D
+
+    def _vector(self, name: str, what: str, t: torch.Tensor, dtype: torch.dtype, n: int) -> int:
+        if t.get_device() != self.device:
+            self._away(name, t)
+        if t.dtype != dtype or t.shape != (n,) or not t.is_contiguous():
+            raise ValueError(f"{name}: {what} is not a contiguous {str(dtype)[6:]} [{n}]")
+        return t.data_ptr()
+
+    def _check_cache(self, name: str, c: KVCache) -> _Cache:
+        if c.k_data.dim() != 4:
+            raise ValueError(f"{name}: the cache's k_data has {c.k_data.dim()} dimensions instead of four")
+        P, H, page, _ = c.k_data.shape
+        if not 1 <= c.head_dim <= 256 or not 16 <= page <= 1024 or page & (page - 1):
+            raise ValueError(f"{name}: a cache of pages of {page} tokens and heads of {c.head_dim} channels")
+        row = 64 if c.head_dim <= 64 else 128 if c.head_dim <= 128 else 256
+        for t, last in ((c.k_data, row // 2), (c.k_scales, row // 32), (c.v_data, row // 2), (c.v_scales, row // 32)):
+            if t.get_device() != self.device:
+                self._away(name, t)
+            if t.dtype != torch.uint8 or t.shape != (P, H, page, last) or not t.is_contiguous():
+                raise ValueError(f"{name}: the cache's tensors are contiguous uint8 [{P}, {H}, {page}, {row // 2}] and [.., {row // 32}]")
+        return _Cache(c.k_data.data_ptr(), c.k_scales.data_ptr(), c.v_data.data_ptr(), c.v_scales.data_ptr(), P, page, H, c.head_dim)
+
+    def kv_cache(self, pages: int, page: int, heads: int, head_dim: int) -> KVCache:
+        """An empty cache of `pages` pages of `page` tokens (a power of two, 16 .. 1024)."""
+        if pages < 1:
+            raise ValueError(f"kv_cache: {pages} pages")
+        sizes = cache_size(pages, page, heads, head_dim)
+        return KVCache(*(torch.zeros((pages, heads, page, n // (pages * heads * page)), dtype=torch.uint8, device=self._on) for n in sizes * 2), head_dim)
+
+    def rotate_heads(self, q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions: Optional[torch.Tensor] = None,
+                     frequencies: Optional[torch.Tensor] = None, *, q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None,
+                     eps: float = 1e-6, paired: bool = False, v: Optional[torch.Tensor] = None, cache: Optional[KVCache] = None,
+                     slots: Optional[torch.Tensor] = None, keys_out: Optional[bool] = None):
+        """(q, k) with each head of q[T, Hq, D] and k[T, Hkv, D] (f16, bf16; tokens may be apart) normalised, where there is a weight[D], and its first
+        2 len(frequencies) channels rotated by positions[T] (int32) x frequencies (float32).  With a cache keys and v go to its places slots[T] (int32), and
+        k is returned only if keys_out says so."""
+        name, x = "rotate_heads", q if q is not None else k
+        if x is None:
+            raise ValueError("rotate_heads: neither q nor k")
+        if (cache is None) != (v is None) or (cache is None) != (slots is None) or (cache is not None and k is None):
+            raise ValueError("rotate_heads: a cache comes with k, v and slots")
+        dtype = x.dtype
+        code, (T, Hq, D, ldq) = _code(dtype, name), self._heads(name, x)
+        Hkv = ldk = ldv = 0
+        to_k = cache is None if keys_out is None else keys_out
+        qp = kp = vp = qo = ko = qw = kw = sp = pp = fp = c = None
+        if k is not None:
+            Tk, Hkv, Dk, ldk = self._heads(name, k)
+            if k.dtype != dtype or Tk != T or Dk != D:
+                raise ValueError("rotate_heads: k is not of the tokens, channels and type of q")
+            kp = k.data_ptr()
+            if cache is None and not to_k:
+                raise ValueError("rotate_heads: keys go neither to a cache nor out")
+        if q is None:
+            Hq = ldq = 0
+        else:
+            qp = q.data_ptr()
+            qo = _EMPTY((T, Hq, D), (Hq * D, D, 1), dtype=dtype, device=self._on)
+        k_out = None
+        if k is not None and to_k:
+            k_out = _EMPTY((T, Hkv, D), (Hkv * D, D, 1), dtype=dtype, device=self._on)
+            ko = k_out.data_ptr()
+        if q_weight is not None:
+            qw = self._vector(name, "q_weight", q_weight, dtype, D)
+        if k_weight is not None:
+            kw = self._vector(name, "k_weight", k_weight, dtype, D)
+        rotary = 0
+        if frequencies is not None:
+            rotary = 2 * frequencies.numel()
+            fp = self._vector(name, "frequencies", frequencies, torch.float32, rotary // 2)
+            if positions is None:
+                raise ValueError("rotate_heads: frequencies without positions")
+            pp = self._vector(name, "positions", positions, torch.int32, T)
+        if cache is not None:
+            Tv, Hv, Dv, ldv = self._heads(name, v)
+            if v.dtype != dtype or (Tv, Hv, Dv) != (T, Hkv, D):
+                raise ValueError("rotate_heads: v is not of the shape and type of k")
+            vp, sp = v.data_ptr(), self._vector(name, "slots", slots, torch.int32, T)
+            c = C.byref(self._check_cache(name, cache))
+        self._sync_stream()
+        rc = self._lib.esparse_rotate_heads(self._h, C.byref(_Heads(Hq, Hkv, D, rotary, int(paired), eps)), T, code, qp, ldq, qw, kp, ldk, kw, pp, fp, _ptr(qo), ko, vp,
+                                            ldv, c, sp)
+        if rc:
+            self._check(rc)
+        return qo, k_out
+
+    def cache_read(self, cache: KVCache, slots: torch.Tensor, dtype: torch.dtype = torch.bfloat16):
+        """(keys, values) [T, heads, D] at the places slots[T] (int32) of a cache."""
+        code, c, T = _code(dtype, "cache_read", f32=True), self._check_cache("cache_read", cache), slots.numel()
+        sp = self._vector("cache_read", "slots", slots, torch.int32, T)
+        H, D = c.heads, c.head_dim
+        k, v = (_EMPTY((T, H, D), (H * D, D, 1), dtype=dtype, device=self._on) for _ in range(2))
+        self._sync_stream()
+        rc = self._lib.esparse_cache_read(self._h, C.byref(c), sp, T, code, k.data_ptr(), v.data_ptr())
+        if rc:
+            self._check(rc)
+        return k, v
+
+    def cache_attention(self, q: torch.Tensor, cache: KVCache, table: torch.Tensor, lengths: torch.Tensor, *, starts: Optional[torch.Tensor] = None,
+                        scale: Optional[float] = None, out: Optional[torch.Tensor] = None, lse: bool = False):
+        """softmax(scale q . k) v of queries q[T, Hq, D] (f16, bf16; tokens may be apart) over a cache: sequence b has lengths[b] tokens in the pages table[b], its
+        queries are rows starts[b] .. starts[b + 1] - 1 of q, its last tokens (without starts: row b).  scale: D ** -0.5 if not given.  lse=True: (out, ln sum exp [T, Hq])."""
+        name, dtype = "cache_attention", q.dtype
+        code, (T, Hq, D, ldq), c = _code(dtype, name), self._heads(name, q), self._check_cache(name, cache)
+        if D != c.head_dim or Hq % c.heads:
+            raise ValueError(f"cache_attention: {Hq} heads of {D} channels on a cache of {c.heads} of {c.head_dim}")
+        if table.get_device() != self.device:
+            self._away(name, table)
+        if table.dtype != torch.int32 or table.dim() != 2 or not table.is_contiguous():
+            raise ValueError("cache_attention: table is not a contiguous int32 matrix")
+        B, width = table.shape
+        lp, sp = self._vector(name, "lengths", lengths, torch.int32, B), None
+        if starts is not None:
+            sp = self._vector(name, "starts", starts, torch.int32, B + 1)
+        elif T != B:
+            raise ValueError(f"cache_attention: {T} queries of {B} sequences without starts")
+        if out is None:
+            out = _EMPTY((T, Hq, D), (Hq * D, D, 1), dtype=dtype, device=self._on)
+        elif out.get_device() != self.device:
+            self._away(name, out)
+        elif out.dtype != dtype or out.shape != q.shape or not out.is_contiguous():
+            raise ValueError("cache_attention: out is not a contiguous tensor of the shape and type of q")
+        sums = self._empty(T, Hq, torch.float32) if lse else None
+        nbytes = _known_attention_workspace(c.pages, c.page, c.heads, D, T, B, Hq, width, starts is not None)
+        ws = _EMPTY((nbytes,), (1,), dtype=torch.uint8, device=self._on) if nbytes else None
+        self._sync_stream()
+        rc = self._lib.esparse_cache_attention(self._h, q.data_ptr(), ldq, T, Hq, code, C.byref(c), table.data_ptr(), width, lp, sp, B,
+                                               D ** -0.5 if scale is None else scale, out.data_ptr(), _ptr(sums), _ptr(ws), nbytes)
+        if rc:
+            self._check(rc)
+        return (out, sums) if lse else out
+
+    def sample(self, logits: torch.Tensor, u: torch.Tensor, *, temperature: Optional[torch.Tensor] = None, top_k: Optional[torch.Tensor] = None,
+               top_p: Optional[torch.Tensor] = None, min_p: Optional[torch.Tensor] = None):
+        """(tokens int64 [R], logprob float32 [R]) drawn from logits[R, V] (f16, bf16, f32; rows may be apart) with the uniform numbers u[R] (float32, [0, 1)); temperature,
+        top_p, min_p (float32) and top_k (int32) hold one number for each row."""
+        name = "sample"
+        code, (R, V, ld) = _code(logits.dtype, name, f32=True), self._rows(name, logits)
+        up, tp, kp, pp, mp = self._vector(name, "u", u, torch.float32, R), None, None, None, None
+        if temperature is not None:
+            tp = self._vector(name, "temperature", temperature, torch.float32, R)
+        if top_k is not None:
+            kp = self._vector(name, "top_k", top_k, torch.int32, R)
+        if top_p is not None:
+            pp = self._vector(name, "top_p", top_p, torch.float32, R)
+        if min_p is not None:
+            mp = self._vector(name, "min_p", min_p, torch.float32, R)
+        tokens = _EMPTY((R,), (1,), dtype=torch.int64, device=self._on)
+        logprob = _EMPTY((R,), (1,), dtype=torch.float32, device=self._on)
+        nbytes = _known_sample_workspace(R, V)
+        ws = _EMPTY((nbytes,), (1,), dtype=torch.uint8, device=self._on)
+        self._sync_stream()
+        rc = self._lib.esparse_sample(self._h, logits.data_ptr(), R, V, ld, code, tp, kp, pp, mp, up, tokens.data_ptr(), logprob.data_ptr(), _ptr(ws), nbytes)
+        if rc:
+            self._check(rc)
+        return tokens, logprob

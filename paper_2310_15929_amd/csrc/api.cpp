@@ -945,4 +945,183 @@ int esparse_token_logprobs(esparse_ctx* ctx, const void* logits, long long R, lo
   return esp_token_logprobs_device(ctx, logits, R, V, ld, dtype, reinterpret_cast<const long long*>(tokens), top, logprob, entropy, top_ids, top_logprobs, workspace);
 }
 
+// ---- heads, the cache in 4 bits, attention over it, tokens drawn --------------------------------------
+// a stretch of memory that a call writes or reads; nothing that is written may share a byte with another
+struct Stretch {
+  const void* p;
+  size_t bytes;
+};
+static bool apart(const Stretch* all, int written, int n) {
+  for (int i = 0; i < written; i++)
+    for (int j = i + 1; j < n; j++)
+      if (overlap(all[i].p, all[i].bytes, all[j].p, all[j].bytes)) return false;
+  return true;
+}
+
+// heads up to 2^16 and 2^26 rows (heads of tokens): a launch has a thread for eight channels of a row
+static constexpr int kMaxHeads = 1 << 16;
+static constexpr long long kMaxHeadRows = 1ll << 26;
+static bool cache_sizes(long long pages, int page, int heads, int head_dim) {
+  return pages >= 0 && page >= 16 && page <= 1024 && (page & (page - 1)) == 0 && heads >= 1 && heads <= kMaxHeads && head_dim >= 1 && head_dim <= 256 &&
+         pages < (1ll << 31) / page && pages * page <= (1ll << 38) / heads;
+}
+
+int esparse_cache_size(long long pages, int page, int heads, int head_dim, size_t* data_bytes, size_t* scale_bytes) {
+  if (!cache_sizes(pages, page, heads, head_dim)) return ESPARSE_EINVAL;
+  const size_t rows = (size_t)pages * page * heads, row = esp_cache_row(head_dim);
+  if (data_bytes) *data_bytes = rows * (row / 2);
+  if (scale_bytes) *scale_bytes = rows * (row / 32);
+  return ESPARSE_OK;
+}
+
+static int check_cache(esparse_ctx* ctx, const esparse_cache* c, size_t* data, size_t* scales) {
+  ESP_REQUIRE(ctx, esparse_cache_size(c->pages, c->page, c->heads, c->head_dim, data, scales) == ESPARSE_OK, ESPARSE_EINVAL,
+              "a cache of %lld pages of %d tokens, %d heads of %d channels is out of range", c->pages, c->page, c->heads, c->head_dim);
+  ESP_REQUIRE(ctx, c->pages == 0 || (c->k_data && c->k_scales && c->v_data && c->v_scales), ESPARSE_EINVAL, "a pointer of the cache is null");
+  ESP_REQUIRE(ctx, esp_aligned16(c->k_data) && esp_aligned16(c->k_scales) && esp_aligned16(c->v_data) && esp_aligned16(c->v_scales), ESPARSE_EINVAL,
+              "a pointer of the cache is not 16-byte aligned");
+  return ESPARSE_OK;
+}
+
+int esparse_rotate_heads(esparse_ctx* ctx, const esparse_heads* h, long long T, esparse_dtype dtype, const void* q, long long ldq, const void* q_weight,
+                         const void* k, long long ldk, const void* k_weight, const int32_t* positions, const float* frequencies, void* q_out, void* k_out,
+                         const void* v, long long ldv, const esparse_cache* cache, const int32_t* slots) {
+  if (!ctx) return ESPARSE_EINVAL;
+  int rc = check_dtype(ctx, dtype);
+  if (rc) return rc;
+  ESP_REQUIRE(ctx, h, ESPARSE_EINVAL, "heads is null");
+  ESP_REQUIRE(ctx, T >= 0 && T <= kMaxRows, ESPARSE_EINVAL, "%lld tokens are outside [0, 2^22)", T);
+  ESP_REQUIRE(ctx, h->head_dim >= 1 && h->head_dim <= 256, ESPARSE_EINVAL, "head_dim = %d is outside [1, 256]", h->head_dim);
+  ESP_REQUIRE(ctx, h->rotary >= 0 && h->rotary <= h->head_dim && h->rotary % 2 == 0, ESPARSE_EINVAL, "rotary = %d is not an even number up to head_dim = %d", h->rotary,
+              h->head_dim);
+  ESP_REQUIRE(ctx, h->paired == 0 || h->paired == 1, ESPARSE_EINVAL, "paired = %d is neither 0 nor 1", h->paired);
+  ESP_REQUIRE(ctx, std::isfinite(h->eps) && h->eps >= 0, ESPARSE_EINVAL, "eps is negative or not finite");
+  ESP_REQUIRE(ctx, !q || (h->q_heads >= 1 && h->q_heads <= kMaxHeads), ESPARSE_EINVAL, "q_heads = %d is outside [1, 2^16]", h->q_heads);
+  ESP_REQUIRE(ctx, !k || (h->kv_heads >= 1 && h->kv_heads <= kMaxHeads), ESPARSE_EINVAL, "kv_heads = %d is outside [1, 2^16]", h->kv_heads);
+  size_t data = 0, scales = 0;
+  if (cache) {
+    if ((rc = check_cache(ctx, cache, &data, &scales))) return rc;
+    ESP_REQUIRE(ctx, cache->head_dim == h->head_dim && (!k || cache->heads == h->kv_heads), ESPARSE_EINVAL, "the cache has %d heads of %d channels, the keys %d of %d", cache->heads,
+                cache->head_dim, h->kv_heads, h->head_dim);
+  }
+  if (T == 0) return ESPARSE_OK;
+  ESP_REQUIRE(ctx, q || k, ESPARSE_EINVAL, "q and k are null");
+  const long long D = h->head_dim, q_row = q ? h->q_heads * D : 0, k_row = k ? h->kv_heads * D : 0;
+  ESP_REQUIRE(ctx, T * ((q ? h->q_heads : 0) + 2ll * (k ? h->kv_heads : 0)) <= kMaxHeadRows, ESPARSE_EINVAL, "more than 2^26 heads of tokens");
+  ESP_REQUIRE(ctx, !q == !q_out, ESPARSE_EINVAL, "q and q_out come together");
+  ESP_REQUIRE(ctx, !k == !(k_out || cache), ESPARSE_EINVAL, "keys come with k_out or a cache");
+  ESP_REQUIRE(ctx, !cache == !v && !cache == !slots, ESPARSE_EINVAL, "the cache, v and slots come together");
+  ESP_REQUIRE(ctx, (q || !q_weight) && (k || !k_weight), ESPARSE_EINVAL, "a weight comes without heads");
+  ESP_REQUIRE(ctx, h->rotary == 0 || (positions && frequencies), ESPARSE_EINVAL, "positions / frequencies is null");
+  if ((q && (rc = check_stride(ctx, T, q_row, ldq, "ldq"))) || (k && (rc = check_stride(ctx, T, k_row, ldk, "ldk"))) || (v && (rc = check_stride(ctx, T, k_row, ldv, "ldv")))) return rc;
+  ESP_REQUIRE(ctx, aligned_to(q, 2) && aligned_to(k, 2) && aligned_to(v, 2) && aligned_to(q_weight, 2) && aligned_to(k_weight, 2) && aligned_to(q_out, 2) && aligned_to(k_out, 2) &&
+                       aligned_to(positions, 4) && aligned_to(frequencies, 4) && aligned_to(slots, 4),
+              ESPARSE_EINVAL, "a pointer is not aligned to its type");
+  const esparse_cache none = {};
+  const esparse_cache& c = cache ? *cache : none;
+  const Stretch all[] = {{q_out, 2 * (size_t)(T * q_row)}, {k_out, 2 * (size_t)(T * k_row)}, {c.k_data, data}, {c.k_scales, scales}, {c.v_data, data}, {c.v_scales, scales},
+                         {q, q ? rows_bytes(T, q_row, ldq, 2) : 0}, {k, k ? rows_bytes(T, k_row, ldk, 2) : 0}, {v, v ? rows_bytes(T, k_row, ldv, 2) : 0}, {q_weight, 2 * (size_t)D},
+                         {k_weight, 2 * (size_t)D}, {positions, 4 * (size_t)T}, {frequencies, 2 * (size_t)h->rotary}, {slots, 4 * (size_t)T}};
+  ESP_REQUIRE(ctx, apart(all, 6, 14), ESPARSE_EINVAL, "an output or the cache overlaps an input or another output");
+  const DeviceOfCall device(ctx->device);
+  ESP_HIP(ctx, device.error());
+  return esp_rotate_heads_device(ctx, h, T, dtype, q, ldq, q_weight, k, ldk, k_weight, positions, frequencies, q_out, k_out, v, ldv, cache, slots);
+}
+
+int esparse_cache_read(esparse_ctx* ctx, const esparse_cache* cache, const int32_t* slots, long long T, esparse_dtype dtype, void* k_out, void* v_out) {
+  if (!ctx) return ESPARSE_EINVAL;
+  int rc = check_dtype_or_f32(ctx, dtype);
+  if (rc) return rc;
+  ESP_REQUIRE(ctx, cache, ESPARSE_EINVAL, "cache is null");
+  size_t data = 0, scales = 0;
+  if ((rc = check_cache(ctx, cache, &data, &scales))) return rc;
+  ESP_REQUIRE(ctx, T >= 0 && T <= kMaxRows && T * cache->heads <= kMaxHeadRows, ESPARSE_EINVAL, "%lld tokens of %d heads are out of range", T, cache->heads);
+  if (T == 0) return ESPARSE_OK;
+  ESP_REQUIRE(ctx, slots && (k_out || v_out), ESPARSE_EINVAL, "slots, or both outputs, are null");
+  ESP_REQUIRE(ctx, aligned_to(slots, 4) && aligned_to(k_out, dtype_bytes(dtype)) && aligned_to(v_out, dtype_bytes(dtype)), ESPARSE_EINVAL, "a pointer is not aligned to its type");
+  const size_t out = (size_t)T * cache->heads * cache->head_dim * dtype_bytes(dtype);
+  const Stretch all[] = {{k_out, out}, {v_out, out}, {cache->k_data, data}, {cache->k_scales, scales}, {cache->v_data, data}, {cache->v_scales, scales}, {slots, 4 * (size_t)T}};
+  ESP_REQUIRE(ctx, apart(all, 2, 7), ESPARSE_EINVAL, "an output overlaps an input or the other output");
+  const DeviceOfCall device(ctx->device);
+  ESP_HIP(ctx, device.error());
+  return esp_cache_read_device(ctx, cache, slots, T, dtype, k_out, v_out);
+}
+
+// sequences and rows: a launch has up to 2^23 workgroups for tiles of rows of a head
+static bool attention_sizes(const esparse_cache* c, long long T, int B, int q_heads, long long width, int ragged) {
+  return cache_sizes(c->pages, c->page, c->heads, c->head_dim) && T >= 0 && T <= kMaxRows && B >= 0 && B <= kMaxRows && q_heads >= 1 && q_heads <= kMaxHeads &&
+         q_heads % c->heads == 0 && width >= 0 && width < (1ll << 31) / c->page && (ragged == 0 || ragged == 1) && (ragged || T == B) && (T + B) * q_heads <= kMaxHeadRows / 16;
+}
+
+int esparse_cache_attention_workspace(const esparse_cache* cache, long long T, int B, int q_heads, long long width, int ragged, size_t* bytes) {
+  if (!bytes || !cache || !attention_sizes(cache, T, B, q_heads, width, ragged)) return ESPARSE_EINVAL;
+  *bytes = T && B ? esp_cache_attention_workspace(cache, T, B, q_heads, width, ragged) : 0;
+  return ESPARSE_OK;
+}
+
+int esparse_cache_attention(esparse_ctx* ctx, const void* q, long long ldq, long long T, int q_heads, esparse_dtype dtype, const esparse_cache* cache,
+                            const int32_t* table, long long width, const int32_t* lengths, const int32_t* starts, int B, double scale, void* out, float* lse,
+                            void* workspace, size_t workspace_bytes) {
+  if (!ctx) return ESPARSE_EINVAL;
+  int rc = check_dtype(ctx, dtype);
+  if (rc) return rc;
+  ESP_REQUIRE(ctx, cache, ESPARSE_EINVAL, "cache is null");
+  size_t data = 0, scales = 0;
+  if ((rc = check_cache(ctx, cache, &data, &scales))) return rc;
+  ESP_REQUIRE(ctx, starts || T == B, ESPARSE_EINVAL, "%lld queries of %d sequences without starts", T, B);
+  ESP_REQUIRE(ctx, attention_sizes(cache, T, B, q_heads, width, starts != nullptr), ESPARSE_EINVAL,
+              "T = %lld, B = %d, q_heads = %d (on %d heads) or width = %lld out of range", T, B, q_heads, cache->heads, width);
+  ESP_REQUIRE(ctx, std::isfinite(scale), ESPARSE_EINVAL, "scale is not finite");
+  if (T == 0 || B == 0) return ESPARSE_OK;
+  ESP_REQUIRE(ctx, q && out && lengths && (table || width == 0), ESPARSE_EINVAL, "q / out / lengths / table is null");
+  const long long row = (long long)q_heads * cache->head_dim;
+  if ((rc = check_stride(ctx, T, row, ldq, "ldq"))) return rc;
+  ESP_REQUIRE(ctx, aligned_to(q, 2) && aligned_to(out, 2) && aligned_to(lse, 4) && aligned_to(table, 4) && aligned_to(lengths, 4) && aligned_to(starts, 4), ESPARSE_EINVAL,
+              "a pointer is not aligned to its type");
+  const size_t need = esp_cache_attention_workspace(cache, T, B, q_heads, width, starts != nullptr);
+  ESP_REQUIRE(ctx, need == 0 || workspace, ESPARSE_EINVAL, "workspace is null, %zu bytes needed", need);
+  ESP_REQUIRE(ctx, need == 0 || workspace_bytes >= need, ESPARSE_EWORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, need);
+  ESP_REQUIRE(ctx, need == 0 || aligned_to(workspace, 256), ESPARSE_EINVAL, "workspace is not 256-byte aligned");
+  const Stretch all[] = {{out, 2 * (size_t)(T * row)}, {lse, 4 * (size_t)T * q_heads}, {workspace, need}, {q, rows_bytes(T, row, ldq, 2)}, {cache->k_data, data},
+                         {cache->k_scales, scales}, {cache->v_data, data}, {cache->v_scales, scales}, {table, 4 * (size_t)B * (size_t)width}, {lengths, 4 * (size_t)B},
+                         {starts, 4 * ((size_t)B + 1)}};
+  ESP_REQUIRE(ctx, apart(all, 3, 11), ESPARSE_EINVAL, "an output or the workspace overlaps an input or another output");
+  const DeviceOfCall device(ctx->device);
+  ESP_HIP(ctx, device.error());
+  return esp_cache_attention_device(ctx, q, ldq, T, q_heads, dtype, cache, table, width, lengths, starts, B, scale, out, lse, workspace);
+}
+
+int esparse_sample_workspace(long long R, long long V, size_t* bytes) {
+  if (!bytes || R < 0 || R > kMaxRows || V < 1 || V > ESPARSE_MAX_VOCABULARY || R * V > kMaxValues) return ESPARSE_EINVAL;
+  *bytes = R ? esp_sample_workspace(R, V) : 0;
+  return ESPARSE_OK;
+}
+
+int esparse_sample(esparse_ctx* ctx, const void* logits, long long R, long long V, long long ld, esparse_dtype dtype, const float* temperature,
+                   const int32_t* top_k, const float* top_p, const float* min_p, const float* u, int64_t* tokens, float* logprob, void* workspace,
+                   size_t workspace_bytes) {
+  if (!ctx) return ESPARSE_EINVAL;
+  const int rc = check_dtype_or_f32(ctx, dtype);
+  if (rc) return rc;
+  ESP_REQUIRE(ctx, V <= ESPARSE_MAX_VOCABULARY, ESPARSE_EUNSUPPORTED, "V = %lld is more than %lld", V, (long long)ESPARSE_MAX_VOCABULARY);
+  ESP_REQUIRE(ctx, R >= 0 && R <= kMaxRows && V >= 1 && R * V <= kMaxValues, ESPARSE_EINVAL, "R = %lld or V = %lld out of range", R, V);
+  if (R == 0) return ESPARSE_OK;
+  ESP_REQUIRE(ctx, logits && u && tokens, ESPARSE_EINVAL, "logits / u / tokens is null");
+  ESP_REQUIRE(ctx, ld >= V && ld < (1ll << 31), ESPARSE_EINVAL, "ld = %lld is less than V = %lld, or too large", ld, V);
+  ESP_REQUIRE(ctx, aligned_to(logits, dtype_bytes(dtype)) && aligned_to(temperature, 4) && aligned_to(top_k, 4) && aligned_to(top_p, 4) && aligned_to(min_p, 4) && aligned_to(u, 4) &&
+                       aligned_to(tokens, 8) && aligned_to(logprob, 4),
+              ESPARSE_EINVAL, "a pointer is not aligned to its type");
+  const size_t need = esp_sample_workspace(R, V);
+  ESP_REQUIRE(ctx, workspace, ESPARSE_EINVAL, "workspace is null, %zu bytes needed", need);
+  ESP_REQUIRE(ctx, workspace_bytes >= need, ESPARSE_EWORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, need);
+  ESP_REQUIRE(ctx, aligned_to(workspace, 256), ESPARSE_EINVAL, "workspace is not 256-byte aligned");
+  const size_t rows4 = 4 * (size_t)R;
+  const Stretch all[] = {{tokens, 2 * rows4}, {logprob, rows4}, {workspace, need}, {logits, rows_bytes(R, V, ld, dtype_bytes(dtype))}, {temperature, rows4}, {top_k, rows4},
+                         {top_p, rows4}, {min_p, rows4}, {u, rows4}};
+  ESP_REQUIRE(ctx, apart(all, 3, 9), ESPARSE_EINVAL, "an output or the workspace overlaps an input or another output");
+  const DeviceOfCall device(ctx->device);
+  ESP_HIP(ctx, device.error());
+  return esp_sample_device(ctx, logits, R, V, ld, dtype, temperature, top_k, top_p, min_p, u, reinterpret_cast<long long*>(tokens), logprob, workspace);
+}
+
 }  // extern "C"

@@ -197,3 +197,17 @@ int esp_rms_norm_device(esparse_ctx* ctx, const void* x, long long ldx, const vo
 size_t esp_token_logprobs_workspace(long long R, long long V, int dtype, int top);
 int esp_token_logprobs_device(esparse_ctx* ctx, const void* logits, long long R, long long V, long long ld, int dtype, const long long* tokens, int top,
                               float* logprob, float* entropy, int32_t* top_ids, float* top_logprobs, void* ws);
+
+// heads, the cache in 4 bits, attention over it, tokens drawn
+static inline int esp_cache_row(int head_dim) { return head_dim <= 64 ? 64 : (head_dim <= 128 ? 128 : 256); }  // channels of a row
+int esp_rotate_heads_device(esparse_ctx* ctx, const esparse_heads* h, long long T, int dtype, const void* q, long long ldq, const void* q_weight, const void* k,
+                            long long ldk, const void* k_weight, const int32_t* positions, const float* frequencies, void* q_out, void* k_out, const void* v,
+                            long long ldv, const esparse_cache* cache, const int32_t* slots);
+int esp_cache_read_device(esparse_ctx* ctx, const esparse_cache* cache, const int32_t* slots, long long T, int dtype, void* k_out, void* v_out);
+size_t esp_cache_attention_workspace(const esparse_cache* cache, long long T, int B, int q_heads, long long width, bool ragged);
+int esp_cache_attention_device(esparse_ctx* ctx, const void* q, long long ldq, long long T, int q_heads, int dtype, const esparse_cache* cache,
+                               const int32_t* table, long long width, const int32_t* lengths, const int32_t* starts, int B, double scale, void* out, float* lse,
+                               void* workspace);
+size_t esp_sample_workspace(long long R, long long V);
+int esp_sample_device(esparse_ctx* ctx, const void* logits, long long R, long long V, long long ld, int dtype, const float* temperature, const int32_t* top_k,
+                      const float* top_p, const float* min_p, const float* u, long long* tokens, float* logprob, void* ws);

@@ -142,6 +142,27 @@ __device__ __forceinline__ MxCodes mx_encode(const float (&v)[8], unsigned e) {
   return r;
 }
 
+// eight 4-bit codes as an operand of the 16-bit matrix instruction, times the scale s = 2^(E - 127).  bf16: exact up to the
+// type's largest number.  f16: rounded to even where the scaled number is none (no multiple of 2^-24), infinite beyond 65504
+template <int DT>
+__device__ __forceinline__ uint4 mx_widen(uint32_t w, float s) {
+  uint4 r = {0u, 0u, 0u, 0u};
+#if defined(__HIP_DEVICE_COMPILE__)
+  if (DT == ESPARSE_F16) {
+    r.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, 0));
+    r.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, 1));
+    r.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, 2));
+    r.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, 3));
+  } else {
+    r.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 0));
+    r.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 1));
+    r.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 2));
+    r.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 3));
+  }
+#endif
+  return r;
+}
+
 // the four scales of 16 lanes (128 channels), as the 32-bit word they are stored as; every lane of the 16 gets it
 __device__ __forceinline__ uint32_t mx_scale_word(unsigned e, unsigned lane) {
   uint32_t w = e << (8u * ((lane >> 2) & 3u));

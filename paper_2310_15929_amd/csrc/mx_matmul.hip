@@ -83,27 +83,6 @@ __device__ __forceinline__ floatx4_t mx_mfma(uint4 a, uint32_t as, const MxB<ACT
 // The scale of the widening conversions, from the low byte of e: they take its exponent alone (tested for all 256), with 0 for 2^-127 and 255 for NaN
 __device__ __forceinline__ float mx_widen_scale(uint32_t e) { return __builtin_bit_cast(float, e << 23); }
 
-// one 32-bit word of a weight unit (eight channels) as the A operand of the 16-bit instruction, times 2^(E - 127).  bf16: exact up to the
-// type's largest number.  f16: rounded to even where the scaled number is none (no multiple of 2^-24), infinite beyond 65504
-template <int DT>
-__device__ __forceinline__ uint4 mx_widen(uint32_t w, float s) {
-  uint4 r = {0u, 0u, 0u, 0u};
-#if defined(__HIP_DEVICE_COMPILE__)
-  if (DT == ESPARSE_F16) {
-    r.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, 0));
-    r.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, 1));
-    r.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, 2));
-    r.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, s, 3));
-  } else {
-    r.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 0));
-    r.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 1));
-    r.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 2));
-    r.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 3));
-  }
-#endif
-  return r;
-}
-
 __device__ __forceinline__ uint16_t to_16(float f, int out) { return out == ESPARSE_F16 ? esp_from_float<ESPARSE_F16>(f) : esp_from_float<ESPARSE_BF16>(f); }
 // four neighbouring output features of a token
 __device__ __forceinline__ void store_4(const MxGemmArgs& a, long long t, long long n, floatx4_t v) {

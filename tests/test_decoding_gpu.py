@@ -1,0 +1,615 @@
+"""Heads, the cache in 4 bits, attention over it and the draw of a token on the GPU, against plain 64-bit implementations (oracle/decoding_oracle.py).
+
+Tolerances are derived, not fitted.  A rounding to 16 bits is off by at most half a step: 2^-8 (bf16), 2^-11 (f16) of the value.  Attention: the probabilities are rounded to 16 bits
+(half a step of each; f16: 2^-25 below 2^-14), scores are fp32 sums of D exact products (D 2^-23 of their magnitudes) and go through an fp32 product and exponential (2^-21 of their size), the output is
+rounded once.  The relative error of a probability counts for the sum and for the product: twice.  The smallest normal number of 32 bits is 2^-126: the exponential of less is 0
+and a product of less may be, so that each of n tokens can lose 2^-126 (1 + |v|) where the largest probability, before the division by their sum (1 or more), is 1.
+"""
+import ctypes as C
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2310_15929_amd as esp
+from oracle import decoding_oracle as orc
+
+pytestmark = pytest.mark.gpu
+
+TORCH = {"f16": torch.float16, "bf16": torch.bfloat16, "f32": torch.float32}
+HALF = {torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 ** -8, torch.float32: 2.0 ** -24}
+TINY = {torch.float16: 2.0 ** -25, torch.bfloat16: 2.0 ** -134, torch.float32: 2.0 ** -150}
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    assert torch.cuda.is_available()
+    return esp.Context(0)
+
+
+def _rng(*key):
+    return np.random.default_rng([int.from_bytes(str(k).encode(), "little") % (1 << 31) for k in key])
+
+
+def _np(t):
+    return t.double().cpu().numpy()
+
+
+def _i32(a):
+    return torch.tensor(np.asarray(a), dtype=torch.int32, device="cuda")
+
+
+def _freq(rotary, base=1e6):
+    return (base ** (-np.arange(rotary // 2) * 2.0 / max(rotary, 1))).astype(np.float32)
+
+
+def _close16(got, want, dtype, what=""):
+    tol = (HALF[dtype] + 2.0 ** -23) * np.abs(want) + TINY[dtype]
+    ok = np.abs(got - want) <= tol
+    assert ok.all(), (what, np.abs(got - want)[~ok].max())
+
+
+def _stored(cache, slots):
+    """(bytes, scales) of keys and values at slots, [T, heads, ..]"""
+    P, H, page, _ = cache.k_data.shape
+    s = np.asarray(slots)
+    out = []
+    for t in (cache.k_data, cache.k_scales, cache.v_data, cache.v_scales):
+        out.append(t.cpu().numpy()[s // page, :, s % page])
+    return out
+
+
+# ---- heads ------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("T,Hq,Hkv,D,rotary,paired,norm,page", [
+    (1, 1, 1, 1, 0, False, False, 16), (1, 4, 4, 64, 64, False, True, 16), (3, 5, 1, 6, 6, False, True, 32), (7, 6, 2, 33, 20, True, True, 16),
+    (5, 4, 2, 80, 36, False, False, 64), (5, 4, 2, 80, 36, True, True, 64), (9, 15, 5, 96, 96, False, True, 16), (17, 8, 8, 128, 128, False, True, 1024),
+    (4, 3, 3, 128, 64, False, False, 128), (6, 2, 1, 200, 200, False, True, 64), (33, 7, 7, 256, 256, True, True, 32), (2, 40, 40, 128, 128, False, False, 16),
+    (1500, 2, 1, 72, 48, False, True, 64)])
+def test_heads(ctx, T, Hq, Hkv, D, rotary, paired, norm, page, dtype):
+    rng, dt = _rng(T, Hq, D, rotary, dtype), TORCH[dtype]
+    qkv = torch.from_numpy(rng.standard_normal((T, Hq + 2 * Hkv, D)) * np.exp(rng.standard_normal(D))).to(dt).cuda()
+    q, k, v = qkv.split((Hq, Hkv, Hkv), 1)
+    qw, kw = (torch.from_numpy(1 + 0.2 * rng.standard_normal(D)).to(dt).cuda() for _ in range(2)) if norm else (None, None)
+    positions = rng.integers(0, 1 << 20, T).astype(np.int32)
+    positions[0] = 0
+    freq = _freq(rotary) if rotary else None
+    pages = -(-T // page) + 2
+    cache = ctx.kv_cache(pages, page, Hkv, D)
+    slots = rng.permutation(pages * page)[:T].astype(np.int32)
+    tf = torch.from_numpy(freq).cuda() if rotary else None
+    for keys_out in (True, False):
+        qo, ko = ctx.rotate_heads(q, k, _i32(positions) if rotary else None, tf, q_weight=qw, k_weight=kw, paired=paired, v=v, cache=cache, slots=_i32(slots), keys_out=keys_out)
+        want_q = orc.rotate(_np(q), None if qw is None else _np(qw), 1e-6, positions, freq, paired)
+        want_k = orc.rotate(_np(k), None if kw is None else _np(kw), 1e-6, positions, freq, paired)
+        # (sines and cosines of the oracle are off by the rounding of its angle)
+        slack = 2.0 ** -52 * (1 << 20) * np.abs(want_q).max()
+        assert (np.abs(_np(qo) - want_q) <= (HALF[dt] + 2.0 ** -23) * np.abs(want_q) + TINY[dt] + slack).all()
+        assert (ko is None) != keys_out
+        if keys_out:
+            assert (np.abs(_np(ko) - want_k) <= (HALF[dt] + 2.0 ** -23) * np.abs(want_k) + TINY[dt] + 2.0 ** -32 * np.abs(want_k).max()).all()
+        kd, ks, vd, vs = _stored(cache, slots)
+        for x, d, s in ((want_k, kd, ks), (_np(v), vd, vs)):
+            wd, ws = orc.cache_rows(x)
+            assert np.array_equal(s, ws) and np.array_equal(orc.cache_values(d, s, D), orc.cache_values(wd, ws, D))
+            assert (orc.cache_values(d, s, orc.row_of(D))[..., D:] == 0).all()
+    free = np.setdiff1d(np.arange(pages * page), slots)
+    assert all((t == 0).all() for t in _stored(cache, free))
+    gk, gv = ctx.cache_read(cache, _i32(slots), torch.float32)
+    assert np.array_equal(_np(gk), orc.cache_values(kd, ks, D)) and np.array_equal(_np(gv), orc.cache_values(vd, vs, D))
+
+
+@pytest.mark.parametrize("D", [64, 96, 128, 256])
+def test_results_on_a_border_of_two_codes(ctx, D):
+    """Rows of one magnitude have the norm as an exact number: their quotients are weights, many of them right between two codes; position 0 turns nothing."""
+    rng = _rng("border", D)
+    T, weights = 40, np.array([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 6.0, 0.5, 7.0])
+    mag = 2.0 ** rng.integers(-6, 6, (T, 1, 1)) * rng.choice([1.0, 1.5, 3.0, 1.25], (T, 1, 1))
+    x = mag * rng.choice([-1.0, 1.0], (T, 2, D))
+    w = rng.choice(weights, D)
+    w[::32] = 7.0
+    k, kw = torch.from_numpy(x).to(torch.float16).cuda(), torch.from_numpy(w).to(torch.float16).cuda()
+    cache = ctx.kv_cache(3, 16, 2, D)
+    slots = np.arange(T)
+    for freq in (None, torch.from_numpy(_freq(D)).cuda()):
+        ctx.rotate_heads(None, k, _i32(np.zeros(T)) if freq is not None else None, freq, k_weight=kw, eps=0.0, v=k, cache=cache, slots=_i32(slots))
+        kd, ks, _, _ = _stored(cache, slots)
+        wd, ws = orc.cache_rows(np.sign(x) * w)
+        assert np.array_equal(ks, ws) and np.array_equal(kd, wd)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_far_positions(ctx, dtype):
+    """Angles of 2^31 - 1 radians and more, against integers of any size."""
+    import fractions
+    positions, freq = np.array([2 ** 31 - 1, -2 ** 31, 123456789, 16777217], np.int32), np.array([1.0, 0.7310585975646973, 3e-5, 97.53099822998047], np.float32)
+    pi = fractions.Fraction(3141592653589793238462643383279502884197169399375105820974944, 10 ** 60)
+    q = torch.zeros(4, 1, 8, dtype=TORCH[dtype])
+    q[:, 0, :4] = 1.0
+    qo, _ = ctx.rotate_heads(q.cuda(), None, torch.from_numpy(positions).cuda(), torch.from_numpy(freq).cuda())
+    want = np.zeros((4, 1, 8))
+    for t in range(4):
+        for i in range(4):
+            a = fractions.Fraction(int(positions[t])) * fractions.Fraction(float(freq[i]))
+            a = float(a - 2 * pi * round(a / (2 * pi)))
+            want[t, 0, i], want[t, 0, i + 4] = math.cos(a), math.sin(a)
+    assert (np.abs(_np(qo) - want) <= (HALF[TORCH[dtype]] + 2.0 ** -23) * np.abs(want) + 2.0 ** -40).all()
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_heads_that_are_not_finite(ctx, dtype):
+    D, dt = 128, TORCH[dtype]
+    x = torch.ones(4, 1, D, dtype=dt)
+    x[0, 0, 5], x[1, 0, 70], x[2] = math.nan, math.inf, 0.0
+    pos, freq, slots = _i32([1, 1, 1, 1]), torch.from_numpy(_freq(64)).cuda(), _i32([0, 1, 2, 3])
+    w = torch.ones(D, dtype=dt).cuda()
+    cache = ctx.kv_cache(1, 16, 1, D)
+    _, k = ctx.rotate_heads(None, x.cuda(), pos, freq, v=x.cuda(), cache=cache, slots=slots, keys_out=True)
+    k = _np(k)
+    assert set(np.flatnonzero(np.isnan(k[0, 0]))) == {5, 37} and set(np.flatnonzero(~np.isfinite(k[1, 0]))) == {70} and (k[2] == 0).all()
+    gk, gv = (_np(t) for t in ctx.cache_read(cache, slots, dt))
+    assert np.isnan(gk[0, 0, :64]).all() and np.isfinite(gk[0, 0, 64:]).all() and np.isnan(gk[1, 0, 64:96]).all() and np.isnan(gv[0, 0, :32]).all() and np.isfinite(gv[0, 0, 32:]).all()
+    q, _ = ctx.rotate_heads(x.cuda(), None, pos, freq, q_weight=w, eps=0.0)
+    q = _np(q)
+    assert np.isnan(q[0]).all() and np.isnan(q[2]).all() and np.isfinite(q[3]).all() and np.isnan(q[1, 0, 70]) and (q[1, 0, 64:70] == 0).all()
+
+
+def test_slots_given_twice_and_slots_that_are_none(ctx):
+    rng = _rng("slots")
+    T, H, D, page = 900, 2, 64, 32
+    k, v = (torch.from_numpy(rng.standard_normal((T, H, D))).to(torch.bfloat16).cuda() for _ in range(2))
+    cache = ctx.kv_cache(4, page, H, D)
+    slots = rng.integers(0, 100, T).astype(np.int32)
+    slots[::7], slots[::11], slots[::13] = -1, 128, 2 ** 31 - 1
+    ctx.rotate_heads(None, k, v=v, cache=cache, slots=_i32(slots))
+    for s in range(128):
+        at = np.flatnonzero(slots == s)
+        kd, ks, vd, vs = (t[0] for t in _stored(cache, [s]))
+        if not len(at):
+            assert (kd == 0).all() and (vs == 0).all()
+            continue
+        wd, ws = orc.cache_rows(_np(k[at[-1]:at[-1] + 1]))
+        xd, xs = orc.cache_rows(_np(v[at[-1]:at[-1] + 1]))
+        assert np.array_equal(ks, ws[0]) and np.array_equal(vs, xs[0]) and np.array_equal(kd, wd[0]) and np.array_equal(vd, xd[0])
+    a, b = ctx.cache_read(cache, _i32([-1, 128, -2 ** 31]), torch.float16)
+    assert (a == 0).all() and (b == 0).all()
+
+
+@pytest.mark.parametrize("offset,gap", [(0, 0), (1, 3), (3, 64), (7, 1)])
+def test_tokens_apart_and_unaligned(ctx, offset, gap):
+    T, H, D = 9, 3, 100
+    base = torch.from_numpy(_rng("apart", gap).standard_normal(T * (H * D + gap) + offset)).to(torch.float16).cuda()
+    q = torch.as_strided(base, (T, H, D), (H * D + gap, D, 1), offset)
+    pos = np.arange(T, dtype=np.int32) * 1000
+    qo, ko = ctx.rotate_heads(q, q, _i32(pos), torch.from_numpy(_freq(D)).cuda())
+    want = orc.rotate(_np(q), None, 0, pos, _freq(D), False)
+    assert torch.equal(qo, ko) and (np.abs(_np(qo) - want) <= (HALF[torch.float16] + 2.0 ** -23) * np.abs(want) + 2.0 ** -25).all()
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+def test_cache_read_of_every_code_and_scale(ctx, dtype):
+    dt = TORCH[dtype]
+    page, H, D = 1024, 1, 64
+    cache = ctx.kv_cache(1, page, H, D)
+    data = np.tile(np.arange(256, dtype=np.uint8), 128).reshape(1, 1, page, 32)
+    scales = np.repeat(np.arange(256, dtype=np.uint8), 8).reshape(1, 1, page, 2)
+    cache.k_data.copy_(torch.from_numpy(data)), cache.k_scales.copy_(torch.from_numpy(scales))
+    slots = np.arange(page, dtype=np.int32)
+    k, _ = ctx.cache_read(cache, _i32(slots), dt)
+    want = torch.from_numpy(orc.cache_values(data[0, 0], scales[0, 0], D)).to(dt)
+    assert np.array_equal(_np(k)[:, 0], want.double().numpy(), equal_nan=True)
+
+
+# ---- attention --------------------------------------------------------------------------------------
+def _pool(rng, pages, H, page, D, low=-4, high=1):
+    row = orc.row_of(D)
+    data = rng.integers(0, 256, (pages, H, page, row // 2)).astype(np.uint8)
+    scales = (127 + rng.integers(low, high, (pages, H, page, row // 32))).astype(np.uint8)
+    # the channels from D on are zero, as they are written
+    code = np.stack((data & 15, data >> 4), -1).reshape(pages, H, page, row)
+    code[..., D:] = 0
+    return code[..., 0::2] | code[..., 1::2] << 4, scales
+
+
+def _cache(k, v, D):
+    return esp.KVCache(*(torch.from_numpy(t).cuda() for t in (*k, *v)), D)
+
+
+def _gather(pool, table_row, n, page, h, D):
+    """Values [n, D] of one head and which tokens are there."""
+    data, scales = pool
+    out, there = np.zeros((n, D)), np.zeros(n, bool)
+    for at in range(0, n, page):
+        p = table_row[at // page]
+        if 0 <= p < len(data):
+            m = min(page, n - at)
+            out[at:at + m] = orc.cache_values(data[p, h, :m], scales[p, h, :m], D)
+            there[at:at + m] = True
+    return out, there
+
+
+def _check_attention(ctx, q, k, v, table, lengths, starts, page, D, dtype, scale=None, heads=None, lse=True, got=None):
+    """q[T, Hq, D] on the GPU; k, v: (bytes, scales)."""
+    dt = TORCH[dtype]
+    T, Hq, _ = q.shape
+    H = k[0].shape[1]
+    cache = _cache(k, v, D)
+    s = D ** -0.5 if scale is None else scale
+    if got is None:
+        got = ctx.cache_attention(q, cache, _i32(table), _i32(lengths), starts=None if starts is None else _i32(starts), scale=scale, lse=True)
+    out, sums = (_np(t) for t in got)
+    qn = _np(q)
+    bounds = np.arange(len(lengths) + 1) if starts is None else starts
+    for b, n in enumerate(lengths):
+        lo, hi = bounds[b], bounds[b + 1]
+        m = hi - lo
+        for h in (range(Hq) if heads is None else heads):
+            kk, there = _gather(k, table[b], n, page, h // (Hq // H), D)
+            vv, _ = _gather(v, table[b], n, page, h // (Hq // H), D)
+            place = np.flatnonzero(there)
+            last = np.array([np.searchsorted(place, n - m + i, side="right") - 1 for i in range(m)])
+            want, wl, spread, mass, off = orc.attend(qn[lo:hi, h], kk[there], vv[there], s, last)
+            half = HALF[dt]
+            tol = half * np.abs(want) + TINY[dt] + (half + 2 * off[:, None] + n * 2.0 ** -23) * spread * 1.01 + (2.0 ** -24 * mass if dtype == "f16" else 0) + 2.0 ** -126 * (mass + n)
+            bad = ~(np.abs(out[lo:hi, h] - want) <= tol)
+            assert not bad.any(), (b, h, n, m, np.argwhere(bad)[:5], out[lo:hi, h][bad][:5], want[bad][:5], tol[bad][:5])
+            none = np.isinf(wl)
+            assert np.array_equal(np.isneginf(sums[lo:hi, h]), none) and (np.abs(sums[lo:hi, h] - wl)[~none] <= (2 * off + n * 2.0 ** -23 + np.abs(wl) * 2.0 ** -22 + 2.0 ** -21)[~none]).all()
+    return got
+
+
+def _tables(rng, lengths, page, extra=3):
+    need = [-(-n // page) for n in lengths]
+    order = rng.permutation(sum(need) + extra)
+    table = np.full((len(lengths), max(max(need), 1) + 1), -1, np.int32)
+    at = 0
+    for b, n in enumerate(need):
+        table[b, :n] = order[at:at + n]
+        at += n
+    return table, len(order)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("lengths,Hq,H,D,page", [
+    ([1], 1, 1, 1, 16), ([0, 1, 2, 15, 16, 17, 31, 32, 33], 2, 2, 64, 16), ([63, 64, 65, 127, 128, 129, 0], 8, 2, 128, 64), ([300, 5, 1000], 20, 5, 80, 32),
+    ([777], 32, 32, 128, 64), ([513, 511], 17, 1, 256, 128), ([2049], 40, 2, 33, 1024), ([40] * 70, 4, 4, 64, 16), ([5000], 6, 1, 192, 16)])
+def test_attention_of_one_token_each(ctx, lengths, Hq, H, D, page, dtype):
+    rng = _rng("one", len(lengths), Hq, D, dtype)
+    table, pages = _tables(rng, lengths, page)
+    k, v = _pool(rng, pages, H, page, D), _pool(rng, pages, H, page, D)
+    q = torch.from_numpy(rng.standard_normal((len(lengths), Hq, D))).to(TORCH[dtype]).cuda()
+    _check_attention(ctx, q, k, v, table, lengths, None, page, D, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("lengths,queries,Hq,H,D,page", [
+    ([5, 40, 100], [5, 1, 3], 4, 2, 64, 16), ([70, 3, 0, 200], [70, 7, 2, 31], 3, 1, 128, 32), ([260, 1, 130], [130, 0, 130], 10, 5, 80, 64),
+    ([400], [400], 2, 2, 128, 64), ([333, 150], [33, 150], 12, 2, 256, 16), ([129, 64, 65, 1], [129, 64, 65, 1], 1, 1, 96, 16), ([600], [300], 8, 1, 128, 128)])
+def test_attention_of_several_tokens(ctx, lengths, queries, Hq, H, D, page, dtype):
+    """Prompts, drafts, sequences without queries or with more queries than tokens."""
+    rng = _rng("several", *lengths, D, dtype)
+    table, pages = _tables(rng, lengths, page)
+    k, v = _pool(rng, pages, H, page, D), _pool(rng, pages, H, page, D)
+    starts = np.concatenate(([0], np.cumsum(queries)))
+    q = torch.from_numpy(rng.standard_normal((starts[-1], Hq, D))).to(TORCH[dtype]).cuda()
+    _check_attention(ctx, q, k, v, table, lengths, starts, page, D, dtype)
+
+
+@pytest.mark.parametrize("nq", [1, 3, 200])
+def test_attention_leaves_out_pages_that_are_none(ctx, nq):
+    rng = _rng("pages", nq)
+    lengths, page, D, H = [333, 260], 32, 128, 2
+    table, pages = _tables(rng, lengths, page)
+    table[0, 2], table[0, 5], table[0, 10], table[1, 0] = -1, pages, 2 ** 31 - 1, -2 ** 31
+    k, v = _pool(rng, pages, H, page, D), _pool(rng, pages, H, page, D)
+    starts = None if nq == 1 else np.array([0, nq, 2 * nq])
+    q = torch.from_numpy(rng.standard_normal((2 * nq, 4, D))).to(torch.float16).cuda()
+    _check_attention(ctx, q, k, v, table, lengths, starts, page, D, "f16")
+    table[0] = -1
+    out, sums = _check_attention(ctx, q, k, v, table, lengths, starts, page, D, "f16")
+    assert (out[:nq] == 0).all() and torch.isneginf(sums[:nq]).all()
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("nq", [1, 5, 160])
+def test_attention_is_not_touched_by_what_it_does_not_see(ctx, nq, dtype):
+    """Bytes behind a sequence, and later tokens of a prompt, hold NaN and the largest scales."""
+    rng = _rng("unseen", nq, dtype)
+    D, page, H, n = 128, 32, 2, 209
+    table, pages = _tables(rng, [n], page)
+    k, v = _pool(rng, pages, H, page, D), _pool(rng, pages, H, page, D)
+    q = torch.from_numpy(rng.standard_normal((nq, 4, D))).to(TORCH[dtype]).cuda()
+    starts = None if nq == 1 else np.array([0, nq])
+    first = ctx.cache_attention(q, _cache(k, v, D), _i32(table), _i32([n]), starts=None if starts is None else _i32(starts), lse=True)
+    for t in (k, v):
+        t[1][:] = np.where(np.isin(np.arange(pages), table[0, : -(-n // page)])[:, None, None, None], t[1], 255)
+        t[1][table[0, n // page], :, n % page:] = 255
+    again = ctx.cache_attention(q, _cache(k, v, D), _i32(table), _i32([n]), starts=None if starts is None else _i32(starts), lse=True)
+    assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+    # a value without number: its block of channels, for the queries that see the token; a key: all of their channels
+    seen = n - 1 - nq // 2   # the token of the middle query
+    at = (table[0, seen // page], 0, seen % page)
+    v[1][at + (2,)] = 255
+    third = ctx.cache_attention(q, _cache(k, v, D), _i32(table), _i32([n]), starts=None if starts is None else _i32(starts), lse=True)
+    o, w = _np(third[0]), _np(first[0])
+    sees = np.arange(nq) + n - nq >= seen
+    assert np.isnan(o[sees][:, :2, 64:96]).all() and np.array_equal(o[~sees], w[~sees]) and np.array_equal(o[:, 2:], w[:, 2:])
+    assert np.array_equal(o[:, :2, :64], w[:, :2, :64]) and np.array_equal(o[:, :2, 96:], w[:, :2, 96:]) and torch.equal(third[1], first[1])
+    k[1][at + (1,)] = 255
+    o = _np(ctx.cache_attention(q, _cache(k, v, D), _i32(table), _i32([n]), starts=None if starts is None else _i32(starts)))
+    assert np.isnan(o[sees][:, :2]).all() and np.array_equal(o[~sees], w[~sees]) and np.array_equal(o[:, 2:], w[:, 2:])
+
+
+def test_attention_leaves_rows_of_no_sequence(ctx):
+    rng = _rng("rows")
+    D, page, H = 64, 16, 1
+    lengths, starts = [40, 9], np.array([2, 5, 14])
+    table, pages = _tables(rng, lengths, page)
+    k, v = _pool(rng, pages, H, page, D), _pool(rng, pages, H, page, D)
+    q = torch.from_numpy(rng.standard_normal((20, 3, D))).to(torch.bfloat16).cuda()
+    out = torch.full_like(q, 7.0)
+    got, sums = ctx.cache_attention(q, _cache(k, v, D), _i32(table), _i32(lengths), starts=_i32(starts), out=out, lse=True)
+    assert got is out and (out[:2] == 7).all() and (out[14:] == 7).all()
+    _check_attention(ctx, q, k, v, table, lengths, starts, page, D, "bf16", got=(got, sums))
+    # starts that go past the rows, or back, and lengths past the table reach nothing outside
+    for bad, n in (([0, 20, 900], [40, 9]), ([0, 30, 10], [40, 9]), ([-5, 3, 20], [2 ** 31 - 1, -3])):
+        ctx.cache_attention(q, _cache(k, v, D), _i32(table), _i32(n), starts=_i32(bad), out=out)
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dtype,factor", [("f16", 30.0), ("bf16", 300.0)])
+def test_attention_with_sharp_scores(ctx, dtype, factor):
+    """Scores hundreds apart: probabilities of 0 and 1, maxima that keep rising."""
+    rng = _rng("sharp", dtype)
+    lengths, page, D, H = [700, 90], 16, 128, 1
+    table, pages = _tables(rng, lengths, page)
+    k, v = _pool(rng, pages, H, page, D), _pool(rng, pages, H, page, D)
+    q = torch.from_numpy(factor * rng.standard_normal((90, 2, D))).to(TORCH[dtype]).cuda()
+    _check_attention(ctx, q, k, v, table, lengths, np.array([0, 50, 90]), page, D, dtype)
+    _check_attention(ctx, q[:2], k, v, table, lengths, None, page, D, dtype, scale=-0.05)
+
+
+def test_attention_long_context(ctx):
+    rng = _rng("long")
+    n, page, D, H = 40001, 64, 128, 2
+    table, pages = _tables(rng, [n, 17], page)
+    k, v = _pool(rng, pages, H, page, D), _pool(rng, pages, H, page, D)
+    q = torch.from_numpy(2 * rng.standard_normal((2, 16, D))).to(torch.bfloat16).cuda()
+    _check_attention(ctx, q, k, v, table, [n, 17], None, page, D, "bf16", heads=[0, 7, 8, 15])
+
+
+def test_attention_queries_apart(ctx):
+    rng = _rng("apart")
+    lengths, page, D, H = [100, 50], 16, 80, 2
+    table, pages = _tables(rng, lengths, page)
+    k, v = _pool(rng, pages, H, page, D), _pool(rng, pages, H, page, D)
+    base = torch.from_numpy(rng.standard_normal(1 + 33 * (4 * D + 5))).to(torch.float16).cuda()
+    q = torch.as_strided(base, (33, 4, D), (4 * D + 5, D, 1), 1)
+    _check_attention(ctx, q, k, v, table, lengths, np.array([0, 30, 33]), page, D, "f16")
+
+
+def test_attention_beyond_32_bits(ctx):
+    """A pool of more than 2^32 bytes of keys: pages at its end."""
+    page, D, H = 64, 256, 8
+    pages = (1 << 32) // (page * H * D // 2) + 40
+    cache = ctx.kv_cache(pages, page, H, D)
+    rng = _rng("far")
+    n, T = 150, 150
+    table = np.array([[pages - 1, 3, pages - 2]], np.int32)
+    slots = table[0][np.arange(T) // page].astype(np.int64) * page + np.arange(T) % page
+    x = [torch.from_numpy(rng.standard_normal((T, H, D))).to(torch.bfloat16).cuda() for _ in range(2)]
+    ctx.rotate_heads(None, x[0], v=x[1], cache=cache, slots=_i32(slots))
+    k, v = (_np(t) for t in ctx.cache_read(cache, _i32(slots), torch.float32))
+    for got, given in ((k, x[0]), (v, x[1])):
+        wd, ws = orc.cache_rows(_np(given))
+        assert np.array_equal(got, orc.cache_values(wd, ws, D))
+    q = torch.from_numpy(rng.standard_normal((1, H, D))).to(torch.bfloat16).cuda()
+    out = _np(ctx.cache_attention(q, cache, _i32(table), _i32([n])))
+    for h in range(H):
+        want, _, spread, _, off = orc.attend(_np(q)[:, h], k[:, h], v[:, h], D ** -0.5, [n - 1])
+        assert (np.abs(out[:, h] - want) <= 2.0 ** -8 * np.abs(want) + (2.0 ** -8 + 2 * off[:, None] + n * 2.0 ** -23) * 1.01 * spread).all()
+
+
+def test_attention_captured_and_replayed(ctx):
+    rng = _rng("graph")
+    B, page, D, H, Hq = 3, 16, 128, 2, 8
+    table, pages = _tables(rng, [3000, 700, 20], page)
+    k, v = _pool(rng, pages, H, page, D), _pool(rng, pages, H, page, D)
+    cache, t = _cache(k, v, D), _i32(table)
+    q = torch.from_numpy(rng.standard_normal((B, Hq, D))).to(torch.float16).cuda()
+    lengths = _i32([3000, 700, 20])
+    ctx.cache_attention(q, cache, t, lengths)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = ctx.cache_attention(q, cache, t, lengths)
+    for now in ([3000, 700, 20], [1, 0, 20], [2999, 31, 7], [100, 700, 1]):
+        lengths.copy_(_i32(now))
+        q.mul_(-1.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, ctx.cache_attention(q, cache, t, lengths)), now
+
+
+# ---- drawing ----------------------------------------------------------------------------------------
+def _draw(ctx, x, u, what="", **cuts):
+    """x[R, V] on the GPU; cuts: a number or one for each row."""
+    R = len(x)
+    per_row = {n: np.broadcast_to(np.asarray(c), (R,)) for n, c in cuts.items()}
+    given = {n: torch.tensor(c.copy(), dtype=torch.int32 if n == "top_k" else torch.float32, device="cuda") for n, c in per_row.items()}
+    tokens, logprob = ctx.sample(x, torch.tensor(u, dtype=torch.float32, device="cuda"), **given)
+    got, lp, xn, un = tokens.cpu().numpy(), _np(logprob), _np(x), np.asarray(u, np.float32)
+    for r in range(R):
+        args = {n: (int(c[r]) if n == "top_k" else float(np.float32(c[r]))) for n, c in per_row.items()}
+        token, want, _ = orc.sample(xn[r], un[r], **args)
+        assert got[r] == token, (what, r, got[r], token, un[r], args)
+        assert (math.isnan(want) and math.isnan(lp[r])) or abs(lp[r] - want) <= 2.0 ** -24 * abs(want) + 2.0 ** -30, (what, r, lp[r], want)
+    return got
+
+
+CUTS = [dict(), dict(temperature=0.7), dict(top_k=1), dict(top_k=7), dict(top_p=0.5), dict(temperature=1.5, top_p=0.95), dict(min_p=0.1), dict(temperature=0.0),
+        dict(temperature=2.0, top_k=40, top_p=0.9, min_p=0.02), dict(temperature=0.3, top_k=1000, top_p=0.999), dict(top_p=0.0), dict(min_p=1.0), dict(top_p=1.0, top_k=0, min_p=0.0)]
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("R,V", [(1, 1), (5, 2), (3, 7), (4, 255), (6, 1000), (3, 4096), (2, 4097), (3, 20011), (40, 5003)])
+def test_drawn_tokens(ctx, R, V, dtype):
+    rng = _rng("draw", R, V, dtype)
+    x = torch.from_numpy(3 * rng.standard_normal((R, V))).to(TORCH[dtype]).cuda()
+    for i, cuts in enumerate(CUTS):
+        _draw(ctx, x, rng.random(R), str(cuts), **cuts)
+    _draw(ctx, x, np.linspace(0, 1, R), temperature=rng.choice([0.0, 0.5, 1.0, 3.0], R), top_k=rng.integers(-1, V + 2, R), top_p=rng.choice([0.2, 0.9, 1.5], R),
+          min_p=rng.choice([0.0, 0.01, 0.3], R))
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+def test_drawn_from_large_vocabularies(ctx, dtype):
+    rng = _rng("large", dtype)
+    for R, V in ((2, 131072), (20, 131075), (1, 1 << 20), (3, 300001)):
+        x = torch.from_numpy(2 * rng.standard_normal((R, V), dtype=np.float32)).to(TORCH[dtype])
+        x[:, rng.integers(0, V, 30)] += 8
+        for cuts in (dict(), dict(top_p=0.95), dict(top_k=50, top_p=0.9), dict(top_k=20000, temperature=1.2), dict(top_p=0.9999), dict(min_p=1e-3, temperature=0.8)):
+            _draw(ctx, x.cuda(), rng.random(R), str((V, cuts)), **cuts)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+def test_drawn_among_equal_logits(ctx, dtype):
+    """Rows of one value and of few: cuts fall among thousands of equal values, the lower indices are kept."""
+    rng = _rng("equal", dtype)
+    V = 30011
+    rows = [np.zeros(V), np.full(V, -7.5), rng.integers(0, 2, V) * 2.0, rng.integers(-3, 3, V).astype(float), np.where(np.arange(V) % 2, 0.0, -0.0),
+            np.where(rng.random(V) < 0.9, -np.inf, 1.0), np.where(np.arange(V) == 20000, 5.0, -100.0), np.linspace(-1e4, 1e4, V)]
+    x = torch.from_numpy(np.stack(rows)).to(TORCH[dtype]).cuda()
+    for cuts in (dict(), dict(top_k=1), dict(top_k=4999), dict(top_p=0.3), dict(top_k=9000, top_p=0.77), dict(min_p=0.5), dict(temperature=100.0, top_p=0.6), dict(temperature=1e-3)):
+        for u in (0.0, 0.35, 1 - 2.0 ** -24):
+            _draw(ctx, x, np.full(len(rows), u), str(cuts), **cuts)
+
+
+def test_drawn_tokens_follow_their_shares(ctx):
+    """Every token in turn: u just above and below the border of two shares, where 64 bits tell them apart."""
+    V = 64
+    w = np.random.default_rng(5).integers(1, 9, V).astype(float)
+    x = np.log(w).astype(np.float32)
+    share = np.exp(x.astype(np.float64))
+    upto = np.cumsum(share) / share.sum()
+    u = np.concatenate([np.float32(upto) - 2.0 ** -20, np.float32(upto[:-1]) + 2.0 ** -20]).astype(np.float32)
+    got = _draw(ctx, torch.from_numpy(np.tile(x, (len(u), 1))).cuda(), u)
+    assert list(got[:V]) == list(range(V)) and list(got[V:]) == list(range(1, V))
+
+
+def test_drawn_rows_that_are_not_finite(ctx):
+    V = 9000
+    x = torch.zeros(7, V)
+    x[0, 8999], x[1, 5], x[2, :], x[3, :4000] = math.nan, math.inf, -math.inf, -math.inf
+    x[4, 17] = -math.inf
+    got = _draw(ctx, x.cuda(), np.full(7, 0.25), temperature=[1, 1, 1, 1, 1, math.inf, -1.0], top_k=np.full(7, 5000))
+    assert list(got[[0, 1, 2, 5, 6]]) == [-1] * 5 and got[3] >= 4000
+    got = _draw(ctx, x.cuda(), [0.5, 0.5, 0.5, math.nan, 2.0, -1.0, 0.999], top_p=[0.5, 0.5, 0.5, math.nan, -1.0, 0.5, 0.5], min_p=[0, 0, 0, math.nan, 7.0, 0, 0])
+    assert got[3] == 4000
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_drawn_at_extreme_scales(ctx, dtype):
+    rng = _rng("extreme", dtype)
+    x = torch.from_numpy(np.concatenate([rng.standard_normal((1, 5000)) * s for s in (1e-30, 1e-5, 1e30, 3e37)])).to(TORCH[dtype]).cuda()
+    for t in (1e-38, 1e-20, 1.0, 1e20, 3e38):
+        for cuts in (dict(), dict(top_k=37), dict(top_p=0.4), dict(min_p=0.9)):
+            _draw(ctx, x, rng.random(4), str((t, cuts)), temperature=t, **cuts)
+
+
+def test_drawn_rows_apart_and_repeatable(ctx):
+    rng = _rng("apart")
+    base = torch.from_numpy(2 * rng.standard_normal(3 + 50 * 9001)).to(torch.bfloat16).cuda()
+    x = torch.as_strided(base, (50, 8190), (9001, 1), 3)
+    u = rng.random(50)
+    first = _draw(ctx, x, u, top_p=0.9, top_k=300)
+    given = dict(top_p=torch.full((50,), 0.9, device="cuda"), top_k=torch.full((50,), 300, dtype=torch.int32, device="cuda"))
+    uu = torch.tensor(u, dtype=torch.float32, device="cuda")
+    want = ctx.sample(x, uu, **given)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = ctx.sample(x, uu, **given)
+    for _ in range(4):
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out[0], want[0]) and torch.equal(out[1], want[1]) and list(first) == want[0].tolist()
+        assert torch.equal(ctx.sample(x, uu, **given)[1], want[1])
+
+
+# ---- together ---------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_steps_of_decoding(ctx, dtype):
+    """A prompt and then tokens one by one through the library's calls: norm, products in 4 bits, heads, cache, attention, logits, a token; the caches and attention of
+    every step against 64 bits, the tokens against the logits, on a stream of its own."""
+    dt, rng = TORCH[dtype], _rng("steps", dtype)
+    K, Hq, H, D, V, page, eps = 256, 4, 2, 64, 1000, 16, 1e-5
+
+    def weight(n, k):
+        return ctx.mx_pack(ctx.mx_quantize(torch.from_numpy(rng.standard_normal((n, k)) * k ** -0.5).to(dt).cuda(), esp.MX_FP4))
+    w_qkv, w_out, w_logits = weight((Hq + 2 * H) * D, K), weight(K, Hq * D), weight(V, K)
+    norm, embed = torch.ones(K, dtype=dt, device="cuda"), torch.from_numpy(rng.standard_normal((V, K))).to(dt).cuda()
+    qw = torch.from_numpy(1 + 0.1 * rng.standard_normal(D)).to(dt).cuda()
+    freq = _freq(D, 1e4)
+    tf, stream = torch.from_numpy(freq).cuda(), torch.cuda.Stream()
+    prompts = [list(rng.integers(0, V, n)) for n in (21, 1, 38)]
+    cache, tables, texts, new = ctx.kv_cache(12, page, H, D), np.array([[7, 2, 9, 0], [1, 3, 4, 5], [6, 8, 10, 11]], np.int32), [list(p) for p in prompts], [list(p) for p in prompts]
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        for step in range(6):
+            starts = np.concatenate(([0], np.cumsum([len(n) for n in new])))
+            positions = np.concatenate([np.arange(len(t) - len(n), len(t)) for t, n in zip(texts, new)])
+            slots = np.concatenate([tables[b][p // page] * page + p % page for b, p in enumerate(np.split(positions, starts[1:-1]))])
+            h = embed[torch.tensor(np.concatenate(new), device="cuda")]
+            y, _ = ctx.rms_norm(h, norm, eps)
+            qkv = ctx.mx_gemm(y, w_qkv).unflatten(1, (Hq + 2 * H, D))
+            q, k, v = qkv.split((Hq, H, H), 1)
+            q, _ = ctx.rotate_heads(q, k, _i32(positions), tf, q_weight=qw, k_weight=qw, eps=eps, v=v, cache=cache, slots=_i32(slots))
+            lengths = [len(t) for t in texts]
+            got = ctx.cache_attention(q, cache, _i32(tables), _i32(lengths), starts=_i32(starts) if step else _i32(starts), lse=True)
+            last = torch.tensor(starts[1:] - 1, device="cuda")
+            y, _ = ctx.rms_norm(ctx.mx_gemm(got[0].flatten(1), w_out)[last], norm, eps, residual=h[last].contiguous())
+            logits = ctx.mx_gemm(y, w_logits, dtype=torch.float32)
+            u = rng.random(3).astype(np.float32)
+            cuts = dict(temperature=torch.full((3,), 0.8, device="cuda"), top_k=torch.full((3,), 50, dtype=torch.int32, device="cuda"), top_p=torch.full((3,), 0.9, device="cuda"))
+            tokens, logprob = ctx.sample(logits, torch.from_numpy(u).cuda(), **cuts)
+            lp = ctx.token_logprobs(logits, tokens).logprob
+            stream.synchronize()
+            kd, ks, vd, vs = _stored(cache, slots)
+            want = orc.cache_rows(orc.rotate(_np(k), _np(qw), eps, positions, freq, False))
+            assert np.array_equal(kd, want[0]) and np.array_equal(ks, want[1]) and np.array_equal(vd, orc.cache_rows(_np(v))[0])
+            pools = [t.cpu().numpy() for t in (cache.k_data, cache.k_scales, cache.v_data, cache.v_scales)]
+            _check_attention(ctx, q, pools[:2], pools[2:], tables, lengths, starts, page, D, dtype, got=got)
+            for b in range(3):
+                token, share, kept = orc.sample(_np(logits)[b], u[b], float(np.float32(0.8)), 50, float(np.float32(0.9)))
+                assert token == int(tokens[b]) and abs(share - float(logprob[b])) <= 2.0 ** -24 * abs(share) + 2.0 ** -30 and math.isfinite(float(lp[b]))
+                texts[b].append(token)
+                new[b] = [token]
+
+
+def test_steps_on_another_stream_and_other_workspaces(ctx):
+    """Two graphs of attention replayed in turn, and calls on two streams at once, each with a workspace of its own."""
+    rng = _rng("streams")
+    page, D, H, n = 64, 128, 1, 20000
+    table, pages = _tables(rng, [n], page)
+    k, v = _pool(rng, pages, H, page, D), _pool(rng, pages, H, page, D)
+    cache, t, lengths = _cache(k, v, D), _i32(table), _i32([n])
+    qs = [torch.from_numpy(rng.standard_normal((1, 8, D))).to(torch.float16).cuda() for _ in range(2)]
+    want = [ctx.cache_attention(q, cache, t, lengths) for q in qs]
+    torch.cuda.synchronize()
+    graphs, outs = [], []
+    for q in qs:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(ctx.cache_attention(q, cache, t, lengths))
+        graphs.append(g)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(5):
+        got = []
+        for g, o in zip(graphs, outs):
+            g.replay()
+        for s, q in zip(streams, qs):
+            with torch.cuda.stream(s):
+                got.append(ctx.cache_attention(q, cache, t, lengths))
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs + got, want + want))
