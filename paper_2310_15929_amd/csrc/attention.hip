@@ -351,6 +351,217 @@ __global__ void __launch_bounds__(256) k_attend_join(const AttendArgs a) {
   }
 }
 
+// ---- prompts: many rows of a sequence ----------------------------------------------------------------
+// A workgroup of W waves takes 32 W rows, 32 a wave as the columns of the 32 x 32 instruction (lane 32 h + c: operands hold k = 8 h .. 8 h + 7 of row / column c, results rows
+// 8 (j / 4) + 4 h + j % 4 of column c).  The tokens come in tiles that all waves share, brought to 16 bits once, in two buffers: while one is multiplied the
+// codes of the tile after the next are on their way and the next is written to the other buffer.
+template <int DP>
+constexpr int kTile = DP == 256 ? 32 : 64;  // tokens of a tile
+template <int DP>
+constexpr int kKRow = DP + 8;   // 16-bit numbers from token to token: sixteen rows of 16 bytes lie in different banks
+template <int DP>
+constexpr int kWideV = DP + 32;  // four rows of 64 bytes do
+template <int DP>
+constexpr int kBuffer = kTile<DP> * (kKRow<DP> + kWideV<DP>);
+
+template <int DT>
+__device__ __forceinline__ floatx16_t mfma32(uint4 a, uint4 b, floatx16_t c) {
+  if (DT == ESPARSE_F16) return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8_t, a), __builtin_bit_cast(half8_t, b), c, 0, 0, 0);
+  else return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
+}
+
+template <int DT, int DP, int W>
+__global__ void __launch_bounds__(64 * W) k_attend_many(const AttendArgs a) {
+  constexpr int TT = kTile<DP>, TB = TT / 32, NS = DP / 16, ND = DP / 32, THREADS = 64 * W;
+  constexpr int CH = TT * DP / 32;                       // pieces of 16 bytes (a block) of the keys of a tile, and of the values
+  constexpr int ITEMS = (2 * CH + THREADS - 1) / THREADS;  // of a thread
+  static_assert(CH % 64 == 0, "whole waves");
+  extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+  __shared__ unsigned long long odd[2][2 * CH / 64];  // keys whose page is none, values without number
+  uint16_t* buffers = reinterpret_cast<uint16_t*>(lds);
+  const int wave = wave_uniform((int)(threadIdx.x >> 6)), lane = (int)(threadIdx.x & 63u), c = lane & 31, h = lane >> 5;
+  // the tiles that see most first; neighbouring workgroups (which go to different L2s) take different heads
+  const int head = (int)(blockIdx.x % (unsigned)a.Hkv), tile = a.tiles - 1 - (int)(blockIdx.x / (unsigned)a.Hkv);
+  const Tile t = find_tile(a, tile, 32 * W);
+  if (t.first >= (long long)t.queries * a.group) return;
+  const int tiles = (t.end + TT - 1) / TT;
+  const int32_t* table = a.table + (long long)t.b * a.width;
+
+  const int row = t.first + 32 * wave + c, query = row / a.group;
+  const bool live = query < t.queries;
+  const int sees = live ? t.length - t.queries + query : -1;
+  uint4 q[NS];
+#pragma unroll
+  for (int s = 0; s < NS; s++) {
+    uint32_t v[4] = {0u, 0u, 0u, 0u};
+    const int ch = 16 * s + 8 * h;
+    if (live) load_8(a.q + (t.start + query) * a.ldq + (long long)(head * a.group + row % a.group) * a.D + ch, a.D - ch, v);
+    // the maxima are taken of the products themselves: with a negative scale of those with the sign turned, with none of zeros
+    const uint32_t sign = a.c < 0.f ? 0x80008000u : 0u, some = a.c == 0.f ? 0u : ~0u;
+    q[s] = uint4{(v[0] ^ sign) & some, (v[1] ^ sign) & some, (v[2] ^ sign) & some, (v[3] ^ sign) & some};
+  }
+  const float scale = a.c == 0.f ? 1.f : fabsf(a.c);
+  // the wave's rows see all tokens up to `all` and none from `most` on
+  const int first_row = t.first + 32 * wave, last_row = min(first_row + 31, t.queries * a.group - 1);
+  const bool any = first_row <= last_row;
+  const int all = any ? t.length - t.queries + first_row / a.group : 0, most = any ? t.length - t.queries + last_row / a.group + 1 : 0;
+
+  floatx16_t o[ND];
+#pragma unroll
+  for (int n = 0; n < ND; n++)
+#pragma unroll
+    for (int j = 0; j < 16; j++) o[n][j] = 0.f;
+  float m = -__builtin_inff(), l = 0.f;
+
+  uint4 code[ITEMS];
+  unsigned scl[ITEMS];
+  bool there[ITEMS];
+  auto fetch = [&](int i) {
+#pragma unroll
+    for (int it = 0; it < ITEMS; it++) {
+      const int item = it * THREADS + (int)threadIdx.x, piece = item % CH, token = i * TT + piece / (DP / 32), block = piece % (DP / 32);
+      const bool keys = item < CH;
+      there[it] = false;
+      code[it] = uint4{0u, 0u, 0u, 0u};
+      scl[it] = 0;
+      if (item < 2 * CH && token < t.end) {
+        const int page = table[token >> a.page_bits];
+        there[it] = page >= 0 && page < a.pages;
+        if (there[it]) {
+          const long long r = (((long long)page * a.Hkv + head) << a.page_bits) + (token & ((1 << a.page_bits) - 1));
+          code[it] = *reinterpret_cast<const uint4*>((keys ? a.k_data : a.v_data) + r * (DP / 2) + 16 * block);
+          scl[it] = (keys ? a.k_scales : a.v_scales)[r * (DP / 32) + block];
+        }
+      }
+    }
+  };
+  auto put = [&](int buffer) {
+    uint16_t* kb = buffers + buffer * kBuffer<DP>;
+    uint16_t* vb = kb + TT * kKRow<DP>;
+#pragma unroll
+    for (int it = 0; it < ITEMS; it++) {
+      const int item = it * THREADS + (int)threadIdx.x, piece = item % CH, token = piece / (DP / 32), block = piece % (DP / 32);
+      if (item >= 2 * CH) break;
+      const bool keys = item < CH, bad = keys ? !there[it] : scl[it] == 255u;
+      const unsigned long long marks = __ballot(bad);
+      if (lane == 0) odd[buffer][item / 64] = marks;
+      uint16_t* to = (keys ? kb + token * kKRow<DP> : vb + token * kWideV<DP>) + 32 * block;
+      const float by = mx_scale(!keys && bad ? 0u : scl[it]);
+      const uint32_t w[4] = {code[it].x, code[it].y, code[it].z, code[it].w};
+#pragma unroll
+      for (int j = 0; j < 4; j++) *reinterpret_cast<uint4*>(to + 8 * j) = mx_widen<DT>(!keys && bad ? 0u : w[j], by);
+    }
+  };
+  if (tiles > 0) {
+    fetch(0);
+    put(0);
+    fetch(1);
+  }
+  for (int i = 0; i < tiles; i++) {
+    __syncthreads();
+    if (i + 1 < tiles) {
+      put((i + 1) & 1);
+      fetch(i + 2);
+    }
+    const int begin = i * TT;
+    if (begin >= most) continue;
+    const uint16_t* kb = buffers + (i & 1) * kBuffer<DP>;
+    const uint16_t* vb = kb + TT * kKRow<DP>;
+    floatx16_t x[TB];
+#pragma unroll
+    for (int b = 0; b < TB; b++) {
+#pragma unroll
+      for (int j = 0; j < 16; j++) x[b][j] = 0.f;
+#pragma unroll
+      for (int s = 0; s < NS; s++) x[b] = mfma32<DT>(*reinterpret_cast<const uint4*>(kb + (32 * b + c) * kKRow<DP> + 16 * s + 8 * h), q[s], x[b]);
+    }
+    unsigned long long gone = 0, none = 0;
+#pragma unroll
+    for (int w = 0; w < CH / 64; w++) gone |= odd[i & 1][w], none |= odd[i & 1][CH / 64 + w];
+    if (begin + TT - 1 > all || wave_uniform((int)(gone != 0))) {
+#pragma unroll
+      for (int b = 0; b < TB; b++)
+#pragma unroll
+        for (int j = 0; j < 16; j++) {
+          const int at = 32 * b + 8 * (j / 4) + 4 * h + j % 4, piece = at * (DP / 32);
+          if (begin + at > sees || (odd[i & 1][piece / 64] >> (piece % 64) & 1ull)) x[b][j] = -__builtin_inff();
+        }
+    }
+    float top = m;
+#pragma unroll
+    for (int b = 0; b < TB; b++)
+#pragma unroll
+      for (int j = 0; j < 16; j++) top = fmaxf(top, x[b][j]);
+    top = fmaxf(top, __shfl_xor(top, 32));
+    const float base = top == -__builtin_inff() ? 0.f : top * scale;
+    if (__ballot(top > m)) {
+      const float shrink = m == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(m * scale - base);
+      l *= shrink;
+#pragma unroll
+      for (int n = 0; n < ND; n++)
+#pragma unroll
+        for (int j = 0; j < 16; j++) o[n][j] *= shrink;
+      m = top;
+    }
+    uint4 p[2 * TB];
+#pragma unroll
+    for (int b = 0; b < TB; b++) {
+#pragma unroll
+      for (int j = 0; j < 16; j++) {
+        x[b][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][j], scale, -base));
+        l += x[b][j];
+      }
+#pragma unroll
+      for (int s = 0; s < 2; s++)
+        p[2 * b + s] = uint4{pack_2<DT>(x[b][8 * s], x[b][8 * s + 1]), pack_2<DT>(x[b][8 * s + 2], x[b][8 * s + 3]), pack_2<DT>(x[b][8 * s + 4], x[b][8 * s + 5]),
+                             pack_2<DT>(x[b][8 * s + 6], x[b][8 * s + 7])};
+    }
+#pragma unroll
+    for (int n = 0; n < ND; n++)
+#pragma unroll
+      for (int s = 0; s < 2 * TB; s++) {
+        const uint16_t* at = vb + (16 * s + 4 * h + ((lane & 15) >> 2)) * kWideV<DP> + 32 * n + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+        const uint2 lo = read_transposed(at), hi = read_transposed(at + 8 * kWideV<DP>);
+        o[n] = mfma32<DT>(uint4{lo.x, lo.y, hi.x, hi.y}, p[s], o[n]);
+      }
+    if (wave_uniform((int)(none != 0))) {  // blocks without number: NaN for the rows that see them
+      for (int w = 0; w < CH / 64; w++)
+        for (unsigned long long left = odd[i & 1][CH / 64 + w]; left; left &= left - 1) {
+          const int piece = 64 * w + (int)__builtin_ctzll(left);
+          if (begin + piece / (DP / 32) <= sees) {
+#pragma unroll
+            for (int n = 0; n < ND; n++)
+              if (n == piece % (DP / 32))
+#pragma unroll
+                for (int j = 0; j < 16; j++) o[n][j] = __builtin_nanf("");
+          }
+        }
+    }
+  }
+  l += __shfl_xor(l, 32);
+  if (!live) return;
+  const long long place = (t.start + query) * ((long long)a.Hkv * a.group) + head * a.group + row % a.group;
+  const float by = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+  for (int n = 0; n < ND; n++)
+#pragma unroll
+    for (int j = 0; j < 16; j += 4) {
+      const int ch = 32 * n + 8 * (j / 4) + 4 * h;
+      uint16_t* to = a.out + place * a.D + ch;
+      uint16_t v[4];
+#pragma unroll
+      for (int e = 0; e < 4; e++) v[e] = esp_from_float<DT>(l == 0.f ? 0.f : o[n][j + e] * by);
+      if (ch + 4 <= a.D) {
+        __builtin_memcpy(to, v, 8);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; e++)
+          if (ch + e < a.D) to[e] = v[e];
+      }
+    }
+  if (a.lse && h == 0) a.lse[place] = l == 0.f ? -__builtin_inff() : ((m == -__builtin_inff() ? 0.f : m * scale) + log2f(l)) * 0.6931471805599453f;
+}
+
 long long tiles_of(long long T, int B, int group, bool ragged, int rows) {
   return ragged ? T * group / rows + B : (long long)B * ((group + rows - 1) / rows);
 }
@@ -362,8 +573,13 @@ int most_pieces(long long items, long long tokens) {
 
 }  // namespace
 
+// Rows of a sequence from which the tiles of 128 rows are used, and from which those of 256 are: on average, the lengths are not known here
+constexpr long long MANY = 64, MOST = 1024;
+long long rows_each(long long T, int B, int group, bool ragged) { return ragged ? T * group / B : group; }
+
 size_t esp_cache_attention_workspace(const esparse_cache* cache, long long T, int B, int q_heads, long long width, bool ragged) {
   const int group = q_heads / cache->heads, dp = esp_cache_row(cache->head_dim);
+  if (rows_each(T, B, group, ragged) >= MANY) return 0;
   const long long items = tiles_of(T, B, group, ragged, ROWS) * cache->heads;
   const int pieces = most_pieces(items, width * cache->page);
   return pieces == 1 ? 0 : (size_t)items * pieces * (ROWS * dp + 2 * ROWS) * sizeof(float);
@@ -381,10 +597,40 @@ int esp_cache_attention_device(esparse_ctx* ctx, const void* q, long long ldq, l
   a.ldq = ldq, a.T = T, a.pages = cache->pages, a.width = width;
   a.B = B, a.Hkv = cache->heads, a.group = q_heads / cache->heads, a.D = cache->head_dim, a.page_bits = __builtin_ctz((unsigned)cache->page);
   a.c = (float)(scale * 1.4426950408889634);
+  const int row = esp_cache_row(a.D);
+  const long long each = rows_each(T, B, a.group, starts != nullptr);
+  if (each >= MANY) {
+    const int waves = each >= MOST ? 8 : 4;
+    a.tiles = (int)tiles_of(T, B, a.group, starts != nullptr, 32 * waves);
+    const dim3 grid((unsigned)a.tiles * (unsigned)a.Hkv);
+#define GO(DT, DP, W)                                                                            \
+  {                                                                                              \
+    static std::atomic<unsigned long long> done{0};                                              \
+    constexpr size_t bytes = (size_t)2 * kBuffer<DP> * 2;                                        \
+    ESP_HIP(ctx, raise_dynamic_lds(done, ctx->device, &k_attend_many<DT, DP, W>, bytes));        \
+    hipLaunchKernelGGL((k_attend_many<DT, DP, W>), grid, dim3(64 * W), bytes, ctx->stream, a);   \
+  }
+#define ROW(DT, W)                  \
+  {                                 \
+    if (row == 64) GO(DT, 64, W)    \
+    else if (row == 128) GO(DT, 128, W) \
+    else GO(DT, 256, W)             \
+  }
+    if (dtype == ESPARSE_F16) {
+      if (waves == 8) ROW(ESPARSE_F16, 8)
+      else ROW(ESPARSE_F16, 4)
+    } else {
+      if (waves == 8) ROW(ESPARSE_BF16, 8)
+      else ROW(ESPARSE_BF16, 4)
+    }
+#undef ROW
+#undef GO
+    ESP_HIP(ctx, hipGetLastError());
+    return ESPARSE_OK;
+  }
   const long long tiles = tiles_of(T, B, a.group, starts != nullptr, ROWS);
   a.tiles = (int)tiles;
   a.pieces = most_pieces(tiles * a.Hkv, width * cache->page);
-  const int row = esp_cache_row(a.D);
   const dim3 grid((unsigned)(tiles * a.Hkv * a.pieces));
 #define GO(DT, DP)                                                                                                                 \
   {                                                                                                                                \

@@ -285,7 +285,7 @@ def test_attention_of_one_token_each(ctx, lengths, Hq, H, D, page, dtype):
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
 @pytest.mark.parametrize("lengths,queries,Hq,H,D,page", [
     ([5, 40, 100], [5, 1, 3], 4, 2, 64, 16), ([70, 3, 0, 200], [70, 7, 2, 31], 3, 1, 128, 32), ([260, 1, 130], [130, 0, 130], 10, 5, 80, 64),
-    ([400], [400], 2, 2, 128, 64), ([333, 150], [33, 150], 12, 2, 256, 16), ([129, 64, 65, 1], [129, 64, 65, 1], 1, 1, 96, 16), ([600], [300], 8, 1, 128, 128)])
+    ([400], [400], 2, 2, 128, 64), ([1500, 300], [1100, 290], 3, 1, 80, 32), ([1030], [1030], 1, 1, 256, 16), ([2100], [1025], 2, 2, 50, 64), ([333, 150], [33, 150], 12, 2, 256, 16), ([129, 64, 65, 1], [129, 64, 65, 1], 1, 1, 96, 16), ([600], [300], 8, 1, 128, 128)])
 def test_attention_of_several_tokens(ctx, lengths, queries, Hq, H, D, page, dtype):
     """Prompts, drafts, sequences without queries or with more queries than tokens."""
     rng = _rng("several", *lengths, D, dtype)
@@ -367,7 +367,9 @@ def test_attention_with_sharp_scores(ctx, dtype, factor):
     k, v = _pool(rng, pages, H, page, D), _pool(rng, pages, H, page, D)
     q = torch.from_numpy(factor * rng.standard_normal((90, 2, D))).to(TORCH[dtype]).cuda()
     _check_attention(ctx, q, k, v, table, lengths, np.array([0, 50, 90]), page, D, dtype)
-    _check_attention(ctx, q[:2], k, v, table, lengths, None, page, D, dtype, scale=-0.05)
+    for scale in (-0.05, 0.0):
+        _check_attention(ctx, q[:2], k, v, table, lengths, None, page, D, dtype, scale=scale)
+        _check_attention(ctx, q, k, v, table, lengths, np.array([0, 50, 90]), page, D, dtype, scale=scale)
 
 
 def test_attention_long_context(ctx):
