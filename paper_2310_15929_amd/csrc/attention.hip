@@ -24,6 +24,7 @@ constexpr int STRIP = 32;      // tokens of a step
 constexpr int ROWS = 16;       // rows of a tile
 constexpr int WAVES = 4;
 constexpr int LEAST = 8;       // strips of a piece, where a long sequence is cut
+constexpr int MOST_PIECES = 512;
 
 struct AttendArgs {
   const uint16_t* q;
@@ -109,15 +110,37 @@ __device__ __forceinline__ void load_codes(const unsigned char* data, const unsi
   }
 }
 
-// maximum over the four lanes of a column
+// maximum and sum over the lanes that are 32, and 16 and 32, apart
+#if defined(__HIP_DEVICE_COMPILE__)
+#define HALVES(v, op)                                                                                                         \
+  const auto w = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, v), __builtin_bit_cast(unsigned, v), false, false); \
+  v = op(__builtin_bit_cast(float, (unsigned)w[0]), __builtin_bit_cast(float, (unsigned)w[1]));
+#define QUARTERS(v, op)                                                                                                       \
+  const auto u = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, v), __builtin_bit_cast(unsigned, v), false, false); \
+  v = op(__builtin_bit_cast(float, (unsigned)u[0]), __builtin_bit_cast(float, (unsigned)u[1]));
+#else
+#define HALVES(v, op)
+#define QUARTERS(v, op)
+#endif
+__device__ __forceinline__ float add(float a, float b) { return a + b; }
+__device__ __forceinline__ float half_max(float v) {
+  HALVES(v, fmaxf)
+  return v;
+}
+__device__ __forceinline__ float half_sum(float v) {
+  HALVES(v, add)
+  return v;
+}
 __device__ __forceinline__ float column_max(float v) {
-  v = fmaxf(v, __shfl_xor(v, 16));
-  return fmaxf(v, __shfl_xor(v, 32));
+  QUARTERS(v, fmaxf)
+  return half_max(v);
 }
 __device__ __forceinline__ float column_sum(float v) {
-  v += __shfl_xor(v, 16);
-  return v + __shfl_xor(v, 32);
+  QUARTERS(v, add)
+  return half_sum(v);
 }
+#undef HALVES
+#undef QUARTERS
 
 typedef short esp_short4 __attribute__((ext_vector_type(4)));
 // four rows of 16-bit numbers, 16 columns: lane c of 16 hands in columns 4 (c % 4) .. + 3 of row c / 4 and gets column c of the four rows
@@ -137,20 +160,50 @@ __device__ __forceinline__ void wave_fence() {
 #endif
 }
 
+// Results of matrix instructions are read from here on: 32 clocks, more than the longest of them needs.  The compiler counts these within a stretch of code without branches;
+// behind a branch it has read the last number of a result a clock after its instruction.
+template <class V>
+__device__ __forceinline__ void settle(V& v) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile("s_nop 15\n\ts_nop 15" : "+v"(v));
+#else
+  (void)v;
+#endif
+}
+// ... of several, after one settle()
+template <class V>
+__device__ __forceinline__ void settled(V& v) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile("" : "+v"(v));
+#else
+  (void)v;
+#endif
+}
+
 template <int DT>
 __device__ __forceinline__ uint32_t pack_2(float a, float b) {
   return esp_from_float<DT>(a) | (uint32_t)esp_from_float<DT>(b) << 16;
 }
 
 template <int DP>
-constexpr int kVRow = DP + 16;  // 16-bit numbers from token to token in LDS: eight tokens' columns lie in different banks
+constexpr int kHalf = DP == 256 ? 128 : DP;  // channels of V in LDS at a time
+template <int DP>
+constexpr int kVRow = kHalf<DP> + 16;  // 16-bit numbers from token to token in LDS: eight tokens' columns lie in different banks
 template <int DP>
 constexpr int kPartial = ROWS * DP + 2 * ROWS;
 
-// One tile of 16 rows and a piece of its tokens: the waves take strips in turn, their results are joined in LDS
+// the codes of a strip, and which of its groups of 16 tokens are in a page
+template <int DP>
+struct Strip {
+  Codes<DP> k[2], v[2];
+  bool there[2];
+};
+
+// One tile of 16 rows and a piece of its tokens: the waves take strips in turn, their results are joined in LDS.  A wave asks for its next strip, and for the pages of the one after that,
+// before it works on one.
 template <int DT, int DP>
 __global__ void __launch_bounds__(64 * WAVES) k_attend_few(const AttendArgs a) {
-  constexpr int NS = DP / 32, ND = DP / 16;
+  constexpr int NS = DP / 32, ND = DP / 16, NH = DP / kHalf<DP>, NE = DP == 256 ? 2 : 1;
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   __shared__ float stat[2][WAVES][ROWS];
   const int wave = wave_uniform((int)(threadIdx.x >> 6)), lane = (int)(threadIdx.x & 63u), c = lane & 15, g = lane >> 4;
@@ -163,6 +216,35 @@ __global__ void __launch_bounds__(64 * WAVES) k_attend_few(const AttendArgs a) {
   if (piece >= pieces) return;
   const int strips = (t.end + STRIP - 1) / STRIP;
   const int from = (int)((long long)strips * piece / pieces), to = (int)((long long)strips * (piece + 1) / pieces);
+  const int32_t* table = a.table + (long long)t.b * a.width;
+
+  auto pages_of = [&](int strip, int (&page)[2]) {
+#pragma unroll
+    for (int u = 0; u < 2; u++) {
+      const int at = strip * STRIP + 16 * u;
+      page[u] = strip < to && at < t.end ? wave_uniform(table[at >> a.page_bits]) : -1;
+    }
+  };
+  auto load = [&](int strip, const int (&page)[2], Strip<DP>& o) {
+#pragma unroll
+    for (int u = 0; u < 2; u++) {
+      o.there[u] = page[u] >= 0 && page[u] < a.pages;
+      if (o.there[u]) {
+        const int at = strip * STRIP + 16 * u;
+        const long long r = (((long long)page[u] * a.Hkv + head) << a.page_bits) + (at & ((1 << a.page_bits) - 1)) + c;
+        load_codes<DP>(a.k_data, a.k_scales, r, g, o.k[u]);
+        load_codes<DP>(a.v_data, a.v_scales, r, g, o.v[u]);
+      } else {
+        o.k[u] = Codes<DP>{};
+        o.v[u] = Codes<DP>{};
+      }
+    }
+  };
+  Strip<DP> next;
+  int page[2];
+  pages_of(from + wave, page);
+  load(from + wave, page, next);
+  pages_of(from + wave + WAVES, page);
 
   const int row = t.first + c, query = row / a.group;
   const bool live = query < t.queries;
@@ -179,54 +261,26 @@ __global__ void __launch_bounds__(64 * WAVES) k_attend_few(const AttendArgs a) {
 #pragma unroll
   for (int n = 0; n < ND; n++) o[n] = floatx4_t{0.f, 0.f, 0.f, 0.f};
   float m = -__builtin_inff(), l = 0.f;
-  const int32_t* table = a.table + (long long)t.b * a.width;
 
   for (int strip = from + wave; strip < to; strip += WAVES) {
-    Codes<DP> kc[2], vc[2];
-    bool there[2];
-    int page[2];
-#pragma unroll
-    for (int u = 0; u < 2; u++) {
-      const int at = strip * STRIP + 16 * u;
-      page[u] = at < t.end ? wave_uniform(table[at >> a.page_bits]) : -1;
-      there[u] = page[u] >= 0 && page[u] < a.pages;
-    }
-#pragma unroll
-    for (int u = 0; u < 2; u++) {
-      if (there[u]) {
-        const int at = strip * STRIP + 16 * u;
-        const long long r = (((long long)page[u] * a.Hkv + head) << a.page_bits) + (at & ((1 << a.page_bits) - 1)) + c;
-        load_codes<DP>(a.k_data, a.k_scales, r, g, kc[u]);
-        load_codes<DP>(a.v_data, a.v_scales, r, g, vc[u]);
-      }
-      if (!there[u] || strip * STRIP + 16 * u + c >= t.end) {  // tokens that no row sees: no numbers of theirs take part
-        if (!there[u]) kc[u] = Codes<DP>{};
-        vc[u] = Codes<DP>{};
-      }
-    }
-    // V into LDS
-    unsigned long long odd[2][DP == 256 ? 2 : 1];
-    wave_fence();
-#pragma unroll
-    for (int u = 0; u < 2; u++) {
-#pragma unroll
-      for (int i = 0; i < (DP == 256 ? 2 : 1); i++) odd[u][i] = __ballot(vc[u].e[i] == 255u);
-#pragma unroll
-      for (int s = 0; s < NS; s++) {
-        const unsigned e = vc[u].e[DP == 256 ? s / 4 : 0];
-        *reinterpret_cast<uint4*>(vt + (16 * u + c) * kVRow<DP> + channel_of<DP>(s, g)) = mx_widen<DT>(e == 255u ? 0u : vc[u].w[s], mx_scale(e == 255u ? 0u : e));
-      }
-    }
-    wave_fence();
+    Strip<DP> now = next;
+    load(strip + WAVES, page, next);
+    pages_of(strip + 2 * WAVES, page);
     // scores
     float x[2][4];
+    floatx4_t acc[2];
 #pragma unroll
     for (int u = 0; u < 2; u++) {
-      floatx4_t acc = {0.f, 0.f, 0.f, 0.f};
+      acc[u] = floatx4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int s = 0; s < NS; s++) acc = mfma16<DT>(mx_widen<DT>(kc[u].w[s], mx_scale(kc[u].e[DP == 256 ? s / 4 : 0])), qv[s], acc);
+      for (int s = 0; s < NS; s++) acc[u] = mfma16<DT>(mx_widen<DT>(now.k[u].w[s], mx_scale(now.k[u].e[DP == 256 ? s / 4 : 0])), qv[s], acc[u]);
+    }
+    settled(acc[0]);
+    settle(acc[1]);
 #pragma unroll
-      for (int j = 0; j < 4; j++) x[u][j] = there[u] && strip * STRIP + 16 * u + 4 * g + j <= sees ? acc[j] * a.c : -__builtin_inff();
+    for (int u = 0; u < 2; u++) {
+#pragma unroll
+      for (int j = 0; j < 4; j++) x[u][j] = now.there[u] && strip * STRIP + 16 * u + 4 * g + j <= sees ? acc[u][j] * a.c : -__builtin_inff();
     }
     float top = m;
 #pragma unroll
@@ -234,9 +288,16 @@ __global__ void __launch_bounds__(64 * WAVES) k_attend_few(const AttendArgs a) {
 #pragma unroll
       for (int j = 0; j < 4; j++) top = fmaxf(top, x[u][j]);
     top = column_max(top);
-    const float base = top == -__builtin_inff() ? 0.f : top, shrink = __builtin_amdgcn_exp2f(m - base);
-    m = top;
-    l *= shrink;
+    const float base = top == -__builtin_inff() ? 0.f : top;
+    if (__ballot(top > m)) {  // (else all have kept their maxima)
+      const float shrink = __builtin_amdgcn_exp2f(m - base);
+      l *= shrink;
+#pragma unroll
+      for (int n = 0; n < ND; n++)
+#pragma unroll
+        for (int j = 0; j < 4; j++) o[n][j] *= shrink;
+      m = top;
+    }
 #pragma unroll
     for (int u = 0; u < 2; u++)
 #pragma unroll
@@ -245,19 +306,41 @@ __global__ void __launch_bounds__(64 * WAVES) k_attend_few(const AttendArgs a) {
         l += x[u][j];
       }
     const uint4 p = {pack_2<DT>(x[0][0], x[0][1]), pack_2<DT>(x[0][2], x[0][3]), pack_2<DT>(x[1][0], x[1][1]), pack_2<DT>(x[1][2], x[1][3])};
+    // V through LDS
+    unsigned long long odd[2][NE];
 #pragma unroll
-    for (int n = 0; n < ND; n++) {
-      const uint16_t* at = vt + (4 * g + (c >> 2)) * kVRow<DP> + 16 * n + 4 * (c & 3);
-      const uint2 lo = read_transposed(at), hi = read_transposed(at + 16 * kVRow<DP>);
+    for (int u = 0; u < 2; u++) {
+      if (strip * STRIP + 16 * u + c >= t.end) now.v[u] = Codes<DP>{};  // tokens that no row sees: no numbers of theirs take part
 #pragma unroll
-      for (int j = 0; j < 4; j++) o[n][j] *= shrink;
-      o[n] = mfma16<DT>(uint4{lo.x, lo.y, hi.x, hi.y}, p, o[n]);
+      for (int i = 0; i < NE; i++) odd[u][i] = __ballot(now.v[u].e[i] == 255u);
     }
+#pragma unroll
+    for (int hh = 0; hh < NH; hh++) {
+      wave_fence();
+#pragma unroll
+      for (int u = 0; u < 2; u++) {
+        const unsigned e = now.v[u].e[hh];
+        const float by = mx_scale(e == 255u ? 0u : e);
+#pragma unroll
+        for (int s = 0; s < NS / NH; s++)
+          *reinterpret_cast<uint4*>(vt + (16 * u + c) * kVRow<DP> + channel_of<DP>(s, g)) = mx_widen<DT>(e == 255u ? 0u : now.v[u].w[NS / NH * hh + s], by);
+      }
+      wave_fence();
+#pragma unroll
+      for (int n = 0; n < ND / NH; n++) {
+        const uint16_t* at = vt + (4 * g + (c >> 2)) * kVRow<DP> + 16 * n + 4 * (c & 3);
+        const uint2 lo = read_transposed(at), hi = read_transposed(at + 16 * kVRow<DP>);
+        o[ND / NH * hh + n] = mfma16<DT>(uint4{lo.x, lo.y, hi.x, hi.y}, p, o[ND / NH * hh + n]);
+      }
+    }
+#pragma unroll
+    for (int n = 0; n < ND - 1; n++) settled(o[n]);
+    settle(o[ND - 1]);
     // blocks without numbers: NaN for the rows that see them
 #pragma unroll
     for (int u = 0; u < 2; u++)
 #pragma unroll
-      for (int i = 0; i < (DP == 256 ? 2 : 1); i++)
+      for (int i = 0; i < NE; i++)
         for (unsigned long long left = odd[u][i]; left; left &= left - 1) {
           const int who = (int)__builtin_ctzll(left);
           const int block = DP == 64 ? (who >> 4) >> 1 : 4 * i + (who >> 4);
@@ -271,41 +354,46 @@ __global__ void __launch_bounds__(64 * WAVES) k_attend_few(const AttendArgs a) {
   l = column_sum(l);
 
   // the waves' results
-  __syncthreads();
-  float* mine = reinterpret_cast<float*>(lds) + wave * (ROWS * DP);
   if (g == 0) {
     stat[0][wave][c] = m;
     stat[1][wave][c] = l;
   }
-#pragma unroll
-  for (int n = 0; n < ND; n++) *reinterpret_cast<floatx4_t*>(mine + c * DP + 16 * n + 4 * g) = o[n];
-  __syncthreads();
+  constexpr int ROW = kHalf<DP> + 4;  // numbers from row to row in LDS: the four lanes of a column and their neighbours in different banks
+  static_assert(ROWS * ROW * 4 <= STRIP * kVRow<DP> * 2, "a wave's sums fit where its values were");
+  const float* sums = reinterpret_cast<const float*>(lds);
+  float* mine = reinterpret_cast<float*>(vt);
   float* part = a.partial + ((long long)(tile * a.Hkv + head) * a.pieces + piece) * kPartial<DP>;
-  for (int at = (int)threadIdx.x * 4; at < ROWS * DP; at += 64 * WAVES * 4) {
-    const int r = at / DP, ch = at % DP;
-    float top = -__builtin_inff();
 #pragma unroll
-    for (int w = 0; w < WAVES; w++) top = fmaxf(top, stat[0][w][r]);
-    const float base = top == -__builtin_inff() ? 0.f : top;
-    floatx4_t sum = {0.f, 0.f, 0.f, 0.f};
-    float all = 0.f;
+  for (int hh = 0; hh < NH; hh++) {
+    __syncthreads();
 #pragma unroll
-    for (int w = 0; w < WAVES; w++) {
-      const float f = __builtin_amdgcn_exp2f(stat[0][w][r] - base);
-      const floatx4_t v = *reinterpret_cast<const floatx4_t*>(reinterpret_cast<const float*>(lds) + w * (ROWS * DP) + at);
+    for (int n = 0; n < ND / NH; n++) *reinterpret_cast<floatx4_t*>(mine + c * ROW + 16 * n + 4 * g) = o[ND / NH * hh + n];
+    __syncthreads();
+    for (int at = (int)threadIdx.x * 4; at < ROWS * kHalf<DP>; at += 64 * WAVES * 4) {
+      const int r = at / kHalf<DP>, in = at % kHalf<DP>, ch = hh * kHalf<DP> + in;
+      float top = -__builtin_inff();
 #pragma unroll
-      for (int j = 0; j < 4; j++) sum[j] += v[j] * f;
-      all += stat[1][w][r] * f;
-    }
-    if (pieces > 1) {
-      *reinterpret_cast<floatx4_t*>(part + at) = sum;
-      if (ch == 0) {
-        part[ROWS * DP + r] = top;
-        part[ROWS * DP + ROWS + r] = all;
+      for (int w = 0; w < WAVES; w++) top = fmaxf(top, stat[0][w][r]);
+      const float base = top == -__builtin_inff() ? 0.f : top;
+      floatx4_t sum = {0.f, 0.f, 0.f, 0.f};
+      float all = 0.f;
+#pragma unroll
+      for (int w = 0; w < WAVES; w++) {
+        const float f = __builtin_amdgcn_exp2f(stat[0][w][r] - base);
+        const floatx4_t v = *reinterpret_cast<const floatx4_t*>(sums + w * (STRIP * kVRow<DP> / 2) + r * ROW + in);
+#pragma unroll
+        for (int j = 0; j < 4; j++) sum[j] += v[j] * f;
+        all += stat[1][w][r] * f;
       }
-    } else {
       const int of = t.first + r, qi = of / a.group;
-      if (qi < t.queries) {
+      if (qi >= t.queries) continue;
+      if (pieces > 1) {
+        *reinterpret_cast<floatx4_t*>(part + r * DP + ch) = sum;
+        if (ch == 0) {
+          part[ROWS * DP + r] = top;
+          part[ROWS * DP + ROWS + r] = all;
+        }
+      } else {
         const long long place = (t.start + qi) * ((long long)a.Hkv * a.group) + head * a.group + of % a.group;
         const float by = all == 0.f ? 0.f : 1.f / all;
 #pragma unroll
@@ -317,38 +405,63 @@ __global__ void __launch_bounds__(64 * WAVES) k_attend_few(const AttendArgs a) {
   }
 }
 
-// pieces of a tile, joined in order
+// The pieces of a row, joined: a workgroup for each row of a tile; its groups of DP / 4 threads (four channels each) take pieces in turn and their sums are added in order
 template <int DT, int DP>
 __global__ void __launch_bounds__(256) k_attend_join(const AttendArgs a) {
-  const int head = (int)(blockIdx.x % (unsigned)a.Hkv), tile = (int)(blockIdx.x / (unsigned)a.Hkv);
+  constexpr int QUADS = DP / 4, GROUPS = 256 / QUADS;
+  __shared__ float factor[MOST_PIECES], sums[MOST_PIECES], waves[4];
+  __shared__ floatx4_t of_group[GROUPS][QUADS];
+  const int r = (int)(blockIdx.x % ROWS), head = (int)(blockIdx.x / ROWS % (unsigned)a.Hkv), tile = (int)(blockIdx.x / ROWS / (unsigned)a.Hkv);
   const Tile t = find_tile(a, tile, ROWS);
-  if (t.first >= (long long)t.queries * a.group) return;
+  const int of = t.first + r, qi = of / a.group;
+  if (qi >= t.queries) return;
   const int pieces = pieces_of(t.end, a.pieces);
   if (pieces == 1) return;
   const float* part = a.partial + (long long)(tile * a.Hkv + head) * a.pieces * kPartial<DP>;
-  for (int at = (int)threadIdx.x * 4; at < ROWS * DP; at += 1024) {
-    const int r = at / DP, ch = at % DP, of = t.first + r, qi = of / a.group;
-    if (qi >= t.queries) continue;
-    float top = -__builtin_inff();
-    for (int i = 0; i < pieces; i++) top = fmaxf(top, part[(long long)i * kPartial<DP> + ROWS * DP + r]);
-    const float base = top == -__builtin_inff() ? 0.f : top;
-    floatx4_t sum = {0.f, 0.f, 0.f, 0.f};
-    float all = 0.f;
-    for (int i = 0; i < pieces; i++) {
-      const float* p = part + (long long)i * kPartial<DP>;
-      const float f = __builtin_amdgcn_exp2f(p[ROWS * DP + r] - base);
-      const floatx4_t v = *reinterpret_cast<const floatx4_t*>(p + at);
-#pragma unroll
-      for (int j = 0; j < 4; j++) sum[j] += v[j] * f;
-      all += p[ROWS * DP + ROWS + r] * f;
-    }
-    const long long place = (t.start + qi) * ((long long)a.Hkv * a.group) + head * a.group + of % a.group;
-    const float by = all == 0.f ? 0.f : 1.f / all;
-#pragma unroll
-    for (int j = 0; j < 4; j++)
-      if (ch + j < a.D) a.out[place * a.D + ch + j] = esp_from_float<DT>(all == 0.f ? 0.f : sum[j] * by);
-    if (a.lse && ch == 0) a.lse[place] = all == 0.f ? -__builtin_inff() : (base + log2f(all)) * 0.6931471805599453f;
+  const int quad = (int)threadIdx.x % QUADS, group = (int)threadIdx.x / QUADS;
+  float top = -__builtin_inff();
+  for (int i = (int)threadIdx.x; i < pieces; i += 256) {
+    const float v = part[(long long)i * kPartial<DP> + ROWS * DP + r];
+    factor[i] = v;
+    sums[i] = part[(long long)i * kPartial<DP> + ROWS * DP + ROWS + r];
+    top = fmaxf(top, v);
   }
+#pragma unroll
+  for (int o = 32; o; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+  if ((threadIdx.x & 63u) == 0) waves[threadIdx.x >> 6] = top;
+  __syncthreads();
+  top = fmaxf(fmaxf(waves[0], waves[1]), fmaxf(waves[2], waves[3]));
+  const float base = top == -__builtin_inff() ? 0.f : top;
+  floatx4_t sum = {0.f, 0.f, 0.f, 0.f};
+  float all = 0.f;
+#pragma unroll 4
+  for (int i = group; i < pieces; i += GROUPS) {
+    const floatx4_t v = *reinterpret_cast<const floatx4_t*>(part + (long long)i * kPartial<DP> + r * DP + 4 * quad);
+    const float f = __builtin_amdgcn_exp2f(factor[i] - base);
+#pragma unroll
+    for (int j = 0; j < 4; j++) sum[j] += v[j] * f;
+    all += sums[i] * f;
+  }
+  of_group[group][quad] = sum;
+  __syncthreads();
+  if (quad == 0) factor[group] = all;  // (all have read the factors)
+  __syncthreads();
+  if (group) return;
+  all = 0.f;
+  sum = floatx4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < GROUPS; i++) {
+    const floatx4_t v = of_group[i][quad];
+#pragma unroll
+    for (int j = 0; j < 4; j++) sum[j] += v[j];
+    all += factor[i];
+  }
+  const long long place = (t.start + qi) * ((long long)a.Hkv * a.group) + head * a.group + of % a.group;
+  const float by = all == 0.f ? 0.f : 1.f / all;
+#pragma unroll
+  for (int j = 0; j < 4; j++)
+    if (4 * quad + j < a.D) a.out[place * a.D + 4 * quad + j] = esp_from_float<DT>(all == 0.f ? 0.f : sum[j] * by);
+  if (a.lse && quad == 0) a.lse[place] = all == 0.f ? -__builtin_inff() : (base + log2f(all)) * 0.6931471805599453f;
 }
 
 // ---- prompts: many rows of a sequence ----------------------------------------------------------------
@@ -371,7 +484,7 @@ __device__ __forceinline__ floatx16_t mfma32(uint4 a, uint4 b, floatx16_t c) {
 }
 
 template <int DT, int DP, int W>
-__global__ void __launch_bounds__(64 * W) k_attend_many(const AttendArgs a) {
+__global__ void __launch_bounds__(64 * W, 2) k_attend_many(const AttendArgs a) {
   constexpr int TT = kTile<DP>, TB = TT / 32, NS = DP / 16, ND = DP / 32, THREADS = 64 * W;
   constexpr int CH = TT * DP / 32;                       // pieces of 16 bytes (a block) of the keys of a tile, and of the values
   constexpr int ITEMS = (2 * CH + THREADS - 1) / THREADS;  // of a thread
@@ -475,6 +588,9 @@ __global__ void __launch_bounds__(64 * W) k_attend_many(const AttendArgs a) {
 #pragma unroll
       for (int s = 0; s < NS; s++) x[b] = mfma32<DT>(*reinterpret_cast<const uint4*>(kb + (32 * b + c) * kKRow<DP> + 16 * s + 8 * h), q[s], x[b]);
     }
+#pragma unroll
+    for (int b = 0; b < TB - 1; b++) settled(x[b]);
+    settle(x[TB - 1]);
     unsigned long long gone = 0, none = 0;
 #pragma unroll
     for (int w = 0; w < CH / 64; w++) gone |= odd[i & 1][w], none |= odd[i & 1][CH / 64 + w];
@@ -492,7 +608,7 @@ __global__ void __launch_bounds__(64 * W) k_attend_many(const AttendArgs a) {
     for (int b = 0; b < TB; b++)
 #pragma unroll
       for (int j = 0; j < 16; j++) top = fmaxf(top, x[b][j]);
-    top = fmaxf(top, __shfl_xor(top, 32));
+    top = half_max(top);
     const float base = top == -__builtin_inff() ? 0.f : top * scale;
     if (__ballot(top > m)) {
       const float shrink = m == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(m * scale - base);
@@ -524,6 +640,9 @@ __global__ void __launch_bounds__(64 * W) k_attend_many(const AttendArgs a) {
         const uint2 lo = read_transposed(at), hi = read_transposed(at + 8 * kWideV<DP>);
         o[n] = mfma32<DT>(uint4{lo.x, lo.y, hi.x, hi.y}, p[s], o[n]);
       }
+#pragma unroll
+    for (int n = 0; n < ND - 1; n++) settled(o[n]);
+    settle(o[ND - 1]);
     if (wave_uniform((int)(none != 0))) {  // blocks without number: NaN for the rows that see them
       for (int w = 0; w < CH / 64; w++)
         for (unsigned long long left = odd[i & 1][CH / 64 + w]; left; left &= left - 1) {
@@ -538,7 +657,7 @@ __global__ void __launch_bounds__(64 * W) k_attend_many(const AttendArgs a) {
         }
     }
   }
-  l += __shfl_xor(l, 32);
+  l = half_sum(l);
   if (!live) return;
   const long long place = (t.start + query) * ((long long)a.Hkv * a.group) + head * a.group + row % a.group;
   const float by = l == 0.f ? 0.f : 1.f / l;
@@ -568,7 +687,7 @@ long long tiles_of(long long T, int B, int group, bool ragged, int rows) {
 // pieces that a sequence is cut into at most: until the workgroups fill the chip, for the longest that the table has room for
 int most_pieces(long long items, long long tokens) {
   const long long strips = (tokens + STRIP - 1) / STRIP, longest = (strips + LEAST - 1) / LEAST, want = (1024 + items - 1) / items;
-  return (int)std::max<long long>(1, std::min(longest, want));
+  return (int)std::max<long long>(1, std::min({longest, want, (long long)MOST_PIECES}));
 }
 
 }  // namespace
@@ -636,10 +755,9 @@ int esp_cache_attention_device(esparse_ctx* ctx, const void* q, long long ldq, l
   {                                                                                                                                \
     static std::atomic<unsigned long long> done{0};                                                                                \
     constexpr size_t bytes = (size_t)WAVES * STRIP * kVRow<DP> * 2;                                                                \
-    static_assert(bytes >= (size_t)WAVES * ROWS * DP * 4, "the joined sums fit");                                                  \
     ESP_HIP(ctx, raise_dynamic_lds(done, ctx->device, &k_attend_few<DT, DP>, bytes));                                              \
     hipLaunchKernelGGL((k_attend_few<DT, DP>), grid, dim3(64 * WAVES), bytes, ctx->stream, a);                                     \
-    if (a.pieces > 1) hipLaunchKernelGGL((k_attend_join<DT, DP>), dim3((unsigned)(tiles * a.Hkv)), dim3(256), 0, ctx->stream, a);  \
+    if (a.pieces > 1) hipLaunchKernelGGL((k_attend_join<DT, DP>), dim3((unsigned)(tiles * a.Hkv * ROWS)), dim3(256), 0, ctx->stream, a);  \
   }
   if (dtype == ESPARSE_F16) {
     if (row == 64) GO(ESPARSE_F16, 64)
