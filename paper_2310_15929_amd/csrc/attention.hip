@@ -202,7 +202,7 @@ struct Strip {
 // One tile of 16 rows and a piece of its tokens: the waves take strips in turn, their results are joined in LDS.  A wave asks for its next strip, and for the pages of the one after that,
 // before it works on one.
 template <int DT, int DP>
-__global__ void __launch_bounds__(64 * WAVES) k_attend_few(const AttendArgs a) {
+__global__ void __launch_bounds__(64 * WAVES, DP == 256 ? 2 : 3) k_attend_few(const AttendArgs a) {
   constexpr int NS = DP / 32, ND = DP / 16, NH = DP / kHalf<DP>, NE = DP == 256 ? 2 : 1;
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   __shared__ float stat[2][WAVES][ROWS];
@@ -333,10 +333,15 @@ __global__ void __launch_bounds__(64 * WAVES) k_attend_few(const AttendArgs a) {
         o[ND / NH * hh + n] = mfma16<DT>(uint4{lo.x, lo.y, hi.x, hi.y}, p, o[ND / NH * hh + n]);
       }
     }
-#pragma unroll
-    for (int n = 0; n < ND - 1; n++) settled(o[n]);
-    settle(o[ND - 1]);
     // blocks without numbers: NaN for the rows that see them
+    unsigned long long some = 0;
+#pragma unroll
+    for (int u = 0; u < 2; u++)
+#pragma unroll
+      for (int i = 0; i < NE; i++) some |= odd[u][i];
+    if (!some) continue;
+#pragma unroll
+    for (int n = 0; n < ND; n++) settle(o[n]);
 #pragma unroll
     for (int u = 0; u < 2; u++)
 #pragma unroll
@@ -352,6 +357,8 @@ __global__ void __launch_bounds__(64 * WAVES) k_attend_few(const AttendArgs a) {
         }
   }
   l = column_sum(l);
+#pragma unroll
+  for (int n = 0; n < ND; n++) settle(o[n]);
 
   // the waves' results
   if (g == 0) {
