@@ -36,6 +36,7 @@ struct AttendArgs {
   long long ldq, T, pages;
   long long width;  // pages of a row of the table
   int B, Hkv, group, D, page_bits, tiles, pieces;
+  int rows;  // of a tile that can be anything
   float c;  // scale log2(e)
 };
 
@@ -418,7 +419,8 @@ __global__ void __launch_bounds__(256) k_attend_join(const AttendArgs a) {
   constexpr int QUADS = DP / 4, GROUPS = 256 / QUADS;
   __shared__ float factor[MOST_PIECES], sums[MOST_PIECES], waves[4];
   __shared__ floatx4_t of_group[GROUPS][QUADS];
-  const int r = (int)(blockIdx.x % ROWS), head = (int)(blockIdx.x / ROWS % (unsigned)a.Hkv), tile = (int)(blockIdx.x / ROWS / (unsigned)a.Hkv);
+  const unsigned rows = (unsigned)a.rows;
+  const int r = (int)(blockIdx.x % rows), head = (int)(blockIdx.x / rows % (unsigned)a.Hkv), tile = (int)(blockIdx.x / rows / (unsigned)a.Hkv);
   const Tile t = find_tile(a, tile, ROWS);
   const int of = t.first + r, qi = of / a.group;
   if (qi >= t.queries) return;
@@ -647,10 +649,9 @@ __global__ void __launch_bounds__(64 * W, 2) k_attend_many(const AttendArgs a) {
         const uint2 lo = read_transposed(at), hi = read_transposed(at + 8 * kWideV<DP>);
         o[n] = mfma32<DT>(uint4{lo.x, lo.y, hi.x, hi.y}, p[s], o[n]);
       }
-#pragma unroll
-    for (int n = 0; n < ND - 1; n++) settled(o[n]);
-    settle(o[ND - 1]);
     if (wave_uniform((int)(none != 0))) {  // blocks without number: NaN for the rows that see them
+#pragma unroll
+      for (int n = 0; n < ND; n++) settle(o[n]);
       for (int w = 0; w < CH / 64; w++)
         for (unsigned long long left = odd[i & 1][CH / 64 + w]; left; left &= left - 1) {
           const int piece = 64 * w + (int)__builtin_ctzll(left);
@@ -664,6 +665,8 @@ __global__ void __launch_bounds__(64 * W, 2) k_attend_many(const AttendArgs a) {
         }
     }
   }
+#pragma unroll
+  for (int n = 0; n < ND; n++) settle(o[n]);
   l = half_sum(l);
   if (!live) return;
   const long long place = (t.start + query) * ((long long)a.Hkv * a.group) + head * a.group + row % a.group;
@@ -693,7 +696,7 @@ long long tiles_of(long long T, int B, int group, bool ragged, int rows) {
 }
 // pieces that a sequence is cut into at most: until the workgroups fill the chip, for the longest that the table has room for
 int most_pieces(long long items, long long tokens) {
-  const long long strips = (tokens + STRIP - 1) / STRIP, longest = (strips + LEAST - 1) / LEAST, want = (1024 + items - 1) / items;
+  const long long strips = (tokens + STRIP - 1) / STRIP, longest = (strips + LEAST - 1) / LEAST, want = items >= 256 ? (4096 + items - 1) / items : (1024 + items - 1) / items;
   return (int)std::max<long long>(1, std::min({longest, want, (long long)MOST_PIECES}));
 }
 
@@ -757,6 +760,7 @@ int esp_cache_attention_device(esparse_ctx* ctx, const void* q, long long ldq, l
   const long long tiles = tiles_of(T, B, a.group, starts != nullptr, ROWS);
   a.tiles = (int)tiles;
   a.pieces = most_pieces(tiles * a.Hkv, width * cache->page);
+  a.rows = starts ? ROWS : std::min(ROWS, a.group);
   const dim3 grid((unsigned)(tiles * a.Hkv * a.pieces));
 #define GO(DT, DP)                                                                                                                 \
   {                                                                                                                                \
@@ -764,7 +768,7 @@ int esp_cache_attention_device(esparse_ctx* ctx, const void* q, long long ldq, l
     constexpr size_t bytes = (size_t)WAVES * STRIP * kVRow<DP> * 2;                                                                \
     ESP_HIP(ctx, raise_dynamic_lds(done, ctx->device, &k_attend_few<DT, DP>, bytes));                                              \
     hipLaunchKernelGGL((k_attend_few<DT, DP>), grid, dim3(64 * WAVES), bytes, ctx->stream, a);                                     \
-    if (a.pieces > 1) hipLaunchKernelGGL((k_attend_join<DT, DP>), dim3((unsigned)(tiles * a.Hkv * ROWS)), dim3(256), 0, ctx->stream, a);  \
+    if (a.pieces > 1) hipLaunchKernelGGL((k_attend_join<DT, DP>), dim3((unsigned)(tiles * a.Hkv * a.rows)), dim3(256), 0, ctx->stream, a);  \
   }
   if (dtype == ESPARSE_F16) {
     if (row == 64) GO(ESPARSE_F16, 64)
