@@ -181,10 +181,6 @@ __device__ __forceinline__ void settled(V& v) {
 #endif
 }
 
-template <int DT>
-__device__ __forceinline__ uint32_t pack_2(float a, float b) {
-  return esp_from_float<DT>(a) | (uint32_t)esp_from_float<DT>(b) << 16;
-}
 
 template <int DP>
 constexpr int kHalf = DP == 256 ? 128 : DP;  // channels of V in LDS at a time

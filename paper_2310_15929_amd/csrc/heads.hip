@@ -13,6 +13,7 @@
 namespace {
 
 constexpr int NT = 256;
+constexpr int PASSES = 2;  // rows of a lane that are loaded together
 
 struct RotateArgs {
   const uint16_t *q, *k, *v, *qw, *kw;
@@ -24,7 +25,7 @@ struct RotateArgs {
   long long ldq, ldk, ldv, T, tokens;  // tokens: places of the cache
   int Hq, Hkv, D, rotary, paired, page_bits;
   int rows, chunks;  // rows of a token, workgroups that share them
-  double eps;
+  double eps, per_channel;  // 1 / D
 };
 
 template <int DT>
@@ -34,6 +35,32 @@ __device__ __forceinline__ void widen_8(const uint32_t (&v)[4], double (&y)[8]) 
     y[2 * i] = esp_to_float<DT>((uint16_t)v[i]);
     y[2 * i + 1] = esp_to_float<DT>((uint16_t)(v[i] >> 16));
   }
+}
+
+// sine and cosine of f turns, |f| <= 1/2 (and a little), by their series within an eighth of a turn: the first terms left out are below 2^-54
+__device__ __forceinline__ void turn_by(double f, double& s, double& c) {
+  const double n = __builtin_rint(4. * f), x = (f - 0.25 * n) * 6.283185307179586, z = x * x;
+  double a = -1. / 1307674368000., b = 1. / 20922789888000.;
+  a = __builtin_fma(a, z, 1. / 6227020800.);
+  b = __builtin_fma(b, z, -1. / 87178291200.);
+  a = __builtin_fma(a, z, -1. / 39916800.);
+  b = __builtin_fma(b, z, 1. / 479001600.);
+  a = __builtin_fma(a, z, 1. / 362880.);
+  b = __builtin_fma(b, z, -1. / 3628800.);
+  a = __builtin_fma(a, z, -1. / 5040.);
+  b = __builtin_fma(b, z, 1. / 40320.);
+  a = __builtin_fma(a, z, 1. / 120.);
+  b = __builtin_fma(b, z, -1. / 720.);
+  a = __builtin_fma(a, z, -1. / 6.);
+  b = __builtin_fma(b, z, 1. / 24.);
+  b = __builtin_fma(b, z, -0.5);
+  a = __builtin_fma(a * z, x, x);
+  b = __builtin_fma(b, z, 1.);
+  const int q = (int)n & 3;
+  s = q & 1 ? b : a;
+  c = q & 1 ? a : b;
+  s = q & 2 ? -s : s;
+  c = q == 1 || q == 2 ? -c : c;
 }
 
 // sum over the LN lanes of a row
@@ -48,6 +75,16 @@ __device__ __forceinline__ double row_sum(double v) {
 __device__ __forceinline__ double over(double p, double by, double rest_n) {
   const double q = p * by;
   return __builtin_fma(__builtin_fma(-q, rest_n, p), by, q);
+}
+
+// 1 / sqrt(v), to 2^-46: the instruction's 24 bits and one step of Newton's
+__device__ __forceinline__ double inverse_root(double v) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  const double r = __builtin_amdgcn_rsq(v);
+#else
+  const double r = v;
+#endif
+  return v == __builtin_inf() ? 0. : r * __builtin_fma(-0.5 * v * r, r, 1.5);
 }
 
 // to 24 bits with the last one odd where something was lost: rounding that to 4 bits gives what rounding v would
@@ -71,13 +108,34 @@ __device__ __forceinline__ void put_row(unsigned char* data, unsigned char* scal
 }
 
 template <int DT, int DP>
-__global__ void __launch_bounds__(NT) k_rotate_heads(const RotateArgs a) {
+__global__ void __launch_bounds__(NT, 4) k_rotate_heads(const RotateArgs a) {
   constexpr int LN = DP / 8, ROWS = NT / LN;  // lanes of a row, rows of a pass
   __shared__ double turn[2][DP / 2];          // cos, sin
   const long long t = blockIdx.x / (unsigned)a.chunks;
   const int chunk = (int)(blockIdx.x % (unsigned)a.chunks);
   const unsigned lane = threadIdx.x % LN;
   const int c0 = (int)lane * 8, half = a.rotary / 2;
+  const int first = (int)((long long)a.rows * chunk / a.chunks), end = (int)((long long)a.rows * (chunk + 1) / a.chunks);
+  // the rows of the first passes are on their way while the angles are computed
+  uint32_t ahead[PASSES][4];
+  auto row_at = [&](int r, int& kind, int& head) {  // kind: 0 queries, 1 keys, 2 values
+    kind = r < a.Hq ? 0 : (r < a.Hq + a.Hkv ? 1 : 2);
+    head = kind == 0 ? r : (kind == 1 ? r - a.Hq : r - a.Hq - a.Hkv);
+    return (kind == 0 ? a.q + t * a.ldq : (kind == 1 ? a.k + t * a.ldk : a.v + t * a.ldv)) + (long long)head * a.D;
+  };
+  auto fetch = [&](int r0) {
+#pragma unroll
+    for (int u = 0; u < PASSES; u++) {
+      const int r = r0 + u * ROWS + (int)(threadIdx.x / LN);
+      int kind, head;
+      const uint16_t* x = row_at(r < end ? r : first, kind, head);
+      load_8(x + c0, r < end ? a.D - c0 : 0, ahead[u]);
+    }
+  };
+  fetch(first);
+  uint32_t weight[2][4] = {};
+  if (a.qw) load_8(a.qw + c0, a.D - c0, weight[0]);
+  if (a.kw) load_8(a.kw + c0, a.D - c0, weight[1]);
   if ((int)threadIdx.x < half) {
     // position x frequency in turns, to 2^-50 of one: the product of a 31-bit and a 24-bit number and 1 / 2 pi in two pieces each
     const double p = a.positions[t], f = a.frequencies[threadIdx.x], angle = p * f;
@@ -85,7 +143,7 @@ __global__ void __launch_bounds__(NT) k_rotate_heads(const RotateArgs a) {
     const double turns = angle * hi;
     const double rest = __builtin_fma(angle, hi, -turns) + (angle * lo + __builtin_fma(p, f, -angle) * hi);
     double s, c;
-    sincospi(2. * ((turns - __builtin_rint(turns)) + rest), &s, &c);
+    turn_by((turns - __builtin_rint(turns)) + rest, s, c);
     turn[0][threadIdx.x] = c;
     turn[1][threadIdx.x] = s;
   }
@@ -95,32 +153,87 @@ __global__ void __launch_bounds__(NT) k_rotate_heads(const RotateArgs a) {
   if (a.slots) {
     const int32_t mine = a.slots[t];
     if (mine >= 0 && mine < a.tokens) slot = mine;
-    for (long long j = t + 1 + threadIdx.x; j < a.T; j += NT) later |= a.slots[j] == mine;
+    // (the waves that have no angles look through those behind it, sixteen of a thread at a time)
+    if (threadIdx.x >= NT / 2) {
+      for (long long j = t + 1 + 4 * (long long)(threadIdx.x - NT / 2); j < a.T; j += 8 * NT) {
+        int32_t s[4][4];
+#pragma unroll
+        for (int u = 0; u < 4; u++) {
+          const long long i = j + u * 2 * NT;
+          if (i + 4 <= a.T) {
+            __builtin_memcpy(s[u], a.slots + i, 16);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; e++) s[u][e] = i + e < a.T ? a.slots[i + e] : -1;
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < 4; u++)
+#pragma unroll
+          for (int e = 0; e < 4; e++) later |= s[u][e] == mine && mine >= 0;
+      }
+    }
   }
   if (__syncthreads_or(later)) slot = -1;
   const long long place = slot < 0 ? 0 : ((slot >> a.page_bits) * a.Hkv << a.page_bits) + (slot & ((1ll << a.page_bits) - 1));
-  // this lane's angles: the partner of channel i is i +- half, or i +- 1
-  double cs[8], sn[8];
+  // What this lane's channels and their partners (i +- half, or i +- 1) are multiplied with: cosine and sine, times the weights of the kind of head at hand, so that a channel takes
+  // a product, a multiply-add and one division by the norm
+  double own[8], other[8];
+  // the partners of eight values v of a row x (0 where there is none)
+  auto partners = [&](const uint32_t (&v)[4], const uint16_t* x, bool live, uint32_t (&p)[4]) {
 #pragma unroll
-  for (int i = 0; i < 8; i++) {
-    const int ch = c0 + i;
-    const bool turned = ch < a.rotary;
-    const bool second = a.paired ? (i & 1) : ch >= half;
-    const int at = !turned ? 0 : (a.paired ? ch >> 1 : (second ? ch - half : ch));
-    cs[i] = turned ? turn[0][at] : 1.;
-    sn[i] = turned ? (second ? turn[1][at] : -turn[1][at]) : 0.;
-  }
-  const int first = (int)((long long)a.rows * chunk / a.chunks), end = (int)((long long)a.rows * (chunk + 1) / a.chunks);
-  for (int r0 = first; r0 < end; r0 += ROWS) {
-    const int r = r0 + (int)(threadIdx.x / LN);
+    for (int i = 0; i < 4; i++) p[i] = 0u;
+    if (a.paired) {
+#pragma unroll
+      for (int i = 0; i < 4; i++) p[i] = v[i] >> 16 | v[i] << 16;
+    } else if ((half & 7) == 0) {  // a lane of the same row has them
+      const int from = (int)(threadIdx.x & 63u) + (c0 < half ? half / 8 : -(half / 8));
+#pragma unroll
+      for (int i = 0; i < 4; i++) p[i] = (uint32_t)__shfl((int)v[i], c0 < a.rotary ? from : 0);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; i++) {
+        const int ch = c0 + i;
+        if (live && ch < a.rotary) p[i / 2] |= (uint32_t)x[ch < half ? ch + half : ch - half] << (16 * (i & 1));
+      }
+    }
+  };
+  auto factors = [&](int kind) {
+    const uint16_t* w = kind ? a.kw : a.qw;
+    uint32_t g[4], p[4];
+#pragma unroll
+    for (int i = 0; i < 4; i++) g[i] = kind ? weight[1][i] : weight[0][i];
+    if (w) partners(g, w, true, p);
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+      const int ch = c0 + i;
+      const bool turned = ch < a.rotary, second = a.paired ? (i & 1) : ch >= half;
+      const int at = !turned ? 0 : (a.paired ? ch >> 1 : (second ? ch - half : ch));
+      own[i] = turned ? turn[0][at] : 1.;
+      other[i] = turned ? (second ? turn[1][at] : -turn[1][at]) : 0.;
+      if (w) {
+        own[i] *= (double)esp_to_float<DT>((uint16_t)(g[i / 2] >> (16 * (i & 1))));
+        other[i] *= (double)esp_to_float<DT>((uint16_t)(p[i / 2] >> (16 * (i & 1))));
+      }
+    }
+  };
+  int known = -1;  // the kind that they are of
+  for (int r1 = first; r1 < end; r1 += PASSES * ROWS) {
+    if (r1 > first) fetch(r1);
+#pragma unroll 1
+  for (int u = 0; u < PASSES; u++) {
+    const int r = r1 + u * ROWS + (int)(threadIdx.x / LN);
+    if (r1 + u * ROWS >= end) break;
     const bool live = r < end;
-    // 0 queries, 1 keys, 2 values
-    const int kind = r < a.Hq ? 0 : (r < a.Hq + a.Hkv ? 1 : 2);
-    const int head = kind == 0 ? r : (kind == 1 ? r - a.Hq : r - a.Hq - a.Hkv);
-    const uint16_t* x = kind == 0 ? a.q + t * a.ldq : (kind == 1 ? a.k + t * a.ldk : a.v + t * a.ldv);
-    x += (long long)head * a.D;
-    uint32_t v[4] = {0u, 0u, 0u, 0u};
-    if (live) load_8(x + c0, a.D - c0, v);
+    int kind, head;
+    const uint16_t* x = row_at(live ? r : first, kind, head);
+    uint32_t v[4];
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+      v[i] = ahead[0][i];
+#pragma unroll
+      for (int e = 1; e < PASSES; e++) v[i] = u == e ? ahead[e][i] : v[i];
+    }
     const long long row = place + ((long long)head << a.page_bits);
     MxCodes codes = {0u, 0u};
     unsigned e = 0;
@@ -129,6 +242,7 @@ __global__ void __launch_bounds__(NT) k_rotate_heads(const RotateArgs a) {
       codes = mx_encode<DT, ESPARSE_MX_FP4>(v, e);
     } else {
       const uint16_t* w = kind == 0 ? a.qw : a.kw;
+      const bool exact = kind == 1 && a.slots;  // (what is rounded to 16 bits has no border that a last bit decides)
       double y[8], z[8];
       widen_8<DT>(v, y);
       double by = 1., n = 0.;
@@ -136,66 +250,46 @@ __global__ void __launch_bounds__(NT) k_rotate_heads(const RotateArgs a) {
         double s = 0.;
 #pragma unroll
         for (int i = 0; i < 8; i++) s = __builtin_fma(y[i], y[i], s);
-        n = __builtin_sqrt(row_sum<LN>(s) / (double)a.D + a.eps);
-        by = 1. / n;
-        n = __builtin_isfinite(n) ? n : 0.;
-        uint32_t g[4] = {0u, 0u, 0u, 0u};
-        if (live) load_8(w + c0, a.D - c0, g);
-        widen_8<DT>(g, z);
-#pragma unroll
-        for (int i = 0; i < 8; i++) y[i] = over(y[i] * z[i], by, n);
-      }
-      if (half) {
-        if (a.paired) {
-#pragma unroll
-          for (int i = 0; i < 8; i++) z[i] = y[i ^ 1];
+        s = row_sum<LN>(s);
+        if (exact) {
+          n = __builtin_sqrt(s / (double)a.D + a.eps);
+          by = 1. / n;
+          n = __builtin_isfinite(n) ? n : 0.;
         } else {
-          uint32_t p[4] = {0u, 0u, 0u, 0u}, g[4] = {0u, 0u, 0u, 0u};
-          if (live && c0 < a.rotary) {
-            if ((half & 7) == 0) {
-              const int from = c0 < half ? c0 + half : c0 - half;
-              load_8(x + from, a.D - from, p);
-              if (w) load_8(w + from, a.D - from, g);
-            } else {  // a lane's eight partners are not neighbours
-#pragma unroll
-              for (int i = 0; i < 8; i++) {
-                const int ch = c0 + i;
-                if (ch < a.rotary) {
-                  const int from = ch < half ? ch + half : ch - half;
-                  p[i / 2] |= (uint32_t)x[from] << (16 * (i & 1));
-                  if (w) g[i / 2] |= (uint32_t)w[from] << (16 * (i & 1));
-                }
-              }
-            }
-          }
-          widen_8<DT>(p, z);
-          if (w) {
-            double u[8];
-            widen_8<DT>(g, u);
-#pragma unroll
-            for (int i = 0; i < 8; i++) z[i] = over(z[i] * u[i], by, n);
-          }
+          by = inverse_root(__builtin_fma(s, a.per_channel, a.eps));
         }
-        // (a channel that is not turned keeps its value, whatever its partner holds)
+      }
+      if (half || w) {
+        if (known != kind) factors(kind);
+        known = kind;
+        uint32_t p[4];
+        partners(v, x, live, p);
+        widen_8<DT>(p, z);
 #pragma unroll
-        for (int i = 0; i < 8; i++)
-          if (c0 + i < a.rotary) y[i] = __builtin_fma(z[i], sn[i], y[i] * cs[i]);
+        for (int i = 0; i < 8; i++) {
+          y[i] *= own[i];
+          if (c0 + i < a.rotary) y[i] = __builtin_fma(z[i], other[i], y[i]);  // (a channel that is not turned keeps its value, whatever its partner holds)
+        }
+        if (w) {
+#pragma unroll
+          for (int i = 0; i < 8; i++) y[i] = exact ? over(y[i], by, n) : y[i] * by;
+        }
       }
 #pragma unroll
       for (int i = 0; i < 8; i++)
         if (c0 + i >= a.D) y[i] = 0.;  // (0 times an infinite 1 / norm is no 0)
       uint16_t* out = kind == 0 ? a.q_out : a.k_out;
       if (out && live) {
-        uint16_t o[8];
+        uint32_t o[4];
 #pragma unroll
-        for (int i = 0; i < 8; i++) o[i] = esp_from_float<DT>((float)y[i]);
+        for (int i = 0; i < 4; i++) o[i] = pack_2<DT>((float)y[2 * i], (float)y[2 * i + 1]);
         out += (t * (kind == 0 ? a.Hq : a.Hkv) + head) * a.D + c0;
         if (a.D - c0 >= 8) {
           store_stream_16(out, o);
         } else {
 #pragma unroll
           for (int i = 0; i < 8; i++)
-            if (c0 + i < a.D) out[i] = o[i];
+            if (c0 + i < a.D) out[i] = (uint16_t)(o[i / 2] >> (16 * (i & 1)));
         }
       }
       if (kind == 1 && a.slots) {
@@ -216,6 +310,7 @@ __global__ void __launch_bounds__(NT) k_rotate_heads(const RotateArgs a) {
       }
     }
     if (kind && live && slot >= 0) put_row<DP>(kind == 1 ? a.k_data : a.v_data, kind == 1 ? a.k_scales : a.v_scales, row, lane, codes, e);
+  }
   }
 }
 
@@ -294,7 +389,7 @@ int esp_rotate_heads_device(esparse_ctx* ctx, const esparse_heads* h, long long 
   a.q_out = (uint16_t*)q_out, a.k_out = (uint16_t*)k_out;
   a.positions = positions, a.frequencies = frequencies;
   a.ldq = ldq, a.ldk = ldk, a.ldv = ldv, a.T = T;
-  a.Hq = q ? h->q_heads : 0, a.Hkv = k ? h->kv_heads : 0, a.D = h->head_dim, a.rotary = h->rotary, a.paired = h->paired, a.eps = h->eps;
+  a.Hq = q ? h->q_heads : 0, a.Hkv = k ? h->kv_heads : 0, a.D = h->head_dim, a.rotary = h->rotary, a.paired = h->paired, a.eps = h->eps, a.per_channel = 1. / h->head_dim;
   if (cache) {
     a.slots = slots;
     a.k_data = (unsigned char*)cache->k_data, a.k_scales = (unsigned char*)cache->k_scales;

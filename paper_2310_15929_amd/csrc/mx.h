@@ -39,6 +39,14 @@ __device__ __forceinline__ uint32_t mx_saturate_fp8(uint32_t w) {
   return w - ((((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7);
 }
 
+// two numbers in 16 bits, rounded to even by one instruction (bf16), or one each
+template <int DT>
+__device__ __forceinline__ uint32_t pack_2(float a, float b) {
+  const esp_float2 v = {a, b};
+  if constexpr (DT == ESPARSE_F16) return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, esp_half2));
+  else return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, esp_bf16x2));
+}
+
 // a lane's neighbours: the other lanes of its quad, and of its row of 16 by rotation
 template <int CTRL>
 __device__ __forceinline__ uint32_t lane_move(uint32_t v) {
