@@ -10,7 +10,8 @@
 //           hands a lane four tokens of one channel.  P is rounded to the 16 bits of the output's type, as V is held: the matrix instruction takes both so; sums
 //           and statistics are in 32 bits.
 // The statistics of a row are those of a column of X^T: they stay in the lane but for two exchanges (lanes 16 and 32 apart) a strip of 32 tokens.
-// A block without number (scale 255) of V is left out of the product and put into the rows that see its token afterwards, so that masked tokens cannot reach a row.
+// A block of V that has no numbers in 16 bits (scale 255, or so large that some would be infinite) is left out of the product and makes the rows that see its token NaN afterwards, so that
+// masked tokens cannot reach a row.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -83,6 +84,10 @@ __device__ __forceinline__ int pieces_of(int end, int pieces) {
   const int strips = (end + STRIP - 1) / STRIP, most = (strips + LEAST - 1) / LEAST;
   return most < pieces ? (most > 0 ? most : 1) : pieces;
 }
+
+// the largest scale with which all codes have numbers of the type: 6 x 2^13 and 6 x 2^125
+template <int DT>
+constexpr unsigned kLargest = DT == ESPARSE_F16 ? 140 : 252;
 
 // channels of a lane's operand of step s (eight of them)
 template <int DP>
@@ -309,7 +314,7 @@ __global__ void __launch_bounds__(64 * WAVES, DP == 256 ? 2 : 3) k_attend_few(co
     for (int u = 0; u < 2; u++) {
       if (strip * STRIP + 16 * u + c >= t.end) now.v[u] = Codes<DP>{};  // tokens that no row sees: no numbers of theirs take part
 #pragma unroll
-      for (int i = 0; i < NE; i++) odd[u][i] = __ballot(now.v[u].e[i] == 255u);
+      for (int i = 0; i < NE; i++) odd[u][i] = __ballot(now.v[u].e[i] > kLargest<DT>);
     }
 #pragma unroll
     for (int hh = 0; hh < NH; hh++) {
@@ -317,10 +322,11 @@ __global__ void __launch_bounds__(64 * WAVES, DP == 256 ? 2 : 3) k_attend_few(co
 #pragma unroll
       for (int u = 0; u < 2; u++) {
         const unsigned e = now.v[u].e[hh];
-        const float by = mx_scale(e == 255u ? 0u : e);
+        const bool bad = e > kLargest<DT>;
+        const float by = mx_scale(bad ? 0u : e);
 #pragma unroll
         for (int s = 0; s < NS / NH; s++)
-          *reinterpret_cast<uint4*>(vt + (16 * u + c) * kVRow<DP> + channel_of<DP>(s, g)) = mx_widen<DT>(e == 255u ? 0u : now.v[u].w[NS / NH * hh + s], by);
+          *reinterpret_cast<uint4*>(vt + (16 * u + c) * kVRow<DP> + channel_of<DP>(s, g)) = mx_widen<DT>(bad ? 0u : now.v[u].w[NS / NH * hh + s], by);
       }
       wave_fence();
 #pragma unroll
@@ -560,7 +566,7 @@ __global__ void __launch_bounds__(64 * W, 2) k_attend_many(const AttendArgs a) {
     for (int it = 0; it < ITEMS; it++) {
       const int item = it * THREADS + (int)threadIdx.x, piece = item % CH, token = piece / (DP / 32), block = piece % (DP / 32);
       if (item >= 2 * CH) break;
-      const bool keys = item < CH, bad = keys ? !there[it] : scl[it] == 255u;
+      const bool keys = item < CH, bad = keys ? !there[it] : scl[it] > kLargest<DT>;
       const unsigned long long marks = __ballot(bad);
       if (lane == 0) odd[buffer][item / 64] = marks;
       uint16_t* to = (keys ? kb + token * kKRow<DP> : vb + token * kWideV<DP>) + 32 * block;

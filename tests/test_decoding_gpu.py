@@ -341,6 +341,23 @@ def test_attention_is_not_touched_by_what_it_does_not_see(ctx, nq, dtype):
     assert np.isnan(o[sees][:, :2]).all() and np.array_equal(o[~sees], w[~sees]) and np.array_equal(o[:, 2:], w[:, 2:])
 
 
+@pytest.mark.parametrize("dtype,scale", [("f16", 141), ("f16", 200), ("bf16", 253)])
+@pytest.mark.parametrize("nq", [3, 160])
+def test_attention_is_not_touched_by_values_beyond_the_type(ctx, nq, dtype, scale):
+    rng = _rng("beyond", nq, dtype)
+    D, page, H, n = 64, 16, 1, 190
+    table, pages = _tables(rng, [n], page)
+    k, v = _pool(rng, pages, H, page, D), _pool(rng, pages, H, page, D)
+    q = torch.from_numpy(rng.standard_normal((nq, 2, D))).to(TORCH[dtype]).cuda()
+    starts = _i32([0, nq])
+    first = _np(ctx.cache_attention(q, _cache(k, v, D), _i32(table), _i32([n]), starts=starts))
+    v[1][table[0, (n - 2) // page], 0, (n - 2) % page, 1] = scale   # the last token but one
+    o = _np(ctx.cache_attention(q, _cache(k, v, D), _i32(table), _i32([n]), starts=starts))
+    assert np.array_equal(o[:-2], first[:-2]) and np.array_equal(o[:, :, :32], first[:, :, :32]) and np.isnan(o[-2:, :, 32:]).all()
+    v[1][table[0, (n - 2) // page], 0, (n - 2) % page, 1] = 140 if dtype == "f16" else 252
+    assert np.isfinite(_np(ctx.cache_attention(q, _cache(k, v, D), _i32(table), _i32([n]), starts=starts))).all()
+
+
 def test_attention_leaves_rows_of_no_sequence(ctx):
     rng = _rng("rows")
     D, page, H = 64, 16, 1
