@@ -505,6 +505,24 @@ def test_drawn_among_equal_logits(ctx, dtype):
             _draw(ctx, x, np.full(len(rows), u), str(cuts), **cuts)
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+def test_drawn_with_a_cut_right_below_zero(ctx, dtype):
+    """Many logits of exactly 0 and -0, and the cut among the numbers just below: the zeros lie in the range above the cut's, and count once."""
+    rng = _rng("zero", dtype)
+    V = 6000
+    x = np.full((4, V), -30.0)
+    x[:, rng.permutation(V)[:2500]] = -0.06 * rng.random(2500) - 1e-3
+    x[:, rng.permutation(V)[:900]] = np.where(rng.random(900) < 0.5, 0.0, -0.0)
+    x[:, 77] = 1.5
+    t = torch.from_numpy(x).to(TORCH[dtype]).cuda()
+    for top_p in (0.4, 0.5, 0.7, 0.9):
+        for u in np.linspace(0, 0.999, 7):
+            _draw(ctx, t, np.full(4, u), str((top_p, u)), top_p=top_p)
+            _draw(ctx, t, np.full(4, u), str((top_p, u)), top_p=top_p, min_p=float(np.exp(-1.53)))
+            _draw(ctx, t, np.full(4, u), str((top_p, u)), min_p=float(np.exp(-1.53)))
+    _draw(ctx, t, rng.random(4), top_k=2400)
+
+
 def test_drawn_tokens_follow_their_shares(ctx):
     """Every token in turn: u just above and below the border of two shares, where 64 bits tell them apart."""
     V = 64
