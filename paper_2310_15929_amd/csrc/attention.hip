@@ -704,13 +704,20 @@ int most_pieces(long long items, long long tokens) {
 
 }  // namespace
 
-// Rows of a sequence from which the tiles of 128 rows are used, and from which those of 256 are: on average, the lengths are not known here
-constexpr long long MANY = 64, MOST = 1024;
-long long rows_each(long long T, int B, int group, bool ragged) { return ragged ? T * group / B : group; }
+// Waves of a workgroup of the kernel for many rows (128 or 256 rows), 0: the kernel for few rows.  Both take a time that grows with the lengths, which are not known here.  The kernel for few rows
+// spreads any number of rows over the chip by cutting the tokens into pieces, the other needs workgroups: one sequence of 8192 tokens, 64 heads on 8 of 128 channels, with 16, 64,
+// 256, 512, 1024 queries 30, 76, 206, 363, 557 us against 296, 305, 304, 304, 327; 16 heads on 4 of 256 channels with 16, 256, 1024 queries 25, 171, 485 against 900 throughout.
+// So by the number of tiles of sixteen rows; and of few rows for each sequence most of a tile of 128 would be empty.
+constexpr long long MANY_ROWS = 64, MOST_ROWS = 1024;
+int waves_of_many(long long T, int B, int group, int Hkv, int row, bool ragged) {
+  const long long each = ragged ? T * group / B : group, tiles = (T * group + ROWS - 1) / ROWS * Hkv;
+  if (each < MANY_ROWS || tiles < (row == 256 ? 2048 : 1536)) return 0;
+  return each >= MOST_ROWS && tiles_of(T, B, group, ragged, 256) * Hkv >= 256 ? 8 : 4;
+}
 
 size_t esp_cache_attention_workspace(const esparse_cache* cache, long long T, int B, int q_heads, long long width, bool ragged) {
   const int group = q_heads / cache->heads, dp = esp_cache_row(cache->head_dim);
-  if (rows_each(T, B, group, ragged) >= MANY) return 0;
+  if (waves_of_many(T, B, group, cache->heads, dp, ragged)) return 0;
   const long long items = tiles_of(T, B, group, ragged, ROWS) * cache->heads;
   const int pieces = most_pieces(items, width * cache->page);
   return pieces == 1 ? 0 : (size_t)items * pieces * (ROWS * dp + 2 * ROWS) * sizeof(float);
@@ -729,9 +736,7 @@ int esp_cache_attention_device(esparse_ctx* ctx, const void* q, long long ldq, l
   a.B = B, a.Hkv = cache->heads, a.group = q_heads / cache->heads, a.D = cache->head_dim, a.page_bits = __builtin_ctz((unsigned)cache->page);
   a.c = (float)(scale * 1.4426950408889634);
   const int row = esp_cache_row(a.D);
-  const long long each = rows_each(T, B, a.group, starts != nullptr);
-  if (each >= MANY) {
-    const int waves = each >= MOST ? 8 : 4;
+  if (const int waves = waves_of_many(T, B, a.group, a.Hkv, row, starts != nullptr)) {
     a.tiles = (int)tiles_of(T, B, a.group, starts != nullptr, 32 * waves);
     const dim3 grid((unsigned)a.tiles * (unsigned)a.Hkv);
 #define GO(DT, DP, W)                                                                            \

@@ -285,7 +285,10 @@ def test_attention_of_one_token_each(ctx, lengths, Hq, H, D, page, dtype):
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
 @pytest.mark.parametrize("lengths,queries,Hq,H,D,page", [
     ([5, 40, 100], [5, 1, 3], 4, 2, 64, 16), ([70, 3, 0, 200], [70, 7, 2, 31], 3, 1, 128, 32), ([260, 1, 130], [130, 0, 130], 10, 5, 80, 64),
-    ([400], [400], 2, 2, 128, 64), ([1500, 300], [1100, 290], 3, 1, 80, 32), ([1030], [1030], 1, 1, 256, 16), ([2100], [1025], 2, 2, 50, 64), ([333, 150], [33, 150], 12, 2, 256, 16), ([129, 64, 65, 1], [129, 64, 65, 1], 1, 1, 96, 16), ([600], [300], 8, 1, 128, 128)])
+    ([400], [400], 2, 2, 128, 64), ([1500, 300], [1100, 290], 3, 1, 80, 32), ([1030], [1030], 1, 1, 256, 16), ([2100], [1025], 2, 2, 50, 64), ([333, 150], [33, 150], 12, 2, 256, 16), ([129, 64, 65, 1], [129, 64, 65, 1], 1, 1, 96, 16), ([600], [300], 8, 1, 128, 128),
+    # enough rows for tiles of 128, and of 256
+    ([500, 130], [300, 130], 64, 8, 80, 16), ([400], [350], 96, 2, 256, 32), ([70, 333, 0, 40], [70, 333, 0, 60], 64, 2, 64, 64), ([1100], [1050], 64, 8, 128, 64),
+    ([700], [600], 128, 4, 50, 16), ([300, 290], [280, 280], 128, 1, 192, 16)])
 def test_attention_of_several_tokens(ctx, lengths, queries, Hq, H, D, page, dtype):
     """Prompts, drafts, sequences without queries or with more queries than tokens."""
     rng = _rng("several", *lengths, D, dtype)
@@ -293,33 +296,34 @@ def test_attention_of_several_tokens(ctx, lengths, queries, Hq, H, D, page, dtyp
     k, v = _pool(rng, pages, H, page, D), _pool(rng, pages, H, page, D)
     starts = np.concatenate(([0], np.cumsum(queries)))
     q = torch.from_numpy(rng.standard_normal((starts[-1], Hq, D))).to(TORCH[dtype]).cuda()
-    _check_attention(ctx, q, k, v, table, lengths, starts, page, D, dtype)
+    _check_attention(ctx, q, k, v, table, lengths, starts, page, D, dtype, heads=None if Hq <= 20 else [0, Hq // 2 + 1, Hq - 1])
 
 
-@pytest.mark.parametrize("nq", [1, 3, 200])
-def test_attention_leaves_out_pages_that_are_none(ctx, nq):
+@pytest.mark.parametrize("nq,Hq", [(1, 4), (3, 4), (200, 4), (200, 64), (200, 180)])
+def test_attention_leaves_out_pages_that_are_none(ctx, nq, Hq):
     rng = _rng("pages", nq)
     lengths, page, D, H = [333, 260], 32, 128, 2
     table, pages = _tables(rng, lengths, page)
     table[0, 2], table[0, 5], table[0, 10], table[1, 0] = -1, pages, 2 ** 31 - 1, -2 ** 31
     k, v = _pool(rng, pages, H, page, D), _pool(rng, pages, H, page, D)
     starts = None if nq == 1 else np.array([0, nq, 2 * nq])
-    q = torch.from_numpy(rng.standard_normal((2 * nq, 4, D))).to(torch.float16).cuda()
-    _check_attention(ctx, q, k, v, table, lengths, starts, page, D, "f16")
+    q = torch.from_numpy(rng.standard_normal((2 * nq, Hq, D))).to(torch.float16).cuda()
+    heads = [0, 1, Hq - 1]
+    _check_attention(ctx, q, k, v, table, lengths, starts, page, D, "f16", heads=heads)
     table[0] = -1
-    out, sums = _check_attention(ctx, q, k, v, table, lengths, starts, page, D, "f16")
+    out, sums = _check_attention(ctx, q, k, v, table, lengths, starts, page, D, "f16", heads=heads)
     assert (out[:nq] == 0).all() and torch.isneginf(sums[:nq]).all()
 
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
-@pytest.mark.parametrize("nq", [1, 5, 160])
-def test_attention_is_not_touched_by_what_it_does_not_see(ctx, nq, dtype):
+@pytest.mark.parametrize("nq,Hq", [(1, 4), (5, 4), (160, 4), (160, 192), (160, 512)])
+def test_attention_is_not_touched_by_what_it_does_not_see(ctx, nq, Hq, dtype):
     """Bytes behind a sequence, and later tokens of a prompt, hold NaN and the largest scales."""
     rng = _rng("unseen", nq, dtype)
     D, page, H, n = 128, 32, 2, 209
     table, pages = _tables(rng, [n], page)
     k, v = _pool(rng, pages, H, page, D), _pool(rng, pages, H, page, D)
-    q = torch.from_numpy(rng.standard_normal((nq, 4, D))).to(TORCH[dtype]).cuda()
+    q = torch.from_numpy(rng.standard_normal((nq, Hq, D))).to(TORCH[dtype]).cuda()
     starts = None if nq == 1 else np.array([0, nq])
     first = ctx.cache_attention(q, _cache(k, v, D), _i32(table), _i32([n]), starts=None if starts is None else _i32(starts), lse=True)
     for t in (k, v):
@@ -334,21 +338,21 @@ def test_attention_is_not_touched_by_what_it_does_not_see(ctx, nq, dtype):
     third = ctx.cache_attention(q, _cache(k, v, D), _i32(table), _i32([n]), starts=None if starts is None else _i32(starts), lse=True)
     o, w = _np(third[0]), _np(first[0])
     sees = np.arange(nq) + n - nq >= seen
-    assert np.isnan(o[sees][:, :2, 64:96]).all() and np.array_equal(o[~sees], w[~sees]) and np.array_equal(o[:, 2:], w[:, 2:])
-    assert np.array_equal(o[:, :2, :64], w[:, :2, :64]) and np.array_equal(o[:, :2, 96:], w[:, :2, 96:]) and torch.equal(third[1], first[1])
+    assert np.isnan(o[sees][:, :Hq // 2, 64:96]).all() and np.array_equal(o[~sees], w[~sees]) and np.array_equal(o[:, Hq // 2:], w[:, Hq // 2:])
+    assert np.array_equal(o[:, :Hq // 2, :64], w[:, :Hq // 2, :64]) and np.array_equal(o[:, :Hq // 2, 96:], w[:, :Hq // 2, 96:]) and torch.equal(third[1], first[1])
     k[1][at + (1,)] = 255
     o = _np(ctx.cache_attention(q, _cache(k, v, D), _i32(table), _i32([n]), starts=None if starts is None else _i32(starts)))
-    assert np.isnan(o[sees][:, :2]).all() and np.array_equal(o[~sees], w[~sees]) and np.array_equal(o[:, 2:], w[:, 2:])
+    assert np.isnan(o[sees][:, :Hq // 2]).all() and np.array_equal(o[~sees], w[~sees]) and np.array_equal(o[:, Hq // 2:], w[:, Hq // 2:])
 
 
 @pytest.mark.parametrize("dtype,scale", [("f16", 141), ("f16", 200), ("bf16", 253)])
-@pytest.mark.parametrize("nq", [3, 160])
-def test_attention_is_not_touched_by_values_beyond_the_type(ctx, nq, dtype, scale):
+@pytest.mark.parametrize("nq,Hq", [(3, 2), (160, 2), (160, 192), (160, 512)])
+def test_attention_is_not_touched_by_values_beyond_the_type(ctx, nq, Hq, dtype, scale):
     rng = _rng("beyond", nq, dtype)
     D, page, H, n = 64, 16, 1, 190
     table, pages = _tables(rng, [n], page)
     k, v = _pool(rng, pages, H, page, D), _pool(rng, pages, H, page, D)
-    q = torch.from_numpy(rng.standard_normal((nq, 2, D))).to(TORCH[dtype]).cuda()
+    q = torch.from_numpy(rng.standard_normal((nq, Hq, D))).to(TORCH[dtype]).cuda()
     starts = _i32([0, nq])
     first = _np(ctx.cache_attention(q, _cache(k, v, D), _i32(table), _i32([n]), starts=starts))
     v[1][table[0, (n - 2) // page], 0, (n - 2) % page, 1] = scale   # the last token but one
@@ -384,9 +388,11 @@ def test_attention_with_sharp_scores(ctx, dtype, factor):
     k, v = _pool(rng, pages, H, page, D), _pool(rng, pages, H, page, D)
     q = torch.from_numpy(factor * rng.standard_normal((90, 2, D))).to(TORCH[dtype]).cuda()
     _check_attention(ctx, q, k, v, table, lengths, np.array([0, 50, 90]), page, D, dtype)
+    wide = q.repeat(1, 140, 1)   # enough heads for the kernel of many rows
+    _check_attention(ctx, wide, k, v, table, lengths, np.array([0, 50, 90]), page, D, dtype, heads=[0, 279])
     for scale in (-0.05, 0.0):
         _check_attention(ctx, q[:2], k, v, table, lengths, None, page, D, dtype, scale=scale)
-        _check_attention(ctx, q, k, v, table, lengths, np.array([0, 50, 90]), page, D, dtype, scale=scale)
+        _check_attention(ctx, wide, k, v, table, lengths, np.array([0, 50, 90]), page, D, dtype, scale=scale, heads=[0, 279])
 
 
 def test_attention_long_context(ctx):
