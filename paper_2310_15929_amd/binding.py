@@ -828,18 +828,21 @@ class Context:
         return t.data_ptr()
 
     def _check_cache(self, name: str, c: KVCache) -> _Cache:
-        if c.k_data.dim() != 4:
-            raise ValueError(f"{name}: the cache's k_data has {c.k_data.dim()} dimensions instead of four")
-        P, H, page, _ = c.k_data.shape
-        if not 1 <= c.head_dim <= 256 or not 16 <= page <= 1024 or page & (page - 1):
-            raise ValueError(f"{name}: a cache of pages of {page} tokens and heads of {c.head_dim} channels")
-        row = 64 if c.head_dim <= 64 else 128 if c.head_dim <= 128 else 256
-        for t, last in ((c.k_data, row // 2), (c.k_scales, row // 32), (c.v_data, row // 2), (c.v_scales, row // 32)):
-            if t.get_device() != self.device:
-                self._away(name, t)
-            if t.dtype != torch.uint8 or t.shape != (P, H, page, last) or not t.is_contiguous():
-                raise ValueError(f"{name}: the cache's tensors are contiguous uint8 [{P}, {H}, {page}, {row // 2}] and [.., {row // 32}]")
-        return _Cache(c.k_data.data_ptr(), c.k_scales.data_ptr(), c.v_data.data_ptr(), c.v_scales.data_ptr(), P, page, H, c.head_dim)
+        kd, ks, vd, vs, D = c.k_data, c.k_scales, c.v_data, c.v_scales, c.head_dim
+        shape = kd.shape
+        if len(shape) != 4:
+            raise ValueError(f"{name}: the cache's k_data has {len(shape)} dimensions instead of four")
+        P, H, page, half = shape
+        if not 1 <= D <= 256 or not 16 <= page <= 1024 or page & (page - 1):
+            raise ValueError(f"{name}: a cache of pages of {page} tokens and heads of {D} channels")
+        at, u8 = self.device, torch.uint8
+        if kd.get_device() != at or ks.get_device() != at or vd.get_device() != at or vs.get_device() != at:
+            self._away(name, kd, ks, vd, vs)
+        if (half != (32 if D <= 64 else 64 if D <= 128 else 128) or vd.shape != shape or ks.shape != (P, H, page, half // 16) or vs.shape != ks.shape
+                or kd.dtype != u8 or ks.dtype != u8 or vd.dtype != u8 or vs.dtype != u8
+                or not (kd.is_contiguous() and ks.is_contiguous() and vd.is_contiguous() and vs.is_contiguous())):
+            raise ValueError(f"{name}: the cache's tensors are contiguous uint8 [{P}, {H}, {page}, row / 2] and [.., row / 32], row = 64, 128 or 256 for {D} channels")
+        return _Cache(kd.data_ptr(), ks.data_ptr(), vd.data_ptr(), vs.data_ptr(), P, page, H, D)
 
     def kv_cache(self, pages: int, page: int, heads: int, head_dim: int) -> KVCache:
         """An empty cache of `pages` pages of `page` tokens (a power of two, 16 .. 1024)."""
@@ -910,7 +913,9 @@ class Context:
         code, c, T = _code(dtype, "cache_read", f32=True), self._check_cache("cache_read", cache), slots.numel()
         sp = self._vector("cache_read", "slots", slots, torch.int32, T)
         H, D = c.heads, c.head_dim
-        k, v = (_EMPTY((T, H, D), (H * D, D, 1), dtype=dtype, device=self._on) for _ in range(2))
+        shape, strides = (T, H, D), (H * D, D, 1)
+        k = _EMPTY(shape, strides, dtype=dtype, device=self._on)
+        v = _EMPTY(shape, strides, dtype=dtype, device=self._on)
         self._sync_stream()
         rc = self._lib.esparse_cache_read(self._h, C.byref(c), sp, T, code, k.data_ptr(), v.data_ptr())
         if rc:

@@ -9,6 +9,9 @@
 //           way P^T is an operand as it stands.  V needs token and channel exchanged: it goes through LDS in 16 bits and comes back by the transposing read, which
 //           hands a lane four tokens of one channel.  P is rounded to the 16 bits of the output's type, as V is held: the matrix instruction takes both so; sums
 //           and statistics are in 32 bits.
+// Bound by memory at one token a sequence where there is work for the chip: 48 sequences of 500 to 4096 tokens, 32 heads of 128 channels, 115 us (4.2 TB/s; a copy reaches 4.9), by
+// the few waves that its registers leave to cover the latency of a strip (a third of a wave's time it waits for memory, a fifth for a slot of the vector unit, which is busy 55 %);
+// 131072 tokens, 64 heads on 8, 33 us and 5 to join the pieces (3.8 TB/s).  256 channels take twice the registers: 21 sequences of five tokens each, 16 heads on 4, 83 us (1.3 TB/s).
 // The statistics of a row are those of a column of X^T: they stay in the lane but for two exchanges (lanes 16 and 32 apart) a strip of 32 tokens.
 // A block of V that has no numbers in 16 bits (scale 255, or so large that some would be infinite) is left out of the product and makes the rows that see its token NaN afterwards, so that
 // masked tokens cannot reach a row.
@@ -479,6 +482,9 @@ __global__ void __launch_bounds__(256) k_attend_join(const AttendArgs a) {
 // A workgroup of W waves takes 32 W rows, 32 a wave as the columns of the 32 x 32 instruction (lane 32 h + c: operands hold k = 8 h .. 8 h + 7 of row / column c, results rows
 // 8 (j / 4) + 4 h + j % 4 of column c).  The tokens come in tiles that all waves share, brought to 16 bits once, in two buffers: while one is multiplied the
 // codes of the tile after the next are on their way and the next is written to the other buffer.
+// Measured: 8192 tokens, 64 heads on 8 of 128 channels 1390 us (790 TFLOP/s, where a large library product of the type reaches 1570; the matrix pipe is busy 30 %, the vector unit 50 %,
+// mostly with exponentials): two waves a SIMD do not cover each other's waits.  The keys a tile ahead of the values, so that their products stand beside the exponentials, a higher priority of the waves
+// in the products, and 32 tokens a tile were built and were slower (1490, 1500, 1520).
 template <int DP>
 constexpr int kTile = DP == 256 ? 32 : 64;  // tokens of a tile
 template <int DP>
