@@ -393,7 +393,7 @@ int esparse_cache_read(esparse_ctx* ctx, const esparse_cache* cache, const int32
  * Negative lengths count as 0, longer ones than the table has room for as that; tokens in a page outside [0, pages) are left out, as are all rows of q that belong to no sequence: those rows of
  * out and lse are left as they were.  Tokens that a query does not see do not touch it, whatever their places hold.
  * Keys, probabilities and values take part in the 16 bits of dtype, which hold the cache's numbers as said at esparse_mx_gemm; sums and statistics are in 32 bits.
- * q must be finite; a key without number (scale 255) makes the queries that see it NaN, such a block of a value its channels, and so does one whose scale is beyond 2^13 (f16) or 2^125
+ * scale: up to 1e38.  q must be finite; a key without number (scale 255) makes the queries that see it NaN, such a block of a value its channels, and so does one whose scale is beyond 2^13 (f16) or 2^125
  * (bf16): some of its numbers are beyond the type.
  * workspace: DEVICE scratch of esparse_cache_attention_workspace bytes (host only; may be 0; it reads the cache's sizes alone; ragged: 1 with starts, else 0), 256-byte aligned, overwritten.
  * Outputs and workspace may not overlap inputs or each other.  T = 0 or B = 0 is a no-op.  The order of a row's sums follows from the sizes and the sequence's length.

@@ -1071,7 +1071,7 @@ int esparse_cache_attention(esparse_ctx* ctx, const void* q, long long ldq, long
   ESP_REQUIRE(ctx, starts || T == B, ESPARSE_EINVAL, "%lld queries of %d sequences without starts", T, B);
   ESP_REQUIRE(ctx, attention_sizes(cache, T, B, q_heads, width, starts != nullptr), ESPARSE_EINVAL,
               "T = %lld, B = %d, q_heads = %d (on %d heads) or width = %lld out of range", T, B, q_heads, cache->heads, width);
-  ESP_REQUIRE(ctx, std::isfinite(scale), ESPARSE_EINVAL, "scale is not finite");
+  ESP_REQUIRE(ctx, std::fabs(scale) <= 1e38, ESPARSE_EINVAL, "scale is not a number up to 1e38");
   if (T == 0 || B == 0) return ESPARSE_OK;
   ESP_REQUIRE(ctx, q && out && lengths && (table || width == 0), ESPARSE_EINVAL, "q / out / lengths / table is null");
   const long long row = (long long)q_heads * cache->head_dim;

@@ -53,7 +53,8 @@ struct Tile {
 
 __device__ __forceinline__ long long clamp_to(long long v, long long lo, long long hi) { return v < lo ? lo : (v > hi ? hi : v); }
 
-// Tiles of sequence b begin at floor(starts[b] group / rows) + b: enough for all of its rows, found by counting the sequences that begin no later (64 at a time)
+// Tiles of sequence b begin at floor(starts[b] group / rows) + b: enough for all of its rows.  The last
+// sequence that begins no later is looked for among 64 at a time
 __device__ __forceinline__ Tile find_tile(const AttendArgs& a, int tile, int rows) {
   Tile t;
   if (!a.starts) {
@@ -63,15 +64,15 @@ __device__ __forceinline__ Tile find_tile(const AttendArgs& a, int tile, int row
     t.start = t.b;
     t.queries = 1;
   } else {
-    int before = 0;
-    for (int b0 = 0; b0 < a.B; b0 += 64) {
-      const int b = b0 + (int)(threadIdx.x & 63u);
-      const bool yes = b < a.B && clamp_to(a.starts[b < a.B ? b : 0], 0, a.T) * a.group / rows + b <= tile;
+    int lo = 0, hi = a.B;
+    while (hi - lo > 1) {
+      const int step = (hi - lo + 63) / 64, b = lo + (int)(threadIdx.x & 63u) * step;
+      const bool yes = b < hi && clamp_to(a.starts[b < hi ? b : lo], 0, a.T) * a.group / rows + b <= tile;
       const int found = (int)__popcll(__ballot(yes));
-      before += found;
-      if (found < 64) break;
+      lo += found > 0 ? (found - 1) * step : 0;
+      hi = lo + step < hi ? lo + step : hi;
     }
-    t.b = wave_uniform(before > 0 ? before - 1 : 0);
+    t.b = wave_uniform(lo);
     t.start = clamp_to(a.starts[t.b], 0, a.T);
     const long long stop = clamp_to(a.starts[t.b + 1], t.start, a.T);
     t.queries = (int)(stop - t.start);

@@ -669,7 +669,7 @@ __global__ void __launch_bounds__(NT) k_rows(const SampleArgs a) {
   Pick<u64, u64> by_number = {-1, 0, 0};
   if (counts(k)) by_number = pick<u64, u64>([&](int i) { return (u64)s.row_count[i]; }, row_weights, (u64)k);
   const u64 upto = by_number.part >= 0 ? by_number.before + s.row_count[by_number.part] : 0ull;
-  const bool cut_k = upto >= (u64)k && counts(k), all_listed = cut_k && upto <= LIST;
+  const bool cut_k = counts(k) && upto >= (u64)k, all_listed = counts(k) && upto <= LIST;  // (without the first: the row has fewer values than top_k)
   double total = 0.;  // of what is kept so far
   if (!all_listed) {
     if (!weighed) weigh_row<DT>(row, s);
@@ -690,7 +690,7 @@ __global__ void __launch_bounds__(NT) k_rows(const SampleArgs a) {
     const bool by_weight = phase > 0;
     bool fill = false;
     if (phase == 0) {
-      if (!cut_k) continue;
+      if (!cut_k && !all_listed) continue;
       bin = by_number.part;
       need = (u64)k;
       fill = all_listed;

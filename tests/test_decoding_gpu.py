@@ -529,6 +529,34 @@ def test_drawn_with_a_cut_right_below_zero(ctx, dtype):
     _draw(ctx, t, rng.random(4), top_k=2400)
 
 
+@pytest.mark.parametrize("left", [1, 20, 70, 3000, 5000])
+def test_drawn_from_rows_with_fewer_values_than_top_k(ctx, left):
+    """A mask leaves fewer values than top_k asks for: in a list, or too many for one."""
+    rng = _rng("left", left)
+    V = 20000
+    x = np.full((5, V), -np.inf)
+    for r in range(5):
+        x[r, rng.permutation(V)[:left]] = 2 * rng.standard_normal(left)
+    for dtype in ("bf16", "f32"):
+        t = torch.from_numpy(x).to(TORCH[dtype]).cuda()
+        for cuts in (dict(top_k=left + 50), dict(top_k=left + 50, top_p=0.8), dict(top_k=min(left + 1, 2000), min_p=0.05, temperature=0.7), dict(top_k=V)):
+            _draw(ctx, t, rng.random(5), str((left, cuts)), **cuts)
+
+
+def test_attention_of_many_sequences(ctx):
+    """More sequences than are looked through at once, most of them without queries."""
+    rng = _rng("many sequences")
+    B, page, D, H = 5000, 16, 64, 1
+    queries = np.where(rng.random(B) < 0.03, rng.integers(1, 4, B), 0)
+    queries[-1] = 2
+    lengths = list(np.where(queries > 0, rng.integers(1, 40, B), 0))
+    table, pages = _tables(rng, lengths, page)
+    k, v = _pool(rng, pages, H, page, D), _pool(rng, pages, H, page, D)
+    starts = np.concatenate(([0], np.cumsum(queries)))
+    q = torch.from_numpy(rng.standard_normal((starts[-1], 2, D))).to(torch.bfloat16).cuda()
+    _check_attention(ctx, q, k, v, table, lengths, starts, page, D, "bf16")
+
+
 def test_drawn_tokens_follow_their_shares(ctx):
     """Every token in turn: u just above and below the border of two shares, where 64 bits tell them apart."""
     V = 64

@@ -137,7 +137,7 @@ LONG = CACHE[:4] + (4096, 64, 2, 128)
 
 @pytest.mark.parametrize("rc,change", [
     (EUNSUPPORTED, dict(dtype=2)), (EINVAL, dict(cache=None)), (EINVAL, dict(T=6)), (EINVAL, dict(T=-1, starts=_at(5))), (EINVAL, dict(heads=7)), (EINVAL, dict(heads=0)), (EINVAL, dict(width=-1)),
-    (EINVAL, dict(width=1 << 40)), (EINVAL, dict(scale=math.inf)), (EINVAL, dict(q=None)), (EINVAL, dict(out=None)), (EINVAL, dict(lengths=None)), (EINVAL, dict(table=None)), (EINVAL, dict(ldq=1023)),
+    (EINVAL, dict(width=1 << 40)), (EINVAL, dict(scale=math.inf)), (EINVAL, dict(scale=1e39)), (EINVAL, dict(scale=math.nan)), (EINVAL, dict(q=None)), (EINVAL, dict(out=None)), (EINVAL, dict(lengths=None)), (EINVAL, dict(table=None)), (EINVAL, dict(ldq=1023)),
     (EINVAL, dict(q=_at(0) + 1)), (EINVAL, dict(lse=_at(2) + 2)), (EINVAL, dict(table=_at(3) + 2)), (EINVAL, dict(starts=_at(5) + 1)), (EINVAL, dict(ws=None)), (EINVAL, dict(ws=_at(6) + 128)),
     (EWORKSPACE, dict(room=-1)), (EINVAL, dict(out=_at(0))), (EINVAL, dict(out=_at(8))), (EINVAL, dict(lse=_at(1) + 4)), (EINVAL, dict(ws=_at(11))), (EINVAL, dict(ws=_at(3))), (EINVAL, dict(B=-5, T=-5)),
     (EINVAL, dict(cache=LONG[:3] + (None,) + LONG[4:])), (0, dict(T=0, B=0)), (0, dict(T=0, starts=_at(5)))])
