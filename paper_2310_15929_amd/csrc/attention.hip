@@ -77,6 +77,7 @@ __device__ __forceinline__ Tile find_tile(const AttendArgs& a, int tile, int row
     const long long stop = clamp_to(a.starts[t.b + 1], t.start, a.T);
     t.queries = (int)(stop - t.start);
     t.first = (int)(tile - (t.start * a.group / rows + t.b)) * rows;
+    if (t.first < 0) t.first = t.queries = 0;  // rows in front of the first sequence: of none
   }
   t.length = (int)clamp_to(a.lengths[t.b], 0, a.width << a.page_bits);
   const long long all = (long long)t.queries * a.group;

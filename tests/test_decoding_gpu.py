@@ -543,6 +543,21 @@ def test_drawn_from_rows_with_fewer_values_than_top_k(ctx, left):
             _draw(ctx, t, rng.random(5), str((left, cuts)), **cuts)
 
 
+@pytest.mark.parametrize("Hq,first", [(2, 50), (160, 170)])
+def test_attention_leaves_rows_in_front_of_the_first_sequence(ctx, Hq, first):
+    """More of them than a tile has, for both kernels."""
+    rng = _rng("front", Hq)
+    D, page, H = 64, 16, 1
+    lengths, starts = [200, 9], np.array([first, first + 150, first + 155])
+    table, pages = _tables(rng, lengths, page)
+    k, v = _pool(rng, pages, H, page, D), _pool(rng, pages, H, page, D)
+    q = torch.from_numpy(rng.standard_normal((first + 160, Hq, D))).to(torch.bfloat16).cuda()
+    out = torch.full_like(q, 7.0)
+    got = ctx.cache_attention(q, _cache(k, v, D), _i32(table), _i32(lengths), starts=_i32(starts), out=out, lse=True)
+    assert (out[:first] == 7).all() and (out[first + 155:] == 7).all()
+    _check_attention(ctx, q, k, v, table, lengths, starts, page, D, "bf16", got=got, heads=[0, Hq - 1])
+
+
 def test_attention_of_many_sequences(ctx):
     """More sequences than are looked through at once, most of them without queries."""
     rng = _rng("many sequences")
