@@ -5,10 +5,10 @@
 // rotary / 2 is no multiple of eight they are read again).  Everything up to the rounding is in 64 bits: the angles of far positions are lost in 32,
 // and a number on the border of two 4-bit codes goes where the exact one would (sqrt and the corrected quotient are exact where the exact result is
 // short enough to be such a border; what is rounded to 16 bits does without that).  The angles of a token are computed once per workgroup, whose
-// rows all belong to one token, while its first rows are on their way.
+// rows all belong to one token, while its first row is on its way.
 // Bound by the vector unit (80 % of its slots) rather than memory, with the start of a workgroup - positions, angles, factors: twice as many workgroups for the same rows take twice the time.
-// Measured: 1 token of 32 + 32 + 32 heads of 128 channels 5.5 us, 4096 tokens of 64 + 8 + 8 heads 75 us (2.1 TB/s); without the rows' loads ahead, with a division by the norm for each channel and
-// its partner, and with the library's sine and cosine 88.  k_cache_read: 4096 tokens of 8 heads of both kinds 5.6 us (4 TB/s).
+// Measured: 1 token of 32 + 32 + 32 heads of 128 channels 6 us, 4096 tokens of 64 + 8 + 8 heads 74 us (2.2 TB/s); with a division by the norm for each channel and
+// its partner, without the row ahead, and with the library's sine and cosine 88; with five rows ahead (spilled registers) 93, with two 75.  k_cache_read: 4096 tokens of 8 heads of both kinds 5.6 us (4 TB/s).
 #include <hip/hip_runtime.h>
 
 #include "mx.h"
@@ -16,7 +16,6 @@
 namespace {
 
 constexpr int NT = 256;
-constexpr int PASSES = 2;  // rows of a lane that are loaded together
 
 struct RotateArgs {
   const uint16_t *q, *k, *v, *qw, *kw;
@@ -119,21 +118,18 @@ __global__ void __launch_bounds__(NT, 4) k_rotate_heads(const RotateArgs a) {
   const unsigned lane = threadIdx.x % LN;
   const int c0 = (int)lane * 8, half = a.rotary / 2;
   const int first = (int)((long long)a.rows * chunk / a.chunks), end = (int)((long long)a.rows * (chunk + 1) / a.chunks);
-  // the rows of the first passes are on their way while the angles are computed
-  uint32_t ahead[PASSES][4];
+  // a row is on its way while the one before it, or the angles, are computed
+  uint32_t ahead[4];
   auto row_at = [&](int r, int& kind, int& head) {  // kind: 0 queries, 1 keys, 2 values
     kind = r < a.Hq ? 0 : (r < a.Hq + a.Hkv ? 1 : 2);
     head = kind == 0 ? r : (kind == 1 ? r - a.Hq : r - a.Hq - a.Hkv);
     return (kind == 0 ? a.q + t * a.ldq : (kind == 1 ? a.k + t * a.ldk : a.v + t * a.ldv)) + (long long)head * a.D;
   };
   auto fetch = [&](int r0) {
-#pragma unroll
-    for (int u = 0; u < PASSES; u++) {
-      const int r = r0 + u * ROWS + (int)(threadIdx.x / LN);
-      int kind, head;
-      const uint16_t* x = row_at(r < end ? r : first, kind, head);
-      load_8(x + c0, r < end ? a.D - c0 : 0, ahead[u]);
-    }
+    const int r = r0 + (int)(threadIdx.x / LN);
+    int kind, head;
+    const uint16_t* x = row_at(r < end ? r : first, kind, head);
+    load_8(x + c0, r < end ? a.D - c0 : 0, ahead);
   };
   fetch(first);
   uint32_t weight[2][4] = {};
@@ -221,99 +217,91 @@ __global__ void __launch_bounds__(NT, 4) k_rotate_heads(const RotateArgs a) {
     }
   };
   int known = -1;  // the kind that they are of
-  for (int r1 = first; r1 < end; r1 += PASSES * ROWS) {
-    if (r1 > first) fetch(r1);
-#pragma unroll 1
-    for (int u = 0; u < PASSES; u++) {
-      const int r = r1 + u * ROWS + (int)(threadIdx.x / LN);
-      if (r1 + u * ROWS >= end) break;
-      const bool live = r < end;
-      int kind, head;
-      const uint16_t* x = row_at(live ? r : first, kind, head);
-      uint32_t v[4];
+  for (int r0 = first; r0 < end; r0 += ROWS) {
+    const int r = r0 + (int)(threadIdx.x / LN);
+    const bool live = r < end;
+    int kind, head;
+    const uint16_t* x = row_at(live ? r : first, kind, head);
+    uint32_t v[4];
 #pragma unroll
-      for (int i = 0; i < 4; i++) {
-        v[i] = ahead[0][i];
+    for (int i = 0; i < 4; i++) v[i] = ahead[i];
+    if (r0 + ROWS < end) fetch(r0 + ROWS);
+    const long long row = place + ((long long)head << a.page_bits);
+    MxCodes codes = {0u, 0u};
+    unsigned e = 0;
+    if (kind == 2) {
+      e = mx_block_exponent<DT, ESPARSE_MX_FP4>(v);
+      codes = mx_encode<DT, ESPARSE_MX_FP4>(v, e);
+    } else {
+      const uint16_t* w = kind == 0 ? a.qw : a.kw;
+      const bool exact = kind == 1 && a.slots;  // (what is rounded to 16 bits has no border that a last bit decides)
+      double y[8], z[8];
+      widen_8<DT>(v, y);
+      double by = 1., n = 0.;
+      if (w) {
+        double s = 0.;
 #pragma unroll
-        for (int e = 1; e < PASSES; e++) v[i] = u == e ? ahead[e][i] : v[i];
+        for (int i = 0; i < 8; i++) s = __builtin_fma(y[i], y[i], s);
+        s = row_sum<LN>(s);
+        if (exact) {
+          n = __builtin_sqrt(s / (double)a.D + a.eps);
+          by = 1. / n;
+          n = __builtin_isfinite(n) ? n : 0.;
+        } else {
+          by = inverse_root(__builtin_fma(s, a.per_channel, a.eps));
+        }
       }
-      const long long row = place + ((long long)head << a.page_bits);
-      MxCodes codes = {0u, 0u};
-      unsigned e = 0;
-      if (kind == 2) {
-        e = mx_block_exponent<DT, ESPARSE_MX_FP4>(v);
-        codes = mx_encode<DT, ESPARSE_MX_FP4>(v, e);
-      } else {
-        const uint16_t* w = kind == 0 ? a.qw : a.kw;
-        const bool exact = kind == 1 && a.slots;  // (what is rounded to 16 bits has no border that a last bit decides)
-        double y[8], z[8];
-        widen_8<DT>(v, y);
-        double by = 1., n = 0.;
+      if (half || w) {
+        if (known != kind) factors(kind);
+        known = kind;
+        uint32_t p[4];
+        partners(v, x, live, p);
+        widen_8<DT>(p, z);
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+          y[i] *= own[i];
+          if (c0 + i < a.rotary) y[i] = __builtin_fma(z[i], other[i], y[i]);  // (a channel that is not turned keeps its value, whatever its partner holds)
+        }
         if (w) {
-          double s = 0.;
 #pragma unroll
-          for (int i = 0; i < 8; i++) s = __builtin_fma(y[i], y[i], s);
-          s = row_sum<LN>(s);
-          if (exact) {
-            n = __builtin_sqrt(s / (double)a.D + a.eps);
-            by = 1. / n;
-            n = __builtin_isfinite(n) ? n : 0.;
-          } else {
-            by = inverse_root(__builtin_fma(s, a.per_channel, a.eps));
-          }
-        }
-        if (half || w) {
-          if (known != kind) factors(kind);
-          known = kind;
-          uint32_t p[4];
-          partners(v, x, live, p);
-          widen_8<DT>(p, z);
-#pragma unroll
-          for (int i = 0; i < 8; i++) {
-            y[i] *= own[i];
-            if (c0 + i < a.rotary) y[i] = __builtin_fma(z[i], other[i], y[i]);  // (a channel that is not turned keeps its value, whatever its partner holds)
-          }
-          if (w) {
-#pragma unroll
-            for (int i = 0; i < 8; i++) y[i] = exact ? over(y[i], by, n) : y[i] * by;
-          }
-        }
-#pragma unroll
-        for (int i = 0; i < 8; i++)
-          if (c0 + i >= a.D) y[i] = 0.;  // (0 times an infinite 1 / norm is no 0)
-        uint16_t* out = kind == 0 ? a.q_out : a.k_out;
-        if (out && live) {
-          uint32_t o[4];
-#pragma unroll
-          for (int i = 0; i < 4; i++) o[i] = pack_2<DT>((float)y[2 * i], (float)y[2 * i + 1]);
-          out += (t * (kind == 0 ? a.Hq : a.Hkv) + head) * a.D + c0;
-          if (a.D - c0 >= 8) {
-            store_stream_16(out, o);
-          } else {
-#pragma unroll
-            for (int i = 0; i < 8; i++)
-              if (c0 + i < a.D) out[i] = (uint16_t)(o[i / 2] >> (16 * (i & 1)));
-          }
-        }
-        if (kind == 1 && a.slots) {
-          uint32_t top = 0;
-#pragma unroll
-          for (int i = 0; i < 8; i++) {
-            const uint32_t h = (uint32_t)(__builtin_bit_cast(unsigned long long, y[i]) >> 32) & 0x7fffffffu;
-            top = h > top ? h : top;
-          }
-          // floor(log2) of the block's largest, less 2, from its exponent
-          const int lead = (int)(quad_max(top) >> 20);
-          const int ex = lead - 1023 - 2 + 127;
-          e = lead == 2047 ? 255u : (ex < 0 ? 0u : (ex > 254 ? 254u : (unsigned)ex));
-          float f[8];
-#pragma unroll
-          for (int i = 0; i < 8; i++) f[i] = to_odd_24(__builtin_ldexp(y[i], 127 - (int)e));
-          codes = mx_encode<ESPARSE_MX_FP4>(f, e == 255u ? 255u : 127u);
+          for (int i = 0; i < 8; i++) y[i] = exact ? over(y[i], by, n) : y[i] * by;
         }
       }
-      if (kind && live && slot >= 0) put_row<DP>(kind == 1 ? a.k_data : a.v_data, kind == 1 ? a.k_scales : a.v_scales, row, lane, codes, e);
+#pragma unroll
+      for (int i = 0; i < 8; i++)
+        if (c0 + i >= a.D) y[i] = 0.;  // (0 times an infinite 1 / norm is no 0)
+      uint16_t* out = kind == 0 ? a.q_out : a.k_out;
+      if (out && live) {
+        uint32_t o[4];
+#pragma unroll
+        for (int i = 0; i < 4; i++) o[i] = pack_2<DT>((float)y[2 * i], (float)y[2 * i + 1]);
+        out += (t * (kind == 0 ? a.Hq : a.Hkv) + head) * a.D + c0;
+        if (a.D - c0 >= 8) {
+          store_stream_16(out, o);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; i++)
+            if (c0 + i < a.D) out[i] = (uint16_t)(o[i / 2] >> (16 * (i & 1)));
+        }
+      }
+      if (kind == 1 && a.slots) {
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < 8; i++) {
+          const uint32_t h = (uint32_t)(__builtin_bit_cast(unsigned long long, y[i]) >> 32) & 0x7fffffffu;
+          top = h > top ? h : top;
+        }
+        // floor(log2) of the block's largest, less 2, from its exponent
+        const int lead = (int)(quad_max(top) >> 20);
+        const int ex = lead - 1023 - 2 + 127;
+        e = lead == 2047 ? 255u : (ex < 0 ? 0u : (ex > 254 ? 254u : (unsigned)ex));
+        float f[8];
+#pragma unroll
+        for (int i = 0; i < 8; i++) f[i] = to_odd_24(__builtin_ldexp(y[i], 127 - (int)e));
+        codes = mx_encode<ESPARSE_MX_FP4>(f, e == 255u ? 255u : 127u);
+      }
     }
+    if (kind && live && slot >= 0) put_row<DP>(kind == 1 ? a.k_data : a.v_data, kind == 1 ? a.k_scales : a.v_scales, row, lane, codes, e);
   }
 }
 

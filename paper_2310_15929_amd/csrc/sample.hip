@@ -26,7 +26,7 @@ constexpr int NT = 512;        // threads of a row (8 for each of the 64 element
 constexpr int PT = 512;        // threads of a piece
 constexpr int LIST = 3328;     // values that a list holds
 constexpr int MOST = 2048;     // with top_k up to this the pieces count values and leave their weights to the list
-constexpr int COPIES = 4;      // of a piece's ranges, for neighbouring lanes: their values are alike, and additions to one place wait for each other
+constexpr int COPIES = 4;      // of a piece's ranges, for neighbouring lanes: additions to one place wait for each other (64 x 131072 equal values 586 -> 568 us; no difference where they are spread)
 constexpr double STEPS = 8.;   // ranges for each doubling of the weight
 constexpr double LOG2E = 1.4426950408889634;
 
