@@ -97,14 +97,16 @@ __device__ __forceinline__ float to_odd_24(double v) {
   return (float)__builtin_bit_cast(double, b);
 }
 
-// a row of a head in the cache: eight channels of this lane, the scales of the row's lanes
+// a row of a head in the cache: eight channels of this lane, the scales of the row's lanes.  Only lanes of the same row exchange anything: the neighbours may be of rows that are not kept, whose
+// lanes are off here and give zeros.
 template <int DP>
 __device__ __forceinline__ void put_row(unsigned char* data, unsigned char* scales, long long row, unsigned lane, MxCodes c, unsigned e) {
   *reinterpret_cast<uint32_t*>(data + row * (DP / 2) + 4 * lane) = c.lo;
-  const uint32_t w = mx_scale_word(e, threadIdx.x);  // four blocks of 16 lanes
   if constexpr (DP == 64) {
-    if (lane == 0) *reinterpret_cast<uint16_t*>(scales + row * 2) = (uint16_t)(w >> (threadIdx.x & 8u ? 16 : 0));
+    const uint32_t other = lane_move<0x141>(e);  // eight lanes in reverse: the first gets the second block's
+    if (lane == 0) *reinterpret_cast<uint16_t*>(scales + row * 2) = (uint16_t)(e | other << 8);
   } else {
+    const uint32_t w = mx_scale_word(e, threadIdx.x);  // four blocks of 16 lanes
     if ((lane & 15u) == 0u) *reinterpret_cast<uint32_t*>(scales + row * (DP / 32) + lane / 4) = w;
   }
 }

@@ -100,6 +100,27 @@ def test_heads(ctx, T, Hq, Hkv, D, rotary, paired, norm, page, dtype):
     assert np.array_equal(_np(gk), orc.cache_values(kd, ks, D)) and np.array_equal(_np(gv), orc.cache_values(vd, vs, D))
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("T", [1, 37, 2000])
+@pytest.mark.parametrize("Hq,Hkv,D", [(15, 5, 64), (1, 1, 50), (71, 1, 33), (32, 1, 64), (0, 3, 64), (2, 1, 40), (9, 3, 128), (5, 1, 256)])
+def test_rows_of_the_cache_whose_neighbours_are_not_kept(ctx, Hq, Hkv, D, T, dtype):
+    """Rows of a wave next to queries, to no row at all, and to tokens without a place: each has its scales whatever its neighbours are."""
+    rng, dt = _rng("neighbours", Hq, Hkv, D, T, dtype), TORCH[dtype]
+    x = torch.from_numpy(rng.standard_normal((T, Hq + 2 * Hkv, D)) * np.exp(rng.standard_normal(D))).to(dt).cuda()
+    q, k, v = x.split((Hq, Hkv, Hkv), 1)
+    pages = -(-T // 16) + 1
+    cache, slots = ctx.kv_cache(pages, 16, Hkv, D), rng.permutation(pages * 16)[:T].astype(np.int32)
+    given = slots.copy()
+    given[2::3] = -1
+    ctx.rotate_heads(q if Hq else None, k, v=v, cache=cache, slots=_i32(given))
+    kept = given >= 0
+    stored = _stored(cache, slots[kept])
+    for n, got in ((k, stored[:2]), (v, stored[2:])):
+        wd, ws = orc.cache_rows(_np(n)[kept])
+        assert np.array_equal(got[1], ws) and np.array_equal(orc.cache_values(*got, D), orc.cache_values(wd, ws, D))
+    assert all((t == 0).all() for t in _stored(cache, np.setdiff1d(np.arange(pages * 16), slots[kept])))
+
+
 @pytest.mark.parametrize("D", [64, 96, 128, 256])
 def test_results_on_a_border_of_two_codes(ctx, D):
     """Rows of one magnitude have the norm as an exact number: their quotients are weights, many of them right between two codes; position 0 turns nothing."""
