@@ -393,8 +393,10 @@ int esparse_cache_read(esparse_ctx* ctx, const esparse_cache* cache, const int32
  * Negative lengths count as 0, longer ones than the table has room for as that; tokens in a page outside [0, pages) are left out, as are all rows of q that belong to no sequence: those rows of
  * out and lse are left as they were.  Tokens that a query does not see do not touch it, whatever their places hold.
  * Keys, probabilities and values take part in the 16 bits of dtype, which hold the cache's numbers as said at esparse_mx_gemm; sums and statistics are in 32 bits.
- * scale: up to 1e38.  q must be finite; a key without number (scale 255) makes the queries that see it NaN, such a block of a value its channels, and so does one whose scale is beyond 2^13 (f16) or 2^125
- * (bf16): some of its numbers are beyond the type.
+ * scale: up to 1e38, of either sign; differences of scores and their exponentials are taken so that it may carry scores out of fp32 (the largest then has all of the weight; lse is infinite where
+ * it is beyond fp32 itself).  The products q . k are fp32: a row with one of plus infinity (in the direction of scale) is NaN, one of minus infinity has no weight, and a row that sees no other is NaN.
+ * q must be finite; a key without number (scale 255) makes the queries that see it NaN, such a block of a value its channels, and so does a block of a value whose scale is beyond 2^13 (f16) or
+ * 2^125 (bf16): some of its numbers are beyond the type.  (Numbers of keys beyond the type are infinite.)
  * workspace: DEVICE scratch of esparse_cache_attention_workspace bytes (host only; may be 0; it reads the cache's sizes alone; ragged: 1 with starts, else 0), 256-byte aligned, overwritten.
  * Outputs and workspace may not overlap inputs or each other.  T = 0 or B = 0 is a no-op.  The order of a row's sums follows from the sizes and the sequence's length.
  * Does not synchronise; can be captured, and replayed with other contents of table, lengths and starts.  Errors: EINVAL, EUNSUPPORTED (dtype), EWORKSPACE, EHIP. */

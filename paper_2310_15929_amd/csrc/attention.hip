@@ -1,5 +1,7 @@
 // Attention over a cache held in microscaled 4 bits (include/esparse.h, csrc/heads.hip): o = sum_j p_j v_j, p = softmax(scale q.k_j), one pass over the tokens
-// with the running maximum m and sum l of the softmax:  m' = max(m, x_j), l' = l 2^(c (m - m')) + sum 2^(c (x_j - m')), o' likewise, c = scale log2(e).
+// with the running maximum m and sum l of the softmax:  m' = max(m, x_j), l' = l 2^(c (m - m')) + sum 2^(c (x_j - m')), o' likewise, c = |scale| log2(e).
+// x_j are the products q.k_j themselves (with a negative scale q has its sign turned, with none it is zeros) and their distances to the maximum are what is multiplied: a scale cannot take
+// them out of fp32 but to minus infinity, where the exponential is 0 as it should be.
 //
 // The rows of a tile are the queries of one head of the cache, (token, query head of the group) in order: 16 of them are the columns of the 16-bit matrix
 // instruction (lane l = 16 g + c: operands hold k = 8 g .. 8 g + 7 of row / column c, results rows 4 g + j of column c).
@@ -18,6 +20,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 
 #include "intrinsics.h"
 #include "mx.h"
@@ -41,7 +44,8 @@ struct AttendArgs {
   long long width;  // pages of a row of the table
   int B, Hkv, group, D, page_bits, tiles, pieces;
   int rows;  // of a tile that can be anything
-  float c;  // scale log2(e)
+  float c, natural;      // |scale| log2(e), 1 without scale; |scale|
+  uint32_t flip, keep;   // of two 16-bit numbers of q: signs to turn, bits to keep
 };
 
 // where a tile is: the sequence, its first row, and what its rows see
@@ -88,6 +92,47 @@ __device__ __forceinline__ Tile find_tile(const AttendArgs& a, int tile, int row
 __device__ __forceinline__ int pieces_of(int end, int pieces) {
   const int strips = (end + STRIP - 1) / STRIP, most = (strips + LEAST - 1) / LEAST;
   return most < pieces ? (most > 0 ? most : 1) : pieces;
+}
+
+// c (x - base) is one instruction with c base as a rounded number, as long as that is off by less than a quarter (no more than what the products' own rounding makes of it); scores beyond that,
+// which may leave fp32 when scaled, have the distance to base taken first
+constexpr float NEAR = 0x1p22f;
+// four 16-bit numbers to an address of any alignment that suits one of them.  (As a vector: the compiler makes four stores of a copy whose last number is stored on the other branch too, 5 % of a long
+// prompt's time)
+__device__ __forceinline__ void store_8(uint16_t* p, const uint32_t (&v)[2]) {
+  const esp_u32x2_any w = {v[0], v[1]};
+  *reinterpret_cast<esp_u32x2_any*>(p) = w;
+}
+// what 32 bits of a query (two numbers) take part as
+__device__ __forceinline__ uint32_t oriented(const AttendArgs& a, uint32_t v) { return (v ^ a.flip) & a.keep; }
+// the first of n tokens that is in a page (n: none); the lanes that are here look together
+__device__ __forceinline__ int first_token(const AttendArgs& a, const int32_t* table, int n) {
+  const int pages = (n + (1 << a.page_bits) - 1) >> a.page_bits;
+  const unsigned long long here = __ballot(1);
+  auto rank = [&](int lane) { return (int)__popcll(here & ((1ull << lane) - 1ull)); };
+  for (int p0 = 0; p0 < pages; p0 += (int)__popcll(here)) {
+    const int p = p0 + rank((int)(threadIdx.x & 63u)), page = p < pages ? table[p] : -1;
+    const unsigned long long some = __ballot(page >= 0 && page < a.pages);
+    if (some) return (p0 + rank((int)__builtin_ctzll(some))) << a.page_bits;
+  }
+  return n;
+}
+// What a row is divided by, inverted, and ln sum exp.  A sum of nothing: 0 and minus infinity where the row sees nothing; where it sees tokens (up to `sees`) all of their products are minus infinity
+// in 32 bits, and it has no number.  The rows of a wave are of one sequence, which `table` is of, and see n tokens at most
+struct Sums {
+  float by, lse;
+};
+__device__ __forceinline__ Sums sums_of(const AttendArgs& a, float all, float top, const int32_t* table, int n, int sees) {
+  Sums r = {1.f / all, top * a.natural + log2f(all) * 0.6931471805599453f};
+  if (__ballot(all == 0.f)) {
+    bool some = false;
+    if (__ballot(all == 0.f && sees >= 0)) some = first_token(a, table, n) <= sees;
+    if (all == 0.f) {
+      r.by = some ? __builtin_nanf("") : 0.f;
+      r.lse = some ? __builtin_nanf("") : -__builtin_inff();
+    }
+  }
+  return r;
 }
 
 // the largest scale with which all codes have numbers of the type: 6 x 2^13 and 6 x 2^125
@@ -264,6 +309,10 @@ __global__ void __launch_bounds__(64 * WAVES, DP == 256 ? 2 : 3) k_attend_few(co
     if (live) load_8(a.q + (t.start + query) * a.ldq + (long long)(head * a.group + row % a.group) * a.D + ch, a.D - ch, v);
     qv[s] = uint4{v[0], v[1], v[2], v[3]};
   }
+  if (a.flip | ~a.keep) {  // (else the queries are still on their way)
+#pragma unroll
+    for (int s = 0; s < NS; s++) qv[s] = uint4{oriented(a, qv[s].x), oriented(a, qv[s].y), oriented(a, qv[s].z), oriented(a, qv[s].w)};
+  }
   floatx4_t o[ND];
 #pragma unroll
   for (int n = 0; n < ND; n++) o[n] = floatx4_t{0.f, 0.f, 0.f, 0.f};
@@ -285,10 +334,9 @@ __global__ void __launch_bounds__(64 * WAVES, DP == 256 ? 2 : 3) k_attend_few(co
     settled(acc[0]);
     settle(acc[1]);
 #pragma unroll
-    for (int u = 0; u < 2; u++) {
+    for (int u = 0; u < 2; u++)
 #pragma unroll
-      for (int j = 0; j < 4; j++) x[u][j] = now.there[u] && strip * STRIP + 16 * u + 4 * g + j <= sees ? acc[u][j] * a.c : -__builtin_inff();
-    }
+      for (int j = 0; j < 4; j++) x[u][j] = now.there[u] && strip * STRIP + 16 * u + 4 * g + j <= sees ? acc[u][j] : -__builtin_inff();
     float top = m;
 #pragma unroll
     for (int u = 0; u < 2; u++)
@@ -296,20 +344,28 @@ __global__ void __launch_bounds__(64 * WAVES, DP == 256 ? 2 : 3) k_attend_few(co
       for (int j = 0; j < 4; j++) top = fmaxf(top, x[u][j]);
     top = column_max(top);
     const float base = top == -__builtin_inff() ? 0.f : top;
-    if (__ballot(top > m)) {  // (else all have kept their maxima)
-      const float shrink = __builtin_amdgcn_exp2f(m - base);
+    float scaled = base * a.c;
+    if (__ballot(top > m || !(fabsf(scaled) < NEAR))) {  // (else all have kept their maxima)
+      const float shrink = __builtin_amdgcn_exp2f((m - base) * a.c);
       l *= shrink;
 #pragma unroll
       for (int n = 0; n < ND; n++)
 #pragma unroll
         for (int j = 0; j < 4; j++) o[n][j] *= shrink;
       m = top;
+      if (__ballot(!(fabsf(scaled) < NEAR))) {
+#pragma unroll
+        for (int u = 0; u < 2; u++)
+#pragma unroll
+          for (int j = 0; j < 4; j++) x[u][j] -= base;
+        scaled = 0.f;
+      }
     }
 #pragma unroll
     for (int u = 0; u < 2; u++)
 #pragma unroll
       for (int j = 0; j < 4; j++) {
-        x[u][j] = __builtin_amdgcn_exp2f(x[u][j] - base);
+        x[u][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[u][j], a.c, -scaled));
         l += x[u][j];
       }
     const uint4 p = {pack_2<DT>(x[0][0], x[0][1]), pack_2<DT>(x[0][2], x[0][3]), pack_2<DT>(x[1][0], x[1][1]), pack_2<DT>(x[1][2], x[1][3])};
@@ -394,7 +450,7 @@ __global__ void __launch_bounds__(64 * WAVES, DP == 256 ? 2 : 3) k_attend_few(co
       float all = 0.f;
 #pragma unroll
       for (int w = 0; w < WAVES; w++) {
-        const float f = __builtin_amdgcn_exp2f(stat[0][w][r] - base);
+        const float f = __builtin_amdgcn_exp2f((stat[0][w][r] - base) * a.c);
         const floatx4_t v = *reinterpret_cast<const floatx4_t*>(sums + w * (STRIP * kVRow<DP> / 2) + r * ROW + in);
 #pragma unroll
         for (int j = 0; j < 4; j++) sum[j] += v[j] * f;
@@ -410,11 +466,11 @@ __global__ void __launch_bounds__(64 * WAVES, DP == 256 ? 2 : 3) k_attend_few(co
         }
       } else {
         const long long place = (t.start + qi) * ((long long)a.Hkv * a.group) + head * a.group + of % a.group;
-        const float by = all == 0.f ? 0.f : 1.f / all;
+        const Sums of_row = sums_of(a, all, top, table, t.end, t.length - t.queries + qi);
 #pragma unroll
         for (int j = 0; j < 4; j++)
-          if (ch + j < a.D) a.out[place * a.D + ch + j] = esp_from_float<DT>(all == 0.f ? 0.f : sum[j] * by);
-        if (a.lse && ch == 0) a.lse[place] = all == 0.f ? -__builtin_inff() : (base + log2f(all)) * 0.6931471805599453f;
+          if (ch + j < a.D) a.out[place * a.D + ch + j] = esp_from_float<DT>(sum[j] * of_row.by);
+        if (a.lse && ch == 0) a.lse[place] = of_row.lse;
       }
     }
   }
@@ -453,7 +509,7 @@ __global__ void __launch_bounds__(256) k_attend_join(const AttendArgs a) {
 #pragma unroll 4
   for (int i = group; i < pieces; i += GROUPS) {
     const floatx4_t v = *reinterpret_cast<const floatx4_t*>(part + (long long)i * kPartial<DP> + r * DP + 4 * quad);
-    const float f = __builtin_amdgcn_exp2f(factor[i] - base);
+    const float f = __builtin_amdgcn_exp2f((factor[i] - base) * a.c);
 #pragma unroll
     for (int j = 0; j < 4; j++) sum[j] += v[j] * f;
     all += sums[i] * f;
@@ -472,12 +528,12 @@ __global__ void __launch_bounds__(256) k_attend_join(const AttendArgs a) {
     for (int j = 0; j < 4; j++) sum[j] += v[j];
     all += factor[i];
   }
+  const Sums of_row = sums_of(a, all, top, a.table + (long long)t.b * a.width, t.end, t.length - t.queries + qi);
   const long long place = (t.start + qi) * ((long long)a.Hkv * a.group) + head * a.group + of % a.group;
-  const float by = all == 0.f ? 0.f : 1.f / all;
 #pragma unroll
   for (int j = 0; j < 4; j++)
-    if (4 * quad + j < a.D) a.out[place * a.D + 4 * quad + j] = esp_from_float<DT>(all == 0.f ? 0.f : sum[j] * by);
-  if (a.lse && quad == 0) a.lse[place] = all == 0.f ? -__builtin_inff() : (base + log2f(all)) * 0.6931471805599453f;
+    if (4 * quad + j < a.D) a.out[place * a.D + 4 * quad + j] = esp_from_float<DT>(sum[j] * of_row.by);
+  if (a.lse && quad == 0) a.lse[place] = of_row.lse;
 }
 
 // ---- prompts: many rows of a sequence ----------------------------------------------------------------
@@ -528,11 +584,8 @@ __global__ void __launch_bounds__(64 * W, 2) k_attend_many(const AttendArgs a) {
     uint32_t v[4] = {0u, 0u, 0u, 0u};
     const int ch = 16 * s + 8 * h;
     if (live) load_8(a.q + (t.start + query) * a.ldq + (long long)(head * a.group + row % a.group) * a.D + ch, a.D - ch, v);
-    // the maxima are taken of the products themselves: with a negative scale of those with the sign turned, with none of zeros
-    const uint32_t sign = a.c < 0.f ? 0x80008000u : 0u, some = a.c == 0.f ? 0u : ~0u;
-    q[s] = uint4{(v[0] ^ sign) & some, (v[1] ^ sign) & some, (v[2] ^ sign) & some, (v[3] ^ sign) & some};
+    q[s] = uint4{oriented(a, v[0]), oriented(a, v[1]), oriented(a, v[2]), oriented(a, v[3])};
   }
-  const float scale = a.c == 0.f ? 1.f : fabsf(a.c);
   // the wave's rows see all tokens up to `all` and none from `most` on
   const int first_row = t.first + 32 * wave, last_row = min(first_row + 31, t.queries * a.group - 1);
   const bool any = first_row <= last_row;
@@ -628,22 +681,30 @@ __global__ void __launch_bounds__(64 * W, 2) k_attend_many(const AttendArgs a) {
 #pragma unroll
       for (int j = 0; j < 16; j++) top = fmaxf(top, x[b][j]);
     top = half_max(top);
-    const float base = top == -__builtin_inff() ? 0.f : top * scale;
-    if (__ballot(top > m)) {
-      const float shrink = m == -__builtin_inff() ? 0.f : __builtin_amdgcn_exp2f(m * scale - base);
+    const float base = top == -__builtin_inff() ? 0.f : top;
+    float scaled = base * a.c;
+    if (__ballot(top > m || !(fabsf(scaled) < NEAR))) {
+      const float shrink = __builtin_amdgcn_exp2f((m - base) * a.c);
       l *= shrink;
 #pragma unroll
       for (int n = 0; n < ND; n++)
 #pragma unroll
         for (int j = 0; j < 16; j++) o[n][j] *= shrink;
       m = top;
+      if (__builtin_expect(__ballot(!(fabsf(scaled) < NEAR)) != 0, 0)) {
+#pragma unroll
+        for (int b = 0; b < TB; b++)
+#pragma unroll
+          for (int j = 0; j < 16; j++) x[b][j] -= base;
+        scaled = 0.f;
+      }
     }
     uint4 p[2 * TB];
 #pragma unroll
     for (int b = 0; b < TB; b++) {
 #pragma unroll
       for (int j = 0; j < 16; j++) {
-        x[b][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][j], scale, -base));
+        x[b][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][j], a.c, -scaled));
         l += x[b][j];
       }
 #pragma unroll
@@ -679,26 +740,24 @@ __global__ void __launch_bounds__(64 * W, 2) k_attend_many(const AttendArgs a) {
   for (int n = 0; n < ND; n++) settle(o[n]);
   l = half_sum(l);
   if (!live) return;
+  const Sums of_row = sums_of(a, l, m, table, t.end, sees);
   const long long place = (t.start + query) * ((long long)a.Hkv * a.group) + head * a.group + row % a.group;
-  const float by = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
   for (int n = 0; n < ND; n++)
 #pragma unroll
     for (int j = 0; j < 16; j += 4) {
       const int ch = 32 * n + 8 * (j / 4) + 4 * h;
       uint16_t* to = a.out + place * a.D + ch;
-      uint16_t v[4];
-#pragma unroll
-      for (int e = 0; e < 4; e++) v[e] = esp_from_float<DT>(l == 0.f ? 0.f : o[n][j + e] * by);
+      const uint32_t v[2] = {pack_2<DT>(o[n][j] * of_row.by, o[n][j + 1] * of_row.by), pack_2<DT>(o[n][j + 2] * of_row.by, o[n][j + 3] * of_row.by)};
       if (ch + 4 <= a.D) {
-        __builtin_memcpy(to, v, 8);
+        store_8(to, v);
       } else {
 #pragma unroll
         for (int e = 0; e < 4; e++)
-          if (ch + e < a.D) to[e] = v[e];
+          if (ch + e < a.D) to[e] = (uint16_t)(v[e / 2] >> (16 * (e & 1)));
       }
     }
-  if (a.lse && h == 0) a.lse[place] = l == 0.f ? -__builtin_inff() : ((m == -__builtin_inff() ? 0.f : m * scale) + log2f(l)) * 0.6931471805599453f;
+  if (a.lse && h == 0) a.lse[place] = of_row.lse;
 }
 
 long long tiles_of(long long T, int B, int group, bool ragged, int rows) {
@@ -742,7 +801,11 @@ int esp_cache_attention_device(esparse_ctx* ctx, const void* q, long long ldq, l
   a.out = (uint16_t*)out, a.lse = lse, a.partial = (float*)workspace;
   a.ldq = ldq, a.T = T, a.pages = cache->pages, a.width = width;
   a.B = B, a.Hkv = cache->heads, a.group = q_heads / cache->heads, a.D = cache->head_dim, a.page_bits = __builtin_ctz((unsigned)cache->page);
-  a.c = (float)(scale * 1.4426950408889634);
+  a.c = (float)std::fabs(scale * 1.4426950408889634);
+  a.natural = (float)std::fabs(scale);
+  a.flip = scale < 0 ? 0x80008000u : 0u;
+  a.keep = a.c == 0.f ? 0u : ~0u;
+  if (a.c == 0.f) a.c = 1.f;
   const int row = esp_cache_row(a.D);
   if (const int waves = waves_of_many(T, B, a.group, a.Hkv, row, starts != nullptr)) {
     a.tiles = (int)tiles_of(T, B, a.group, starts != nullptr, 32 * waves);

@@ -416,6 +416,61 @@ def test_attention_with_sharp_scores(ctx, dtype, factor):
         _check_attention(ctx, wide, k, v, table, lengths, np.array([0, 50, 90]), page, D, dtype, scale=scale, heads=[0, 279])
 
 
+@pytest.mark.parametrize("scale", [1e38, -1e38, 1e35, -3e36])
+@pytest.mark.parametrize("nq,Hq,n", [(1, 4, 600), (3, 2, 190), (160, 192, 190)])
+def test_attention_of_the_largest_scales(ctx, nq, Hq, n, scale):
+    """Scores beyond fp32: the largest product has all of the weight, equal ones share it.  The products are whole numbers times 2^-5, exact in fp32."""
+    rng = _rng("scales", nq, n)
+    D, page, H = 64, 16, 1
+    table, pages = _tables(rng, [n], page)
+    k, v = _pool(rng, pages, H, page, D), _pool(rng, pages, H, page, D)
+    q = torch.from_numpy(rng.integers(-2, 3, (nq, Hq, D)).astype(float)).to(torch.bfloat16).cuda()
+    out, sums = (_np(t) for t in ctx.cache_attention(q, _cache(k, v, D), _i32(table), _i32([n]), starts=None if nq == 1 else _i32([0, nq]), scale=scale, lse=True))
+    (kk, _), (vv, _) = _gather(k, table[0], n, page, 0, D), _gather(v, table[0], n, page, 0, D)
+    for h in (0, Hq - 1):
+        for i in range(nq):
+            c = n - nq + i + 1
+            x = kk[:c] @ _np(q)[i, h]
+            best = x.max() if scale > 0 else x.min()
+            of = vv[:c][x == best]
+            assert (np.abs(out[i, h] - of.mean(0)) <= 2.0 ** -8 * np.abs(of.mean(0)) + len(of) * 2.0 ** -23 * np.abs(of).sum(0)).all()
+            want = scale * best + math.log(len(of))
+            with np.errstate(over="ignore"):
+                beyond = np.isinf(np.float32(want))
+            assert sums[i, h] == np.sign(want) * np.inf if beyond else abs(sums[i, h] - want) <= 2.0 ** -22 * abs(want) + 2.0 ** -22
+
+
+@pytest.mark.parametrize("nq,Hq,n", [(1, 2, 700), (5, 2, 190), (160, 192, 190)])
+def test_attention_of_products_beyond_32_bits(ctx, nq, Hq, n):
+    """Products of minus infinity have no weight; rows that see no other, or one of plus infinity, have no number; rows that see nothing are zeros."""
+    rng = _rng("products", nq)
+    D, page, H = 64, 16, 1
+    table, pages = _tables(rng, [n, 2], page)
+    k, v = _pool(rng, pages, H, page, D), _pool(rng, pages, H, page, D)
+    k[0][:], k[1][:] = 0xff, 252                   # -6 x 2^125 throughout
+    q = torch.full((2 * nq, Hq, D), 3e38, dtype=torch.bfloat16, device="cuda")
+    q[:, -1] = 0.0
+    starts = None if nq == 1 else _i32([0, nq, 2 * nq])
+
+    def run():
+        return [_np(t) for t in ctx.cache_attention(q, _cache(k, v, D), _i32(table), _i32([n, 2]), starts=starts, lse=True)]
+    out, sums = run()
+    none = max(nq - 2, 0)
+    blind = slice(nq, nq + none)                   # queries of the second sequence that see nothing
+    assert np.isnan(out[:nq, 0]).all() and np.isnan(sums[:nq, 0]).all() and np.isnan(out[nq + none:, 0]).all() and np.isfinite(out[:, -1]).all()
+    assert (out[blind] == 0).all() and np.isneginf(sums[blind]).all()
+    at = (table[0, 1], 0, 3)                       # token 19: a product of 0
+    k[0][at] = 0
+    out, sums = run()
+    assert np.array_equal(out[:nq, 0], np.tile(_gather(v, table[0], n, page, 0, D)[0][19], (nq, 1))) and (sums[:nq, 0] == 0).all() and np.isnan(out[nq + none:, 0]).all()
+    k[0][at] = 0x77                                # 6
+    out, sums = run()
+    assert np.isnan(out[:nq, 0]).all() and np.isnan(sums[:nq, 0]).all()
+    table[0] = -1
+    out, sums = run()
+    assert (out[:nq] == 0).all() and np.isneginf(sums[:nq]).all()
+
+
 def test_attention_long_context(ctx):
     rng = _rng("long")
     n, page, D, H = 40001, 64, 128, 2
