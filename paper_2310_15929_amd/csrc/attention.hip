@@ -9,8 +9,10 @@
 //           conversion that takes the scale; its j-th word is the operand of step j (which k a channel takes does not matter as long as Q's agrees).
 //   output  O^T[channel, row] += V^T P^T.  The lane holds the probabilities of tokens 4 g + j of two groups of 16 for its row: with the tokens of a step numbered that
 //           way P^T is an operand as it stands.  V needs token and channel exchanged: it goes through LDS in 16 bits and comes back by the transposing read, which
-//           hands a lane four tokens of one channel.  P is rounded to the 16 bits of the output's type, as V is held: the matrix instruction takes both so; sums
-//           and statistics are in 32 bits.
+//           hands a lane four tokens of one channel.  P is rounded to the 16 bits of the output's type, as V is held: the matrix instruction takes both so, and each number is off by at
+//           most half a step of the type, which the output is rounded to as well (the error against 64 bits is 1.15 of that of the rounded output alone); sums and statistics are in 32 bits.
+//           f16 has few exponents: there P is 2^15 at the maximum, so that it keeps its bits down to 2^-29 and vanishes below 2^-40 (with 1 at the maximum a tail of 2^-26 and less was in l
+//           but not in o).
 // Bound by memory at one token a sequence where there is work for the chip: 48 sequences of 500 to 4096 tokens, 32 heads of 128 channels, 115 us (4.2 TB/s; a copy reaches 4.9), by
 // the few waves that its registers leave to cover the latency of a strip (a third of a wave's time it waits for memory, a fifth for a slot of the vector unit, which is busy 55 %);
 // 131072 tokens, 64 heads on 8, 33 us and 5 to join the pieces (3.8 TB/s).  256 channels take twice the registers: 21 sequences of five tokens each, 16 heads on 4, 83 us (1.3 TB/s).
@@ -97,6 +99,9 @@ __device__ __forceinline__ int pieces_of(int end, int pieces) {
 // c (x - base) is one instruction with c base as a rounded number, as long as that is off by less than a quarter (no more than what the products' own rounding makes of it); scores beyond that,
 // which may leave fp32 when scaled, have the distance to base taken first
 constexpr float NEAR = 0x1p22f;
+// the exponent of the largest probability (with the rounding of base above it stays below 65504)
+template <int DT>
+constexpr float kOffset = DT == ESPARSE_F16 ? 15.f : 0.f;
 // four 16-bit numbers to an address of any alignment that suits one of them.  (As a vector: the compiler makes four stores of a copy whose last number is stored on the other branch too, 5 % of a long
 // prompt's time)
 __device__ __forceinline__ void store_8(uint16_t* p, const uint32_t (&v)[2]) {
@@ -122,8 +127,9 @@ __device__ __forceinline__ int first_token(const AttendArgs& a, const int32_t* t
 struct Sums {
   float by, lse;
 };
+template <int DT>
 __device__ __forceinline__ Sums sums_of(const AttendArgs& a, float all, float top, const int32_t* table, int n, int sees) {
-  Sums r = {1.f / all, top * a.natural + log2f(all) * 0.6931471805599453f};
+  Sums r = {1.f / all, top * a.natural + (log2f(all) - kOffset<DT>) * 0.6931471805599453f};
   if (__ballot(all == 0.f)) {
     bool some = false;
     if (__ballot(all == 0.f && sees >= 0)) some = first_token(a, table, n) <= sees;
@@ -365,7 +371,7 @@ __global__ void __launch_bounds__(64 * WAVES, DP == 256 ? 2 : 3) k_attend_few(co
     for (int u = 0; u < 2; u++)
 #pragma unroll
       for (int j = 0; j < 4; j++) {
-        x[u][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[u][j], a.c, -scaled));
+        x[u][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[u][j], a.c, kOffset<DT> - scaled));
         l += x[u][j];
       }
     const uint4 p = {pack_2<DT>(x[0][0], x[0][1]), pack_2<DT>(x[0][2], x[0][3]), pack_2<DT>(x[1][0], x[1][1]), pack_2<DT>(x[1][2], x[1][3])};
@@ -466,7 +472,7 @@ __global__ void __launch_bounds__(64 * WAVES, DP == 256 ? 2 : 3) k_attend_few(co
         }
       } else {
         const long long place = (t.start + qi) * ((long long)a.Hkv * a.group) + head * a.group + of % a.group;
-        const Sums of_row = sums_of(a, all, top, table, t.end, t.length - t.queries + qi);
+        const Sums of_row = sums_of<DT>(a, all, top, table, t.end, t.length - t.queries + qi);
 #pragma unroll
         for (int j = 0; j < 4; j++)
           if (ch + j < a.D) a.out[place * a.D + ch + j] = esp_from_float<DT>(sum[j] * of_row.by);
@@ -528,7 +534,7 @@ __global__ void __launch_bounds__(256) k_attend_join(const AttendArgs a) {
     for (int j = 0; j < 4; j++) sum[j] += v[j];
     all += factor[i];
   }
-  const Sums of_row = sums_of(a, all, top, a.table + (long long)t.b * a.width, t.end, t.length - t.queries + qi);
+  const Sums of_row = sums_of<DT>(a, all, top, a.table + (long long)t.b * a.width, t.end, t.length - t.queries + qi);
   const long long place = (t.start + qi) * ((long long)a.Hkv * a.group) + head * a.group + of % a.group;
 #pragma unroll
   for (int j = 0; j < 4; j++)
@@ -704,7 +710,7 @@ __global__ void __launch_bounds__(64 * W, 2) k_attend_many(const AttendArgs a) {
     for (int b = 0; b < TB; b++) {
 #pragma unroll
       for (int j = 0; j < 16; j++) {
-        x[b][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][j], a.c, -scaled));
+        x[b][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][j], a.c, kOffset<DT> - scaled));
         l += x[b][j];
       }
 #pragma unroll
@@ -740,7 +746,7 @@ __global__ void __launch_bounds__(64 * W, 2) k_attend_many(const AttendArgs a) {
   for (int n = 0; n < ND; n++) settle(o[n]);
   l = half_sum(l);
   if (!live) return;
-  const Sums of_row = sums_of(a, l, m, table, t.end, sees);
+  const Sums of_row = sums_of<DT>(a, l, m, table, t.end, sees);
   const long long place = (t.start + query) * ((long long)a.Hkv * a.group) + head * a.group + row % a.group;
 #pragma unroll
   for (int n = 0; n < ND; n++)

@@ -471,6 +471,37 @@ def test_attention_of_products_beyond_32_bits(ctx, nq, Hq, n):
     assert (out[:nq] == 0).all() and np.isneginf(sums[:nq]).all()
 
 
+@pytest.mark.parametrize("dtype,below", [("f16", 14), ("f16", 22), ("f16", 26), ("bf16", 26)])
+@pytest.mark.parametrize("step", [40001, 32])
+@pytest.mark.parametrize("nq,Hq", [(1, 4), (3, 4), (96, 256)])
+def test_attention_of_a_long_tail(ctx, nq, Hq, step, dtype, below):
+    """A strong token before 40000 weak ones, or one among every 32, the weak of 2^-below of its weight each and with values of one sign: what they weigh in the sum they weigh in the output.  No
+    allowance is made for small probabilities, whose type's bits have to reach down to them."""
+    rng = _rng("tail", nq, Hq, dtype, below)
+    n, D, page, H = 40001, 64, 64, 2
+    table, pages = _tables(rng, [n], page)
+    # channel 0 of a key: 4 for the strong token, 0 for the others, 0.5 in channels that the queries do not have
+    row = np.zeros((pages, H, page, 32), np.uint8)
+    row[:, :, :, 1:] = 0x11
+    scales = np.full((pages, H, page, 2), 127, np.uint8)
+    strong = np.arange(5, n, step)
+    row[table[0, strong // page], :, strong % page, 0] = 0x06
+    k, v = (row, scales), _pool(rng, pages, H, page, D, 6, 10)
+    v[0][:] &= 0x77                                  # positive values
+    v[0][table[0, strong // page], :, strong % page] = 0   # the strong tokens' are 0
+    q = torch.zeros(nq, Hq, D, dtype=TORCH[dtype], device="cuda")
+    q[:, :, 0] = 1.0
+    scale = below * math.log(2.0) / 4
+    out, sums = (_np(t) for t in ctx.cache_attention(q, _cache(k, v, D), _i32(table), _i32([n]), starts=None if nq == 1 else _i32([0, nq]), scale=scale, lse=True))
+    for h in (0, Hq - 1):
+        kk, vv = (_gather(p, table[0], n, page, h // (Hq // H), D)[0] for p in (k, v))
+        for i in (0, nq - 1):
+            want, wl, spread, _, off = orc.attend(_np(q)[i:i + 1, h], kk, vv, scale, [n - nq + i])
+            half = HALF[TORCH[dtype]]
+            assert (np.abs(out[i, h] - want[0]) <= half * want[0] + (half + 2 * off[0] + n * 2.0 ** -23) * 1.01 * spread[0]).all(), (h, i, out[i, h][:4], want[0][:4])
+            assert abs(sums[i, h] - wl[0]) <= 2 * off[0] + n * 2.0 ** -23 + abs(wl[0]) * 2.0 ** -22 + 2.0 ** -21
+
+
 def test_attention_long_context(ctx):
     rng = _rng("long")
     n, page, D, H = 40001, 64, 128, 2
