@@ -223,7 +223,8 @@ __device__ __forceinline__ void wave_fence() {
 }
 
 // Results of matrix instructions are read from here on: 32 clocks, more than the longest of them needs.  The compiler counts these within a stretch of code without branches;
-// behind a branch it has read the last number of a result a clock after its instruction.
+// behind a branch it has read the last number of a result a clock after its instruction.  Two results are named by one statement: their instructions are in front of the wait, what reads them is
+// behind it, however the compiler orders the rest.
 template <class V>
 __device__ __forceinline__ void settle(V& v) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -232,16 +233,14 @@ __device__ __forceinline__ void settle(V& v) {
   (void)v;
 #endif
 }
-// ... of several, after one settle()
 template <class V>
-__device__ __forceinline__ void settled(V& v) {
+__device__ __forceinline__ void settle(V& v, V& w) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  asm volatile("" : "+v"(v));
+  asm volatile("s_nop 15\n\ts_nop 15" : "+v"(v), "+v"(w));
 #else
-  (void)v;
+  (void)v, (void)w;
 #endif
 }
-
 
 template <int DP>
 constexpr int kHalf = DP == 256 ? 128 : DP;  // channels of V in LDS at a time
@@ -337,8 +336,7 @@ __global__ void __launch_bounds__(64 * WAVES, DP == 256 ? 2 : 3) k_attend_few(co
 #pragma unroll
       for (int s = 0; s < NS; s++) acc[u] = mfma16<DT>(mx_widen<DT>(now.k[u].w[s], mx_scale(now.k[u].e[DP == 256 ? s / 4 : 0])), qv[s], acc[u]);
     }
-    settled(acc[0]);
-    settle(acc[1]);
+    settle(acc[0], acc[1]);
 #pragma unroll
     for (int u = 0; u < 2; u++)
 #pragma unroll
@@ -566,7 +564,7 @@ __device__ __forceinline__ floatx16_t mfma32(uint4 a, uint4 b, floatx16_t c) {
 
 template <int DT, int DP, int W>
 __global__ void __launch_bounds__(64 * W, 2) k_attend_many(const AttendArgs a) {
-  constexpr int TT = kTile<DP>, TB = TT / 32, NS = DP / 16, ND = DP / 32, THREADS = 64 * W;
+  constexpr int TT = kTile<DP>, TB = TT / 32 /* 1 or 2 */, NS = DP / 16, ND = DP / 32, THREADS = 64 * W;
   constexpr int CH = TT * DP / 32;                       // pieces of 16 bytes (a block) of the keys of a tile, and of the values
   constexpr int ITEMS = (2 * CH + THREADS - 1) / THREADS;  // of a thread
   static_assert(CH % 64 == 0, "whole waves");
@@ -666,9 +664,8 @@ __global__ void __launch_bounds__(64 * W, 2) k_attend_many(const AttendArgs a) {
 #pragma unroll
       for (int s = 0; s < NS; s++) x[b] = mfma32<DT>(*reinterpret_cast<const uint4*>(kb + (32 * b + c) * kKRow<DP> + 16 * s + 8 * h), q[s], x[b]);
     }
-#pragma unroll
-    for (int b = 0; b < TB - 1; b++) settled(x[b]);
-    settle(x[TB - 1]);
+    if constexpr (TB == 2) settle(x[0], x[1]);
+    else settle(x[0]);
     unsigned long long gone = 0, none = 0;
 #pragma unroll
     for (int w = 0; w < CH / 64; w++) gone |= odd[i & 1][w], none |= odd[i & 1][CH / 64 + w];
