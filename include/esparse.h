@@ -366,6 +366,7 @@ int esparse_token_logprobs(esparse_ctx* ctx, const void* logits, long long R, lo
  * slots[T] (int32).  A token whose slot is no place of the cache is not kept; of tokens given the same slot the last is.
  * NaN and infinities as in esparse_rms_norm; a rotated channel is NaN with its partner.  In the cache a block of 32 channels that holds one reads as NaN.  (Numbers beyond 2^130
  * are limited to 6 x 2^127.)  Outputs and the cache may not overlap inputs or each other.  T = 0 is a no-op.  Does not synchronise; can be captured.
+ * T < 2^22, up to 2^16 heads of a kind, T (q_heads + 2 kv_heads) up to 2^26 (esparse_cache_read: T heads).
  *
  * esparse_cache_read: the numbers of places slots[T] as k_out, v_out[T][heads][head_dim] (f16, bf16 or f32, either may be NULL), each rounded once.  A slot that is no place gives zeros.
  * Errors: EINVAL, EUNSUPPORTED (dtype), EHIP. */
@@ -398,6 +399,7 @@ int esparse_cache_read(esparse_ctx* ctx, const esparse_cache* cache, const int32
  * q must be finite; a key without number (scale 255) makes the queries that see it NaN, such a block of a value its channels, and so does a block of a value whose scale is beyond 2^13 (f16) or
  * 2^125 (bf16): some of its numbers are beyond the type.  (Numbers of keys beyond the type are infinite.)
  * workspace: DEVICE scratch of esparse_cache_attention_workspace bytes (host only; may be 0; it reads the cache's sizes alone; ragged: 1 with starts, else 0), 256-byte aligned, overwritten.
+ * T and B < 2^22, T q_heads up to 2^26, B times the cache's heads up to 2^22, width * page < 2^31.
  * Outputs and workspace may not overlap inputs or each other.  T = 0 or B = 0 is a no-op.  The order of a row's sums follows from the sizes and the sequence's length.
  * Does not synchronise; can be captured, and replayed with other contents of table, lengths and starts.  Errors: EINVAL, EUNSUPPORTED (dtype), EWORKSPACE, EHIP. */
 int esparse_cache_attention_workspace(const esparse_cache* cache, long long T, int B, int q_heads, long long width, int ragged, size_t* bytes);
@@ -414,6 +416,7 @@ int esparse_cache_attention(esparse_ctx* ctx, const void* q, long long ldq, long
  * ln(w / kept sum).  temperature (f32[R]) 0: the largest logit, the lowest index of equal ones, logprob 0.
  * temperature, top_k, top_p, min_p may be NULL (1, all, all, all).  Logits of minus infinity are never drawn.  A row with a NaN or plus infinity, with nothing but minus infinity, or whose
  * temperature is negative, infinite or NaN gives -1 and NaN.  Sums are exact to 2^-40 of the largest weight and do not depend on chance.
+ * R < 2^22, V up to ESPARSE_MAX_VOCABULARY, R V up to 2^34.
  * workspace: DEVICE scratch of esparse_sample_workspace bytes (host only), 256-byte aligned, overwritten.  Outputs and workspace may not overlap inputs or each other.
  * R = 0 is a no-op.  Does not synchronise; can be captured.  Errors: EINVAL, EUNSUPPORTED (dtype, V), EWORKSPACE, EHIP. */
 int esparse_sample_workspace(long long R, long long V, size_t* bytes);

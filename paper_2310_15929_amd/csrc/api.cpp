@@ -1047,10 +1047,11 @@ int esparse_cache_read(esparse_ctx* ctx, const esparse_cache* cache, const int32
   return esp_cache_read_device(ctx, cache, slots, T, dtype, k_out, v_out);
 }
 
-// sequences and rows: a launch has up to 2^23 workgroups for tiles of rows of a head
+// sequences and rows: a launch has up to 2^23 workgroups of 256 threads, one for a tile of 16 rows of a head of the cache, and in ragged batches one more for each sequence
+static constexpr long long kMaxSequenceHeads = 1ll << 22;
 static bool attention_sizes(const esparse_cache* c, long long T, int B, int q_heads, long long width, int ragged) {
   return cache_sizes(c->pages, c->page, c->heads, c->head_dim) && T >= 0 && T <= kMaxRows && B >= 0 && B <= kMaxRows && q_heads >= 1 && q_heads <= kMaxHeads &&
-         q_heads % c->heads == 0 && width >= 0 && width < (1ll << 31) / c->page && (ragged == 0 || ragged == 1) && (ragged || T == B) && (T + B) * q_heads <= kMaxHeadRows / 16;
+         q_heads % c->heads == 0 && width >= 0 && width < (1ll << 31) / c->page && (ragged == 0 || ragged == 1) && (ragged || T == B) && T * q_heads <= kMaxHeadRows && (long long)B * c->heads <= kMaxSequenceHeads;
 }
 
 int esparse_cache_attention_workspace(const esparse_cache* cache, long long T, int B, int q_heads, long long width, int ragged, size_t* bytes) {

@@ -665,6 +665,28 @@ def test_attention_leaves_rows_in_front_of_the_first_sequence(ctx, Hq, first):
     _check_attention(ctx, q, k, v, table, lengths, starts, page, D, "bf16", got=got, heads=[0, Hq - 1])
 
 
+def test_attention_of_more_than_four_million_rows(ctx):
+    """A prompt of 65600 tokens with 65 heads on one, far into it and at its end; many sequences whose rows are as many."""
+    rng = _rng("rows beyond")
+    n, Hq, D, page = 65600, 65, 16, 64
+    table, pages = _tables(rng, [n], page)
+    k, v = _pool(rng, pages, 1, page, D), _pool(rng, pages, 1, page, D)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(4)
+    q = torch.randn(n, Hq, D, device="cuda", generator=g).bfloat16()
+    kk, vv = (_gather(p, table[0], n, page, 0, D)[0] for p in (k, v))
+    for lengths, starts in (([n], [0, n]), ([n, 0, 40, n], [0, 9, 9, 49, n])):
+        tables = np.repeat(table, len(lengths), 0)
+        out, sums = ctx.cache_attention(q, _cache(k, v, D), _i32(tables), _i32(lengths), starts=_i32(starts), lse=True)
+        for i in (0, 8, 9, 48, 49, 1000, 40000, n - 129, n - 1):
+            b = int(np.searchsorted(starts, i, side="right")) - 1
+            last = lengths[b] - (starts[b + 1] - i)
+            for h in (0, 64):
+                want, wl, spread, _, off = orc.attend(_np(q[i:i + 1, h]), kk, vv, D ** -0.5, [last])
+                assert (np.abs(_np(out[i, h]) - want[0]) <= 2.0 ** -8 * np.abs(want[0]) + (2.0 ** -8 + 2 * off[0] + last * 2.0 ** -23) * 1.01 * spread[0]).all(), (lengths, i, h)
+                assert abs(float(sums[i, h]) - wl[0]) <= 2 * off[0] + n * 2.0 ** -23 + abs(wl[0]) * 2.0 ** -22 + 2.0 ** -21
+
+
 def test_attention_of_many_sequences(ctx):
     """More sequences than are looked through at once, most of them without queries."""
     rng = _rng("many sequences")

@@ -90,6 +90,16 @@ def test_workspaces():
     assert one == 0 and two > 0
 
 
+@pytest.mark.parametrize("T,B,Hq,H,ragged", [(65536, 1, 64, 8, True), (1 << 20, 1, 64, 8, True), ((1 << 22) - 1, 1, 16, 16, True), (1 << 17, 1 << 17, 32, 32, False), (1, (1 << 22) - 1, 1, 1, True)])
+def test_attention_of_many_rows_is_taken(T, B, Hq, H, ragged):
+    """As many rows as a launch holds: 2^26 of all heads, and 2^22 heads of sequences."""
+    assert esp.cache_attention_workspace(4096, 64, H, 64, T, B, Hq, 2048, ragged) >= 0
+    for more in (dict(T=2 * T, B=B if ragged else 2 * B), dict(T=T if ragged else 4 * B, B=4 * B)):
+        if more["T"] * Hq > 1 << 26 or more["B"] * H > 1 << 22:
+            with pytest.raises(esp.EsparseError):
+                esp.cache_attention_workspace(4096, 64, H, 64, more["T"], more["B"], Hq, 2048, ragged)
+
+
 # ---- refusals: nothing is launched ------------------------------------------------------------------
 def _rotate(ctx, rc, what=None, **change):
     a = dict(heads=(8, 2, 64, 64, 0, 1e-6), T=5, dtype=0, q=_at(0), ldq=512, qw=_at(1), k=_at(2), ldk=128, kw=_at(3), pos=_at(4), freq=_at(5), qo=_at(6), ko=None,
