@@ -363,7 +363,8 @@ int esparse_token_logprobs(esparse_ctx* ctx, const void* logits, long long R, lo
  *   then pairs (a, b) of its first `rotary` channels (even, 0..head_dim) become (a cos t - b sin t, b cos t + a sin t), t = position frequencies[i] (f32[rotary / 2]),
  *   i < rotary / 2: channels i and i + rotary / 2, or with paired = 1 channels 2 i and 2 i + 1.
  * In 64 bits up to one rounding.  q_out[T][q_heads][head_dim]; keys to k_out[T][kv_heads][head_dim] (may be NULL with a cache) and, with a cache, keys and v to the places
- * slots[T] (int32).  A token whose slot is no place of the cache is not kept; of tokens given the same slot the last is.
+ * slots[T] (int32).  A token whose slot is no place of the cache is not kept; of tokens given the same slot the last is (which takes T^2 / 2 comparisons of
+ * slots: half of the time at 131072 tokens of 80 heads of 128 channels; prompts of hundreds of thousands of tokens go in parts).
  * NaN and infinities as in esparse_rms_norm; a rotated channel is NaN with its partner.  In the cache a block of 32 channels that holds one reads as NaN.  (Numbers beyond 2^130
  * are limited to 6 x 2^127.)  Outputs and the cache may not overlap inputs or each other.  T = 0 is a no-op.  Does not synchronise; can be captured.
  * T < 2^22, up to 2^16 heads of a kind, T (q_heads + 2 kv_heads) up to 2^26 (esparse_cache_read: T heads).

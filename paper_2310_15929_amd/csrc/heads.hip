@@ -148,14 +148,16 @@ __global__ void __launch_bounds__(NT, 4) k_rotate_heads(const RotateArgs a) {
     turn[0][threadIdx.x] = c;
     turn[1][threadIdx.x] = s;
   }
-  // the last of the tokens that are given one place has it
+  // The last of the tokens that are given one place has it: the slots of all later tokens are looked through, T^2 / 2 comparisons in all.  Of a prompt of 4096 tokens of 64 + 8 + 8 heads that is
+  // 6 us of 79, of 65536 tokens 0.6 ms of 1.7, of 131072 tokens 2.1 of 4.3.  (A list of who has which place would need scratch memory of the size of the cache.)  Tokens that have no place look
+  // for nothing.
   long long slot = -1;
   int later = 0;
   if (a.slots) {
     const int32_t mine = a.slots[t];
     if (mine >= 0 && mine < a.tokens) slot = mine;
     // (the waves that have no angles look through those behind it, sixteen of a thread at a time)
-    if (threadIdx.x >= NT / 2) {
+    if (slot >= 0 && threadIdx.x >= NT / 2) {
       for (long long j = t + 1 + 4 * (long long)(threadIdx.x - NT / 2); j < a.T; j += 8 * NT) {
         int32_t s[4][4];
 #pragma unroll
@@ -171,7 +173,7 @@ __global__ void __launch_bounds__(NT, 4) k_rotate_heads(const RotateArgs a) {
 #pragma unroll
         for (int u = 0; u < 4; u++)
 #pragma unroll
-          for (int e = 0; e < 4; e++) later |= s[u][e] == mine && mine >= 0;
+          for (int e = 0; e < 4; e++) later |= s[u][e] == mine;
       }
     }
   }
