@@ -362,7 +362,7 @@ int esparse_token_logprobs(esparse_ctx* ctx, const void* logits, long long R, lo
  *   y = x weight / sqrt(mean(x^2) + eps) over the head_dim channels of a head (weight[head_dim] of type dtype; NULL: y = x);
  *   then pairs (a, b) of its first `rotary` channels (even, 0..head_dim) become (a cos t - b sin t, b cos t + a sin t), t = position frequencies[i] (f32[rotary / 2]),
  *   i < rotary / 2: channels i and i + rotary / 2, or with paired = 1 channels 2 i and 2 i + 1.
- * In 64 bits up to one rounding.  q_out[T][q_heads][head_dim]; keys to k_out[T][kv_heads][head_dim] (may be NULL with a cache) and, with a cache, keys and v to the places
+ * In 64 bits; numbers of q_out and k_out are rounded to fp32 and then to their type (off by half a step of it and 2^-24 of the value at most), numbers of the cache once.  q_out[T][q_heads][head_dim]; keys to k_out[T][kv_heads][head_dim] (may be NULL with a cache) and, with a cache, keys and v to the places
  * slots[T] (int32).  A token whose slot is no place of the cache is not kept; of tokens given the same slot the last is (which takes T^2 / 2 comparisons of
  * slots: half of the time at 131072 tokens of 80 heads of 128 channels; prompts of hundreds of thousands of tokens go in parts).
  * NaN and infinities as in esparse_rms_norm; a rotated channel is NaN with its partner.  In the cache a block of 32 channels that holds one reads as NaN.  (Numbers beyond 2^130
@@ -416,7 +416,8 @@ int esparse_cache_attention(esparse_ctx* ctx, const void* q, long long ldq, long
  * tokens[r] (int64) is the first, by index, up to which more than u[r] (f32, [0, 1); others count as the nearest, NaN as 0) of the kept sum has come; logprob[r] (f32, may be NULL)
  * ln(w / kept sum).  temperature (f32[R]) 0: the largest logit, the lowest index of equal ones, logprob 0.
  * temperature, top_k, top_p, min_p may be NULL (1, all, all, all).  Logits of minus infinity are never drawn.  A row with a NaN or plus infinity, with nothing but minus infinity, or whose
- * temperature is negative, infinite or NaN gives -1 and NaN.  Sums are exact to 2^-40 of the largest weight and do not depend on chance.
+ * temperature is negative, infinite or NaN gives -1 and NaN.  Sums are off by 2^-40 of themselves and V 2^-45 of the
+ * largest weight at most, and do not depend on chance.
  * R < 2^22, V up to ESPARSE_MAX_VOCABULARY, R V up to 2^34.
  * workspace: DEVICE scratch of esparse_sample_workspace bytes (host only), 256-byte aligned, overwritten.  Outputs and workspace may not overlap inputs or each other.
  * R = 0 is a no-op.  Does not synchronise; can be captured.  Errors: EINVAL, EUNSUPPORTED (dtype, V), EWORKSPACE, EHIP. */

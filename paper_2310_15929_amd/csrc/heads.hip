@@ -2,7 +2,8 @@
 // written in 16 bits, keys in 16 bits and, with the values, into the pages of a cache in microscaled 4 bits (include/esparse.h).
 //   y = x w / sqrt(mean(x^2) + eps);  (a, b) -> (a cos t - b sin t, b cos t + a sin t),  t = position x frequency
 // A row (a head of a token) belongs to DP / 8 lanes with eight channels each: the sum of squares goes over the lanes, the partners of a lane's channels are in a lane of the same row (where
-// rotary / 2 is no multiple of eight they are read again).  Everything up to the rounding is in 64 bits: the angles of far positions are lost in 32,
+// rotary / 2 is no multiple of eight they are read again).  Everything up to the rounding (for 16 bits by way of fp32, 2^-24 of a value more: a single rounding takes a few instructions more a number of a
+// kernel that the vector unit bounds) is in 64 bits: the angles of far positions are lost in 32,
 // and a number on the border of two 4-bit codes goes where the exact one would (sqrt and the corrected quotient are exact where the exact result is
 // short enough to be such a border; what is rounded to 16 bits does without that).  The angles of a token are computed once per workgroup, whose
 // rows all belong to one token, while its first row is on its way.

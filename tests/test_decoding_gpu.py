@@ -605,6 +605,17 @@ def test_drawn_from_large_vocabularies(ctx, dtype):
             _draw(ctx, x.cuda(), rng.random(R), str((V, cuts)), **cuts)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_drawn_from_the_largest_vocabulary(ctx, dtype):
+    """2^21 logits: spread, and one large weight before equal ones that each lose the same in a piece's ranges."""
+    V = 1 << 21
+    x = 2 * _rng("largest", dtype).standard_normal((2, V), dtype=np.float32)
+    x[1] = math.log(1000.4 * 2.0 ** -48)
+    x[1, 12345] = 0.0
+    for cuts in (dict(), dict(top_p=0.9), dict(top_k=5000), dict(min_p=1e-4)):
+        _draw(ctx, torch.from_numpy(x).to(TORCH[dtype]).cuda(), [0.37, 0.5], str(cuts), **cuts)
+
+
 @pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
 def test_drawn_among_equal_logits(ctx, dtype):
     """Rows of one value and of few: cuts fall among thousands of equal values, the lower indices are kept."""
