@@ -813,6 +813,43 @@ def test_steps_of_decoding(ctx, dtype):
                 new[b] = [token]
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("Hq,H,D", [(4, 2, 64), (15, 5, 64), (9, 3, 40), (5, 1, 128)])
+def test_steps_of_one_token_each(ctx, Hq, H, D, dtype):
+    """Tokens one by one, without `starts` as a step of one query each is called: heads into the cache, attention over what they and the steps before left there, on rows of odd numbers of heads."""
+    dt, rng, B, page = TORCH[dtype], _rng("one each", Hq, D, dtype), 3, 16
+    freq, tables = _freq(D, 1e4), np.array([[5, 1, 0], [2, 7, 4], [6, 3, 8]], np.int32)
+    cache, lengths = ctx.kv_cache(9, page, H, D), np.array([0, 14, 30])
+    w = torch.from_numpy(1 + 0.1 * rng.standard_normal(D)).to(dt).cuda()
+    held = [np.zeros((0, H, D)) for _ in range(2 * B)]
+    for b, n in enumerate(lengths):                 # what is there before the first step
+        if not n:
+            continue
+        k, v = (torch.from_numpy(rng.standard_normal((n, H, D))).to(dt).cuda() for _ in range(2))
+        at = np.arange(n)
+        ctx.rotate_heads(None, k, v=v, cache=cache, slots=_i32(tables[b][at // page] * page + at % page))
+        held[2 * b], held[2 * b + 1] = (orc.cache_values(*orc.cache_rows(_np(t)), D) for t in (k, v))
+    for _ in range(5):
+        x = torch.from_numpy(rng.standard_normal((B, Hq + 2 * H, D))).to(dt).cuda()
+        q, k, v = x.split((Hq, H, H), 1)
+        slots = tables[np.arange(B), lengths // page] * page + lengths % page
+        qo, _ = ctx.rotate_heads(q, k, _i32(lengths), torch.from_numpy(freq).cuda(), q_weight=w, k_weight=w, v=v, cache=cache, slots=_i32(slots))
+        kept = orc.cache_values(*orc.cache_rows(orc.rotate(_np(k), _np(w), 1e-6, lengths, freq, False)), D), orc.cache_values(*orc.cache_rows(_np(v)), D)
+        lengths = lengths + 1
+        out, sums = ctx.cache_attention(qo, cache, _i32(tables), _i32(lengths), lse=True)
+        again = ctx.cache_attention(qo, cache, _i32(tables), _i32(lengths), starts=_i32(np.arange(B + 1)))
+        for b in range(B):
+            for i in range(2):
+                held[2 * b + i] = np.concatenate((held[2 * b + i], kept[i][b:b + 1]))
+            for h in range(Hq):
+                kk, vv = (held[2 * b + i][:, h // (Hq // H)] for i in range(2))
+                want, wl, spread, _, off = orc.attend(_np(qo)[b:b + 1, h], kk, vv, D ** -0.5, [lengths[b] - 1])
+                tol = HALF[dt] * np.abs(want[0]) + TINY[dt] + (HALF[dt] + 2 * off[0] + lengths[b] * 2.0 ** -23) * 1.01 * spread[0]
+                for got in (out, again):
+                    assert (np.abs(_np(got)[b, h] - want[0]) <= tol).all(), (b, h)
+                assert abs(float(sums[b, h]) - wl[0]) <= 2 * off[0] + lengths[b] * 2.0 ** -23 + abs(wl[0]) * 2.0 ** -22 + 2.0 ** -21
+
+
 def test_steps_on_another_stream_and_other_workspaces(ctx):
     """Two graphs of attention replayed in turn, and calls on two streams at once, each with a workspace of its own."""
     rng = _rng("streams")
