@@ -34,6 +34,7 @@ constexpr int ROWS = 16;       // rows of a tile
 constexpr int WAVES = 4;
 constexpr int LEAST = 8;       // strips of a piece, where a long sequence is cut
 constexpr int MOST_PIECES = 512;
+constexpr uint16_t NAN16 = 0x7fff;  // of both types
 
 struct AttendArgs {
   const uint16_t* q;
@@ -122,23 +123,19 @@ __device__ __forceinline__ int first_token(const AttendArgs& a, const int32_t* t
   }
   return n;
 }
-// What a row is divided by, inverted, and ln sum exp.  A sum of nothing: 0 and minus infinity where the row sees nothing; where it sees tokens (up to `sees`) all of their products are minus infinity
-// in 32 bits, and it has no number.  The rows of a wave are of one sequence, which `table` is of, and see n tokens at most
+// What a row is divided by, inverted, and ln sum exp; a sum of nothing: 0 and minus infinity, as for a row that sees nothing
 struct Sums {
   float by, lse;
 };
 template <int DT>
-__device__ __forceinline__ Sums sums_of(const AttendArgs& a, float all, float top, const int32_t* table, int n, int sees) {
-  Sums r = {1.f / all, top * a.natural + (log2f(all) - kOffset<DT>) * 0.6931471805599453f};
-  if (__ballot(all == 0.f)) {
-    bool some = false;
-    if (__ballot(all == 0.f && sees >= 0)) some = first_token(a, table, n) <= sees;
-    if (all == 0.f) {
-      r.by = some ? __builtin_nanf("") : 0.f;
-      r.lse = some ? __builtin_nanf("") : -__builtin_inff();
-    }
-  }
-  return r;
+__device__ __forceinline__ Sums sums_of(const AttendArgs& a, float all, float top) {
+  return {all == 0.f ? 0.f : 1.f / all, all == 0.f ? -__builtin_inff() : top * a.natural + (log2f(all) - kOffset<DT>) * 0.6931471805599453f};
+}
+// ... but a row that sees tokens, up to `sees` of the n that rows of the tile see, has a sum of nothing where all of its products are minus infinity in 32 bits: it has no number.  (Asked after the
+// outputs are written, when their registers are free.)  The rows of the lanes that are here are of the sequence that `table` is of
+__device__ __forceinline__ bool no_number(const AttendArgs& a, float all, const int32_t* table, int n, int sees) {
+  if (!__ballot(all == 0.f && sees >= 0)) return false;
+  return first_token(a, table, n) <= sees && all == 0.f;
 }
 
 // the largest scale with which all codes have numbers of the type: 6 x 2^13 and 6 x 2^125
@@ -322,6 +319,7 @@ __global__ void __launch_bounds__(64 * WAVES, DP == 256 ? 2 : 3) k_attend_few(co
 #pragma unroll
   for (int n = 0; n < ND; n++) o[n] = floatx4_t{0.f, 0.f, 0.f, 0.f};
   float m = -__builtin_inff(), l = 0.f;
+  bool beyond = false;  // (of some row of the wave)
 
   for (int strip = from + wave; strip < to; strip += WAVES) {
     Strip<DP> now = next;
@@ -349,7 +347,7 @@ __global__ void __launch_bounds__(64 * WAVES, DP == 256 ? 2 : 3) k_attend_few(co
     top = column_max(top);
     const float base = top == -__builtin_inff() ? 0.f : top;
     float scaled = base * a.c;
-    if (__ballot(top > m || !(fabsf(scaled) < NEAR))) {  // (else all have kept their maxima)
+    if (__ballot(top > m) || beyond) {  // (else all have kept their maxima)
       const float shrink = __builtin_amdgcn_exp2f((m - base) * a.c);
       l *= shrink;
 #pragma unroll
@@ -357,7 +355,8 @@ __global__ void __launch_bounds__(64 * WAVES, DP == 256 ? 2 : 3) k_attend_few(co
 #pragma unroll
         for (int j = 0; j < 4; j++) o[n][j] *= shrink;
       m = top;
-      if (__ballot(!(fabsf(scaled) < NEAR))) {
+      beyond = __ballot(!(fabsf(scaled) < NEAR)) != 0;
+      if (__builtin_expect(beyond, 0)) {
 #pragma unroll
         for (int u = 0; u < 2; u++)
 #pragma unroll
@@ -470,11 +469,16 @@ __global__ void __launch_bounds__(64 * WAVES, DP == 256 ? 2 : 3) k_attend_few(co
         }
       } else {
         const long long place = (t.start + qi) * ((long long)a.Hkv * a.group) + head * a.group + of % a.group;
-        const Sums of_row = sums_of<DT>(a, all, top, table, t.end, t.length - t.queries + qi);
+        const Sums of_row = sums_of<DT>(a, all, top);
 #pragma unroll
         for (int j = 0; j < 4; j++)
           if (ch + j < a.D) a.out[place * a.D + ch + j] = esp_from_float<DT>(sum[j] * of_row.by);
         if (a.lse && ch == 0) a.lse[place] = of_row.lse;
+        if (no_number(a, all, table, t.end, t.length - t.queries + qi)) {
+          for (int j = 0; j < 4; j++)
+            if (ch + j < a.D) a.out[place * a.D + ch + j] = NAN16;
+          if (a.lse && ch == 0) a.lse[place] = __builtin_nanf("");
+        }
       }
     }
   }
@@ -532,12 +536,17 @@ __global__ void __launch_bounds__(256) k_attend_join(const AttendArgs a) {
     for (int j = 0; j < 4; j++) sum[j] += v[j];
     all += factor[i];
   }
-  const Sums of_row = sums_of<DT>(a, all, top, a.table + (long long)t.b * a.width, t.end, t.length - t.queries + qi);
+  const Sums of_row = sums_of<DT>(a, all, top);
   const long long place = (t.start + qi) * ((long long)a.Hkv * a.group) + head * a.group + of % a.group;
 #pragma unroll
   for (int j = 0; j < 4; j++)
     if (4 * quad + j < a.D) a.out[place * a.D + 4 * quad + j] = esp_from_float<DT>(sum[j] * of_row.by);
   if (a.lse && quad == 0) a.lse[place] = of_row.lse;
+  if (no_number(a, all, a.table + (long long)t.b * a.width, t.end, t.length - t.queries + qi)) {
+    for (int j = 0; j < 4; j++)
+      if (4 * quad + j < a.D) a.out[place * a.D + 4 * quad + j] = NAN16;
+    if (a.lse && quad == 0) a.lse[place] = __builtin_nanf("");
+  }
 }
 
 // ---- prompts: many rows of a sequence ----------------------------------------------------------------
@@ -601,6 +610,7 @@ __global__ void __launch_bounds__(64 * W, 2) k_attend_many(const AttendArgs a) {
 #pragma unroll
     for (int j = 0; j < 16; j++) o[n][j] = 0.f;
   float m = -__builtin_inff(), l = 0.f;
+  bool beyond = false;  // (of some row of the wave)
 
   uint4 code[ITEMS];
   unsigned scl[ITEMS];
@@ -686,7 +696,7 @@ __global__ void __launch_bounds__(64 * W, 2) k_attend_many(const AttendArgs a) {
     top = half_max(top);
     const float base = top == -__builtin_inff() ? 0.f : top;
     float scaled = base * a.c;
-    if (__ballot(top > m || !(fabsf(scaled) < NEAR))) {
+    if (__ballot(top > m) || beyond) {
       const float shrink = __builtin_amdgcn_exp2f((m - base) * a.c);
       l *= shrink;
 #pragma unroll
@@ -694,7 +704,8 @@ __global__ void __launch_bounds__(64 * W, 2) k_attend_many(const AttendArgs a) {
 #pragma unroll
         for (int j = 0; j < 16; j++) o[n][j] *= shrink;
       m = top;
-      if (__builtin_expect(__ballot(!(fabsf(scaled) < NEAR)) != 0, 0)) {
+      beyond = __ballot(!(fabsf(scaled) < NEAR)) != 0;
+      if (__builtin_expect(beyond, 0)) {
 #pragma unroll
         for (int b = 0; b < TB; b++)
 #pragma unroll
@@ -743,7 +754,7 @@ __global__ void __launch_bounds__(64 * W, 2) k_attend_many(const AttendArgs a) {
   for (int n = 0; n < ND; n++) settle(o[n]);
   l = half_sum(l);
   if (!live) return;
-  const Sums of_row = sums_of<DT>(a, l, m, table, t.end, sees);
+  const Sums of_row = sums_of<DT>(a, l, m);
   const long long place = (t.start + query) * ((long long)a.Hkv * a.group) + head * a.group + row % a.group;
 #pragma unroll
   for (int n = 0; n < ND; n++)
@@ -761,6 +772,12 @@ __global__ void __launch_bounds__(64 * W, 2) k_attend_many(const AttendArgs a) {
       }
     }
   if (a.lse && h == 0) a.lse[place] = of_row.lse;
+  if (no_number(a, l, table, t.end, sees)) {
+    for (int ch = 4 * h; ch < a.D; ch += 8)  // (those that this lane has written)
+      for (int e = 0; e < 4; e++)
+        if (ch + e < a.D) a.out[place * a.D + ch + e] = NAN16;
+    if (a.lse && h == 0) a.lse[place] = __builtin_nanf("");
+  }
 }
 
 long long tiles_of(long long T, int B, int group, bool ragged, int rows) {
