@@ -355,13 +355,15 @@ __global__ void __launch_bounds__(64 * WAVES, DP == 256 ? 2 : 3) k_attend_few(co
 #pragma unroll
         for (int j = 0; j < 4; j++) o[n][j] *= shrink;
       m = top;
-      beyond = __ballot(!(fabsf(scaled) < NEAR)) != 0;
+      const bool row_beyond = !(fabsf(scaled) < NEAR);
+      beyond = __ballot(row_beyond) != 0;
       if (__builtin_expect(beyond, 0)) {
+        const float off = row_beyond ? base : 0.f;
 #pragma unroll
         for (int u = 0; u < 2; u++)
 #pragma unroll
-          for (int j = 0; j < 4; j++) x[u][j] -= base;
-        scaled = 0.f;
+          for (int j = 0; j < 4; j++) x[u][j] -= off;
+        scaled = row_beyond ? 0.f : scaled;
       }
     }
 #pragma unroll
@@ -704,13 +706,15 @@ __global__ void __launch_bounds__(64 * W, 2) k_attend_many(const AttendArgs a) {
 #pragma unroll
         for (int j = 0; j < 16; j++) o[n][j] *= shrink;
       m = top;
-      beyond = __ballot(!(fabsf(scaled) < NEAR)) != 0;
+      const bool row_beyond = !(fabsf(scaled) < NEAR);
+      beyond = __ballot(row_beyond) != 0;
       if (__builtin_expect(beyond, 0)) {
+        const float off = row_beyond ? base : 0.f;
 #pragma unroll
         for (int b = 0; b < TB; b++)
 #pragma unroll
-          for (int j = 0; j < 16; j++) x[b][j] -= base;
-        scaled = 0.f;
+          for (int j = 0; j < 16; j++) x[b][j] -= off;
+        scaled = row_beyond ? 0.f : scaled;
       }
     }
     uint4 p[2 * TB];

@@ -502,6 +502,23 @@ def test_attention_of_a_long_tail(ctx, nq, Hq, step, dtype, below):
             assert abs(sums[i, h] - wl[0]) <= 2 * off[0] + n * 2.0 ** -23 + abs(wl[0]) * 2.0 ** -22 + 2.0 ** -21
 
 
+@pytest.mark.parametrize("nq,Hq", [(1, 6), (5, 6), (160, 192)])
+def test_attention_of_a_head_is_not_touched_by_another(ctx, nq, Hq):
+    """Queries of one head with scores far beyond those of the others, or beyond fp32: the others', whose rows share its waves, keep every bit."""
+    rng = _rng("others", nq)
+    D, page, H, n = 64, 16, 1, 300
+    table, pages = _tables(rng, [n], page)
+    k, v = _pool(rng, pages, H, page, D), _pool(rng, pages, H, page, D)
+    cache, starts = _cache(k, v, D), None if nq == 1 else _i32([0, nq])
+    q = torch.from_numpy(rng.standard_normal((nq, Hq, D))).to(torch.bfloat16).cuda()
+    first = ctx.cache_attention(q, cache, _i32(table), _i32([n]), starts=starts, lse=True)
+    for factor in (0.0, 1e7, 3e37):
+        q[:, 2] = factor * torch.from_numpy(rng.standard_normal((nq, D))).to(torch.bfloat16).cuda()
+        again = ctx.cache_attention(q, cache, _i32(table), _i32([n]), starts=starts, lse=True)
+        for a, b in zip(first, again):
+            assert torch.equal(a[:, :2], b[:, :2]) and torch.equal(a[:, 3:], b[:, 3:]), factor
+
+
 def test_attention_long_context(ctx):
     rng = _rng("long")
     n, page, D, H = 40001, 64, 128, 2
