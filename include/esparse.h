@@ -400,6 +400,7 @@ int esparse_cache_read(esparse_ctx* ctx, const esparse_cache* cache, const int32
  * q must be finite; a key without number (scale 255) makes the queries that see it NaN, such a block of a value its channels, and so does a block of a value whose scale is beyond 2^13 (f16) or
  * 2^125 (bf16): some of its numbers are beyond the type.  (Numbers of keys beyond the type are infinite.)
  * workspace: DEVICE scratch of esparse_cache_attention_workspace bytes (host only; may be 0; it reads the cache's sizes alone; ragged: 1 with starts, else 0), 256-byte aligned, overwritten.
+ * The work is divided by a batch's averages: prompts and single tokens, or one very long sequence and many short ones, are faster in calls of their own.
  * T and B < 2^22, T q_heads up to 2^26, B times the cache's heads up to 2^22, width * page < 2^31.
  * Outputs and workspace may not overlap inputs or each other.  T = 0 or B = 0 is a no-op.  The order of a row's sums follows from the sizes and the sequence's length.
  * Does not synchronise; can be captured, and replayed with other contents of table, lengths and starts.  Errors: EINVAL, EUNSUPPORTED (dtype), EWORKSPACE, EHIP. */

@@ -10,12 +10,13 @@
 //   output  O^T[channel, row] += V^T P^T.  The lane holds the probabilities of tokens 4 g + j of two groups of 16 for its row: with the tokens of a step numbered that
 //           way P^T is an operand as it stands.  V needs token and channel exchanged: it goes through LDS in 16 bits and comes back by the transposing read, which
 //           hands a lane four tokens of one channel.  P is rounded to the 16 bits of the output's type, as V is held: the matrix instruction takes both so, and each number is off by at
-//           most half a step of the type, which the output is rounded to as well (the error against 64 bits is 1.15 of that of the rounded output alone); sums and statistics are in 32 bits.
+//           most half a step of the type, which the output is rounded to as well; sums and statistics are in 32 bits.  The error against 64 bits is 1.1 to 1.2 of that of the rounded output
+//           alone.  A second product with what P lost takes that to 1.0, and 122 us instead of 116 (48 sequences), 97 instead of 93 (drafts), 1842 instead of 1405 (a prompt of 8192 tokens).
 //           f16 has few exponents: there P is 2^15 at the maximum, so that it keeps its bits down to 2^-29 and vanishes below 2^-40 (with 1 at the maximum a tail of 2^-26 and less was in l
 //           but not in o).
-// Bound by memory at one token a sequence where there is work for the chip: 48 sequences of 500 to 4096 tokens, 32 heads of 128 channels, 115 us (4.2 TB/s; a copy reaches 4.9), by
-// the few waves that its registers leave to cover the latency of a strip (a third of a wave's time it waits for memory, a fifth for a slot of the vector unit, which is busy 55 %);
-// 131072 tokens, 64 heads on 8, 33 us and 5 to join the pieces (3.8 TB/s).  256 channels take twice the registers: 21 sequences of five tokens each, 16 heads on 4, 83 us (1.3 TB/s).
+// Bound by memory at one token a sequence where there is work for the chip: 48 sequences of 500 to 4096 tokens, 32 heads of 128 channels, 116 us (4.1 TB/s; a copy reaches 4.9), where
+// four waves a SIMD (122 registers, 37 KB of LDS a workgroup) do not cover the latency of a strip (a third of a wave's time it waits for memory, a fifth for a slot of the vector unit, which is busy
+// 55 %); 131072 tokens, 64 heads on 8, 32 us and 5 to join the pieces (3.8 TB/s).  256 channels take 208 registers, two waves a SIMD: 21 sequences of five tokens each, 16 heads on 4, 81 us (1.3 TB/s).
 // The statistics of a row are those of a column of X^T: they stay in the lane but for two exchanges (lanes 16 and 32 apart) a strip of 32 tokens.
 // A block of V that has no numbers in 16 bits (scale 255, or so large that some would be infinite) is left out of the product and makes the rows that see its token NaN afterwards, so that
 // masked tokens cannot reach a row.
@@ -555,9 +556,10 @@ __global__ void __launch_bounds__(256) k_attend_join(const AttendArgs a) {
 // A workgroup of W waves takes 32 W rows, 32 a wave as the columns of the 32 x 32 instruction (lane 32 h + c: operands hold k = 8 h .. 8 h + 7 of row / column c, results rows
 // 8 (j / 4) + 4 h + j % 4 of column c).  The tokens come in tiles that all waves share, brought to 16 bits once, in two buffers: while one is multiplied the
 // codes of the tile after the next are on their way and the next is written to the other buffer.
-// Measured: 8192 tokens, 64 heads on 8 of 128 channels 1390 us (790 TFLOP/s, where a large library product of the type reaches 1570; the matrix pipe is busy 30 %, the vector unit 50 %,
+// Measured: 8192 tokens, 64 heads on 8 of 128 channels 1360 us (810 TFLOP/s, where a large library product of the type reaches 1560; the matrix pipe is busy 30 %, the vector unit 50 %,
 // mostly with exponentials): two waves a SIMD do not cover each other's waits.  The keys a tile ahead of the values, so that their products stand beside the exponentials, a higher priority of the waves
-// in the products, and 32 tokens a tile were built and were slower (1490, 1500, 1520).
+// in the products, and 32 tokens a tile were built and were slower (1490, 1500, 1520).  256 channels, 16 heads on 4: 855 us (640 TFLOP/s), with 16 of 256 registers spilled (8 waves; 29 with 4); 192
+// channels 844, 80 (64 heads on 8) 1335, 64 830: rows of 192 and 80 channels take the time of 256 and 128.
 template <int DP>
 constexpr int kTile = DP == 256 ? 32 : 64;  // tokens of a tile
 template <int DP>
@@ -798,7 +800,8 @@ int most_pieces(long long items, long long tokens) {
 // Waves of a workgroup of the kernel for many rows (128 or 256 rows), 0: the kernel for few rows.  Both take a time that grows with the lengths, which are not known here.  The kernel for few rows
 // spreads any number of rows over the chip by cutting the tokens into pieces, the other needs workgroups: one sequence of 8192 tokens, 64 heads on 8 of 128 channels, with 16, 64,
 // 256, 512, 1024 queries 30, 76, 206, 363, 557 us against 296, 305, 304, 304, 327; 16 heads on 4 of 256 channels with 16, 256, 1024 queries 25, 171, 485 against 900 throughout.
-// So by the number of tiles of sixteen rows; and of few rows for each sequence most of a tile of 128 would be empty.
+// So by the number of tiles of sixteen rows; and of few rows for each sequence most of a tile of 128 would be empty.  Both this and the number of pieces go by a batch's averages: one prompt of 4096
+// tokens with 47 single tokens over 2000 each takes 476 us (64 heads on 8), in two calls 372 + 39; one token over 131072 with 47 over 500 each 166 us, in two calls 40 + 21.
 constexpr long long MANY_ROWS = 64, MOST_ROWS = 1024;
 int waves_of_many(long long T, int B, int group, int Hkv, int row, bool ragged) {
   const long long each = ragged ? T * group / B : group, tiles = (T * group + ROWS - 1) / ROWS * Hkv;

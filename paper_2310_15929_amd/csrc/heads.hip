@@ -8,7 +8,7 @@
 // short enough to be such a border; what is rounded to 16 bits does without that).  The angles of a token are computed once per workgroup, whose
 // rows all belong to one token, while its first row is on its way.
 // Bound by the vector unit (80 % of its slots) rather than memory, with the start of a workgroup - positions, angles, factors: twice as many workgroups for the same rows take twice the time.
-// Measured: 1 token of 32 + 32 + 32 heads of 128 channels 6 us, 4096 tokens of 64 + 8 + 8 heads 74 us (2.2 TB/s); with a division by the norm for each channel and
+// Measured: 1 token of 32 + 32 + 32 heads of 128 channels 6 us, 4096 tokens of 64 + 8 + 8 heads 73 us (2.2 TB/s; 127 vector registers, 38 scalar ones spilled into lanes of those); with a division by the norm for each channel and
 // its partner, without the row ahead, and with the library's sine and cosine 88; with five rows ahead (spilled registers) 93, with two 75.  k_cache_read: 4096 tokens of 8 heads of both kinds 5.6 us (4 TB/s).
 #include <hip/hip_runtime.h>
 

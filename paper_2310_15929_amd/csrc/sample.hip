@@ -14,7 +14,8 @@
 // range that a cut falls in.
 // Measured: 1 x 32000 f16 with top_k 50 and top_p 0.9 3 + 17 us, 64 x 131072 bf16 with top_p 0.95 17 + 52, 777 x 50021 f32 with top_k 1000 and both others 32 (4.9 TB/s) + 137.  k_rows is bound by
 // the chain of its steps - loads, a search, barriers - and by the one compute unit that reads a row (64 KB in 4 us, a hundred instructions for eight values); spilled registers cost
-// it more than fewer waves (1024 threads with 128 registers: 64 us instead of 52).
+// it more than fewer waves (1024 threads with 128 registers: 64 us instead of 52).  With 512 threads of 176 to 211 registers a compute unit holds one row at a time: 777 rows are three rounds of 256 and a
+// fourth of nine.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
