@@ -440,6 +440,19 @@ def test_attention_of_the_largest_scales(ctx, nq, Hq, n, scale):
             assert sums[i, h] == np.sign(want) * np.inf if beyond else abs(sums[i, h] - want) <= 2.0 ** -22 * abs(want) + 2.0 ** -22
 
 
+@pytest.mark.parametrize("scale", [1e-30, 2e-39, -1e-44, 1e-46, -0.0, -1e-300])
+@pytest.mark.parametrize("nq,Hq", [(3, 2), (160, 192)])
+def test_attention_of_the_smallest_scales(ctx, nq, Hq, scale):
+    """Scales down to and below the smallest numbers of 32 bits: all that a query sees has the same weight, and what it does not see none."""
+    rng = _rng("small scales", nq)
+    D, page, H, lengths = 64, 16, 1, [190, 1]
+    table, pages = _tables(rng, lengths, page)
+    table[0, 3] = -1
+    k, v = _pool(rng, pages, H, page, D), _pool(rng, pages, H, page, D)
+    q = torch.from_numpy(rng.standard_normal((2 * nq, Hq, D))).to(torch.bfloat16).cuda()
+    _check_attention(ctx, q, k, v, table, lengths, np.array([0, nq, 2 * nq]), page, D, "bf16", scale=scale, heads=[0, Hq - 1])
+
+
 @pytest.mark.parametrize("nq,Hq,n", [(1, 2, 700), (5, 2, 190), (160, 192, 190)])
 def test_attention_of_products_beyond_32_bits(ctx, nq, Hq, n):
     """Products of minus infinity have no weight; rows that see no other, or one of plus infinity, have no number; rows that see nothing are zeros."""
